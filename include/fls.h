@@ -369,6 +369,110 @@ int fls_reduce_norm_noalloc(const void* const* grads, uint32_t shard_dim, uint32
 /* Frees the plan and its events/stream.  Device buffers are the caller's and are not touched. */
 int fls_plan_destroy(fls_plan* plan);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * The head of a language model: where the gradients of its largest unit come from.
+ *
+ * A head maps hidden states h (N x d, bf16) with a weight W (V x d, bf16: a view of fls_buffers.param_bf16, or any
+ * other buffer) to logits z = h W^T over a vocabulary of V entries.  The calls below compute a loss of every row and,
+ * on request, the gradients of the weighted sum  L = sum_n w_n loss_n  with respect to h and W, without ever holding the
+ * N x V logits: a first pass keeps per row and per 256 columns the maximum and the sum of exponentials, the gradient
+ * passes form the logits of one piece of the vocabulary again, turn them into dL/dz (bf16) in the workspace and multiply
+ * that by W and h.  Products are bf16 tensor-core products with fp32 accumulation; maxima, sums and losses are held in
+ * fp32 / double; dL/dz is rounded to bf16 once before its products (with fp32 weight gradients it enters the product
+ * with h as two bf16 terms, about 17 bits).  Results do not change from run to run.
+ *
+ * Cross entropy (fls_head_xent), label y, smoothing e, z loss c, lse = log sum_v exp(z_v):
+ *   loss = (1-e) (lse - z_y) + e (lse - mean_v z_v) + c lse^2.
+ * Distillation (fls_head_distill) from a teacher of whom only the k largest logits t_1..t_k at columns i_1..i_k are
+ * known (fls_top_logits), temperature T, p = softmax(z/T):
+ *   FLS_TAIL_RENORM: q = softmax(t/T) over the list;                     KL = sum_j q_j (log q_j - log p_{i_j})
+ *   FLS_TAIL_CLASS:  q_j = exp(t_j/T - teacher_lse), all other columns are one class with q' = max(0, 1 - sum q_j) and
+ *                    p' = sum of p outside the list;                     KL as above + q' (log q' - log p')
+ *   loss = distill_weight T^2 KL + label_weight (lse_1 - z_y), lse_1 at temperature 1.
+ *
+ * Rows that take no part cost nothing: rows with label == ignore_label (distillation: and no teacher entry) are left out
+ * of the products, get loss 0, lse 0 and a zero gradient, and their hidden state may hold anything, NaN included.  A
+ * label outside [0, V) other than ignore_label is not an error the host could see: that row's loss is NaN and it takes
+ * no other part.  Teacher entries with an index outside [0, V) or a logit of -inf are absent; entries of one row should
+ * be distinct (repeated ones count as separate entries). */
+typedef struct fls_head fls_head; /* opaque, created by fls_head_create, freed by fls_head_destroy */
+
+enum { FLS_TAIL_RENORM = 0, FLS_TAIL_CLASS = 1 };
+#define FLS_HEAD_MAX_TOP 128 /* longest teacher list */
+
+typedef struct {
+  uint64_t max_rows;    /* N of the largest call, <= 2^24                                                       */
+  uint64_t vocab;       /* V, 1 .. 2^30                                                                         */
+  uint32_t dim;         /* d, 1 .. 65536                                                                        */
+  uint32_t top;         /* k: teacher entries per row of fls_head_distill, <= FLS_HEAD_MAX_TOP; 0: not used     */
+  uint32_t grads;       /* 1: the workspace has room for gradients; 0: losses only                              */
+  uint32_t grad_dtype;  /* FLS_GRAD_BF16 or FLS_GRAD_F32: element type of grad_weight, as the plan's gradients  */
+  uint32_t any_weight;  /* 1: the workspace has room for a copy of the weight, so that it may start at any element
+                           and have any row stride; 0: the weight must start on a 16-byte boundary and its stride be a
+                           multiple of 8 elements.  dim not a multiple of 8 implies 1                           */
+  uint32_t reserved;    /* 0                                                                                    */
+  uint64_t piece_bytes; /* workspace for dL/dz of one piece of the vocabulary; 0: 256 MiB.  Larger pieces mean fewer
+                           launches; a piece has at least 512 columns                                           */
+} fls_head_desc;
+
+typedef struct {
+  uint64_t workspace_bytes;
+  uint64_t piece_cols;  /* columns of the vocabulary per piece at max_rows                                      */
+  uint64_t pieces;      /* ceil(V / piece_cols) at max_rows                                                     */
+} fls_head_layout;
+
+/* One call's data.  All buffers are device memory of the current device; strides count elements between rows, 0 means
+ * dense.  hidden, grad_hidden and grad_weight may have any element alignment (16-byte aligned rows are faster). */
+typedef struct {
+  uint64_t rows;                /* N, 0 .. max_rows                                                              */
+  const void* hidden;           /* N x d, bf16                                                                   */
+  const void* weight;           /* V x d, bf16                                                                   */
+  const int64_t* labels;        /* N; may be NULL for fls_head_distill with label_weight 0                       */
+  const float* row_weight;      /* N: w_n; NULL: 1 / (rows that take part), the mean                             */
+  float* loss;                  /* N, output                                                                     */
+  float* lse;                   /* N, output (at the temperature of the call)                                    */
+  void* grad_hidden;            /* N x d, bf16, output; NULL: not computed                                       */
+  void* grad_weight;            /* V x d, desc.grad_dtype, output, e.g. a unit of a plan's gradient buffer; NULL: not computed */
+  void* workspace;              /* 256-byte aligned                                                              */
+  uint64_t workspace_bytes;
+  uint64_t hidden_stride, weight_stride, grad_hidden_stride, grad_weight_stride;
+  int64_t ignore_label;
+  uint32_t accumulate;          /* 1: grad_weight is added to (tied embeddings, several micro-batches)           */
+  uint32_t reserved;            /* 0                                                                             */
+} fls_head_io;
+
+typedef struct {
+  const int32_t* top_index;     /* device, N x top, dense                                                        */
+  const float* top_logit;       /* device, N x top, dense                                                        */
+  const float* teacher_lse;     /* device, N: log sum_v exp(t_v / T) over the whole vocabulary; FLS_TAIL_CLASS only */
+  uint32_t tail;                /* FLS_TAIL_*                                                                    */
+  uint32_t reserved;            /* 0                                                                             */
+  double temperature;           /* T > 0                                                                         */
+  double distill_weight, label_weight; /* >= 0                                                                   */
+} fls_distill_desc;
+
+/* Host only.  Errors: FLS_EINVAL (null argument, a size outside its range, unknown grad_dtype, reserved not 0). */
+int fls_head_create(const fls_head_desc* desc, fls_head** out);
+int fls_head_query(const fls_head* head, fls_head_layout* out);
+int fls_head_destroy(fls_head* head);
+
+/* The losses, and the gradients for which a buffer is given, enqueued on cuda_stream; nothing is synchronised or
+ * allocated.  A call with rows = 0 writes a zero grad_weight (or leaves it, with accumulate) and nothing else.
+ * Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, gradients without desc.grads, smoothing outside
+ * [0, 1), a negative or non-finite z_loss, weight or temperature, a stride below d), FLS_EPTR (null, host or overlapping
+ * buffers), FLS_EALIGN (weight without desc.any_weight, float or index buffers off their element size, workspace),
+ * FLS_ESIZE (workspace too small), FLS_ECUDA. */
+int fls_head_xent(fls_head* head, const fls_head_io* io, double label_smoothing, double z_loss, void* cuda_stream);
+int fls_head_distill(fls_head* head, const fls_head_io* io, const fls_distill_desc* distill, void* cuda_stream);
+
+/* Device pointers inside `workspace`, valid once a call that used it has completed: the sticky status word
+ * (FLS_STATUS_WAIT_EXPIRED: a wait inside a kernel ran out, the call's results are incomplete) and the number of rows
+ * that took part in the last call.  Clear the workspace's first 256 bytes before its first use.  Either may be NULL. */
+int fls_head_get_state(const void* workspace, const uint32_t** dev_status, const uint32_t** dev_count);
+
+/* Number of kernels this head has launched so far. */
+int fls_head_get_launch_count(const fls_head* head, uint64_t* launches);
+
 /* Message of the last error on the calling thread ("" if none).  Host string owned by the library. */
 const char* fls_last_error(void);
 

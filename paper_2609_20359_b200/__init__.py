@@ -7,7 +7,7 @@ fls_* name loads libfls.so and raises if it is missing (build it with
 """
 import importlib
 
-_SUBMODULES = ("build", "session", "_binding")
+_SUBMODULES = ("build", "session", "head", "_binding")
 __all__ = list(_SUBMODULES)
 
 

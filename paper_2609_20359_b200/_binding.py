@@ -25,6 +25,8 @@ FLS_MAX_FUSED_GROUPS = 16
 FLS_MAX_STATE_COPIES = 64
 FLS_BUFFER_ALIGN = 32
 FLS_NOALLOC_MAX_ELEMS = 1 << 29
+FLS_TAIL_RENORM, FLS_TAIL_CLASS = 0, 1
+FLS_HEAD_MAX_TOP = 128
 
 EXPORTS = [
     "fls_plan_create", "fls_plan_query", "fls_plan_bind", "fls_sync_step", "fls_sync_step_host", "fls_fedavg",
@@ -34,6 +36,8 @@ EXPORTS = [
     "fls_plan_set_resident", "fls_plan_get_resident", "fls_debug_expire_next_wait",
     "fls_plan_tune", "fls_plan_set_recompute", "fls_plan_set_single_pass", "fls_plan_set_overlap", "fls_set_profiling", "fls_get_kernel_ms", "fls_get_launch_count", "fls_plan_destroy",
     "fls_last_error", "fls_reduce_norm_noalloc",
+    "fls_head_create", "fls_head_query", "fls_head_destroy", "fls_head_xent", "fls_head_distill", "fls_head_get_state",
+    "fls_head_get_launch_count",
 ]
 
 
@@ -79,6 +83,31 @@ class fls_comm_costs(C.Structure):
                 ("hbm_bytes_sync_step", C.c_double), ("hbm_bytes_fedavg", C.c_double)]
 
 
+class fls_head_desc(C.Structure):
+    _fields_ = [("max_rows", C.c_uint64), ("vocab", C.c_uint64), ("dim", C.c_uint32), ("top", C.c_uint32),
+                ("grads", C.c_uint32), ("grad_dtype", C.c_uint32), ("any_weight", C.c_uint32), ("reserved", C.c_uint32),
+                ("piece_bytes", C.c_uint64)]
+
+
+class fls_head_layout(C.Structure):
+    _fields_ = [("workspace_bytes", C.c_uint64), ("piece_cols", C.c_uint64), ("pieces", C.c_uint64)]
+
+
+class fls_head_io(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("hidden", C.c_void_p), ("weight", C.c_void_p), ("labels", C.c_void_p),
+                ("row_weight", C.c_void_p), ("loss", C.c_void_p), ("lse", C.c_void_p), ("grad_hidden", C.c_void_p),
+                ("grad_weight", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("hidden_stride", C.c_uint64), ("weight_stride", C.c_uint64), ("grad_hidden_stride", C.c_uint64),
+                ("grad_weight_stride", C.c_uint64), ("ignore_label", C.c_int64), ("accumulate", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
+class fls_distill_desc(C.Structure):
+    _fields_ = [("top_index", C.c_void_p), ("top_logit", C.c_void_p), ("teacher_lse", C.c_void_p), ("tail", C.c_uint32),
+                ("reserved", C.c_uint32), ("temperature", C.c_double), ("distill_weight", C.c_double),
+                ("label_weight", C.c_double)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} not found: build it with `python -m paper_2609_20359_b200.build` "
@@ -118,6 +147,13 @@ def _load() -> C.CDLL:
     lib.fls_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
     lib.fls_plan_destroy.argtypes = [P]
     lib.fls_reduce_norm_noalloc.argtypes = [C.POINTER(C.c_void_p), C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint64, C.c_double, P, P, P]
+    lib.fls_head_create.argtypes = [C.POINTER(fls_head_desc), C.POINTER(P)]
+    lib.fls_head_query.argtypes = [P, C.POINTER(fls_head_layout)]
+    lib.fls_head_destroy.argtypes = [P]
+    lib.fls_head_xent.argtypes = [P, C.POINTER(fls_head_io), C.c_double, C.c_double, P]
+    lib.fls_head_distill.argtypes = [P, C.POINTER(fls_head_io), C.POINTER(fls_distill_desc), P]
+    lib.fls_head_get_state.argtypes = [P, C.POINTER(P), C.POINTER(P)]
+    lib.fls_head_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
     lib.fls_last_error.argtypes = []
     lib.fls_last_error.restype = C.c_char_p
     for name in EXPORTS:
@@ -375,3 +411,44 @@ def fls_last_error() -> str:
 
 
 __all__ = [n for n in dir() if n.startswith(("fls_", "FLS_"))] + ["FlsError", "lib", "LIB_PATH", "EXPORTS"]
+
+
+# ---------------------------------------------------------------------------------------------- language-model head
+def fls_head_create(max_rows: int, vocab: int, dim: int, top: int = 0, grads: bool = True, grad_dtype: int = FLS_GRAD_BF16,
+                    any_weight: bool = False, piece_bytes: int = 0) -> int:
+    """Returns the opaque head handle."""
+    d = fls_head_desc(max_rows, vocab, dim, top, int(grads), grad_dtype, int(any_weight), 0, piece_bytes)
+    out = C.c_void_p()
+    _check(lib.fls_head_create(C.byref(d), C.byref(out)))
+    return out.value
+
+
+def fls_head_query(head: int) -> dict:
+    lay = fls_head_layout()
+    _check(lib.fls_head_query(head, C.byref(lay)))
+    return dict(workspace_bytes=lay.workspace_bytes, piece_cols=lay.piece_cols, pieces=lay.pieces)
+
+
+def fls_head_destroy(head: int) -> None:
+    _check(lib.fls_head_destroy(head))
+
+
+def fls_head_xent(head: int, io: fls_head_io, label_smoothing: float = 0.0, z_loss: float = 0.0, stream=None) -> None:
+    _check(lib.fls_head_xent(head, C.byref(io), label_smoothing, z_loss, _stream_handle(stream)))
+
+
+def fls_head_distill(head: int, io: fls_head_io, distill: fls_distill_desc, stream=None) -> None:
+    _check(lib.fls_head_distill(head, C.byref(io), C.byref(distill), _stream_handle(stream)))
+
+
+def fls_head_get_state(workspace):
+    """(device address of the status word, device address of the number of rows that took part)."""
+    a, b = C.c_void_p(), C.c_void_p()
+    _check(lib.fls_head_get_state(_ptr(workspace), C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def fls_head_get_launch_count(head: int) -> int:
+    n = C.c_uint64()
+    _check(lib.fls_head_get_launch_count(head, C.byref(n)))
+    return n.value

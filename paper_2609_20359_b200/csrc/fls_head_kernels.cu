@@ -1,0 +1,948 @@
+// Kernels of the language-model head: cross entropy and distillation of a linear head without kept logits.
+//
+//   fls_head_map_kernel    which rows take part, and where they go (compaction; ignored rows cost nothing below)
+//   fls_head_pack_kernel   packed copy of their hidden states, the columns that get a value of their own, sorted
+//   fls_head_gemm_kernel   the tensor-core kernel, three epilogues:
+//     kStats    logits tile -> maximum and sum of exponentials per row and 256 columns
+//     kDlogits  logits tile -> dL/dz in bf16 (one piece of the vocabulary)
+//     kGrads    dL/dz of the piece -> rows of grad_weight, and partial sums of grad_hidden
+//   fls_head_rows_kernel   joins the tile sums, losses, coefficients of dL/dz
+//   fls_head_grad_hidden_kernel   sums the partial sums, rounds, puts rows back in the caller's order
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+
+#include "fls_head.h"
+
+namespace fls {
+namespace {
+
+constexpr int kStages = 6;
+constexpr uint32_t kOperandBytes = 128 * kHeadBK * 2;            // one operand of one stage of one CTA: 16 KB
+constexpr uint32_t kStageBytes = 2 * kOperandBytes;
+constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 + 256;
+constexpr int kGemmThreads = 256;                                // warp 0 TMA, 1 MMA, 2 TMEM, 4..7 epilogue
+constexpr uint32_t kWaitLimit = 1u << 22;                        // polls of an mbarrier before a role gives up
+enum { kStats = 0, kDlogits = 1, kGrads = 2 };
+
+// ------------------------------------------------------------------------------------------------ PTX
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint32_t cta_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+// Address, in the cluster's shared window, of the leader CTA's copy of a shared variable.
+__device__ __forceinline__ uint32_t leader_addr(uint32_t a) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(a));
+  return r;
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// False if the phase did not complete within kWaitLimit polls (each poll may sleep in hardware for a while).
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kWaitLimit; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+// A tile of 64 x box-rows elements into this CTA's shared memory; the bytes are counted on the leader's barrier.
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// Arrives on the barrier at this offset in both CTAs when the products issued so far are done.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+      ::"r"(bar), "h"(uint16_t(3)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 32 columns of this thread's row of an accumulator.
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr) : "memory");
+}
+// Waits for this thread's tmem_load calls; the registers pass through so that no use of them moves above it.
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :: "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Shared-memory matrix descriptor, 128-byte swizzle.  Depth-contiguous operand (K-major): rows of 64 elements = 128
+// bytes, 8-row groups 1024 bytes apart (sbo).  Width-contiguous operand (MN-major): blocks of 64 columns x 64 depth
+// rows; 8-row groups 1024 bytes apart (sbo), 64-column blocks 8192 bytes apart (lbo).
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
+  constexpr uint32_t kLbo = 8192 >> 4, kSbo = 1024 >> 4;
+  const uint32_t lo = ((addr >> 4) & 0x3FFF) | (kLbo << 16);
+  const uint32_t hi = kSbo | (1u << 14) | (2u << 29);
+  return (uint64_t(hi) << 32) | lo;
+}
+// fp32 accumulator, bf16 operands, 256 x 256 over the CTA pair.
+__device__ __forceinline__ uint32_t instr_desc(bool a_mn, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) | ((kHeadBN >> 3) << 17) |
+         ((kHeadBM >> 4) << 24);
+}
+
+// ------------------------------------------------------------------------------------------------ work units
+struct Unit {
+  uint32_t grad_hidden;   // kGrads: which of the two products
+  uint32_t m0, n0;        // first row / column of the 256 x 256 tile
+  uint32_t kb0, kbn;      // depth blocks of 64
+  uint32_t split;
+};
+
+// How many parts the depth of the hidden gradient (the piece's columns) is cut into: so many that one part is at most
+// an eighth of a cluster's share of the launch, which keeps the last round of the persistent grid short.
+__host__ __device__ inline uint32_t head_splits(uint32_t tiles, uint32_t depth_blocks, uint32_t clusters, uint32_t max_splits) {
+  uint32_t s = (4 * clusters + tiles - 1) / (tiles ? tiles : 1);
+  if (s > depth_blocks / 4) s = depth_blocks / 4;
+  if (s > max_splits) s = max_splits;
+  return s ? s : 1;
+}
+
+template <int MODE>
+struct Schedule {
+  uint32_t mt, nt, kb, group, n_units, n_gh, splits, kb_gh, planes;
+  __device__ __forceinline__ Schedule(const HeadCall& c, const HeadPiece& p, uint32_t count) {
+    mt = (count + kHeadBM - 1) / kHeadBM;
+    group = c.group_m;
+    planes = c.planes;
+    if constexpr (MODE == kGrads) {
+      nt = (c.dim + kHeadBN - 1) / kHeadBN;
+      kb = (count + kHeadBK - 1) / kHeadBK;
+      kb_gh = (p.width + kHeadBK - 1) / kHeadBK;
+      splits = head_splits(mt * nt, c.piece_cols / kHeadBK, c.clusters, c.max_splits);
+      n_gh = c.want_gh ? mt * nt * splits : 0;
+      n_units = n_gh + (c.want_gw ? (p.width + kHeadBM - 1) / kHeadBM * nt : 0);
+    } else {
+      nt = (p.width + kHeadBN - 1) / kHeadBN;
+      kb = (c.dp + kHeadBK - 1) / kHeadBK;
+      n_units = mt * nt;
+      n_gh = splits = kb_gh = 0;
+    }
+  }
+  __device__ __forceinline__ Unit at(uint32_t u) const {
+    Unit w;
+    w.grad_hidden = 0; w.split = 0; w.kb0 = 0;
+    if constexpr (MODE == kGrads) {
+      if (u < n_gh) {
+        w.grad_hidden = 1;
+        w.split = u / (mt * nt);
+        const uint32_t r = u - w.split * (mt * nt);
+        w.m0 = r / nt * kHeadBM;
+        w.n0 = r % nt * kHeadBN;
+        w.kb0 = uint32_t(uint64_t(kb_gh) * w.split / splits);
+        w.kbn = uint32_t(uint64_t(kb_gh) * (w.split + 1) / splits) - w.kb0;
+      } else {
+        const uint32_t r = u - n_gh;
+        w.m0 = r / nt * kHeadBM;
+        w.n0 = r % nt * kHeadBN;
+        w.kbn = kb * planes;
+      }
+    } else {
+      // all column tiles of a group of row tiles before the next group: the group's hidden rows stay in L2
+      const uint32_t per = group * nt, gi = u / per, r = u - gi * per;
+      const uint32_t gm = min(group, mt - gi * group);
+      w.n0 = r / gm * kHeadBN;
+      w.m0 = (gi * group + r % gm) * kHeadBM;
+      w.kbn = kb;
+    }
+    return w;
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ epilogues
+// First of this row's columns that is not below `col`.
+__device__ __forceinline__ uint32_t lower_slot(const int32_t* idx, uint32_t n, int32_t col) {
+  uint32_t lo = 0;
+  while (n) {
+    const uint32_t h = n >> 1;
+    if (idx[lo + h] < col) { lo += h + 1; n -= h + 1; } else n = h;
+  }
+  return lo;
+}
+
+// Maximum and sum of exponentials of one row of a tile.  Columns with a value of their own (the label, the teacher's
+// list) are written down and left out of the sum, so that "everything else" is known without a cancelling difference.
+template <bool TWO, bool SMOOTH>
+struct StatsRow {
+  float m = -INFINITY, s = 0.f, s1 = 0.f, sz = 0.f;
+  int32_t next = INT_MAX;
+  const int32_t* idx;
+  float* zs;
+  uint32_t ptr, slots;
+  __device__ __forceinline__ void chunk(uint32_t (&r)[32], int32_t col0, uint32_t vocab, float cT, float c1) {
+    float z[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(r[j]);
+    const bool edge = uint32_t(col0) + 32 > vocab;
+    if constexpr (SMOOTH) {
+      float t = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) t += (!edge || uint32_t(col0 + j) < vocab) ? z[j] : 0.f;
+      sz += t;
+    }
+    if (edge) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (uint32_t(col0 + j) >= vocab) z[j] = -INFINITY;
+    }
+    while (next < col0 + 32) {
+      const int off = next - col0;
+      float v = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j == off) { v = z[j]; z[j] = -INFINITY; }
+      const int32_t at = next;
+      do {                                            // repeated columns share the value
+        zs[ptr] = v;
+        ++ptr;
+        next = ptr < slots ? idx[ptr] : INT_MAX;
+      } while (next == at);
+    }
+    float cm = z[0];
+#pragma unroll
+    for (int j = 1; j < 32; ++j) cm = fmaxf(cm, z[j]);
+    if (cm > m) {
+      const float old = m;
+      m = cm;
+      if (old != -INFINITY) {
+        s *= ex2(__fmul_rn(old, cT) - __fmul_rn(m, cT));
+        if constexpr (TWO) s1 *= ex2(__fmul_rn(old, c1) - __fmul_rn(m, c1));
+      }
+    }
+    const float bT = m == -INFINITY ? 0.f : __fmul_rn(m, cT);
+    float t0 = 0.f, t1 = 0.f, t2 = 0.f, t3 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      t0 += ex2(fmaf(z[j], cT, -bT));
+      t1 += ex2(fmaf(z[j + 1], cT, -bT));
+      t2 += ex2(fmaf(z[j + 2], cT, -bT));
+      t3 += ex2(fmaf(z[j + 3], cT, -bT));
+    }
+    s += (t0 + t1) + (t2 + t3);
+    if constexpr (TWO) {
+      const float b1 = m == -INFINITY ? 0.f : __fmul_rn(m, c1);
+      t0 = t1 = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; j += 2) {
+        t0 += ex2(fmaf(z[j], c1, -b1));
+        t1 += ex2(fmaf(z[j + 1], c1, -b1));
+      }
+      s1 += t0 + t1;
+    }
+  }
+};
+
+__device__ __forceinline__ void store32_bf16(uint16_t* dst, const float (&v)[32]) {
+  uint4* o = reinterpret_cast<uint4*>(dst);
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    o[q] = make_uint4(pack_bf16(v[8 * q], v[8 * q + 1]), pack_bf16(v[8 * q + 2], v[8 * q + 3]),
+                      pack_bf16(v[8 * q + 4], v[8 * q + 5]), pack_bf16(v[8 * q + 6], v[8 * q + 7]));
+}
+__device__ __forceinline__ float bf16_round(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+
+// dL/dz of one row of a tile: aT exp(z/T - lse_T) + a1 exp(z - lse_1) - b, then the columns with a value of their own.
+template <bool TWO>
+struct DlogitsRow {
+  float4 k;          // {lse_T log2(e), aT, lse_1 log2(e), a1}; without TWO {lse log2(e) , a, b, -}
+  int32_t next = INT_MAX;
+  const int32_t* idx;
+  const float* val;
+  uint32_t ptr, slots;
+  uint16_t* out;     // this row's columns of the piece, from the tile's first on
+  uint64_t plane;    // elements from the first to the second plane (fp32 weight gradients), else 0
+  __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int32_t col0, int32_t n0, uint32_t vocab, float cT, float c1) {
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float z = __uint_as_float(r[j]);
+      if constexpr (TWO) v[j] = fmaf(k.w, ex2(fmaf(z, c1, -k.z)), k.y * ex2(fmaf(z, cT, -k.x)));
+      else v[j] = fmaf(k.y, ex2(fmaf(z, cT, -k.x)), -k.z);
+    }
+    if (uint32_t(col0) + 32 > vocab) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (uint32_t(col0 + j) >= vocab) v[j] = 0.f;
+    }
+    uint16_t* o = out + (col0 - n0);
+    store32_bf16(o, v);
+    if (plane) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] -= bf16_round(v[j]);
+      store32_bf16(o + plane, v);
+    }
+    while (next < col0 + 32) {          // same thread, same address, after the store above
+      const float x = val[ptr];
+      uint16_t* at = out + (next - n0);
+      at[0] = bf16_bits(x);
+      if (plane) at[plane] = bf16_bits(x - bf16_round(x));
+      ++ptr;
+      next = ptr < slots ? idx[ptr] : INT_MAX;
+    }
+  }
+};
+
+__device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename T>
+__device__ __forceinline__ void store_row32(T* dst, const float (&v)[32], uint32_t n, bool add) {
+  if (n >= 32 && aligned16(dst)) {
+    if constexpr (sizeof(T) == 4) {
+      float4* o = reinterpret_cast<float4*>(dst);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        float4 x = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        if (add) { const float4 y = o[q]; x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; }
+        o[q] = x;
+      }
+    } else {
+      uint4* o = reinterpret_cast<uint4*>(dst);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = v[8 * q + e];
+        if (add) {
+          const uint4 y = o[q];
+          const uint32_t yy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[2 * e] += __uint_as_float(yy[e] << 16);
+            w[2 * e + 1] += __uint_as_float(yy[e] & 0xFFFF0000u);
+          }
+        }
+        o[q] = make_uint4(pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7]));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      if (j < int(n)) {
+        if constexpr (sizeof(T) == 4) dst[j] = add ? dst[j] + v[j] : v[j];
+        else dst[j] = bf16_bits(add ? __uint_as_float(uint32_t(dst[j]) << 16) + v[j] : v[j]);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the kernel
+struct alignas(8) Barriers {
+  uint64_t full[kStages];    // leader: both CTAs' operands of a stage have landed
+  uint64_t empty[kStages];   // both: the products that read a stage are done
+  uint64_t acc_full[2];      // both: an accumulator is complete
+  uint64_t acc_empty[2];     // leader: both CTAs' epilogues have read an accumulator
+  uint32_t tmem;
+  uint32_t gave_up;
+};
+
+template <int MODE, bool TWO, bool SMOOTH>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadCall c, const HeadPiece piece) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Barriers* bars = reinterpret_cast<Barriers*>(tiles + kStages * kStageBytes);
+  const uint32_t tile_base = smem_u32(tiles);
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cta_rank();
+  const uint32_t cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars->acc_full[i]), 1); mbar_init(smem_u32(&bars->acc_empty[i]), 8); }
+    bars->gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars->tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  cluster_sync();
+  fence_after();
+  const uint32_t tmem = bars->tmem;
+
+  const uint32_t count = c.state->count;
+  const Schedule<MODE> plan(c, piece, count);
+  bool ok = true;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      for (uint32_t u = cluster; u < plan.n_units && ok; u += n_clusters) {
+        const Unit w = plan.at(u);
+        const CUtensorMap* ma = w.grad_hidden ? &maps.a1 : &maps.a0;
+        const CUtensorMap* mb = w.grad_hidden ? &maps.b1 : &maps.b0;
+        const int m = int(w.m0 + rank * 128), n = int(w.n0 + rank * 128);
+        for (uint32_t i = 0; i < w.kbn; ++i) {
+          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1)) { ok = false; break; }
+          const uint32_t bar = leader_addr(smem_u32(&bars->full[stage]));
+          if (rank == 0) mbar_expect(smem_u32(&bars->full[stage]), 2 * kStageBytes);
+          const uint32_t sa = tile_base + stage * kStageBytes, sb = sa + kOperandBytes;
+          const int k = int((w.kb0 + i) * kHeadBK);
+          if constexpr (MODE == kGrads) {
+            if (w.grad_hidden) {
+              tma_load(sa, ma, k, m, bar);                               // dL/dz: 128 rows x 64 columns
+              tma_load(sb, mb, n, int(piece.v0) + k, bar);               // weight: 64 rows x 2 x 64 columns
+              tma_load(sb + 8192, mb, n + 64, int(piece.v0) + k, bar);
+            } else {
+              // fp32 weight gradients: the second half of the depth is the second plane of dL/dz against the same rows
+              const uint32_t second = i >= plan.kb ? 1u : 0u;
+              const int kr = int((i - second * plan.kb) * kHeadBK);
+              const int kg = kr + int(second * c.rows_cap);
+              tma_load(sa, ma, m, kg, bar);                              // dL/dz: 64 rows x 2 x 64 columns
+              tma_load(sa + 8192, ma, m + 64, kg, bar);
+              tma_load(sb, mb, n, kr, bar);                              // hidden: 64 rows x 2 x 64 columns
+              tma_load(sb + 8192, mb, n + 64, kr, bar);
+            }
+          } else {
+            tma_load(sa, ma, k, m, bar);                                 // hidden: 128 rows x 64
+            tma_load(sb, mb, k, int(piece.v0) + n, bar);                 // weight: 128 rows x 64
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && lane == 0) {
+      uint32_t stage = 0, phase = 0, buf = 0, acc_phase = 0;
+      for (uint32_t u = cluster; u < plan.n_units && ok; u += n_clusters) {
+        const Unit w = plan.at(u);
+        if (w.kbn == 0) continue;
+        const bool a_mn = MODE == kGrads && !w.grad_hidden, b_mn = MODE == kGrads;
+        const uint32_t idesc = instr_desc(a_mn, b_mn);
+        const uint32_t ka = (a_mn ? 2048u : 32u) >> 4, kb = (b_mn ? 2048u : 32u) >> 4;   // 16 deep, in descriptor units
+        if (!mbar_wait(smem_u32(&bars->acc_empty[buf]), acc_phase ^ 1)) { ok = false; break; }
+        fence_after();
+        const uint32_t acc = tmem + buf * kHeadBN;
+        for (uint32_t i = 0; i < w.kbn; ++i) {
+          if (!mbar_wait(smem_u32(&bars->full[stage]), phase)) { ok = false; break; }
+          fence_after();
+          const uint32_t sa = tile_base + stage * kStageBytes;
+          const uint64_t da = smem_desc(sa), db = smem_desc(sa + kOperandBytes);
+#pragma unroll
+          for (uint32_t j = 0; j < kHeadBK / 16; ++j) mma_f16(acc, da + j * ka, db + j * kb, idesc, (i | j) != 0);
+          mma_commit(smem_u32(&bars->empty[stage]));
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        mma_commit(smem_u32(&bars->acc_full[buf]));
+        if (++buf == 2) { buf = 0; acc_phase ^= 1; }
+      }
+    }
+  } else if (warp >= 4) {
+    const uint32_t quarter = warp & 3;
+    const uint32_t lane_base = tmem + ((quarter * 32) << 16);
+    uint32_t buf = 0, phase = 0;
+    for (uint32_t u = cluster; u < plan.n_units; u += n_clusters) {
+      const Unit w = plan.at(u);
+      const bool empty = w.kbn == 0;
+      const uint32_t row = w.m0 + rank * 128 + quarter * 32 + lane;
+      // what the tile's rows need besides the accumulator is fetched before the wait
+      StatsRow<TWO, SMOOTH> st;
+      DlogitsRow<TWO> dl;
+      if constexpr (MODE == kStats) {
+        st.idx = c.slot_idx + uint64_t(row) * c.slots;
+        st.zs = c.slot_z + uint64_t(row) * c.slots;
+        st.slots = c.slots;
+        st.ptr = c.slots;
+        if (row < count) {
+          st.ptr = lower_slot(st.idx, c.slots, int32_t(w.n0));
+          st.next = st.ptr < c.slots ? st.idx[st.ptr] : INT_MAX;
+        }
+      } else if constexpr (MODE == kDlogits) {
+        dl.idx = c.slot_idx + uint64_t(row) * c.slots;
+        dl.val = c.slot_g + uint64_t(row) * c.slots;
+        dl.slots = c.slots;
+        dl.ptr = c.slots;
+        dl.k = make_float4(0.f, 0.f, 0.f, 0.f);
+        dl.out = c.g + uint64_t(row) * c.piece_cols + w.n0;
+        dl.plane = c.planes == 2 ? uint64_t(c.rows_cap) * c.piece_cols : 0;
+        if (row < count) {
+          dl.k = c.coef[row];
+          dl.ptr = lower_slot(dl.idx, c.slots, int32_t(piece.v0 + w.n0));
+          dl.next = dl.ptr < c.slots ? dl.idx[dl.ptr] : INT_MAX;
+        }
+      }
+      if (!empty) {
+        ok = mbar_wait(smem_u32(&bars->acc_full[buf]), phase);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        fence_after();
+      }
+      const uint32_t acc = lane_base + buf * kHeadBN;
+      uint32_t ra[32], rb[32];
+      auto process = [&](uint32_t (&r)[32], uint32_t chunk) {
+        const int32_t n = int32_t(w.n0 + chunk * 32);
+        if constexpr (MODE == kStats) {
+          st.chunk(r, n, c.vocab, c.cT, c.c1);
+        } else if constexpr (MODE == kDlogits) {
+          dl.chunk(r, int32_t(piece.v0) + n, int32_t(piece.v0 + w.n0), c.vocab, c.cT, c.c1);
+        } else {
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = empty ? 0.f : __uint_as_float(r[j]);
+          if (w.grad_hidden) {
+            // [split][rows_cap][dcap]: whole tiles exist, nothing to guard
+            float* o = c.dh + (uint64_t(w.split) * c.rows_cap + row) * c.dcap + n;
+            if (!empty || piece.first) store_row32<float>(o, v, 32, !piece.first);
+          } else if (row < piece.width && uint32_t(n) < c.dim) {
+            const uint64_t at = uint64_t(piece.v0 + row) * c.grad_weight_stride + n;
+            const uint32_t left = c.dim - uint32_t(n);
+            if (c.grad_f32) store_row32<float>(static_cast<float*>(c.grad_weight) + at, v, left, c.accumulate);
+            else store_row32<uint16_t>(static_cast<uint16_t*>(c.grad_weight) + at, v, left, c.accumulate);
+          }
+        }
+        __syncwarp();
+      };
+      if (empty) {
+#pragma unroll 1
+        for (uint32_t chunk = 0; chunk < 8; ++chunk) process(ra, chunk);
+        continue;
+      }
+      tmem_load(acc, ra);
+#pragma unroll 1
+      for (uint32_t chunk = 0; chunk < 8; chunk += 2) {
+        tmem_wait(ra);
+        tmem_load(acc + (chunk + 1) * 32, rb);
+        process(ra, chunk);
+        tmem_wait(rb);
+        if (chunk + 2 < 8) {
+          tmem_load(acc + (chunk + 2) * 32, ra);
+        } else {
+          fence_before();                       // the accumulator is in registers: the next product may overwrite it
+          if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&bars->acc_empty[buf])));
+        }
+        process(rb, chunk + 1);
+      }
+      if constexpr (MODE == kStats) {
+        const uint64_t at = uint64_t((piece.v0 + w.n0) / kHeadBN) * c.rows_cap + row;
+        c.part_m[at] = st.m;
+        c.part_s[at] = st.s;
+        if constexpr (TWO) c.part_s1[at] = st.s1;
+        if constexpr (SMOOTH) c.part_z[at] = st.sz;
+      }
+      if (++buf == 2) { buf = 0; phase ^= 1; }
+    }
+  }
+  if (!ok) {
+    atomicOr(&c.state->status, uint32_t(FLS_STATUS_WAIT_EXPIRED));
+    bars->gave_up = 1;
+  }
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  // A role that gave up may have copies in flight: let them land (bounded) before shared memory goes away.
+  if (bars->gave_up) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  cluster_sync();
+  if (warp == 2) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rows
+// One block: packed positions of the rows that take part, in order.
+__global__ void __launch_bounds__(1024) fls_head_map_kernel(const __grid_constant__ HeadCall c) {
+  __shared__ uint32_t warp_sum[32];
+  __shared__ uint32_t base;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) base = 0;
+  __syncthreads();
+  for (uint64_t r0 = 0; r0 < c.rows; r0 += 1024) {
+    const uint64_t n = r0 + threadIdx.x;
+    bool active = false, bad = false;
+    if (n < c.rows) {
+      if (c.use_label) {
+        const int64_t y = c.labels[n];
+        bad = y != c.ignore_label && (y < 0 || y >= int64_t(c.vocab));
+        active = y != c.ignore_label;
+      }
+      for (uint32_t k = 0; k < c.top && !active; ++k) {
+        const int32_t i = c.top_index[n * c.top + k];
+        active = i >= 0 && uint32_t(i) < c.vocab && c.top_logit[n * c.top + k] != -INFINITY;
+      }
+      active = active && !bad;
+      if (!active) {
+        c.loss[n] = bad ? NAN : 0.f;
+        c.lse[n] = bad ? NAN : 0.f;
+      }
+    }
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, active);
+    if (lane == 0) warp_sum[warp] = __popc(mask);
+    __syncthreads();
+    if (warp == 0) {
+      uint32_t x = warp_sum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= uint32_t(o)) x += y;
+      }
+      warp_sum[lane] = x;
+    }
+    __syncthreads();
+    const uint32_t before = base + (warp ? warp_sum[warp - 1] : 0) + __popc(mask & ((1u << lane) - 1));
+    if (n < c.rows) {
+      c.pos[n] = active ? int32_t(before) : -1;
+      if (active) c.src[before] = int32_t(n);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) base += warp_sum[31];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) c.state->count = base;
+}
+
+// One block per packed row: its hidden state (zero beyond the rows that take part, up to the next multiple of 256) and
+// its own columns in ascending order.
+__global__ void __launch_bounds__(128) fls_head_pack_kernel(const __grid_constant__ HeadCall c) {
+  __shared__ int32_t s_idx[FLS_HEAD_MAX_TOP + 1];
+  __shared__ float s_t[FLS_HEAD_MAX_TOP + 1];
+  const uint32_t p = blockIdx.x, count = c.state->count;
+  if (p >= (count + kHeadBM - 1) / kHeadBM * kHeadBM) return;
+  const bool live = p < count;
+  const uint64_t n = live ? uint64_t(c.src[p]) : 0;
+  uint16_t* out = c.hp + uint64_t(p) * c.dp;
+  const uint16_t* in = c.hidden + n * c.hidden_stride;
+  if (!live || (c.dim % 8 == 0 && aligned16(in))) {
+    for (uint32_t i = threadIdx.x; i < c.dp / 8; i += blockDim.x)
+      reinterpret_cast<uint4*>(out)[i] = live ? reinterpret_cast<const uint4*>(in)[i] : make_uint4(0, 0, 0, 0);
+  } else {
+    for (uint32_t i = threadIdx.x; i < c.dp; i += blockDim.x) out[i] = i < c.dim ? in[i] : uint16_t(0);
+  }
+  if (!live) return;
+  for (uint32_t i = threadIdx.x; i < c.slots; i += blockDim.x) {
+    int32_t idx = INT_MAX;
+    float t = -INFINITY;
+    if (i < c.top) {
+      const int32_t x = c.top_index[n * c.top + i];
+      const float y = c.top_logit[n * c.top + i];
+      if (x >= 0 && uint32_t(x) < c.vocab && y != -INFINITY) { idx = x; t = y; }
+    } else if (c.use_label) {
+      const int64_t y = c.labels[n];
+      if (y != c.ignore_label) idx = int32_t(y);
+    }
+    s_idx[i] = idx;
+    s_t[i] = t;
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < c.slots; i += blockDim.x) {
+    const int32_t x = s_idx[i];
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < c.slots; ++j) rank += s_idx[j] < x || (s_idx[j] == x && j < i);
+    c.slot_idx[uint64_t(p) * c.slots + rank] = x;
+    c.slot_t[uint64_t(p) * c.slots + rank] = s_t[i];
+  }
+}
+
+__global__ void __launch_bounds__(256) fls_head_pack_weight_kernel(const uint16_t* w, uint64_t stride, uint16_t* out, uint32_t dim, uint32_t dp) {
+  const uint64_t v = blockIdx.x;
+  for (uint32_t i = threadIdx.x; i < dp; i += blockDim.x) out[v * dp + i] = i < dim ? w[v * stride + i] : uint16_t(0);
+}
+
+__device__ __forceinline__ double warp_sum(double x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  return x;
+}
+__device__ __forceinline__ double warp_max(double x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmax(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+  return x;
+}
+
+// 32 packed rows per block.  First the tile sums of each row are joined (coalesced: neighbouring threads are
+// neighbouring rows), then a warp takes a row: its own columns are added to the sums and give loss and gradient.
+// Sums and logarithms are double: a few thousand operations per row beside 2 V d of the products.
+constexpr int kRowsY = 16;
+__global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid_constant__ HeadCall c) {
+  __shared__ float sh_m[kRowsY][32];
+  __shared__ double sh_s[kRowsY][32], sh_s1[kRowsY][32], sh_z[kRowsY][32];
+  __shared__ float row_m[32];
+  __shared__ double sh_q[kRowsY][FLS_HEAD_MAX_TOP + 1];
+  __shared__ int32_t sh_i[kRowsY][FLS_HEAD_MAX_TOP + 1];
+  const uint32_t lane = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const uint32_t count = c.state->count, p0 = blockIdx.x * 32;
+  if (p0 >= count) return;
+  {
+    const uint32_t p = p0 + lane;         // packed rows up to the next multiple of 256 exist
+    float m = -INFINITY;
+    for (uint32_t t = y; t < c.tiles; t += kRowsY) m = fmaxf(m, c.part_m[uint64_t(t) * c.rows_cap + p]);
+    if (p < count)
+      for (uint32_t i = y; i < c.slots; i += kRowsY)
+        if (c.slot_idx[uint64_t(p) * c.slots + i] != INT_MAX) m = fmaxf(m, c.slot_z[uint64_t(p) * c.slots + i]);
+    sh_m[y][lane] = m;
+    __syncthreads();
+    for (int i = 0; i < kRowsY; ++i) m = fmaxf(m, sh_m[i][lane]);
+    if (y == 0) row_m[lane] = m;
+    const float base = m == -INFINITY ? 0.f : m;
+    double s = 0.0, s1 = 0.0, z = 0.0;
+    for (uint32_t t = y; t < c.tiles; t += kRowsY) {
+      const uint64_t at = uint64_t(t) * c.rows_cap + p;
+      const float tm = c.part_m[at], ts = c.part_s[at];
+      // a tile whose every column is left out has m = -inf and s = 0
+      s += double(ts) * (tm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(tm, c.cT) - __fmul_rn(base, c.cT))));
+      if (c.two) s1 += double(c.part_s1[at]) * (tm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(tm, c.c1) - __fmul_rn(base, c.c1))));
+      if (c.smooth) z += double(c.part_z[at]);
+    }
+    sh_s[y][lane] = s;
+    sh_s1[y][lane] = s1;
+    sh_z[y][lane] = z;
+    __syncthreads();
+  }
+  for (uint32_t q = y; q < 32; q += kRowsY) {
+    const uint32_t p = p0 + q;
+    if (p >= count) break;
+    const uint64_t n = uint64_t(c.src[p]);
+    const float mf = row_m[q];
+    const double M = mf == -INFINITY ? 0.0 : double(mf);
+    double denseT = 0.0, dense1 = 0.0, zsum = 0.0;
+    for (int i = 0; i < kRowsY; ++i) { denseT += sh_s[i][q]; dense1 += sh_s1[i][q]; zsum += sh_z[i][q]; }
+    if (!c.two) dense1 = denseT;
+    const int64_t label = c.use_label ? c.labels[n] : c.ignore_label;
+    const bool labelled = c.use_label && label != c.ignore_label;
+    const int32_t* idx = c.slot_idx + uint64_t(p) * c.slots;
+    const float* zs = c.slot_z + uint64_t(p) * c.slots;
+    const float* ts = c.slot_t + uint64_t(p) * c.slots;
+    float* gs = c.slot_g + uint64_t(p) * c.slots;
+
+    // the teacher's probabilities
+    double tmax = -INFINITY;
+    bool nan_t = false;
+    for (uint32_t i = lane; i < c.slots; i += 32)
+      if (idx[i] != INT_MAX && ts[i] != -INFINITY) { tmax = fmax(tmax, double(ts[i])); nan_t |= isnan(ts[i]); }
+    tmax = warp_max(tmax);
+    const bool taught = __any_sync(0xFFFFFFFFu, nan_t) || tmax != -INFINITY;
+    double norm = 0.0;
+    if (taught) {
+      if (c.tail_class) norm = double(c.teacher_lse[n]);
+      else {
+        double a = 0.0;
+        for (uint32_t i = lane; i < c.slots; i += 32)
+          if (idx[i] != INT_MAX && ts[i] != -INFINITY) a += exp((double(ts[i]) - tmax) * c.inv_temp);
+        norm = tmax * c.inv_temp + log(warp_sum(a));
+      }
+    }
+    // own columns: their exponentials, with those of the label apart from the rest
+    double ownT = 0.0, own1 = 0.0, outT = 0.0, eT_label = 0.0, e1_label = 0.0, z_label = 0.0, qsum = 0.0;
+    for (uint32_t i = lane; i < c.slots; i += 32) {
+      double qi = 0.0;
+      const int32_t x = idx[i];
+      if (x != INT_MAX) {
+        if (ts[i] != -INFINITY) { qi = exp(double(ts[i]) * c.inv_temp - norm); qsum += qi; }
+        const bool first = i == 0 || idx[i - 1] != x;
+        if (first) {
+          bool listed = false;
+          for (uint32_t j = i; j < c.slots && idx[j] == x; ++j) listed |= ts[j] != -INFINITY;
+          const double eT = exp((double(zs[i]) - M) * c.inv_temp), e1 = c.two ? exp(double(zs[i]) - M) : eT;
+          if (labelled && int64_t(x) == label) { eT_label = eT; e1_label = e1; z_label = double(zs[i]); }
+          else { ownT += eT; own1 += e1; }
+          if (!listed) outT += eT;             // the label outside the teacher's list belongs to the tail
+        }
+      }
+      sh_i[y][i] = x;
+      sh_q[y][i] = qi;
+    }
+    ownT = warp_sum(ownT); own1 = warp_sum(own1); outT = warp_sum(outT); qsum = warp_sum(qsum);
+    eT_label = warp_sum(eT_label); e1_label = warp_sum(e1_label); z_label = warp_sum(z_label);
+    __syncwarp();
+    const double restT = denseT + ownT, rest1 = dense1 + own1;         // everything but the label
+    const double totT = restT + eT_label, tot1 = rest1 + e1_label;
+    const double lseT = M * c.inv_temp + log(totT), lse1 = c.two ? M + log(tot1) : lseT;
+    // -log p_label; log1p where the label dominates: lse - z would cancel
+    const double nll = !labelled ? 0.0 : (rest1 < e1_label ? log1p(rest1 / e1_label) : (c.two ? lse1 - z_label : lseT - z_label * c.inv_temp));
+    const double w = c.row_weight ? double(c.row_weight[n]) : 1.0 / double(count);
+
+    if (c.top == 0) {
+      const double pl = e1_label / totT, ql = restT / totT, zl = 2.0 * c.z_loss * lseT, eps = c.smoothing;
+      if (lane == 0) {
+        double loss = (1.0 - eps) * nll + c.z_loss * lseT * lseT;
+        if (c.smooth) loss += eps * (lseT - zsum / double(c.vocab));
+        c.loss[n] = float(loss);
+        c.lse[n] = float(lseT);
+        c.coef[p] = make_float4(float(lseT * 1.4426950408889634), float(w * (1.0 + zl)), float(w * eps / double(c.vocab)), 0.f);
+        gs[0] = float(w * (-ql + zl * pl + eps - eps / double(c.vocab)));
+      }
+    } else {
+      double kl = 0.0;
+      for (uint32_t i = lane; i < c.slots; i += 32)
+        if (idx[i] != INT_MAX && ts[i] != -INFINITY) {
+          const double qi = sh_q[y][i];
+          if (qi != 0.0) kl += qi * ((double(ts[i]) * c.inv_temp - norm) - (double(zs[i]) * c.inv_temp - lseT));
+        }
+      kl = warp_sum(kl);
+      double damp = 1.0;
+      if (taught && c.tail_class) {
+        const double qt = fmax(0.0, 1.0 - qsum), tail = denseT + outT;
+        if (qt > 0.0) {
+          kl += qt * (log(qt) - (log(tail) - log(totT)));
+          damp = 1.0 - qt * totT / tail;
+        }
+      }
+      const double a = taught ? c.distill_weight * c.temp * w : 0.0, b = labelled ? c.label_weight * w : 0.0;
+      if (lane == 0) {
+        c.loss[n] = float((taught ? c.distill_weight * c.temp * c.temp * kl : 0.0) + (labelled ? c.label_weight * nll : 0.0));
+        c.lse[n] = float(lseT);
+        if (c.two) c.coef[p] = make_float4(float(lseT * 1.4426950408889634), float(a * damp), float(lse1 * 1.4426950408889634), float(b));
+        else c.coef[p] = make_float4(float(lseT * 1.4426950408889634), float(a * damp + b), 0.f, 0.f);
+      }
+      for (uint32_t i = lane; i < c.slots; i += 32) {
+        const int32_t x = sh_i[y][i];
+        if (x == INT_MAX) continue;
+        double qi = 0.0;
+        bool listed = false;
+        for (uint32_t j = i + 1; j-- > 0 && sh_i[y][j] == x;) { qi += sh_q[y][j]; listed |= ts[j] != -INFINITY; }
+        for (uint32_t j = i + 1; j < c.slots && sh_i[y][j] == x; ++j) { qi += sh_q[y][j]; listed |= ts[j] != -INFINITY; }
+        const double pT = exp(double(zs[i]) * c.inv_temp - lseT);
+        double v = a * (pT * (listed ? 1.0 : damp) - qi);
+        if (labelled) v += b * (int64_t(x) == label ? -rest1 / tot1 : (c.two ? exp(double(zs[i]) - lse1) : pT));
+        gs[i] = float(v);
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(128) fls_head_grad_hidden_kernel(const __grid_constant__ HeadCall c) {
+  const uint64_t n = blockIdx.x;
+  const int32_t p = c.pos[n];
+  uint16_t* out = c.grad_hidden + n * c.grad_hidden_stride;
+  const uint32_t count = c.state->count;
+  const uint32_t mt = (count + kHeadBM - 1) / kHeadBM, nt = (c.dim + kHeadBN - 1) / kHeadBN;
+  const uint32_t splits = head_splits(mt * nt, c.piece_cols / kHeadBK, c.clusters, c.max_splits);
+  const bool vec = c.dim % 8 == 0 && aligned16(out);
+  for (uint32_t i = threadIdx.x * 8; i < c.dim; i += blockDim.x * 8) {
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (p >= 0)
+      for (uint32_t s = 0; s < splits; ++s) {
+        const float4* x = reinterpret_cast<const float4*>(c.dh + (uint64_t(s) * c.rows_cap + p) * c.dcap + i);
+        const float4 a = x[0], b = x[1];
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+      }
+    if (vec)
+      *reinterpret_cast<uint4*>(out + i) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    else
+      for (uint32_t j = 0; j < 8 && i + j < c.dim; ++j) out[i + j] = bf16_bits(v[j]);
+  }
+}
+
+template <int MODE, bool TWO, bool SMOOTH>
+cudaError_t launch_gemm(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
+  auto* k = fls_head_gemm_kernel<MODE, TWO, SMOOTH>;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  k<<<2 * c.clusters, kGemmThreads, kSmemBytes, s>>>(m, c, p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t head_clusters(uint32_t* out) {
+  auto* k = fls_head_gemm_kernel<kStats, false, false>;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(2);
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  int n = 0;
+  e = cudaOccupancyMaxActiveClusters(&n, k, &cfg);
+  *out = uint32_t(n > 0 ? n : 1);
+  return e;
+}
+
+cudaError_t launch_head_rows_map(const HeadCall& c, cudaStream_t s) {
+  fls_head_map_kernel<<<1, 1024, 0, s>>>(c);
+  return cudaGetLastError();
+}
+cudaError_t launch_head_pack(const HeadCall& c, cudaStream_t s) {
+  fls_head_pack_kernel<<<c.rows_cap, 128, 0, s>>>(c);
+  return cudaGetLastError();
+}
+cudaError_t launch_head_pack_weight(const uint16_t* w, uint64_t stride, uint16_t* out, uint32_t vocab, uint32_t dim, uint32_t dp, cudaStream_t s) {
+  fls_head_pack_weight_kernel<<<vocab, 256, 0, s>>>(w, stride, out, dim, dp);
+  return cudaGetLastError();
+}
+cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t s) {
+  const HeadPiece p{0, c.vocab, 0};
+  if (c.two) return launch_gemm<kStats, true, false>(c, m, p, s);
+  if (c.smooth) return launch_gemm<kStats, false, true>(c, m, p, s);
+  return launch_gemm<kStats, false, false>(c, m, p, s);
+}
+cudaError_t launch_head_rows(const HeadCall& c, cudaStream_t s) {
+  fls_head_rows_kernel<<<c.rows_cap / 32, 32 * kRowsY, 0, s>>>(c);
+  return cudaGetLastError();
+}
+cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
+  return c.two ? launch_gemm<kDlogits, true, false>(c, m, p, s) : launch_gemm<kDlogits, false, false>(c, m, p, s);
+}
+cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
+  return launch_gemm<kGrads, false, false>(c, m, p, s);
+}
+cudaError_t launch_head_grad_hidden(const HeadCall& c, cudaStream_t s) {
+  fls_head_grad_hidden_kernel<<<uint32_t(c.rows), 128, 0, s>>>(c);
+  return cudaGetLastError();
+}
+
+}  // namespace fls

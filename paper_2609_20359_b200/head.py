@@ -1,0 +1,152 @@
+"""Head: the loss end of a language model on libfls (device memory and streams only).
+
+All arithmetic happens in libfls through the fls_head_* calls; this class owns one head handle, its workspace and the
+outputs, and checks the tensors it is given.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import _binding as fls
+
+
+def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: int, dtype: torch.dtype, device: torch.device):
+    """Checks a 2-D tensor whose rows are contiguous; returns (address, elements between rows)."""
+    if t.dtype != dtype or t.device != device or t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape [{'N' if rows is None else rows}, {cols}] on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous (stride {t.stride(1)})")
+    if t.shape[0] > 1 and t.stride(0) < cols:
+        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else cols)
+
+
+def _dense(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, device: torch.device):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _empty_on(stream, shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    """Memory whose reuse is ordered by the stream that writes it, which need not be torch's current one."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class Head:
+    """Losses of a linear head without kept logits.
+
+    max_rows, vocab, dim: N of the largest call, V and d.  top: teacher entries per row (0: no distillation).
+    grad_dtype: "bf16" or "f32", the type of weight gradients (as `Session`'s gradient buffers, whose units they may be
+    written into).  grads=False: a workspace for losses only.  any_weight: accept weights of any alignment and stride.
+
+    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  The workspace is
+    used by one call at a time: calls of one Head belong on one stream, or on streams ordered by events.
+    """
+
+    def __init__(self, max_rows: int, vocab: int, dim: int, top: int = 0, grad_dtype: str = "bf16", grads: bool = True,
+                 any_weight: bool = False, piece_bytes: int = 0, device: str = "cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("libfls needs a CUDA device; there is no CPU path")
+        if grad_dtype not in ("bf16", "f32"):
+            raise ValueError("grad_dtype must be 'bf16' or 'f32'")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        torch.cuda.set_device(self.device)
+        self.max_rows, self.vocab, self.dim, self.top = max_rows, vocab, dim, top
+        self.grad_torch_dtype = torch.float32 if grad_dtype == "f32" else torch.bfloat16
+        self.handle = None
+        self.handle = fls.fls_head_create(max_rows, vocab, dim, top, grads, fls.FLS_GRAD_F32 if grad_dtype == "f32" else fls.FLS_GRAD_BF16,
+                                          any_weight, piece_bytes)
+        self.layout = fls.fls_head_query(self.handle)
+        self.workspace = torch.empty(self.layout["workspace_bytes"], dtype=torch.uint8, device=self.device)
+        self.workspace[:256].zero_()
+
+    # ------------------------------------------------------------------ calls
+    def xent(self, hidden, weight, labels, ignore_label: int = -100, label_smoothing: float = 0.0, z_loss: float = 0.0, stream=None):
+        """(loss, lse) of every row, fp32."""
+        io, out = self._io(hidden, weight, labels, ignore_label, None, None, None, False, stream)
+        fls.fls_head_xent(self.handle, io, label_smoothing, z_loss, stream)
+        return out
+
+    def xent_step(self, hidden, weight, labels, grad_hidden=None, grad_weight=None, row_weight=None, accumulate: bool = False,
+                  ignore_label: int = -100, label_smoothing: float = 0.0, z_loss: float = 0.0, stream=None):
+        """(loss, lse); the gradients of sum(row_weight * loss) (default: the mean over the rows that take part) are written
+        to grad_hidden (bf16) and grad_weight, each optional; accumulate adds to grad_weight."""
+        io, out = self._io(hidden, weight, labels, ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream)
+        fls.fls_head_xent(self.handle, io, label_smoothing, z_loss, stream)
+        return out
+
+    def distill(self, hidden, weight, top_index, top_logit, labels=None, teacher_lse=None, temperature: float = 1.0,
+                distill_weight: float = 1.0, label_weight: float = 0.0, ignore_label: int = -100, stream=None):
+        """(loss, lse) against a teacher's top logits; teacher_lse given: what is outside the list counts as one class."""
+        return self._distill(hidden, weight, top_index, top_logit, labels, teacher_lse, temperature, distill_weight, label_weight,
+                             ignore_label, None, None, None, False, stream)
+
+    def distill_step(self, hidden, weight, top_index, top_logit, grad_hidden=None, grad_weight=None, row_weight=None,
+                     accumulate: bool = False, labels=None, teacher_lse=None, temperature: float = 1.0, distill_weight: float = 1.0,
+                     label_weight: float = 0.0, ignore_label: int = -100, stream=None):
+        """As distill, with gradients as in xent_step."""
+        return self._distill(hidden, weight, top_index, top_logit, labels, teacher_lse, temperature, distill_weight, label_weight,
+                             ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream)
+
+    def _distill(self, hidden, weight, top_index, top_logit, labels, teacher_lse, temperature, distill_weight, label_weight,
+                 ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream):
+        if label_weight and labels is None:
+            raise ValueError("label_weight needs labels")
+        io, out = self._io(hidden, weight, labels if label_weight else None, ignore_label, grad_hidden, grad_weight, row_weight, accumulate,
+                            stream)
+        n = io.rows
+        t = fls.fls_distill_desc(_dense(top_index, "top_index", (n, self.top), torch.int32, self.device),
+                                 _dense(top_logit, "top_logit", (n, self.top), torch.float32, self.device),
+                                 _dense(teacher_lse, "teacher_lse", (n,), torch.float32, self.device),
+                                 fls.FLS_TAIL_RENORM if teacher_lse is None else fls.FLS_TAIL_CLASS, 0, temperature, distill_weight,
+                                 label_weight)
+        fls.fls_head_distill(self.handle, io, t, stream)
+        return out
+
+    def _io(self, hidden, weight, labels, ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream):
+        dev = self.device
+        h, hs = _matrix(hidden, "hidden", None, self.dim, torch.bfloat16, dev)
+        n = hidden.shape[0]
+        w, ws = _matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16, dev)
+        gh, ghs = (None, 0) if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", n, self.dim, torch.bfloat16, dev)
+        gw, gws = (None, 0) if grad_weight is None else _matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype, dev)
+        out = _empty_on(stream, (2, n), torch.float32, dev)
+        loss = out.data_ptr()
+        io = fls.fls_head_io(n, h, w, _dense(labels, "labels", (n,), torch.int64, dev),
+                             _dense(row_weight, "row_weight", (n,), torch.float32, dev), loss, loss + 4 * n, gh, gw,
+                             self.workspace.data_ptr(), self.workspace.numel(), hs, ws, ghs, gws, ignore_label, int(accumulate), 0)
+        return io, (out[0], out[1])
+
+    # ------------------------------------------------------------------ what the device wrote beside the outputs
+    def _word(self, i: int) -> torch.Tensor:
+        off = fls.fls_head_get_state(self.workspace)[i] - self.workspace.data_ptr()
+        return self.workspace[off: off + 4].view(torch.int32)[0]
+
+    def status(self) -> int:
+        """FLS_STATUS_* bits of all calls so far (waits for the device)."""
+        return int(self._word(0).item())
+
+    def rows_taking_part(self) -> torch.Tensor:
+        """Rows of the last call that had a label or a teacher entry: a view on the device, rewritten by the next call."""
+        return self._word(1)
+
+    def close(self) -> None:
+        if self.handle is not None:
+            fls.fls_head_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
