@@ -473,6 +473,17 @@ int fls_head_get_state(const void* workspace, const uint32_t** dev_status, const
 /* Number of kernels this head has launched so far. */
 int fls_head_get_launch_count(const fls_head* head, uint64_t* launches);
 
+/* A teacher's top logits: for every row the `top` largest of its `vocab` logits in descending order, equal ones in
+ * ascending index, and lse = log sum_v exp(logit_v / temperature): what fls_head_distill takes (lse as teacher_lse).
+ * logits: device, rows x vocab, FLS_GRAD_BF16 or FLS_GRAD_F32 elements, any alignment of the element size, `stride`
+ * elements between rows (0: dense).  value / index: device, rows x top, dense; lse: device, rows.  -inf is never chosen:
+ * a row with fewer than `top` other logits ends with index -1 and value -inf, which fls_head_distill takes as absent.
+ * NaN ranks above everything; +0 and -0 are equal.  No workspace; one kernel, enqueued on cuda_stream.
+ * Errors: FLS_EINVAL (dtype, vocab outside 1 .. 2^30, rows > 2^24, top outside 1 .. FLS_HEAD_MAX_TOP, temperature,
+ * stride < vocab), FLS_EPTR (null, host or overlapping buffers), FLS_EALIGN, FLS_ECUDA. */
+int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t rows, uint64_t vocab, uint64_t stride, uint32_t top,
+                   double temperature, float* value, int32_t* index, float* lse, void* cuda_stream);
+
 /* Message of the last error on the calling thread ("" if none).  Host string owned by the library. */
 const char* fls_last_error(void);
 

@@ -37,7 +37,7 @@ EXPORTS = [
     "fls_plan_tune", "fls_plan_set_recompute", "fls_plan_set_single_pass", "fls_plan_set_overlap", "fls_set_profiling", "fls_get_kernel_ms", "fls_get_launch_count", "fls_plan_destroy",
     "fls_last_error", "fls_reduce_norm_noalloc",
     "fls_head_create", "fls_head_query", "fls_head_destroy", "fls_head_xent", "fls_head_distill", "fls_head_get_state",
-    "fls_head_get_launch_count",
+    "fls_head_get_launch_count", "fls_top_logits",
 ]
 
 
@@ -154,6 +154,7 @@ def _load() -> C.CDLL:
     lib.fls_head_distill.argtypes = [P, C.POINTER(fls_head_io), C.POINTER(fls_distill_desc), P]
     lib.fls_head_get_state.argtypes = [P, C.POINTER(P), C.POINTER(P)]
     lib.fls_head_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
+    lib.fls_top_logits.argtypes = [P, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint32, C.c_double, P, P, P, P]
     lib.fls_last_error.argtypes = []
     lib.fls_last_error.restype = C.c_char_p
     for name in EXPORTS:
@@ -452,3 +453,9 @@ def fls_head_get_launch_count(head: int) -> int:
     n = C.c_uint64()
     _check(lib.fls_head_get_launch_count(head, C.byref(n)))
     return n.value
+
+
+def fls_top_logits(logits, logit_dtype: int, rows: int, vocab: int, stride: int, top: int, temperature: float, value, index, lse,
+                   stream=None) -> None:
+    _check(lib.fls_top_logits(_ptr(logits), logit_dtype, rows, vocab, stride, top, temperature, _ptr(value), _ptr(index), _ptr(lse),
+                              _stream_handle(stream)))

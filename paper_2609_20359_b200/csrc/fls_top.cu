@@ -1,0 +1,490 @@
+// fls_top_logits: the k largest logits of every row, ties to the lowest index, and the row's log sum exp.
+//
+// One pass over the logits, and a second look at few of them.  A row (or, when there are few rows, one of 2, 4 or 8 parts
+// of a row, the CTAs of a cluster) belongs to a CTA of 512 threads.  While a thread adds up exponentials it keeps the
+// largest logit it has seen.  The k-th largest of the 512 maxima is a lower bound of the k-th largest logit, and a close
+// one: only k threads can have seen a larger one, and of what they saw about 512 ln(512 / (512 - k)) logits are expected
+// to reach it (69 for k = 64).  So only the hot threads' logits, k / 512 of the row and still in L2, are read again.  The
+// candidates are then ranked by counting, on 64-bit keys (value, lowest index first) that are all different, which makes
+// the result independent of the order in which they were found.  Rows with so many equal logits that the candidates do
+// not fit are searched bit by bit instead (fls_top_exact below).
+//
+// Bound by memory: 2 or 4 bytes per logit, read once.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdint>
+#include <cstdio>
+
+#include "fls.h"
+#include "fls_internal.h"
+
+namespace {
+
+constexpr int kTopThreads = 512;
+constexpr int kTopWarps = kTopThreads / 32;
+constexpr uint32_t kCap = 2048;              // candidates that are ranked directly
+constexpr uint32_t kNegInf = 0x007FFFFFu;    // order key of -inf; larger keys may be chosen
+
+struct TopArgs {
+  const void* logits;
+  uint64_t stride;
+  uint32_t vocab, top;
+  float c;                 // log2(e) / T
+  double inv_temp;
+  float* value;
+  int32_t* index;
+  float* lse;
+};
+
+// Monotone map of floats to unsigned integers; -0 equals +0, NaN ranks above everything.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  if (x != x) return 0xFFFFFFFFu;
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  if (k == 0xFFFFFFFFu) return __int_as_float(0x7FC00000);
+  return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
+}
+__device__ __forceinline__ uint64_t key64(uint32_t key, uint32_t idx) { return (uint64_t(key) << 32) | (0xFFFFFFFFu - idx); }
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ uint64_t remote_u64(uint32_t a) {
+  uint64_t x;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(x) : "r"(a) : "memory");
+  return x;
+}
+__device__ __forceinline__ float remote_f32(uint32_t a) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(a) : "memory");
+  return x;
+}
+// max that lets NaN through, so that a thread that met one is known
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int n = 4;
+  __device__ static __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
+    x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+  }
+  __device__ static __forceinline__ float top(const uint4& r) {
+    return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+  }
+  __device__ static __forceinline__ float load(const float* p) { return *p; }
+};
+template <> struct Vec<uint16_t> {
+  static constexpr int n = 8;
+  __device__ static __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  }
+  __device__ static __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  __device__ static __forceinline__ float top(const uint4& r) {
+    const uint32_t m = max2(max2(r.x, r.y), max2(r.z, r.w));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  __device__ static __forceinline__ float load(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
+};
+
+struct Shared {
+  uint64_t cand[kCap];
+  uint64_t best[FLS_HEAD_MAX_TOP];           // this part's result, read by the cluster's first CTA
+  uint64_t merged[8 * FLS_HEAD_MAX_TOP];
+  uint32_t hot[kTopThreads];
+  uint32_t scan[kTopWarps];
+  float wm[kTopWarps], ws[kTopWarps];
+  float m, s;
+  uint32_t n_hot, n_cand, count[3];
+};
+
+// The part of a row that a CTA works on: `lead` single elements, whole 16-byte vectors, `trail` single elements.
+template <typename T>
+struct Part {
+  const T* row;            // the whole row
+  const uint4* vec;        // first vector of the part
+  uint32_t vec0;           // index in the row of its first element
+  uint32_t n_vec;
+  uint32_t lead, trail;    // only the first part has `lead`, only the last `trail`
+  uint32_t trail0;         // index in the row of the first trailing element
+};
+
+// (a - b) / T in powers of two.  Sums are kept relative to 2^(m c), rounded, wherever that is finite; beyond kHuge (masks
+// of the type's lowest value) the difference is taken first.
+constexpr float kHuge = 1e37f;
+__device__ __forceinline__ float log2_ratio(float a, float b, float c) {
+  if (fabsf(a) < kHuge && fabsf(b) < kHuge) return __fmul_rn(a, c) - __fmul_rn(b, c);
+  return (a - b) * c;
+}
+
+// Adds one value to a running maximum and sum of exponentials.
+__device__ __forceinline__ void add_one(float x, float c, float& m, float& s) {
+  const float n = max_nan(m, x);
+  if (n == -INFINITY) return;
+  s = (m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, n, c))) + (x == -INFINITY ? 0.f : ex2(log2_ratio(x, n, c)));
+  m = n;
+}
+
+template <typename T, typename Body>
+__device__ __forceinline__ void for_each(const Part<T>& p, Body&& body) {
+  for (uint32_t i = threadIdx.x; i < p.n_vec; i += kTopThreads) {
+    float x[Vec<T>::n];
+    Vec<T>::unpack(p.vec[i], x);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::n; ++e) body(x[e], p.vec0 + i * Vec<T>::n + e);
+  }
+  if (threadIdx.x < p.lead) body(Vec<T>::load(p.row + threadIdx.x), threadIdx.x);
+  if (threadIdx.x < p.trail) body(Vec<T>::load(p.row + p.trail0 + threadIdx.x), p.trail0 + threadIdx.x);
+}
+
+// For rows with more than kCap candidates (many equal logits): the k-th largest key two bits at a time, then what is
+// above it, then the lowest indices of what equals it: 17 reads of the row, from L2.
+template <typename T>
+__device__ void fls_top_exact(const Part<T>& p, uint32_t top, Shared& sh) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t thr = 0;
+  for (int shift = 30; shift >= 0; shift -= 2) {
+    uint32_t n1 = 0, n2 = 0, n3 = 0;
+    const uint32_t t1 = thr | (1u << shift), t2 = thr | (2u << shift), t3 = thr | (3u << shift);
+    for_each(p, [&](float x, uint32_t) {
+      const uint32_t k = order_key(x);
+      if (k > kNegInf) { n1 += k >= t1; n2 += k >= t2; n3 += k >= t3; }
+    });
+    __syncthreads();
+    if (threadIdx.x < 3) sh.count[threadIdx.x] = 0;
+    __syncthreads();
+    n1 = __reduce_add_sync(0xFFFFFFFFu, n1);
+    n2 = __reduce_add_sync(0xFFFFFFFFu, n2);
+    n3 = __reduce_add_sync(0xFFFFFFFFu, n3);
+    if (lane == 0) { atomicAdd(&sh.count[0], n1); atomicAdd(&sh.count[1], n2); atomicAdd(&sh.count[2], n3); }
+    __syncthreads();
+    thr = sh.count[2] >= top ? t3 : sh.count[1] >= top ? t2 : sh.count[0] >= top ? t1 : thr;
+  }
+  // thr is the k-th largest key (or 0 when fewer than k may be chosen, and then all of them are above it)
+  __syncthreads();
+  if (threadIdx.x == 0) sh.n_cand = 0;
+  __syncthreads();
+  for_each(p, [&](float x, uint32_t idx) {
+    const uint32_t k = order_key(x);
+    if (k > kNegInf && k > thr) sh.cand[atomicAdd(&sh.n_cand, 1u)] = key64(k, idx);
+  });
+  __syncthreads();
+  uint32_t have = sh.n_cand;
+  __syncthreads();
+  if (thr <= kNegInf) return;
+  // equal keys in ascending index: lead, vectors, trail; one block-wide count per 512 vectors
+  auto take = [&](uint32_t n, auto&& visit) {
+    const uint32_t base = have;
+    uint32_t x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+      if (lane >= uint32_t(o)) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) sh.scan[warp] = x;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
+    for (int w = 0; w < kTopWarps; ++w) { if (w < int(warp)) before += sh.scan[w]; total += sh.scan[w]; }
+    uint32_t at = base + before + x - n;
+    if (n) visit(at);
+    have = min(base + total, top);
+  };
+  auto single = [&](uint32_t n, uint32_t first) {
+    const bool mine = threadIdx.x < n;
+    const bool eq = mine && order_key(Vec<T>::load(p.row + first + (mine ? threadIdx.x : 0))) == thr;
+    take(eq ? 1u : 0u, [&](uint32_t at) { if (at < top) sh.cand[at] = key64(thr, first + threadIdx.x); });
+  };
+  single(p.lead, 0);
+  for (uint32_t i0 = 0; i0 < p.n_vec && have < top; i0 += kTopThreads) {
+    const uint32_t i = i0 + threadIdx.x;
+    float x[Vec<T>::n];
+    uint32_t mask = 0;
+    if (i < p.n_vec) {
+      Vec<T>::unpack(p.vec[i], x);
+#pragma unroll
+      for (int e = 0; e < Vec<T>::n; ++e) mask |= uint32_t(order_key(x[e]) == thr) << e;
+    }
+    take(__popc(mask), [&](uint32_t at) {
+#pragma unroll
+      for (int e = 0; e < Vec<T>::n; ++e)
+        if ((mask >> e) & 1) {
+          if (at < top) sh.cand[at] = key64(thr, p.vec0 + i * Vec<T>::n + e);
+          ++at;
+        }
+    });
+  }
+  if (have < top) single(p.trail, p.trail0);
+  __syncthreads();
+  if (threadIdx.x == 0) sh.n_cand = have;
+  __syncthreads();
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __grid_constant__ TopArgs a) {
+  __shared__ Shared sh;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t rank, parts;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+  const uint64_t n = blockIdx.x / parts;
+  constexpr uint32_t VN = Vec<T>::n;
+  Part<T> p;
+  p.row = static_cast<const T*>(a.logits) + n * a.stride;
+  const uint32_t lead = min(a.vocab, uint32_t((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / uint32_t(sizeof(T)));
+  const uint32_t vecs = (a.vocab - lead) / VN;
+  const uint32_t v0 = uint32_t(uint64_t(vecs) * rank / parts), v1 = uint32_t(uint64_t(vecs) * (rank + 1) / parts);
+  p.vec0 = lead + v0 * VN;
+  p.vec = reinterpret_cast<const uint4*>(p.row + p.vec0);
+  p.n_vec = v1 - v0;
+  p.lead = rank == 0 ? lead : 0;
+  p.trail0 = lead + vecs * VN;
+  p.trail = rank == parts - 1 ? a.vocab - p.trail0 : 0;
+
+  // pass 1: maximum and sum of exponentials of what this thread reads
+  float m = -INFINITY, s = 0.f;
+  auto batch = [&](const uint4* r, int cnt) {
+    float t = Vec<T>::top(r[0]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j)
+      if (j < cnt) t = max_nan(t, Vec<T>::top(r[j]));
+    if (t > m || t != t) {                            // larger, or NaN, which stays
+      s = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, t, a.c));
+      m = t;
+    }
+    if (m == -INFINITY) return;
+    const bool huge = !(fabsf(m) < kHuge);
+    const float b = __fmul_rn(m, a.c);
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < cnt) {
+        float x[VN];
+        Vec<T>::unpack(r[j], x);
+        if (huge) {
+#pragma unroll
+          for (int e = 0; e < int(VN); ++e) s0 += ex2((x[e] - m) * a.c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < int(VN); e += 2) { s0 += ex2(fmaf(x[e], a.c, -b)); s1 += ex2(fmaf(x[e + 1], a.c, -b)); }
+        }
+      }
+    s += s0 + s1;
+  };
+  uint32_t i = threadIdx.x;
+  for (; i + 3 * kTopThreads < p.n_vec; i += 4 * kTopThreads) {
+    uint4 r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = p.vec[i + j * kTopThreads];
+    batch(r, 4);
+  }
+  for (; i < p.n_vec; i += kTopThreads) {
+    const uint4 r = p.vec[i];
+    batch(&r, 1);
+  }
+  const uint32_t key = order_key(m);                  // of the vectors only: the single elements are looked at below
+  if (threadIdx.x < p.lead) add_one(Vec<T>::load(p.row + threadIdx.x), a.c, m, s);
+  if (threadIdx.x < p.trail) add_one(Vec<T>::load(p.row + p.trail0 + threadIdx.x), a.c, m, s);
+  if (threadIdx.x == 0) sh.n_hot = sh.n_cand = 0;
+
+  // the block's maximum and sum
+  float bm = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) bm = max_nan(bm, __shfl_xor_sync(0xFFFFFFFFu, bm, o));
+  if (lane == 0) sh.wm[warp] = bm;
+  __syncthreads();
+  bm = sh.wm[lane % kTopWarps];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) bm = max_nan(bm, __shfl_xor_sync(0xFFFFFFFFu, bm, o));
+  float bs = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, bm, a.c));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) bs += __shfl_xor_sync(0xFFFFFFFFu, bs, o);
+  if (lane == 0) sh.ws[warp] = bs;
+
+  // the k-th largest of the 512 maxima, to 16 bits (any value that k maxima reach is a bound)
+  uint32_t thr = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t t = thr | (1u << bit);
+    if (__syncthreads_count(key >= t) >= int(a.top)) thr = t;
+  }
+  thr = max(thr, kNegInf + 1);
+  if (key >= thr) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
+  __syncthreads();
+
+  // pass 2: the hot threads' logits again
+  auto offer = [&](float x, uint32_t idx) {
+    const uint32_t k = order_key(x);
+    if (k >= thr) {
+      const uint32_t at = atomicAdd(&sh.n_cand, 1u);
+      if (at < kCap) sh.cand[at] = key64(k, idx);
+    }
+  };
+  const uint32_t per = (p.n_vec + kTopThreads - 1) / kTopThreads, items = sh.n_hot * per;
+  for (uint32_t w = threadIdx.x; w < items; w += kTopThreads) {
+    const uint32_t h = w / per, v = (w - h * per) * kTopThreads + sh.hot[h];
+    if (v < p.n_vec) {
+      float x[VN];
+      Vec<T>::unpack(p.vec[v], x);
+#pragma unroll
+      for (int e = 0; e < int(VN); ++e) offer(x[e], p.vec0 + v * VN + e);
+    }
+  }
+  if (threadIdx.x < p.lead) offer(Vec<T>::load(p.row + threadIdx.x), threadIdx.x);
+  if (threadIdx.x < p.trail) offer(Vec<T>::load(p.row + p.trail0 + threadIdx.x), p.trail0 + threadIdx.x);
+  __syncthreads();
+  if (sh.n_cand > kCap) fls_top_exact(p, a.top, sh);
+  const uint32_t cands = sh.n_cand;
+
+  // rank by counting: the keys are all different
+  auto put = [&](uint32_t r, uint64_t k) {
+    const bool none = k == 0;
+    a.value[n * a.top + r] = none ? -INFINITY : key_value(uint32_t(k >> 32));
+    a.index[n * a.top + r] = none ? -1 : int32_t(0xFFFFFFFFu - uint32_t(k));
+  };
+  for (uint32_t q = threadIdx.x; q < cands; q += kTopThreads) {
+    const uint64_t k = sh.cand[q];
+    uint32_t r = 0;
+    for (uint32_t j = 0; j < cands; ++j) r += sh.cand[j] > k;
+    if (r < a.top) { if (parts == 1) put(r, k); else sh.best[r] = k; }
+  }
+  for (uint32_t r = cands + threadIdx.x; r < a.top; r += kTopThreads) { if (parts == 1) put(r, 0); else sh.best[r] = 0; }
+  if (threadIdx.x == 0) {
+    float t = 0.f;
+    for (int w = 0; w < kTopWarps; ++w) t += sh.ws[w];
+    sh.m = bm;
+    sh.s = t;
+  }
+  auto put_lse = [&](float mm, double ss) {
+    a.lse[n] = mm == INFINITY ? INFINITY : mm == -INFINITY ? -INFINITY : float(double(mm) * a.inv_temp + log(ss));
+  };
+  if (parts == 1) {
+    if (threadIdx.x == 0) put_lse(sh.m, double(sh.s));
+    return;
+  }
+  // the cluster's first CTA joins the parts: a key's rank is the sum of its ranks in the sorted lists
+  cluster_sync();
+  if (rank == 0) {
+    for (uint32_t q = threadIdx.x; q < parts * a.top; q += kTopThreads) {
+      const uint32_t w = q / a.top;
+      sh.merged[q] = remote_u64(remote(&sh.best[q - w * a.top], w));
+    }
+    if (threadIdx.x == 0) {
+      float mm = -INFINITY;
+      for (uint32_t w = 0; w < parts; ++w) mm = max_nan(mm, remote_f32(remote(&sh.m, w)));
+      double ss = 0.0;
+      for (uint32_t w = 0; w < parts; ++w) {
+        const float pm = remote_f32(remote(&sh.m, w));
+        if (pm != -INFINITY) ss += double(remote_f32(remote(&sh.s, w))) * double(exp2f(log2_ratio(pm, mm, a.c)));
+      }
+      put_lse(mm, ss);
+    }
+  }
+  cluster_sync();
+  if (rank != 0) return;
+  for (uint32_t q = threadIdx.x; q < parts * a.top; q += kTopThreads) {
+    const uint64_t k = sh.merged[q];
+    uint32_t r = 0;
+    for (uint32_t w = 0; w < parts; ++w) {
+      const uint64_t* list = sh.merged + w * a.top;
+      uint32_t lo = 0, len = a.top;                   // first entry not above k
+      while (len) {
+        const uint32_t half = len >> 1;
+        if (list[lo + half] > k) { lo += half + 1; len -= half + 1; } else len = half;
+      }
+      r += lo;
+    }
+    if (k == 0)                                       // empty entries follow all others
+      for (uint32_t j = 0; j < q; ++j) r += sh.merged[j] == 0;
+    if (r < a.top) put(r, k);
+  }
+}
+
+int fail(int code, const char* fmt, ...) {
+  char buf[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  fls::set_last_error(buf);
+  return code;
+}
+
+int check_device(const void* p, uint64_t align, const char* what) {
+  if (!p) return fail(FLS_EPTR, "%s is null", what);
+  if (reinterpret_cast<uintptr_t>(p) % align) return fail(FLS_EALIGN, "%s must start on a %llu-byte boundary", what, (unsigned long long)align);
+  cudaPointerAttributes at{};
+  const cudaError_t e = cudaPointerGetAttributes(&at, p);
+  if (e != cudaSuccess) { cudaGetLastError(); return fail(FLS_ECUDA, "cudaPointerGetAttributes: %s", cudaGetErrorString(e)); }
+  if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged) return fail(FLS_EPTR, "%s is not device memory", what);
+  return FLS_OK;
+}
+
+}  // namespace
+
+extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t rows, uint64_t vocab, uint64_t stride, uint32_t top,
+                              double temperature, float* value, int32_t* index, float* lse, void* cuda_stream) {
+  if (logit_dtype != FLS_GRAD_BF16 && logit_dtype != FLS_GRAD_F32) return fail(FLS_EINVAL, "unknown logit_dtype %u", logit_dtype);
+  if (vocab < 1 || vocab > (1ull << 30)) return fail(FLS_EINVAL, "vocab must be in 1 .. 2^30");
+  if (rows > (1ull << 24)) return fail(FLS_EINVAL, "rows > 2^24");
+  if (top < 1 || top > FLS_HEAD_MAX_TOP) return fail(FLS_EINVAL, "top must be in 1 .. %d", FLS_HEAD_MAX_TOP);
+  if (!(std::isfinite(temperature) && temperature > 0.0)) return fail(FLS_EINVAL, "temperature must be finite and > 0");
+  if (stride == 0) stride = vocab;
+  if (stride < vocab || stride >= (1ull << 36)) return fail(FLS_EINVAL, "stride out of range");
+  if (rows == 0) return FLS_OK;
+  const uint64_t elem = logit_dtype == FLS_GRAD_F32 ? 4 : 2;
+  const struct { const void* p; uint64_t bytes, align; const char* what; } s[4] = {
+      {logits, ((rows - 1) * stride + vocab) * elem, elem, "logits"}, {value, rows * top * 4, 4, "value"},
+      {index, rows * top * 4, 4, "index"}, {lse, rows * 4, 4, "lse"}};
+  for (const auto& x : s)
+    if (int rc = check_device(x.p, x.align, x.what)) return rc;
+  for (int i = 1; i < 4; ++i)
+    for (int j = 0; j < i; ++j) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
+      if (a < b + s[j].bytes && b < a + s[i].bytes) return fail(FLS_EPTR, "%s overlaps %s", s[i].what, s[j].what);
+    }
+  TopArgs a{logits, stride, uint32_t(vocab), top, float(1.4426950408889634 / temperature), 1.0 / temperature, value, index, lse};
+  // Few rows: a row is shared by the CTAs of a cluster, as long as a thread still has a 16-byte vector or two to read.
+  uint32_t parts = 1;
+  while (parts < 8 && rows * parts * 2 <= 296 && vocab * elem >= uint64_t(parts) * 2 * kTopThreads * 16) parts *= 2;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(uint32_t(rows) * parts);
+  cfg.blockDim = dim3(kTopThreads);
+  cfg.stream = static_cast<cudaStream_t>(cuda_stream);
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = parts;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  const cudaError_t e = logit_dtype == FLS_GRAD_F32 ? cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<float>, a)
+                                                    : cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<uint16_t>, a);
+  if (e != cudaSuccess) return fail(FLS_ECUDA, "fls_top_logits: %s", cudaGetErrorString(e));
+  return FLS_OK;
+}

@@ -150,3 +150,35 @@ class Head:
             self.close()
         except Exception:
             pass
+
+
+class TopLogits:
+    """A teacher's top logits: for every row of [N, vocab] logits (bf16 or fp32, rows contiguous) the `top` largest in
+    descending order, equal ones in ascending index, and the row's log sum exp at `temperature`; the three outputs are what
+    `Head.distill` takes as top_logit, top_index and teacher_lse."""
+
+    def __init__(self, max_rows: int, vocab: int, top: int, device: str = "cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("libfls needs a CUDA device; there is no CPU path")
+        if not 1 <= top <= fls.FLS_HEAD_MAX_TOP:
+            raise ValueError(f"top must be in 1 .. {fls.FLS_HEAD_MAX_TOP}")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        torch.cuda.set_device(self.device)
+        self.max_rows, self.vocab, self.top = max_rows, vocab, top
+
+    def __call__(self, logits: torch.Tensor, temperature: float = 1.0, stream=None):
+        """(value fp32 [N, top], index int32 [N, top], lse fp32 [N])"""
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"logits must be bf16 or fp32, got {logits.dtype}")
+        ptr, stride = _matrix(logits, "logits", None, self.vocab, logits.dtype, self.device)
+        n = logits.shape[0]
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows, made for {self.max_rows}")
+        value = _empty_on(stream, (n, self.top), torch.float32, self.device)
+        index = _empty_on(stream, (n, self.top), torch.int32, self.device)
+        lse = _empty_on(stream, (n,), torch.float32, self.device)
+        fls.fls_top_logits(ptr, fls.FLS_GRAD_F32 if logits.dtype == torch.float32 else fls.FLS_GRAD_BF16, n, self.vocab, stride, self.top,
+                           temperature, value, index, lse, stream)
+        return value, index, lse
