@@ -12,6 +12,7 @@ namespace fls {
 constexpr int kHeadBM = 256;      // rows of C per CTA pair (128 per CTA)
 constexpr int kHeadBN = 256;      // columns of C per CTA pair; both CTAs hold all of them for their own rows
 constexpr int kHeadBK = 64;       // depth of one pipeline stage: 64 bf16 = one 128-byte swizzle row
+constexpr int kHeadStatCols = 128; // columns per partial sum of a row
 constexpr int kHeadMaxSplits = 64;
 
 // Head of the workspace: words the device writes.
@@ -30,7 +31,7 @@ struct HeadCall {
   float* slot_t;             // [rows_cap][slots]: the teacher's logit of that column (-inf: label only)
   float* slot_z;             // [rows_cap][slots]: the logit of that column
   float* slot_g;             // [rows_cap][slots]: its gradient
-  float* part_m;             // [tiles][rows_cap]: largest logit of a 256-column tile, slots left out
+  float* part_m;             // [tiles][rows_cap]: largest logit of 128 columns, slots left out
   float* part_s;             // [tiles][rows_cap]: sum of exp((z - m) / T)
   float* part_s1;            // same at temperature 1 (only when T != 1 and labels count)
   float* part_z;             // sum of the logits (only with label smoothing)
@@ -51,12 +52,15 @@ struct HeadCall {
   uint32_t piece_cols, planes;
   uint32_t tail_class, use_label, two, smooth, grad_f32, accumulate;
   uint32_t want_gh, want_gw;
+  uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, bf16 accumulation): plain stores
   uint32_t max_splits, clusters, group_m;
   float c1, cT;              // log2(e), log2(e) / T
   double inv_temp, temp, smoothing, z_loss, distill_weight, label_weight;
 };
 
-struct HeadMaps { CUtensorMap a0, b0, a1, b1; };
+// Operands of the products (kGrads: 0 for the weight's, 1 for the hidden gradient) and where tiles are stored: dL/dz, or
+// grad_weight (store) and the partial sums of grad_hidden (store2).
+struct HeadMaps { CUtensorMap a0, b0, a1, b1, store, store2; };
 
 // One launch of the tensor-core kernel.
 struct HeadPiece {

@@ -40,7 +40,7 @@ struct Regions {
 
 Regions regions(const fls_head_desc& d) {
   const uint64_t cap = up(std::max<uint64_t>(d.max_rows, 1), kHeadBM), dp = up(d.dim, 8), dcap = up(d.dim, kHeadBN);
-  const uint64_t slots = uint64_t(d.top) + 1, tiles = up(d.vocab, kHeadBN) / kHeadBN;
+  const uint64_t slots = uint64_t(d.top) + 1, tiles = up(d.vocab, kHeadBN) / kHeadStatCols;
   const uint64_t planes = d.grad_dtype == FLS_GRAD_F32 ? 2 : 1;
   Regions r{};
   uint64_t at = 256;
@@ -79,12 +79,12 @@ typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, v
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Row-major bf16 matrix, boxes of 64 columns x box_rows, 128-byte swizzle, zeros outside.
-bool encode(EncodeTiled f, CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t stride, uint32_t box_rows) {
+// Row-major bf16 or fp32 matrix, boxes of 128 bytes x box_rows, 128-byte swizzle, zeros outside.
+bool encode(EncodeTiled f, CUtensorMap* m, const void* base, uint64_t cols, uint64_t rows, uint64_t stride, uint32_t box_rows, bool f32 = false) {
   const cuuint64_t dims[2] = {cols, rows};
-  const cuuint64_t strides[1] = {stride * 2};
-  const cuuint32_t box[2] = {64, box_rows}, step[2] = {1, 1};
-  return f(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step,
+  const cuuint64_t strides[1] = {stride * (f32 ? 4 : 2)};
+  const cuuint32_t box[2] = {f32 ? 32u : 64u, box_rows}, step[2] = {1, 1};
+  return f(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step,
            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -195,7 +195,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.dp = uint32_t(up(d.dim, 8));
   c.dcap = uint32_t(up(d.dim, kHeadBN));
   c.slots = c.top + 1;
-  c.tiles = uint32_t(up(d.vocab, kHeadBN) / kHeadBN);
+  c.tiles = uint32_t(up(d.vocab, kHeadBN) / kHeadStatCols);
   c.grad_f32 = d.grad_dtype == FLS_GRAD_F32;
   c.accumulate = io->accumulate;
   c.want_gh = io->grad_hidden != nullptr && io->rows > 0;
@@ -207,6 +207,8 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.c1 = 1.4426950408889634f;
   c.cT = float(1.4426950408889634 * c.inv_temp);
   const bool grads = c.want_gh || c.want_gw;
+  c.direct_store = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 || c.grad_weight_stride * (c.grad_f32 ? 4 : 2) % 16 ||
+                   (c.accumulate && !c.grad_f32);
   if (grads) {
     c.piece_cols = piece_columns(d, r.g_bytes, c.rows_cap, c.planes);
     c.max_splits = uint32_t(std::min<uint64_t>(kHeadMaxSplits, r.dh_bytes / (uint64_t(c.rows_cap) * c.dcap * 4)));
@@ -222,11 +224,16 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   bool ok = encode(h->encode, &fwd.a0, c.hp, c.dp, c.rows_cap, c.dp, 128) && encode(h->encode, &fwd.b0, w, w_cols, d.vocab, w_stride, 128);
   fwd.a1 = fwd.a0;
   fwd.b1 = fwd.b0;
+  fwd.store = fwd.store2 = fwd.a0;
   if (ok && grads)
-    ok = encode(h->encode, &grad.a0, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 64) &&
+    ok = encode(h->encode, &fwd.store, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 32) &&
+         encode(h->encode, &grad.a0, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 64) &&
          encode(h->encode, &grad.b0, c.hp, c.dp, c.rows_cap, c.dp, 64) &&
          encode(h->encode, &grad.a1, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 128) &&
-         encode(h->encode, &grad.b1, w, w_cols, d.vocab, w_stride, 64);
+         encode(h->encode, &grad.b1, w, w_cols, d.vocab, w_stride, 64) &&
+         encode(h->encode, &grad.store2, c.dh, c.dcap, uint64_t(c.max_splits) * c.rows_cap, c.dcap, 32, true) &&
+         (!c.want_gw || c.direct_store ||
+          encode(h->encode, &grad.store, c.grad_weight, d.dim, d.vocab, c.grad_weight_stride, 32, c.grad_f32));
   if (!ok) return fail(FLS_ECUDA, "cuTensorMapEncodeTiled failed");
 
 #define FLS_LAUNCH(call)                                        \

@@ -19,11 +19,13 @@
 namespace fls {
 namespace {
 
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr uint32_t kOperandBytes = 128 * kHeadBK * 2;            // one operand of one stage of one CTA: 16 KB
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
-constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 + 256;
-constexpr int kGemmThreads = 256;                                // warp 0 TMA, 1 MMA, 2 TMEM, 4..7 epilogue
+constexpr int kEpiWarps = 8;                                     // two per lane quarter of TMEM, 128 columns each
+constexpr uint32_t kStoreBytes = 32 * 128;                       // one staged store of one warp: 32 rows of 128 bytes
+constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * 2 * kStoreBytes + 1024 + 256;
+constexpr int kGemmThreads = 128 + 32 * kEpiWarps;               // warp 0 TMA, 1 MMA, 2 TMEM, 4..11 epilogue
 constexpr uint32_t kWaitLimit = 1u << 22;                        // polls of an mbarrier before a role gives up
 enum { kStats = 0, kDlogits = 1, kGrads = 2 };
 
@@ -108,6 +110,18 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
                  "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
                  "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
                :: "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_add(const CUtensorMap* map, int x, int y, uint32_t src) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+__device__ __forceinline__ void st_shared(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void st_shared_u16(uint32_t a, uint16_t x) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(a), "h"(x) : "memory");
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -252,9 +266,10 @@ struct StatsRow {
         next = ptr < slots ? idx[ptr] : INT_MAX;
       } while (next == at);
     }
-    float cm = z[0];
+    float x0 = z[0], x1 = z[1], x2 = z[2], x3 = z[3];
 #pragma unroll
-    for (int j = 1; j < 32; ++j) cm = fmaxf(cm, z[j]);
+    for (int j = 4; j < 32; j += 4) { x0 = fmaxf(x0, z[j]); x1 = fmaxf(x1, z[j + 1]); x2 = fmaxf(x2, z[j + 2]); x3 = fmaxf(x3, z[j + 3]); }
+    const float cm = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
     if (cm > m) {
       const float old = m;
       m = cm;
@@ -286,15 +301,58 @@ struct StatsRow {
   }
 };
 
-__device__ __forceinline__ void store32_bf16(uint16_t* dst, const float (&v)[32]) {
-  uint4* o = reinterpret_cast<uint4*>(dst);
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-    o[q] = make_uint4(pack_bf16(v[8 * q], v[8 * q + 1]), pack_bf16(v[8 * q + 2], v[8 * q + 3]),
-                      pack_bf16(v[8 * q + 4], v[8 * q + 5]), pack_bf16(v[8 * q + 6], v[8 * q + 7]));
-}
 __device__ __forceinline__ float bf16_round(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+
+// A warp's way out: 32 rows x 128 bytes are written to shared memory in the layout that a TMA store with 128-byte
+// swizzle reads (16-byte piece q of row r at q ^ (r & 7): no bank conflicts), and leave as whole lines.  Two buffers.
+struct Stager {
+  uint32_t base, lane, next = 0;
+  __device__ __forceinline__ Stager(uint32_t b, uint32_t l) : base(b), lane(l) {}
+  // Buffer to write next.  Buffers alternate and every acquire is followed by one group (send or skip), so all groups but
+  // the last are older than the buffer's last store; with `both`, the two buffers are taken before anything is sent.
+  __device__ __forceinline__ uint32_t acquire(bool both = false) {
+    if (lane == 0) {
+      if (both) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    }
+    __syncwarp();
+    const uint32_t b = base + next * kStoreBytes;
+    next ^= 1;
+    return b;
+  }
+  __device__ __forceinline__ uint32_t piece(uint32_t buf, uint32_t q) const { return buf + lane * 128 + ((q ^ (lane & 7)) << 4); }
+  __device__ __forceinline__ void send(const CUtensorMap* map, int x, int y, uint32_t buf, bool add) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      if (add) tma_add(map, x, y, buf); else tma_store(map, x, y, buf);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+  __device__ __forceinline__ void skip() {
+    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+  __device__ __forceinline__ void drain() {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    __syncwarp();
+  }
+  // 32 columns as bf16 into the first or second half of a buffer's 64
+  __device__ __forceinline__ void put_bf16(uint32_t buf, uint32_t half, const float (&v)[32]) const {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      st_shared(piece(buf, half * 4 + q), pack_bf16(v[8 * q], v[8 * q + 1]), pack_bf16(v[8 * q + 2], v[8 * q + 3]),
+                pack_bf16(v[8 * q + 4], v[8 * q + 5]), pack_bf16(v[8 * q + 6], v[8 * q + 7]));
+  }
+  __device__ __forceinline__ void put_f32(uint32_t buf, const float (&v)[32]) const {
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      st_shared(piece(buf, q), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+  }
+  __device__ __forceinline__ void put_one(uint32_t buf, uint32_t col, uint16_t x) const {
+    st_shared_u16(piece(buf, col >> 3) + (col & 7) * 2, x);
+  }
+};
 
 // dL/dz of one row of a tile: aT exp(z/T - lse_T) + a1 exp(z - lse_1) - b, then the columns with a value of their own.
 template <bool TWO>
@@ -304,33 +362,32 @@ struct DlogitsRow {
   const int32_t* idx;
   const float* val;
   uint32_t ptr, slots;
-  uint16_t* out;     // this row's columns of the piece, from the tile's first on
-  uint64_t plane;    // elements from the first to the second plane (fp32 weight gradients), else 0
-  __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int32_t col0, int32_t n0, uint32_t vocab, float cT, float c1) {
+  // the first (half 0) or second 32 of the 64 columns from col0 on; lo: buffer of the second term, 0 if there is none
+  __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int32_t col0, uint32_t half, uint32_t vocab, float cT, float c1,
+                                        const Stager& out, uint32_t hi, uint32_t lo) {
     float v[32];
+    const int32_t c0 = col0 + int32_t(half) * 32;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
       const float z = __uint_as_float(r[j]);
       if constexpr (TWO) v[j] = fmaf(k.w, ex2(fmaf(z, c1, -k.z)), k.y * ex2(fmaf(z, cT, -k.x)));
       else v[j] = fmaf(k.y, ex2(fmaf(z, cT, -k.x)), -k.z);
     }
-    if (uint32_t(col0) + 32 > vocab) {
+    if (uint32_t(c0) + 32 > vocab) {
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (uint32_t(col0 + j) >= vocab) v[j] = 0.f;
+        if (uint32_t(c0 + j) >= vocab) v[j] = 0.f;
     }
-    uint16_t* o = out + (col0 - n0);
-    store32_bf16(o, v);
-    if (plane) {
+    out.put_bf16(hi, half, v);
+    if (lo) {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] -= bf16_round(v[j]);
-      store32_bf16(o + plane, v);
+      out.put_bf16(lo, half, v);
     }
-    while (next < col0 + 32) {          // same thread, same address, after the store above
+    while (next < c0 + 32) {            // same thread, same address, after the store above
       const float x = val[ptr];
-      uint16_t* at = out + (next - n0);
-      at[0] = bf16_bits(x);
-      if (plane) at[plane] = bf16_bits(x - bf16_round(x));
+      out.put_one(hi, uint32_t(next - col0), bf16_bits(x));
+      if (lo) out.put_one(lo, uint32_t(next - col0), bf16_bits(x - bf16_round(x)));
       ++ptr;
       next = ptr < slots ? idx[ptr] : INT_MAX;
     }
@@ -395,7 +452,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadCall c, const HeadPiece piece) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  Barriers* bars = reinterpret_cast<Barriers*>(tiles + kStages * kStageBytes);
+  Barriers* bars = reinterpret_cast<Barriers*>(tiles + kStages * kStageBytes + kEpiWarps * 2 * kStoreBytes);
   const uint32_t tile_base = smem_u32(tiles);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
@@ -403,7 +460,7 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars->acc_full[i]), 1); mbar_init(smem_u32(&bars->acc_empty[i]), 8); }
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars->acc_full[i]), 1); mbar_init(smem_u32(&bars->acc_empty[i]), 2 * kEpiWarps); }
     bars->gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -486,13 +543,20 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
       }
     }
   } else if (warp >= 4) {
-    const uint32_t quarter = warp & 3;
-    const uint32_t lane_base = tmem + ((quarter * 32) << 16);
+    const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;    // 32 rows, 128 of the tile's columns
+    const uint32_t lane_base = tmem + ((quarter * 32) << 16) + half * 128;
+    Stager out(tile_base + kStages * kStageBytes + (warp - 4) * 2 * kStoreBytes, lane);
     uint32_t buf = 0, phase = 0;
     for (uint32_t u = cluster; u < plan.n_units; u += n_clusters) {
       const Unit w = plan.at(u);
       const bool empty = w.kbn == 0;
-      const uint32_t row = w.m0 + rank * 128 + quarter * 32 + lane;
+      const uint32_t row0 = w.m0 + rank * 128 + quarter * 32, row = row0 + lane;
+      const uint32_t n0 = w.n0 + half * 128;
+      // Rows nobody reads are left out: beyond the rows that take part, for dL/dz beyond the depth of the weight product.
+      bool work = true;
+      if constexpr (MODE == kStats) work = row0 < count;
+      if constexpr (MODE == kDlogits) work = row0 < (count + kHeadBK - 1) / kHeadBK * kHeadBK;
+      if constexpr (MODE == kGrads) work = w.grad_hidden ? row0 < count : (row0 < piece.width && n0 < c.dim);
       // what the tile's rows need besides the accumulator is fetched before the wait
       StatsRow<TWO, SMOOTH> st;
       DlogitsRow<TWO> dl;
@@ -502,7 +566,7 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         st.slots = c.slots;
         st.ptr = c.slots;
         if (row < count) {
-          st.ptr = lower_slot(st.idx, c.slots, int32_t(w.n0));
+          st.ptr = lower_slot(st.idx, c.slots, int32_t(n0));
           st.next = st.ptr < c.slots ? st.idx[st.ptr] : INT_MAX;
         }
       } else if constexpr (MODE == kDlogits) {
@@ -511,11 +575,9 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         dl.slots = c.slots;
         dl.ptr = c.slots;
         dl.k = make_float4(0.f, 0.f, 0.f, 0.f);
-        dl.out = c.g + uint64_t(row) * c.piece_cols + w.n0;
-        dl.plane = c.planes == 2 ? uint64_t(c.rows_cap) * c.piece_cols : 0;
         if (row < count) {
           dl.k = c.coef[row];
-          dl.ptr = lower_slot(dl.idx, c.slots, int32_t(piece.v0 + w.n0));
+          dl.ptr = lower_slot(dl.idx, c.slots, int32_t(piece.v0 + n0));
           dl.next = dl.ptr < c.slots ? dl.idx[dl.ptr] : INT_MAX;
         }
       }
@@ -526,59 +588,87 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         fence_after();
       }
       const uint32_t acc = lane_base + buf * kHeadBN;
-      uint32_t ra[32], rb[32];
+      uint32_t ra[32], rb[32], hi = 0, lo = 0;
+      // chunk 0..3: 32 columns each
       auto process = [&](uint32_t (&r)[32], uint32_t chunk) {
-        const int32_t n = int32_t(w.n0 + chunk * 32);
+        const uint32_t n = n0 + chunk * 32;
         if constexpr (MODE == kStats) {
-          st.chunk(r, n, c.vocab, c.cT, c.c1);
+          st.chunk(r, int32_t(n), c.vocab, c.cT, c.c1);
         } else if constexpr (MODE == kDlogits) {
-          dl.chunk(r, int32_t(piece.v0) + n, int32_t(piece.v0 + w.n0), c.vocab, c.cT, c.c1);
+          if (!(chunk & 1)) { hi = out.acquire(c.planes == 2); if (c.planes == 2) lo = out.acquire(true); }
+          dl.chunk(r, int32_t(piece.v0 + n0 + (chunk & 2) * 32), chunk & 1, c.vocab, c.cT, c.c1, out, hi, lo);
+          if (chunk & 1) {
+            out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(row0), hi, false);
+            if (lo) out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(c.rows_cap + row0), lo, false);
+          }
         } else {
           float v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = empty ? 0.f : __uint_as_float(r[j]);
           if (w.grad_hidden) {
-            // [split][rows_cap][dcap]: whole tiles exist, nothing to guard
-            float* o = c.dh + (uint64_t(w.split) * c.rows_cap + row) * c.dcap + n;
-            if (!empty || piece.first) store_row32<float>(o, v, 32, !piece.first);
-          } else if (row < piece.width && uint32_t(n) < c.dim) {
-            const uint64_t at = uint64_t(piece.v0 + row) * c.grad_weight_stride + n;
-            const uint32_t left = c.dim - uint32_t(n);
-            if (c.grad_f32) store_row32<float>(static_cast<float*>(c.grad_weight) + at, v, left, c.accumulate);
-            else store_row32<uint16_t>(static_cast<uint16_t*>(c.grad_weight) + at, v, left, c.accumulate);
+            // [split][rows_cap][dcap]; pieces after the first add to their split's sums, one after the other
+            if (!empty || piece.first) {
+              hi = out.acquire();
+              out.put_f32(hi, v);
+              out.send(&maps.store2, int(n), int(w.split * c.rows_cap + row0), hi, !piece.first);
+            }
+          } else if (c.direct_store) {
+            if (row < piece.width && n < c.dim) {
+              const uint64_t at = uint64_t(piece.v0 + row) * c.grad_weight_stride + n;
+              const uint32_t left = c.dim - n;
+              if (c.grad_f32) store_row32<float>(static_cast<float*>(c.grad_weight) + at, v, left, c.accumulate);
+              else store_row32<uint16_t>(static_cast<uint16_t*>(c.grad_weight) + at, v, left, c.accumulate);
+            }
+          } else if (c.grad_f32) {
+            hi = out.acquire();
+            out.put_f32(hi, v);
+            if (n < c.dim) out.send(&maps.store, int(n), int(piece.v0 + row0), hi, c.accumulate); else out.skip();
+          } else {
+            if (!(chunk & 1)) hi = out.acquire();
+            out.put_bf16(hi, chunk & 1, v);
+            if (chunk & 1) {
+              if (n - 32 < c.dim) out.send(&maps.store, int(n - 32), int(piece.v0 + row0), hi, false); else out.skip();
+            }
           }
         }
         __syncwarp();
       };
       if (empty) {
+        if (work) {
 #pragma unroll 1
-        for (uint32_t chunk = 0; chunk < 8; ++chunk) process(ra, chunk);
+          for (uint32_t chunk = 0; chunk < 4; ++chunk) process(ra, chunk);
+        }
         continue;
       }
-      tmem_load(acc, ra);
+      if (work) tmem_load(acc, ra);
 #pragma unroll 1
-      for (uint32_t chunk = 0; chunk < 8; chunk += 2) {
-        tmem_wait(ra);
-        tmem_load(acc + (chunk + 1) * 32, rb);
-        process(ra, chunk);
-        tmem_wait(rb);
-        if (chunk + 2 < 8) {
-          tmem_load(acc + (chunk + 2) * 32, ra);
+      for (uint32_t chunk = 0; chunk < 4; chunk += 2) {
+        if (work) {
+          tmem_wait(ra);
+          tmem_load(acc + (chunk + 1) * 32, rb);
+          process(ra, chunk);
+          tmem_wait(rb);
+        }
+        if (chunk + 2 < 4) {
+          if (work) tmem_load(acc + (chunk + 2) * 32, ra);
         } else {
           fence_before();                       // the accumulator is in registers: the next product may overwrite it
           if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&bars->acc_empty[buf])));
         }
-        process(rb, chunk + 1);
+        if (work) process(rb, chunk + 1);
       }
       if constexpr (MODE == kStats) {
-        const uint64_t at = uint64_t((piece.v0 + w.n0) / kHeadBN) * c.rows_cap + row;
-        c.part_m[at] = st.m;
-        c.part_s[at] = st.s;
-        if constexpr (TWO) c.part_s1[at] = st.s1;
-        if constexpr (SMOOTH) c.part_z[at] = st.sz;
+        if (work) {
+          const uint64_t at = uint64_t(n0 / kHeadStatCols) * c.rows_cap + row;
+          c.part_m[at] = st.m;
+          c.part_s[at] = st.s;
+          if constexpr (TWO) c.part_s1[at] = st.s1;
+          if constexpr (SMOOTH) c.part_z[at] = st.sz;
+        }
       }
       if (++buf == 2) { buf = 0; phase ^= 1; }
     }
+    out.drain();
   }
   if (!ok) {
     atomicOr(&c.state->status, uint32_t(FLS_STATUS_WAIT_EXPIRED));
