@@ -19,6 +19,7 @@ constexpr int kHeadMaxSplits = 64;
 struct HeadState {
   uint32_t status;   // FLS_STATUS_* bits, sticky
   uint32_t count;    // rows of the last call that take part (label or teacher entry present)
+  uint32_t splits;   // parts of the hidden gradient's depth, 1 .. kHeadMaxSplits
 };
 
 // Everything the kernels of one call share.  Packed row p stands for row src[p] of the caller.

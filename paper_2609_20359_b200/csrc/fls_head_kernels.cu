@@ -53,7 +53,7 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // False if the phase did not complete within kWaitLimit polls (each poll may sleep in hardware for a while).
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
@@ -61,7 +61,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     if (ok) return true;
@@ -90,26 +90,19 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// 32 columns of this thread's row of an accumulator.
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
+// 32 columns of this thread's row of an accumulator.  The wait is part of the statement: registers handed through a
+// separate wait would be copied once per value.
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&r)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+        "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
+        "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
+        "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
       : "r"(addr) : "memory");
-}
-// Waits for this thread's tmem_load calls; the registers pass through so that no use of them moves above it.
-__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
-                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
-                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :: "memory");
 }
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, int x, int y, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
@@ -157,13 +150,21 @@ struct Unit {
   uint32_t split;
 };
 
-// How many parts the depth of the hidden gradient (the piece's columns) is cut into: so many that one part is at most
-// an eighth of a cluster's share of the launch, which keeps the last round of the persistent grid short.
-__host__ __device__ inline uint32_t head_splits(uint32_t tiles, uint32_t depth_blocks, uint32_t clusters, uint32_t max_splits) {
-  uint32_t s = (4 * clusters + tiles - 1) / (tiles ? tiles : 1);
-  if (s > depth_blocks / 4) s = depth_blocks / 4;
-  if (s > max_splits) s = max_splits;
-  return s ? s : 1;
+// The hidden gradient's depth (a piece's columns) is cut into `s` parts, each with partial sums of its own.  A cluster
+// works through units u, u + clusters, ...: first those of the hidden gradient (tiles_h * s of kb_h / s blocks), then
+// those of the weight gradient (tiles_w of kb_w blocks).  Time of the busiest cluster in blocks of depth, with kUnitCost
+// for what a unit costs besides its products (its epilogue's tail, the partial sums written and read again).
+constexpr uint32_t kUnitCost = 6;
+__device__ __forceinline__ uint32_t head_makespan(uint32_t s, uint32_t tiles_h, uint32_t kb_h, uint32_t tiles_w, uint32_t kb_w, uint32_t clusters) {
+  const uint32_t units_h = tiles_h * s, units = units_h + tiles_w;
+  const uint32_t len_h = (kb_h + s - 1) / s + kUnitCost, len_w = kb_w + kUnitCost;
+  uint32_t worst = 0;
+  for (int i = 0; i < 2; ++i) {          // the first cluster, and the first one with a unit less of the hidden gradient
+    const uint32_t c = i ? units_h % clusters : 0;
+    const uint32_t nh = (units_h + clusters - 1 - c) / clusters, nu = (units + clusters - 1 - c) / clusters;
+    worst = max(worst, nh * len_h + (nu - nh) * len_w);
+  }
+  return worst;
 }
 
 template <int MODE>
@@ -177,7 +178,7 @@ struct Schedule {
       nt = (c.dim + kHeadBN - 1) / kHeadBN;
       kb = (count + kHeadBK - 1) / kHeadBK;
       kb_gh = (p.width + kHeadBK - 1) / kHeadBK;
-      splits = head_splits(mt * nt, c.piece_cols / kHeadBK, c.clusters, c.max_splits);
+      splits = c.state->splits;
       n_gh = c.want_gh ? mt * nt * splits : 0;
       n_units = n_gh + (c.want_gw ? (p.width + kHeadBM - 1) / kHeadBM * nt : 0);
     } else {
@@ -237,10 +238,7 @@ struct StatsRow {
   const int32_t* idx;
   float* zs;
   uint32_t ptr, slots;
-  __device__ __forceinline__ void chunk(uint32_t (&r)[32], int32_t col0, uint32_t vocab, float cT, float c1) {
-    float z[32];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(r[j]);
+  __device__ __forceinline__ void chunk(float (&z)[32], int32_t col0, uint32_t vocab, float cT, float c1) {
     const bool edge = uint32_t(col0) + 32 > vocab;
     if constexpr (SMOOTH) {
       float t = 0.f;
@@ -363,13 +361,12 @@ struct DlogitsRow {
   const float* val;
   uint32_t ptr, slots;
   // the first (half 0) or second 32 of the 64 columns from col0 on; lo: buffer of the second term, 0 if there is none
-  __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int32_t col0, uint32_t half, uint32_t vocab, float cT, float c1,
+  __device__ __forceinline__ void chunk(float (&v)[32], int32_t col0, uint32_t half, uint32_t vocab, float cT, float c1,
                                         const Stager& out, uint32_t hi, uint32_t lo) {
-    float v[32];
     const int32_t c0 = col0 + int32_t(half) * 32;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-      const float z = __uint_as_float(r[j]);
+      const float z = v[j];
       if constexpr (TWO) v[j] = fmaf(k.w, ex2(fmaf(z, c1, -k.z)), k.y * ex2(fmaf(z, cT, -k.x)));
       else v[j] = fmaf(k.y, ex2(fmaf(z, cT, -k.x)), -k.z);
     }
@@ -588,23 +585,20 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         fence_after();
       }
       const uint32_t acc = lane_base + buf * kHeadBN;
-      uint32_t ra[32], rb[32], hi = 0, lo = 0;
+      uint32_t hi = 0, lo = 0;
       // chunk 0..3: 32 columns each
-      auto process = [&](uint32_t (&r)[32], uint32_t chunk) {
+      auto process = [&](float (&v)[32], uint32_t chunk) {
         const uint32_t n = n0 + chunk * 32;
         if constexpr (MODE == kStats) {
-          st.chunk(r, int32_t(n), c.vocab, c.cT, c.c1);
+          st.chunk(v, int32_t(n), c.vocab, c.cT, c.c1);
         } else if constexpr (MODE == kDlogits) {
           if (!(chunk & 1)) { hi = out.acquire(c.planes == 2); if (c.planes == 2) lo = out.acquire(true); }
-          dl.chunk(r, int32_t(piece.v0 + n0 + (chunk & 2) * 32), chunk & 1, c.vocab, c.cT, c.c1, out, hi, lo);
+          dl.chunk(v, int32_t(piece.v0 + n0 + (chunk & 2) * 32), chunk & 1, c.vocab, c.cT, c.c1, out, hi, lo);
           if (chunk & 1) {
             out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(row0), hi, false);
             if (lo) out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(c.rows_cap + row0), lo, false);
           }
         } else {
-          float v[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = empty ? 0.f : __uint_as_float(r[j]);
           if (w.grad_hidden) {
             // [split][rows_cap][dcap]; pieces after the first add to their split's sums, one after the other
             if (!empty || piece.first) {
@@ -636,26 +630,24 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
       if (empty) {
         if (work) {
 #pragma unroll 1
-          for (uint32_t chunk = 0; chunk < 4; ++chunk) process(ra, chunk);
+          for (uint32_t chunk = 0; chunk < 4; ++chunk) {
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = 0.f;
+            process(v, chunk);
+          }
         }
         continue;
       }
-      if (work) tmem_load(acc, ra);
 #pragma unroll 1
-      for (uint32_t chunk = 0; chunk < 4; chunk += 2) {
-        if (work) {
-          tmem_wait(ra);
-          tmem_load(acc + (chunk + 1) * 32, rb);
-          process(ra, chunk);
-          tmem_wait(rb);
-        }
-        if (chunk + 2 < 4) {
-          if (work) tmem_load(acc + (chunk + 2) * 32, ra);
-        } else {
-          fence_before();                       // the accumulator is in registers: the next product may overwrite it
+      for (uint32_t chunk = 0; chunk < 4; ++chunk) {
+        float v[32];
+        if (work) tmem_load(acc + chunk * 32, v);
+        if (chunk == 3) {                       // the accumulator is in registers: the next product may overwrite it
+          fence_before();
           if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&bars->acc_empty[buf])));
         }
-        if (work) process(rb, chunk + 1);
+        if (work) process(v, chunk);
       }
       if constexpr (MODE == kStats) {
         if (work) {
@@ -810,6 +802,15 @@ __global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid
   __shared__ int32_t sh_i[kRowsY][FLS_HEAD_MAX_TOP + 1];
   const uint32_t lane = threadIdx.x & 31, y = threadIdx.x >> 5;
   const uint32_t count = c.state->count, p0 = blockIdx.x * 32;
+  if (blockIdx.x == 0 && y == kRowsY - 1 && c.piece_cols) {     // how the gradient launches of this call split their depth
+    const uint32_t nt = (c.dim + kHeadBN - 1) / kHeadBN, th = (count + kHeadBM - 1) / kHeadBM * nt, kb_h = c.piece_cols / kHeadBK;
+    const uint32_t tw = c.piece_cols / kHeadBM * nt, kb_w = (count + kHeadBK - 1) / kHeadBK * c.planes;
+    uint32_t best = 0xFFFFFFFFu;
+    for (uint32_t s = lane + 1; s <= min(c.max_splits, kb_h); s += 32)
+      best = min(best, min(head_makespan(s, th, kb_h, tw, kb_w, c.clusters), 0x3FFFFFFu) << 6 | (s - 1));
+    best = __reduce_min_sync(0xFFFFFFFFu, best);
+    if (lane == 0) c.state->splits = (best & 63) + 1;
+  }
   if (p0 >= count) return;
   {
     const uint32_t p = p0 + lane;         // packed rows up to the next multiple of 256 exist
@@ -953,9 +954,7 @@ __global__ void __launch_bounds__(128) fls_head_grad_hidden_kernel(const __grid_
   const uint64_t n = blockIdx.x;
   const int32_t p = c.pos[n];
   uint16_t* out = c.grad_hidden + n * c.grad_hidden_stride;
-  const uint32_t count = c.state->count;
-  const uint32_t mt = (count + kHeadBM - 1) / kHeadBM, nt = (c.dim + kHeadBN - 1) / kHeadBN;
-  const uint32_t splits = head_splits(mt * nt, c.piece_cols / kHeadBK, c.clusters, c.max_splits);
+  const uint32_t splits = c.state->splits;
   const bool vec = c.dim % 8 == 0 && aligned16(out);
   for (uint32_t i = threadIdx.x * 8; i < c.dim; i += blockDim.x * 8) {
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
