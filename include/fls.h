@@ -375,9 +375,9 @@ int fls_plan_destroy(fls_plan* plan);
  * A head maps hidden states h (N x d, bf16) with a weight W (V x d, bf16: a view of fls_buffers.param_bf16, or any
  * other buffer) to logits z = h W^T over a vocabulary of V entries.  The calls below compute a loss of every row and,
  * on request, the gradients of the weighted sum  L = sum_n w_n loss_n  with respect to h and W, without ever holding the
- * N x V logits: a first pass keeps per row and per 256 columns the maximum and the sum of exponentials, the gradient
- * passes form the logits of one piece of the vocabulary again, turn them into dL/dz (bf16) in the workspace and multiply
- * that by W and h.  Products are bf16 tensor-core products with fp32 accumulation; maxima, sums and losses are held in
+ * N x V logits (beyond a workspace of fixed size): a first pass keeps per row and per 128 columns the maximum and the sum
+ * of exponentials, the gradient passes turn the logits of one piece of the vocabulary, formed again or for the last piece
+ * still there, into dL/dz (bf16) in the workspace and multiply that by W and h.  Products are bf16 tensor-core products with fp32 accumulation; maxima, sums and losses are held in
  * fp32 / double; dL/dz is rounded to bf16 once before its products (with fp32 weight gradients it enters the product
  * with h as two bf16 terms, about 17 bits).  Results do not change from run to run.
  *
@@ -411,14 +411,16 @@ typedef struct {
                            and have any row stride; 0: the weight must start on a 16-byte boundary and its stride be a
                            multiple of 8 elements.  dim not a multiple of 8 implies 1                           */
   uint32_t reserved;    /* 0                                                                                    */
-  uint64_t piece_bytes; /* workspace for dL/dz of one piece of the vocabulary; 0: 256 MiB.  Larger pieces mean fewer
-                           launches; a piece has at least 512 columns                                           */
+  uint64_t piece_bytes; /* workspace for one piece of the vocabulary; 0: 1 GiB.  The logits of the last columns, as many
+                           as fit at 4 bytes each, are formed once, those before them twice, in pieces of 2 bytes per
+                           column (fp32 weight gradients: 4); a piece has at least 512 columns                  */
 } fls_head_desc;
 
 typedef struct {
   uint64_t workspace_bytes;
-  uint64_t piece_cols;  /* columns of the vocabulary per piece at max_rows                                      */
-  uint64_t pieces;      /* ceil(V / piece_cols) at max_rows                                                     */
+  uint64_t kept_cols;   /* at max_rows: columns at the end of the vocabulary whose logits are formed once        */
+  uint64_t piece_cols;  /* at max_rows: columns per piece of the others, 0 if there are none                     */
+  uint64_t pieces;      /* at max_rows: pieces of the others                                                     */
 } fls_head_layout;
 
 /* One call's data.  All buffers are device memory of the current device; strides count elements between rows, 0 means

@@ -90,7 +90,7 @@ class fls_head_desc(C.Structure):
 
 
 class fls_head_layout(C.Structure):
-    _fields_ = [("workspace_bytes", C.c_uint64), ("piece_cols", C.c_uint64), ("pieces", C.c_uint64)]
+    _fields_ = [(n, C.c_uint64) for n in ("workspace_bytes", "kept_cols", "piece_cols", "pieces")]
 
 
 class fls_head_io(C.Structure):
@@ -427,7 +427,7 @@ def fls_head_create(max_rows: int, vocab: int, dim: int, top: int = 0, grads: bo
 def fls_head_query(head: int) -> dict:
     lay = fls_head_layout()
     _check(lib.fls_head_query(head, C.byref(lay)))
-    return dict(workspace_bytes=lay.workspace_bytes, piece_cols=lay.piece_cols, pieces=lay.pieces)
+    return {n: getattr(lay, n) for n, _ in fls_head_layout._fields_}
 
 
 def fls_head_destroy(head: int) -> None:

@@ -13,6 +13,7 @@ constexpr int kHeadBM = 256;      // rows of C per CTA pair (128 per CTA)
 constexpr int kHeadBN = 256;      // columns of C per CTA pair; both CTAs hold all of them for their own rows
 constexpr int kHeadBK = 64;       // depth of one pipeline stage: 64 bf16 = one 128-byte swizzle row
 constexpr int kHeadStatCols = 128; // columns per partial sum of a row
+constexpr uint32_t kHeadKeepCols = 2048;
 constexpr int kHeadMaxSplits = 64;
 
 // Head of the workspace: words the device writes.
@@ -38,6 +39,7 @@ struct HeadCall {
   float* part_z;             // sum of the logits (only with label smoothing)
   float4* coef;              // [rows_cap]: see fls_head_rows_kernel
   uint16_t* g;               // [planes][rows_cap][piece_cols]: d loss / d logits of one piece of the vocabulary
+  float* keep_z;             // [rows_cap][keep_pitch]: kept logits, in the bytes of g
   float* dh;                 // [splits][rows_cap][dcap]: partial sums of the hidden gradient
   // problem
   const uint16_t* hidden; uint64_t hidden_stride;
@@ -55,6 +57,9 @@ struct HeadCall {
   uint32_t want_gh, want_gw;
   uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, bf16 accumulation): plain stores
   uint32_t max_splits, clusters, group_m;
+  uint32_t keep_v0;          // columns from here on keep their logits, vocab: none
+  uint32_t keep_pitch;       // kept columns, rounded up to kHeadKeepCols
+  uint32_t split_cols;       // columns of the widest piece, 0 without gradients
   float c1, cT;              // log2(e), log2(e) / T
   double inv_temp, temp, smoothing, z_loss, distill_weight, label_weight;
 };
@@ -67,6 +72,7 @@ struct HeadMaps { CUtensorMap a0, b0, a1, b1, store, store2; };
 struct HeadPiece {
   uint32_t v0, width;        // the columns of the vocabulary it works on
   uint32_t first;            // first piece: the hidden gradient's partial sums are stored, later ones added to
+  uint32_t kept;             // its dL/dz comes from kept logits and lies where they were
 };
 
 cudaError_t launch_head_rows_map(const HeadCall& c, cudaStream_t s);
@@ -75,6 +81,7 @@ cudaError_t launch_head_pack_weight(const uint16_t* w, uint64_t stride, uint16_t
 cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t s);
 cudaError_t launch_head_rows(const HeadCall& c, cudaStream_t s);
 cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s);
+cudaError_t launch_head_rescale(const HeadCall& c, cudaStream_t s);
 cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s);
 cudaError_t launch_head_grad_hidden(const HeadCall& c, cudaStream_t s);
 // clusters of two CTAs that fit on the current device at once

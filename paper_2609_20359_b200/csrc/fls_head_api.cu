@@ -28,8 +28,8 @@ int fail(int code, const char* fmt, ...) {
 int cuda_fail(cudaError_t e, const char* what) { return fail(FLS_ECUDA, "%s: %s", what, cudaGetErrorString(e)); }
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
-constexpr uint64_t kMinPieceCols = 512;
-constexpr uint64_t kDefaultPieceBytes = 256ull << 20;
+constexpr uint64_t kMinPieceCols = 512, kMaxPieceCols = 1ull << 28;
+constexpr uint64_t kDefaultPieceBytes = 1ull << 30;
 constexpr uint64_t kMinPartialBytes = 48ull << 20;   // room for the split sums of grad_hidden when there are few rows
 
 // Byte offsets of the workspace.  Sizes are those of max_rows; a smaller call uses the front of each region.
@@ -56,7 +56,7 @@ Regions regions(const fls_head_desc& d) {
   r.part = take(3 * r.part_bytes);          // maximum, sum, and one of: sum at temperature 1, sum of logits
   r.coef = take(cap * 16);
   if (d.grads) {
-    const uint64_t all = 2 * planes * cap * up(d.vocab, 256);
+    const uint64_t all = 4 * cap * up(d.vocab, kHeadKeepCols);       // every logit kept
     r.g_bytes = std::min(all, std::max(d.piece_bytes ? d.piece_bytes : kDefaultPieceBytes, 2 * planes * cap * kMinPieceCols));
     r.g = take(r.g_bytes);
     r.dh_bytes = std::max(2 * cap * dcap * 4, kMinPartialBytes);
@@ -67,12 +67,22 @@ Regions regions(const fls_head_desc& d) {
   return r;
 }
 
-// Columns per piece: as many as the region holds, evened out over the pieces.
-uint32_t piece_columns(const fls_head_desc& d, uint64_t g_bytes, uint64_t rows_cap, uint64_t planes) {
-  const uint64_t vr = up(d.vocab, 256);
-  const uint64_t most = std::min(vr, std::max<uint64_t>(256, g_bytes / (2 * planes * rows_cap) / 256 * 256));
-  const uint64_t pieces = (vr + most - 1) / most;
-  return uint32_t(up((vr + pieces - 1) / pieces, 256));
+// How the vocabulary is taken apart.  The last columns keep the logits of the statistics pass, 4 bytes each, and get their
+// dL/dz from those; the columns before them are formed again, in pieces of 2 bytes per column and term, evened out.
+struct Pieces { uint32_t keep_v0, keep_pitch, cols; };
+Pieces pieces_of(const fls_head_desc& d, uint64_t g_bytes, uint64_t rows_cap, uint64_t planes) {
+  Pieces p{};
+  const uint64_t keep = std::min(kMaxPieceCols, g_bytes / (4 * rows_cap) / kHeadKeepCols * kHeadKeepCols);
+  const uint64_t v0 = keep >= d.vocab ? 0 : keep ? up(d.vocab - keep, 256) : d.vocab;
+  p.keep_v0 = uint32_t(std::min(v0, d.vocab));
+  p.keep_pitch = uint32_t(up(d.vocab - p.keep_v0, kHeadKeepCols));
+  if (p.keep_v0) {
+    const uint64_t vr = up(p.keep_v0, 256);
+    const uint64_t most = std::min({vr, kMaxPieceCols, std::max<uint64_t>(256, g_bytes / (2 * planes * rows_cap) / 256 * 256)});
+    const uint64_t n = (vr + most - 1) / most;
+    p.cols = uint32_t(up((vr + n - 1) / n, 256));
+  }
+  return p;
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -176,6 +186,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.part_s1 = c.part_z = reinterpret_cast<float*>(ws + r.part + 2 * r.part_bytes);
   c.coef = reinterpret_cast<float4*>(ws + r.coef);
   c.g = reinterpret_cast<uint16_t*>(ws + r.g);
+  c.keep_z = reinterpret_cast<float*>(ws + r.g);
   c.dh = reinterpret_cast<float*>(ws + r.dh);
   c.hidden = static_cast<const uint16_t*>(io->hidden);
   c.hidden_stride = io->hidden_stride ? io->hidden_stride : d.dim;
@@ -207,10 +218,15 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.c1 = 1.4426950408889634f;
   c.cT = float(1.4426950408889634 * c.inv_temp);
   const bool grads = c.want_gh || c.want_gw;
+  c.keep_v0 = c.vocab;
   c.direct_store = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 || c.grad_weight_stride * (c.grad_f32 ? 4 : 2) % 16 ||
                    (c.accumulate && !c.grad_f32);
   if (grads) {
-    c.piece_cols = piece_columns(d, r.g_bytes, c.rows_cap, c.planes);
+    const Pieces p = pieces_of(d, r.g_bytes, c.rows_cap, c.planes);
+    c.keep_v0 = p.keep_v0;
+    c.keep_pitch = p.keep_pitch;
+    c.piece_cols = p.cols;
+    c.split_cols = std::max(p.cols, uint32_t(up(c.vocab - p.keep_v0, 256)));
     c.max_splits = uint32_t(std::min<uint64_t>(kHeadMaxSplits, r.dh_bytes / (uint64_t(c.rows_cap) * c.dcap * 4)));
   }
   if (io->rows == 0 && (!c.want_gw || io->accumulate)) return FLS_OK;
@@ -220,20 +236,28 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   const bool copy = d.dim % 8 || reinterpret_cast<uintptr_t>(w) % 16 || w_stride % 8;
   if (copy) { w = reinterpret_cast<const uint16_t*>(ws + r.wcopy); w_stride = w_cols = c.dp; }
 
-  HeadMaps fwd{}, grad{};
-  bool ok = encode(h->encode, &fwd.a0, c.hp, c.dp, c.rows_cap, c.dp, 128) && encode(h->encode, &fwd.b0, w, w_cols, d.vocab, w_stride, 128);
-  fwd.a1 = fwd.a0;
+  // fwd: logits, and where they or their dL/dz are stored; grad: the two products of a piece, kept the same for the kept one
+  const bool keeps = grads && c.keep_v0 < c.vocab, forms = grads && c.keep_v0 > 0;
+  HeadMaps fwd{}, stat{}, grad{}, kept{};
+  const auto f = h->encode;
+  bool ok = encode(f, &fwd.a0, c.hp, c.dp, c.rows_cap, c.dp, 128) && encode(f, &fwd.b0, w, w_cols, d.vocab, w_stride, 128);
+  fwd.a1 = fwd.store = fwd.store2 = fwd.a0;
   fwd.b1 = fwd.b0;
-  fwd.store = fwd.store2 = fwd.a0;
+  stat = fwd;
   if (ok && grads)
-    ok = encode(h->encode, &fwd.store, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 32) &&
-         encode(h->encode, &grad.a0, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 64) &&
-         encode(h->encode, &grad.b0, c.hp, c.dp, c.rows_cap, c.dp, 64) &&
-         encode(h->encode, &grad.a1, c.g, c.piece_cols, uint64_t(c.planes) * c.rows_cap, c.piece_cols, 128) &&
-         encode(h->encode, &grad.b1, w, w_cols, d.vocab, w_stride, 64) &&
-         encode(h->encode, &grad.store2, c.dh, c.dcap, uint64_t(c.max_splits) * c.rows_cap, c.dcap, 32, true) &&
-         (!c.want_gw || c.direct_store ||
-          encode(h->encode, &grad.store, c.grad_weight, d.dim, d.vocab, c.grad_weight_stride, 32, c.grad_f32));
+    ok = encode(f, &grad.b0, c.hp, c.dp, c.rows_cap, c.dp, 64) && encode(f, &grad.b1, w, w_cols, d.vocab, w_stride, 64) &&
+         encode(f, &grad.store2, c.dh, c.dcap, uint64_t(c.max_splits) * c.rows_cap, c.dcap, 32, true) &&
+         (!c.want_gw || c.direct_store || encode(f, &grad.store, c.grad_weight, d.dim, d.vocab, c.grad_weight_stride, 32, c.grad_f32));
+  kept = grad;
+  if (ok && keeps)
+    ok = encode(f, &stat.store, c.keep_z, c.keep_pitch, c.rows_cap, c.keep_pitch, 32, true) &&
+         encode(f, &kept.a0, c.g, 2ull * c.keep_pitch, c.rows_cap, 2ull * c.keep_pitch, 64) &&
+         encode(f, &kept.a1, c.g, 2ull * c.keep_pitch, c.rows_cap, 2ull * c.keep_pitch, 128);
+  if (ok && forms) {
+    const uint64_t n = uint64_t(c.planes) * c.rows_cap;
+    ok = encode(f, &fwd.store, c.g, c.piece_cols, n, c.piece_cols, 32) && encode(f, &grad.a0, c.g, c.piece_cols, n, c.piece_cols, 64) &&
+         encode(f, &grad.a1, c.g, c.piece_cols, n, c.piece_cols, 128);
+  }
   if (!ok) return fail(FLS_ECUDA, "cuTensorMapEncodeTiled failed");
 
 #define FLS_LAUNCH(call)                                        \
@@ -247,11 +271,15 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   if (copy)
     FLS_LAUNCH(launch_head_pack_weight(static_cast<const uint16_t*>(io->weight), io->weight_stride ? io->weight_stride : d.dim,
                                        reinterpret_cast<uint16_t*>(ws + r.wcopy), c.vocab, c.dim, c.dp, s));
-  FLS_LAUNCH(launch_head_stats(c, fwd, s));
+  FLS_LAUNCH(launch_head_stats(c, stat, s));
   FLS_LAUNCH(launch_head_rows(c, s));
   if (grads) {
-    for (uint32_t v0 = 0; v0 < c.vocab; v0 += c.piece_cols) {
-      const HeadPiece p{v0, std::min(c.piece_cols, c.vocab - v0), v0 == 0};
+    if (keeps) {
+      FLS_LAUNCH(launch_head_rescale(c, s));
+      FLS_LAUNCH(launch_head_grads(c, kept, HeadPiece{c.keep_v0, c.vocab - c.keep_v0, 1, 1}, s));
+    }
+    for (uint32_t v0 = 0; v0 < c.keep_v0; v0 += c.piece_cols) {
+      const HeadPiece p{v0, std::min(c.piece_cols, c.keep_v0 - v0), !keeps && v0 == 0, 0};
       FLS_LAUNCH(launch_head_dlogits(c, fwd, p, s));
       FLS_LAUNCH(launch_head_grads(c, grad, p, s));
     }
@@ -326,10 +354,12 @@ int fls_head_query(const fls_head* head, fls_head_layout* out) {
   if (!head || !out) return fail(FLS_EINVAL, "null argument");
   const fls_head_desc& d = head->desc;
   out->workspace_bytes = head->reg.total;
-  out->piece_cols = out->pieces = 0;
+  out->piece_cols = out->pieces = out->kept_cols = 0;
   if (d.grads) {
-    out->piece_cols = piece_columns(d, head->reg.g_bytes, up(std::max<uint64_t>(d.max_rows, 1), kHeadBM), d.grad_dtype == FLS_GRAD_F32 ? 2 : 1);
-    out->pieces = (d.vocab + out->piece_cols - 1) / out->piece_cols;
+    const Pieces p = pieces_of(d, head->reg.g_bytes, up(std::max<uint64_t>(d.max_rows, 1), kHeadBM), d.grad_dtype == FLS_GRAD_F32 ? 2 : 1);
+    out->piece_cols = p.cols;
+    out->pieces = p.cols ? (p.keep_v0 + p.cols - 1) / p.cols : 0;
+    out->kept_cols = d.vocab - p.keep_v0;
   }
   return FLS_OK;
 }

@@ -3,9 +3,10 @@
 //   fls_head_map_kernel    which rows take part, and where they go (compaction; ignored rows cost nothing below)
 //   fls_head_pack_kernel   packed copy of their hidden states, the columns that get a value of their own, sorted
 //   fls_head_gemm_kernel   the tensor-core kernel, three epilogues:
-//     kStats    logits tile -> maximum and sum of exponentials per row and 256 columns
+//     kStats    logits tile -> maximum and sum of exponentials per row and 128 columns
 //     kDlogits  logits tile -> dL/dz in bf16 (one piece of the vocabulary)
 //     kGrads    dL/dz of the piece -> rows of grad_weight, and partial sums of grad_hidden
+//   fls_head_rescale_kernel   dL/dz of the columns whose logits the statistics pass kept
 //   fls_head_rows_kernel   joins the tile sums, losses, coefficients of dL/dz
 //   fls_head_grad_hidden_kernel   sums the partial sums, rounds, puts rows back in the caller's order
 #include <cuda_bf16.h>
@@ -19,15 +20,23 @@
 namespace fls {
 namespace {
 
-constexpr int kStages = 5;
 constexpr uint32_t kOperandBytes = 128 * kHeadBK * 2;            // one operand of one stage of one CTA: 16 KB
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr int kEpiWarps = 8;                                     // two per lane quarter of TMEM, 128 columns each
 constexpr uint32_t kStoreBytes = 32 * 128;                       // one staged store of one warp: 32 rows of 128 bytes
-constexpr uint32_t kSmemBytes = kStages * kStageBytes + kEpiWarps * 2 * kStoreBytes + 1024 + 256;
+enum { kStats = 0, kDlogits = 1, kGrads = 2 };
+// Shared memory goes to pipeline stages first (row statistics of 2048 x 128256 x 2048 from idle clocks: 775 us with 7
+// stages, 827 us with 5); what stores tiles keeps a 4 KB buffer per epilogue warp, or two for fp32 logits and for two
+// terms of dL/dz.
+template <int MODE, bool FLAG, bool KEEP>
+struct Smem {
+  static constexpr int kBufs = MODE == kStats ? 2 * KEEP : MODE == kDlogits && FLAG ? 2 : 1;
+  static constexpr int kStages = 7 - kBufs;
+  static constexpr uint32_t kBytes = kStages * kStageBytes + kEpiWarps * kBufs * kStoreBytes + 1024 + 256;
+  static_assert(kBytes <= 232448, "shared memory of one CTA");
+};
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;               // warp 0 TMA, 1 MMA, 2 TMEM, 4..11 epilogue
 constexpr uint32_t kWaitLimit = 1u << 22;                        // polls of an mbarrier before a role gives up
-enum { kStats = 0, kDlogits = 1, kGrads = 2 };
 
 // ------------------------------------------------------------------------------------------------ PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
@@ -126,7 +135,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-
 // Shared-memory matrix descriptor, 128-byte swizzle.  Depth-contiguous operand (K-major): rows of 64 elements = 128
 // bytes, 8-row groups 1024 bytes apart (sbo).  Width-contiguous operand (MN-major): blocks of 64 columns x 64 depth
 // rows; 8-row groups 1024 bytes apart (sbo), 64-column blocks 8192 bytes apart (lbo).
@@ -140,6 +148,13 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
 __device__ __forceinline__ uint32_t instr_desc(bool a_mn, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) | ((kHeadBN >> 3) << 17) |
          ((kHeadBM >> 4) << 24);
+}
+
+// Where column n of a piece's dL/dz is in the workspace.  Kept logits (fp32) become dL/dz (bf16) in place, kKeepCols
+// columns at a time: those of the first term in the first half of the block's bytes, the second term's in the other half.
+constexpr uint32_t kKeepCols = kHeadKeepCols;
+__device__ __forceinline__ uint32_t dz_col(const HeadPiece& p, uint32_t n) {
+  return p.kept ? (n / kKeepCols) * (2 * kKeepCols) + n % kKeepCols : n;
 }
 
 // ------------------------------------------------------------------------------------------------ work units
@@ -241,10 +256,13 @@ struct StatsRow {
   __device__ __forceinline__ void chunk(float (&z)[32], int32_t col0, uint32_t vocab, float cT, float c1) {
     const bool edge = uint32_t(col0) + 32 > vocab;
     if constexpr (SMOOTH) {
-      float t = 0.f;
+      float t0 = 0.f, t1 = 0.f;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) t += (!edge || uint32_t(col0 + j) < vocab) ? z[j] : 0.f;
-      sz += t;
+      for (int j = 0; j < 32; j += 2) {
+        t0 += (!edge || uint32_t(col0 + j) < vocab) ? z[j] : 0.f;
+        t1 += (!edge || uint32_t(col0 + j + 1) < vocab) ? z[j + 1] : 0.f;
+      }
+      sz += t0 + t1;
     }
     if (edge) {
 #pragma unroll
@@ -303,17 +321,23 @@ __device__ __forceinline__ float bf16_round(float x) { return __bfloat162float(_
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
 // A warp's way out: 32 rows x 128 bytes are written to shared memory in the layout that a TMA store with 128-byte
-// swizzle reads (16-byte piece q of row r at q ^ (r & 7): no bank conflicts), and leave as whole lines.  Two buffers.
+// swizzle reads (16-byte piece q of row r at q ^ (r & 7): no bank conflicts), and leave as whole lines.
+template <int BUFS>
 struct Stager {
   uint32_t base, lane, next = 0;
   __device__ __forceinline__ Stager(uint32_t b, uint32_t l) : base(b), lane(l) {}
-  // Buffer to write next.  Buffers alternate and every acquire is followed by one group (send or skip), so all groups but
-  // the last are older than the buffer's last store; with `both`, the two buffers are taken before anything is sent.
-  __device__ __forceinline__ uint32_t acquire(bool both = false) {
-    if (lane == 0) {
-      if (both) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-    }
+  // Buffer to write next.  Buffers take turns and every acquire is followed by one group (send or skip), so with two of
+  // them all groups but the last are older than the buffer's last store.
+  __device__ __forceinline__ uint32_t acquire() {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BUFS == 2 ? 1 : 0) : "memory");
+    __syncwarp();
+    const uint32_t b = base + next * kStoreBytes;
+    if constexpr (BUFS == 2) next ^= 1;
+    return b;
+  }
+  // the other buffer too, before anything is sent from the first
+  __device__ __forceinline__ uint32_t acquire_next() {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
     const uint32_t b = base + next * kStoreBytes;
     next ^= 1;
@@ -353,16 +377,16 @@ struct Stager {
 };
 
 // dL/dz of one row of a tile: aT exp(z/T - lse_T) + a1 exp(z - lse_1) - b, then the columns with a value of their own.
-template <bool TWO>
+template <bool TWO, bool PLANES, int BUFS>
 struct DlogitsRow {
   float4 k;          // {lse_T log2(e), aT, lse_1 log2(e), a1}; without TWO {lse log2(e) , a, b, -}
   int32_t next = INT_MAX;
   const int32_t* idx;
   const float* val;
   uint32_t ptr, slots;
-  // the first (half 0) or second 32 of the 64 columns from col0 on; lo: buffer of the second term, 0 if there is none
+  // the first (half 0) or second 32 of the 64 columns from col0 on; lo: buffer of the second term (PLANES)
   __device__ __forceinline__ void chunk(float (&v)[32], int32_t col0, uint32_t half, uint32_t vocab, float cT, float c1,
-                                        const Stager& out, uint32_t hi, uint32_t lo) {
+                                        const Stager<BUFS>& out, uint32_t hi, uint32_t lo) {
     const int32_t c0 = col0 + int32_t(half) * 32;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
@@ -376,7 +400,7 @@ struct DlogitsRow {
         if (uint32_t(c0 + j) >= vocab) v[j] = 0.f;
     }
     out.put_bf16(hi, half, v);
-    if (lo) {
+    if constexpr (PLANES) {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] -= bf16_round(v[j]);
       out.put_bf16(lo, half, v);
@@ -384,7 +408,7 @@ struct DlogitsRow {
     while (next < c0 + 32) {            // same thread, same address, after the store above
       const float x = val[ptr];
       out.put_one(hi, uint32_t(next - col0), bf16_bits(x));
-      if (lo) out.put_one(lo, uint32_t(next - col0), bf16_bits(x - bf16_round(x)));
+      if constexpr (PLANES) out.put_one(lo, uint32_t(next - col0), bf16_bits(x - bf16_round(x)));
       ++ptr;
       next = ptr < slots ? idx[ptr] : INT_MAX;
     }
@@ -435,21 +459,25 @@ __device__ __forceinline__ void store_row32(T* dst, const float (&v)[32], uint32
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
+template <int STAGES>
 struct alignas(8) Barriers {
-  uint64_t full[kStages];    // leader: both CTAs' operands of a stage have landed
-  uint64_t empty[kStages];   // both: the products that read a stage are done
+  uint64_t full[STAGES];    // leader: both CTAs' operands of a stage have landed
+  uint64_t empty[STAGES];   // both: the products that read a stage are done
   uint64_t acc_full[2];      // both: an accumulator is complete
   uint64_t acc_empty[2];     // leader: both CTAs' epilogues have read an accumulator
   uint32_t tmem;
   uint32_t gave_up;
 };
 
-template <int MODE, bool TWO, bool SMOOTH>
+// TWO: two temperatures.  FLAG: label smoothing (kStats), dL/dz as two bf16 terms (kDlogits).  KEEP (kStats): the
+// logits of the columns from c.keep_v0 on stay in the workspace.
+template <int MODE, bool TWO, bool FLAG, bool KEEP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadCall c, const HeadPiece piece) {
+  constexpr int kStages = Smem<MODE, FLAG, KEEP>::kStages, kBufs = Smem<MODE, FLAG, KEEP>::kBufs;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  Barriers* bars = reinterpret_cast<Barriers*>(tiles + kStages * kStageBytes + kEpiWarps * 2 * kStoreBytes);
+  auto* bars = reinterpret_cast<Barriers<kStages>*>(tiles + kStages * kStageBytes + kEpiWarps * kBufs * kStoreBytes);
   const uint32_t tile_base = smem_u32(tiles);
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
@@ -491,16 +519,17 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
           const int k = int((w.kb0 + i) * kHeadBK);
           if constexpr (MODE == kGrads) {
             if (w.grad_hidden) {
-              tma_load(sa, ma, k, m, bar);                               // dL/dz: 128 rows x 64 columns
+              tma_load(sa, ma, int(dz_col(piece, uint32_t(k))), m, bar);  // dL/dz: 128 rows x 64 columns
               tma_load(sb, mb, n, int(piece.v0) + k, bar);               // weight: 64 rows x 2 x 64 columns
               tma_load(sb + 8192, mb, n + 64, int(piece.v0) + k, bar);
             } else {
               // fp32 weight gradients: the second half of the depth is the second plane of dL/dz against the same rows
               const uint32_t second = i >= plan.kb ? 1u : 0u;
               const int kr = int((i - second * plan.kb) * kHeadBK);
-              const int kg = kr + int(second * c.rows_cap);
-              tma_load(sa, ma, m, kg, bar);                              // dL/dz: 64 rows x 2 x 64 columns
-              tma_load(sa + 8192, ma, m + 64, kg, bar);
+              const int kg = kr + (piece.kept ? 0 : int(second * c.rows_cap));
+              const int mx = int(dz_col(piece, uint32_t(m))) + (piece.kept ? int(second * kKeepCols) : 0);
+              tma_load(sa, ma, mx, kg, bar);                             // dL/dz: 64 rows x 2 x 64 columns
+              tma_load(sa + 8192, ma, mx + 64, kg, bar);
               tma_load(sb, mb, n, kr, bar);                              // hidden: 64 rows x 2 x 64 columns
               tma_load(sb + 8192, mb, n + 64, kr, bar);
             }
@@ -542,7 +571,7 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
   } else if (warp >= 4) {
     const uint32_t quarter = warp & 3, half = (warp - 4) >> 2;    // 32 rows, 128 of the tile's columns
     const uint32_t lane_base = tmem + ((quarter * 32) << 16) + half * 128;
-    Stager out(tile_base + kStages * kStageBytes + (warp - 4) * 2 * kStoreBytes, lane);
+    Stager<kBufs> out(tile_base + kStages * kStageBytes + (warp - 4) * kBufs * kStoreBytes, lane);
     uint32_t buf = 0, phase = 0;
     for (uint32_t u = cluster; u < plan.n_units; u += n_clusters) {
       const Unit w = plan.at(u);
@@ -551,12 +580,12 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
       const uint32_t n0 = w.n0 + half * 128;
       // Rows nobody reads are left out: beyond the rows that take part, for dL/dz beyond the depth of the weight product.
       bool work = true;
-      if constexpr (MODE == kStats) work = row0 < count;
+      if constexpr (MODE == kStats) work = row0 < (KEEP ? (count + kHeadBK - 1) / kHeadBK * kHeadBK : count);
       if constexpr (MODE == kDlogits) work = row0 < (count + kHeadBK - 1) / kHeadBK * kHeadBK;
       if constexpr (MODE == kGrads) work = w.grad_hidden ? row0 < count : (row0 < piece.width && n0 < c.dim);
       // what the tile's rows need besides the accumulator is fetched before the wait
-      StatsRow<TWO, SMOOTH> st;
-      DlogitsRow<TWO> dl;
+      StatsRow<TWO, FLAG> st;
+      DlogitsRow<TWO, FLAG, kBufs> dl;
       if constexpr (MODE == kStats) {
         st.idx = c.slot_idx + uint64_t(row) * c.slots;
         st.zs = c.slot_z + uint64_t(row) * c.slots;
@@ -590,13 +619,23 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
       auto process = [&](float (&v)[32], uint32_t chunk) {
         const uint32_t n = n0 + chunk * 32;
         if constexpr (MODE == kStats) {
+          if constexpr (KEEP) {
+            if (n0 >= c.keep_v0) {
+              hi = out.acquire();
+              out.put_f32(hi, v);
+              out.send(&maps.store, int(n - c.keep_v0), int(row0), hi, false);
+            }
+          }
           st.chunk(v, int32_t(n), c.vocab, c.cT, c.c1);
         } else if constexpr (MODE == kDlogits) {
-          if (!(chunk & 1)) { hi = out.acquire(c.planes == 2); if (c.planes == 2) lo = out.acquire(true); }
+          if (!(chunk & 1)) {
+            hi = out.acquire();
+            if constexpr (FLAG) lo = out.acquire_next();
+          }
           dl.chunk(v, int32_t(piece.v0 + n0 + (chunk & 2) * 32), chunk & 1, c.vocab, c.cT, c.c1, out, hi, lo);
           if (chunk & 1) {
             out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(row0), hi, false);
-            if (lo) out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(c.rows_cap + row0), lo, false);
+            if constexpr (FLAG) out.send(&maps.store, int(n0 + (chunk & 2) * 32), int(c.rows_cap + row0), lo, false);
           }
         } else {
           if (w.grad_hidden) {
@@ -655,7 +694,7 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
           c.part_m[at] = st.m;
           c.part_s[at] = st.s;
           if constexpr (TWO) c.part_s1[at] = st.s1;
-          if constexpr (SMOOTH) c.part_z[at] = st.sz;
+          if constexpr (FLAG) c.part_z[at] = st.sz;
         }
       }
       if (++buf == 2) { buf = 0; phase ^= 1; }
@@ -802,9 +841,9 @@ __global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid
   __shared__ int32_t sh_i[kRowsY][FLS_HEAD_MAX_TOP + 1];
   const uint32_t lane = threadIdx.x & 31, y = threadIdx.x >> 5;
   const uint32_t count = c.state->count, p0 = blockIdx.x * 32;
-  if (blockIdx.x == 0 && y == kRowsY - 1 && c.piece_cols) {     // how the gradient launches of this call split their depth
-    const uint32_t nt = (c.dim + kHeadBN - 1) / kHeadBN, th = (count + kHeadBM - 1) / kHeadBM * nt, kb_h = c.piece_cols / kHeadBK;
-    const uint32_t tw = c.piece_cols / kHeadBM * nt, kb_w = (count + kHeadBK - 1) / kHeadBK * c.planes;
+  if (blockIdx.x == 0 && y == kRowsY - 1 && c.split_cols) {     // how the gradient launches of this call split their depth
+    const uint32_t nt = (c.dim + kHeadBN - 1) / kHeadBN, th = (count + kHeadBM - 1) / kHeadBM * nt, kb_h = c.split_cols / kHeadBK;
+    const uint32_t tw = c.split_cols / kHeadBM * nt, kb_w = (count + kHeadBK - 1) / kHeadBK * c.planes;
     uint32_t best = 0xFFFFFFFFu;
     for (uint32_t s = lane + 1; s <= min(c.max_splits, kb_h); s += 32)
       best = min(best, min(head_makespan(s, th, kb_h, tw, kb_w, c.clusters), 0x3FFFFFFu) << 6 | (s - 1));
@@ -950,6 +989,51 @@ __global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid
   }
 }
 
+// dL/dz of the kept columns, in place: reads 4 bytes and writes 2 (two terms: 4) per element instead of forming the logit
+// again.  The same operations on the same fp32 logit as in the kDlogits epilogue: the same bits.
+template <bool TWO>
+__global__ void __launch_bounds__(256) fls_head_rescale_kernel(const __grid_constant__ HeadCall c) {
+  static_assert(kKeepCols == 256 * 8, "one thread, eight columns");
+  const uint32_t row = blockIdx.x, count = c.state->count, col0 = blockIdx.y * kKeepCols;
+  if (row >= (count + kHeadBK - 1) / kHeadBK * kHeadBK) return;
+  float* z = c.keep_z + uint64_t(row) * c.keep_pitch + col0;
+  uint16_t* g = reinterpret_cast<uint16_t*>(z);
+  const uint32_t t = threadIdx.x * 8, n = c.keep_v0 + col0 + t;
+  float v[8];
+  if (row < count) {
+    const float4 k = c.coef[row];
+    const float4 a = reinterpret_cast<const float4*>(z + t)[0], b = reinterpret_cast<const float4*>(z + t)[1];
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (TWO) v[j] = fmaf(k.w, ex2(fmaf(x[j], c.c1, -k.z)), k.y * ex2(fmaf(x[j], c.cT, -k.x)));
+      else v[j] = fmaf(k.y, ex2(fmaf(x[j], c.cT, -k.x)), -k.z);
+      if (n + j >= c.vocab) v[j] = 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+  }
+  __syncthreads();
+  *reinterpret_cast<uint4*>(g + t) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  if (c.planes == 2) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] -= bf16_round(v[j]);
+    *reinterpret_cast<uint4*>(g + kKeepCols + t) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  }
+  __syncthreads();
+  if (row >= count) return;
+  const int32_t first = int32_t(c.keep_v0 + col0);
+  for (uint32_t i = threadIdx.x; i < c.slots; i += 256) {
+    const int32_t x = c.slot_idx[uint64_t(row) * c.slots + i] - first;
+    if (x >= 0 && x < int32_t(kKeepCols)) {
+      const float y = c.slot_g[uint64_t(row) * c.slots + i];
+      g[x] = bf16_bits(y);
+      if (c.planes == 2) g[kKeepCols + x] = bf16_bits(y - bf16_round(y));
+    }
+  }
+}
+
 __global__ void __launch_bounds__(128) fls_head_grad_hidden_kernel(const __grid_constant__ HeadCall c) {
   const uint64_t n = blockIdx.x;
   const int32_t p = c.pos[n];
@@ -971,19 +1055,21 @@ __global__ void __launch_bounds__(128) fls_head_grad_hidden_kernel(const __grid_
   }
 }
 
-template <int MODE, bool TWO, bool SMOOTH>
+template <int MODE, bool TWO, bool FLAG, bool KEEP = false>
 cudaError_t launch_gemm(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
-  auto* k = fls_head_gemm_kernel<MODE, TWO, SMOOTH>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  auto* k = fls_head_gemm_kernel<MODE, TWO, FLAG, KEEP>;
+  constexpr uint32_t kBytes = Smem<MODE, FLAG, KEEP>::kBytes;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
   if (e != cudaSuccess) return e;
-  k<<<2 * c.clusters, kGemmThreads, kSmemBytes, s>>>(m, c, p);
+  k<<<2 * c.clusters, kGemmThreads, kBytes, s>>>(m, c, p);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t head_clusters(uint32_t* out) {
-  auto* k = fls_head_gemm_kernel<kStats, false, false>;
+  auto* k = fls_head_gemm_kernel<kStats, false, false, false>;      // the modes differ little in shared memory and not in CTAs per SM
+  constexpr uint32_t kSmemBytes = Smem<kStats, false, false>::kBytes;
   cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
@@ -1014,7 +1100,12 @@ cudaError_t launch_head_pack_weight(const uint16_t* w, uint64_t stride, uint16_t
   return cudaGetLastError();
 }
 cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t s) {
-  const HeadPiece p{0, c.vocab, 0};
+  const HeadPiece p{0, c.vocab, 0, 0};
+  if (c.keep_v0 < c.vocab) {
+    if (c.two) return launch_gemm<kStats, true, false, true>(c, m, p, s);
+    if (c.smooth) return launch_gemm<kStats, false, true, true>(c, m, p, s);
+    return launch_gemm<kStats, false, false, true>(c, m, p, s);
+  }
   if (c.two) return launch_gemm<kStats, true, false>(c, m, p, s);
   if (c.smooth) return launch_gemm<kStats, false, true>(c, m, p, s);
   return launch_gemm<kStats, false, false>(c, m, p, s);
@@ -1024,7 +1115,14 @@ cudaError_t launch_head_rows(const HeadCall& c, cudaStream_t s) {
   return cudaGetLastError();
 }
 cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
+  if (c.planes == 2) return c.two ? launch_gemm<kDlogits, true, true>(c, m, p, s) : launch_gemm<kDlogits, false, true>(c, m, p, s);
   return c.two ? launch_gemm<kDlogits, true, false>(c, m, p, s) : launch_gemm<kDlogits, false, false>(c, m, p, s);
+}
+cudaError_t launch_head_rescale(const HeadCall& c, cudaStream_t s) {
+  const dim3 grid(c.rows_cap, c.keep_pitch / kKeepCols);
+  if (c.two) fls_head_rescale_kernel<true><<<grid, 256, 0, s>>>(c);
+  else fls_head_rescale_kernel<false><<<grid, 256, 0, s>>>(c);
+  return cudaGetLastError();
 }
 cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
   return launch_gemm<kGrads, false, false>(c, m, p, s);
