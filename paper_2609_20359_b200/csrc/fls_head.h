@@ -26,6 +26,8 @@ struct HeadState {
 // Everything the kernels of one call share.  Packed row p stands for row src[p] of the caller.
 struct HeadCall {
   HeadState* state;
+  uint32_t* row_mask;        // [rows / 32]: a bit per row that takes part
+  uint32_t* row_count;       // [rows / 256]: rows that take part among 256
   int32_t* pos;              // [rows]: packed row of a row, -1 if it takes no part
   int32_t* src;              // [rows_cap]: row of a packed row
   uint16_t* hp;              // [rows_cap][dp]: packed hidden rows, zero up to the next multiple of 256 rows
@@ -57,6 +59,7 @@ struct HeadCall {
   uint32_t want_gh, want_gw;
   uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, bf16 accumulation): plain stores
   uint32_t max_splits, clusters, group_m;
+  uint32_t prefetch_weight;  // one row tile, and the weight is the caller's: fetched ahead of the packed rows
   uint32_t keep_v0;          // columns from here on keep their logits, vocab: none
   uint32_t keep_pitch;       // kept columns, rounded up to kHeadKeepCols
   uint32_t split_cols;       // columns of the widest piece, 0 without gradients

@@ -34,7 +34,7 @@ constexpr uint64_t kMinPartialBytes = 48ull << 20;   // room for the split sums 
 
 // Byte offsets of the workspace.  Sizes are those of max_rows; a smaller call uses the front of each region.
 struct Regions {
-  uint64_t pos, src, hp, slot_idx, slot_t, slot_z, slot_g, part, coef, g, dh, wcopy, total;
+  uint64_t mask, counts, pos, src, hp, slot_idx, slot_t, slot_z, slot_g, part, coef, g, dh, wcopy, total;
   uint64_t part_bytes, g_bytes, dh_bytes;
 };
 
@@ -45,6 +45,8 @@ Regions regions(const fls_head_desc& d) {
   Regions r{};
   uint64_t at = 256;
   auto take = [&](uint64_t bytes) { const uint64_t o = at; at += up(bytes, 256); return o; };
+  r.mask = take(cap / 8);
+  r.counts = take(cap / 256 * 4);
   r.pos = take(cap * 4);
   r.src = take(cap * 4);
   r.hp = take(cap * dp * 2);
@@ -174,6 +176,8 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
 
   char* ws = static_cast<char*>(io->workspace);
   c.state = reinterpret_cast<HeadState*>(ws);
+  c.row_mask = reinterpret_cast<uint32_t*>(ws + r.mask);
+  c.row_count = reinterpret_cast<uint32_t*>(ws + r.counts);
   c.pos = reinterpret_cast<int32_t*>(ws + r.pos);
   c.src = reinterpret_cast<int32_t*>(ws + r.src);
   c.hp = reinterpret_cast<uint16_t*>(ws + r.hp);
@@ -234,6 +238,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   const uint16_t* w = static_cast<const uint16_t*>(io->weight);
   uint64_t w_stride = io->weight_stride ? io->weight_stride : d.dim, w_cols = d.dim;
   const bool copy = d.dim % 8 || reinterpret_cast<uintptr_t>(w) % 16 || w_stride % 8;
+  c.prefetch_weight = c.rows_cap == kHeadBM && !copy;
   if (copy) { w = reinterpret_cast<const uint16_t*>(ws + r.wcopy); w_stride = w_cols = c.dp; }
 
   // fwd: logits, and where they or their dL/dz are stored; grad: the two products of a piece, kept the same for the kept one
@@ -266,7 +271,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
     if (e_ != cudaSuccess) return cuda_fail(e_, "head kernel"); \
     ++h->launches;                                              \
   } while (0)
-  FLS_LAUNCH(launch_head_rows_map(c, s));
+  if (io->rows > 256) FLS_LAUNCH(launch_head_rows_map(c, s));
   FLS_LAUNCH(launch_head_pack(c, s));
   if (copy)
     FLS_LAUNCH(launch_head_pack_weight(static_cast<const uint16_t*>(io->weight), io->weight_stride ? io->weight_stride : d.dim,

@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <utility>
 
 #include "fls_head.h"
 
@@ -49,6 +50,10 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
+// Programmatic dependent launch: the next kernel of the call may start (its blocks wait in pdl_wait) / everything the
+// kernels before this one wrote is visible.  Every kernel of a call waits, so completion carries over several kernels.
+__device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Address, in the cluster's shared window, of the leader CTA's copy of a shared variable.
 __device__ __forceinline__ uint32_t leader_addr(uint32_t a) {
   uint32_t r;
@@ -82,6 +87,9 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
   asm volatile(
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
       ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap* map, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
 }
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
@@ -493,11 +501,18 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars->tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  if (MODE == kStats && threadIdx.x == 0 && c.prefetch_weight) {
+    // One row tile: this cluster's first columns are known before the packed rows are, and the weight is nothing that an
+    // earlier kernel of the call wrote.  It comes from memory while they are still packed.
+    for (uint32_t k = 0; k < c.dp; k += kHeadBK) tma_prefetch(&maps.b0, int(k), int(cluster * kHeadBN + rank * 128));
+  }
   fence_before();
   __syncthreads();
   cluster_sync();
   fence_after();
   const uint32_t tmem = bars->tmem;
+  pdl_launch();
+  pdl_wait();
 
   const uint32_t count = c.state->count;
   const Schedule<MODE> plan(c, piece, count);
@@ -720,100 +735,123 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
 }
 
 // ------------------------------------------------------------------------------------------------ rows
-// One block: packed positions of the rows that take part, in order.
-__global__ void __launch_bounds__(1024) fls_head_map_kernel(const __grid_constant__ HeadCall c) {
-  __shared__ uint32_t warp_sum[32];
-  __shared__ uint32_t base;
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) base = 0;
-  __syncthreads();
-  for (uint64_t r0 = 0; r0 < c.rows; r0 += 1024) {
-    const uint64_t n = r0 + threadIdx.x;
-    bool active = false, bad = false;
-    if (n < c.rows) {
-      if (c.use_label) {
-        const int64_t y = c.labels[n];
-        bad = y != c.ignore_label && (y < 0 || y >= int64_t(c.vocab));
-        active = y != c.ignore_label;
-      }
-      for (uint32_t k = 0; k < c.top && !active; ++k) {
-        const int32_t i = c.top_index[n * c.top + k];
-        active = i >= 0 && uint32_t(i) < c.vocab && c.top_logit[n * c.top + k] != -INFINITY;
-      }
-      active = active && !bad;
-      if (!active) {
-        c.loss[n] = bad ? NAN : 0.f;
-        c.lse[n] = bad ? NAN : 0.f;
-      }
-    }
-    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, active);
-    if (lane == 0) warp_sum[warp] = __popc(mask);
-    __syncthreads();
-    if (warp == 0) {
-      uint32_t x = warp_sum[lane];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-        if (lane >= uint32_t(o)) x += y;
-      }
-      warp_sum[lane] = x;
-    }
-    __syncthreads();
-    const uint32_t before = base + (warp ? warp_sum[warp - 1] : 0) + __popc(mask & ((1u << lane) - 1));
-    if (n < c.rows) {
-      c.pos[n] = active ? int32_t(before) : -1;
-      if (active) c.src[before] = int32_t(n);
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) base += warp_sum[31];
-    __syncthreads();
+// Which rows take part is a bit per row, and a count per 256 rows.
+constexpr uint32_t kRowChunk = 256;
+
+// One thread per row.  Rows that take no part get their outputs here.
+__device__ __forceinline__ bool row_active(const HeadCall& c, uint64_t n, bool write) {
+  bool active = false, bad = false;
+  if (c.use_label) {
+    const int64_t y = c.labels[n];
+    bad = y != c.ignore_label && (y < 0 || y >= int64_t(c.vocab));
+    active = y != c.ignore_label;
   }
-  if (threadIdx.x == 0) c.state->count = base;
+  for (uint32_t k = 0; k < c.top && !active; ++k) {
+    const int32_t i = c.top_index[n * c.top + k];
+    active = i >= 0 && uint32_t(i) < c.vocab && c.top_logit[n * c.top + k] != -INFINITY;
+  }
+  active = active && !bad;
+  if (!active && write) {
+    c.loss[n] = bad ? NAN : 0.f;
+    c.lse[n] = bad ? NAN : 0.f;
+  }
+  return active;
 }
 
-// One block per packed row: its hidden state (zero beyond the rows that take part, up to the next multiple of 256) and
-// its own columns in ascending order.
-__global__ void __launch_bounds__(128) fls_head_pack_kernel(const __grid_constant__ HeadCall c) {
+__global__ void __launch_bounds__(kRowChunk) fls_head_map_kernel(const __grid_constant__ HeadCall c) {
+  pdl_launch();
+  pdl_wait();
+  const uint64_t n = uint64_t(blockIdx.x) * kRowChunk + threadIdx.x;
+  const bool active = n < c.rows && row_active(c, n, true);
+  const uint32_t mask = __ballot_sync(0xFFFFFFFFu, active);
+  if ((threadIdx.x & 31) == 0) c.row_mask[n / 32] = mask;
+  const int count = __syncthreads_count(active);
+  if (threadIdx.x == 0) c.row_count[blockIdx.x] = uint32_t(count);
+}
+
+// One block per row: its packed position is the number of rows before it that take part.  A row that does is copied there
+// with its own columns in ascending order; block i also clears packed row i if that is one of those between the rows that
+// take part and the next multiple of 256.  ONE_CHUNK: at most 256 rows; every block looks at all of them itself and the map
+// kernel is not needed.
+template <bool ONE_CHUNK>
+__global__ void __launch_bounds__(256) fls_head_pack_kernel(const __grid_constant__ HeadCall c) {
   __shared__ int32_t s_idx[FLS_HEAD_MAX_TOP + 1];
   __shared__ float s_t[FLS_HEAD_MAX_TOP + 1];
-  const uint32_t p = blockIdx.x, count = c.state->count;
-  if (p >= (count + kHeadBM - 1) / kHeadBM * kHeadBM) return;
-  const bool live = p < count;
-  const uint64_t n = live ? uint64_t(c.src[p]) : 0;
+  __shared__ uint32_t s_mask[kRowChunk / 32], s_before, s_count;
+  const uint32_t i = blockIdx.x, chunk = i / kRowChunk;
+  if (threadIdx.x == 0) s_before = s_count = 0;
+  pdl_launch();
+  pdl_wait();
+  __syncthreads();
+  if constexpr (ONE_CHUNK) {
+    const uint64_t n = threadIdx.x;
+    const bool active = n < c.rows && row_active(c, n, i == 0);
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, active);
+    if ((threadIdx.x & 31) == 0) s_mask[threadIdx.x / 32] = mask;
+    s_count = uint32_t(__syncthreads_count(active));
+  } else {
+    if (threadIdx.x < kRowChunk / 32) s_mask[threadIdx.x] = chunk * kRowChunk < c.rows ? c.row_mask[chunk * (kRowChunk / 32) + threadIdx.x] : 0u;
+    uint32_t before = 0, all = 0;
+    for (uint32_t k = threadIdx.x; k < uint32_t((c.rows + kRowChunk - 1) / kRowChunk); k += blockDim.x) {
+      const uint32_t x = c.row_count[k];
+      all += x;
+      before += k < chunk ? x : 0u;
+    }
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    all = __reduce_add_sync(0xFFFFFFFFu, all);
+    if ((threadIdx.x & 31) == 0) { atomicAdd(&s_before, before); atomicAdd(&s_count, all); }
+    __syncthreads();
+  }
+  const uint32_t count = s_count, bit = i % kRowChunk;
+  uint32_t p = s_before;
+  for (uint32_t w = 0; w < bit / 32; ++w) p += __popc(s_mask[w]);
+  p += __popc(s_mask[bit / 32] & ((1u << (bit & 31)) - 1));
+  const bool active = (s_mask[bit / 32] >> (bit & 31)) & 1;
+  if (threadIdx.x == 0) {
+    if (i == 0) c.state->count = count;
+    if (i < c.rows) c.pos[i] = active ? int32_t(p) : -1;
+    if (active) c.src[p] = int32_t(i);
+  }
+  if (i >= count && i < (count + kHeadBM - 1) / kHeadBM * kHeadBM) {
+    uint4* out = reinterpret_cast<uint4*>(c.hp + uint64_t(i) * c.dp);
+    for (uint32_t k = threadIdx.x; k < c.dp / 8; k += blockDim.x) out[k] = make_uint4(0, 0, 0, 0);
+  }
+  if (!active) return;
+  const uint64_t n = i;
   uint16_t* out = c.hp + uint64_t(p) * c.dp;
   const uint16_t* in = c.hidden + n * c.hidden_stride;
-  if (!live || (c.dim % 8 == 0 && aligned16(in))) {
-    for (uint32_t i = threadIdx.x; i < c.dp / 8; i += blockDim.x)
-      reinterpret_cast<uint4*>(out)[i] = live ? reinterpret_cast<const uint4*>(in)[i] : make_uint4(0, 0, 0, 0);
+  if (c.dim % 8 == 0 && aligned16(in)) {
+    for (uint32_t k = threadIdx.x; k < c.dp / 8; k += blockDim.x) reinterpret_cast<uint4*>(out)[k] = reinterpret_cast<const uint4*>(in)[k];
   } else {
-    for (uint32_t i = threadIdx.x; i < c.dp; i += blockDim.x) out[i] = i < c.dim ? in[i] : uint16_t(0);
+    for (uint32_t k = threadIdx.x; k < c.dp; k += blockDim.x) out[k] = k < c.dim ? in[k] : uint16_t(0);
   }
-  if (!live) return;
-  for (uint32_t i = threadIdx.x; i < c.slots; i += blockDim.x) {
+  for (uint32_t k = threadIdx.x; k < c.slots; k += blockDim.x) {
     int32_t idx = INT_MAX;
     float t = -INFINITY;
-    if (i < c.top) {
-      const int32_t x = c.top_index[n * c.top + i];
-      const float y = c.top_logit[n * c.top + i];
+    if (k < c.top) {
+      const int32_t x = c.top_index[n * c.top + k];
+      const float y = c.top_logit[n * c.top + k];
       if (x >= 0 && uint32_t(x) < c.vocab && y != -INFINITY) { idx = x; t = y; }
     } else if (c.use_label) {
       const int64_t y = c.labels[n];
       if (y != c.ignore_label) idx = int32_t(y);
     }
-    s_idx[i] = idx;
-    s_t[i] = t;
+    s_idx[k] = idx;
+    s_t[k] = t;
   }
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < c.slots; i += blockDim.x) {
-    const int32_t x = s_idx[i];
+  for (uint32_t k = threadIdx.x; k < c.slots; k += blockDim.x) {
+    const int32_t x = s_idx[k];
     uint32_t rank = 0;
-    for (uint32_t j = 0; j < c.slots; ++j) rank += s_idx[j] < x || (s_idx[j] == x && j < i);
+    for (uint32_t j = 0; j < c.slots; ++j) rank += s_idx[j] < x || (s_idx[j] == x && j < k);
     c.slot_idx[uint64_t(p) * c.slots + rank] = x;
-    c.slot_t[uint64_t(p) * c.slots + rank] = s_t[i];
+    c.slot_t[uint64_t(p) * c.slots + rank] = s_t[k];
   }
 }
 
 __global__ void __launch_bounds__(256) fls_head_pack_weight_kernel(const uint16_t* w, uint64_t stride, uint16_t* out, uint32_t dim, uint32_t dp) {
+  pdl_launch();
+  pdl_wait();
   const uint64_t v = blockIdx.x;
   for (uint32_t i = threadIdx.x; i < dp; i += blockDim.x) out[v * dp + i] = i < dim ? w[v * stride + i] : uint16_t(0);
 }
@@ -829,19 +867,19 @@ __device__ __forceinline__ double warp_max(double x) {
   return x;
 }
 
-// 32 packed rows per block.  First the tile sums of each row are joined (coalesced: neighbouring threads are
-// neighbouring rows), then a warp takes a row: its own columns are added to the sums and give loss and gradient.
-// Sums and logarithms are double: a few thousand operations per row beside 2 V d of the products.
-constexpr int kRowsY = 16;
-__global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid_constant__ HeadCall c) {
-  __shared__ float sh_m[kRowsY][32];
-  __shared__ double sh_s[kRowsY][32], sh_s1[kRowsY][32], sh_z[kRowsY][32];
-  __shared__ float row_m[32];
-  __shared__ double sh_q[kRowsY][FLS_HEAD_MAX_TOP + 1];
-  __shared__ int32_t sh_i[kRowsY][FLS_HEAD_MAX_TOP + 1];
+// Eight packed rows per block.  First the partial sums of each row are joined: a warp reads four columns' worth of eight
+// neighbouring rows, whole 32-byte sectors.  Then a warp takes a row: its own columns are added to the sums and give loss
+// and gradient.  Sums over the row and logarithms are double: a few hundred operations beside 2 V d of the products.
+constexpr uint32_t kRowsPerBlock = 8;
+__global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constant__ HeadCall c) {
+  __shared__ float sh_m[32][kRowsPerBlock], sh_s[32][kRowsPerBlock], sh_s1[32][kRowsPerBlock], sh_z[32][kRowsPerBlock];
+  __shared__ double sh_q[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
+  __shared__ int32_t sh_i[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
   const uint32_t lane = threadIdx.x & 31, y = threadIdx.x >> 5;
-  const uint32_t count = c.state->count, p0 = blockIdx.x * 32;
-  if (blockIdx.x == 0 && y == kRowsY - 1 && c.split_cols) {     // how the gradient launches of this call split their depth
+  pdl_launch();
+  pdl_wait();
+  const uint32_t count = c.state->count, p0 = blockIdx.x * kRowsPerBlock;
+  if (blockIdx.x == 0 && y == 7 && c.split_cols) {     // how the gradient launches of this call split their depth
     const uint32_t nt = (c.dim + kHeadBN - 1) / kHeadBN, th = (count + kHeadBM - 1) / kHeadBM * nt, kb_h = c.split_cols / kHeadBK;
     const uint32_t tw = c.split_cols / kHeadBM * nt, kb_w = (count + kHeadBK - 1) / kHeadBK * c.planes;
     uint32_t best = 0xFFFFFFFFu;
@@ -852,40 +890,50 @@ __global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid
   }
   if (p0 >= count) return;
   {
-    const uint32_t p = p0 + lane;         // packed rows up to the next multiple of 256 exist
-    float m = -INFINITY;
-    for (uint32_t t = y; t < c.tiles; t += kRowsY) m = fmaxf(m, c.part_m[uint64_t(t) * c.rows_cap + p]);
-    if (p < count)
-      for (uint32_t i = y; i < c.slots; i += kRowsY)
-        if (c.slot_idx[uint64_t(p) * c.slots + i] != INT_MAX) m = fmaxf(m, c.slot_z[uint64_t(p) * c.slots + i]);
-    sh_m[y][lane] = m;
-    __syncthreads();
-    for (int i = 0; i < kRowsY; ++i) m = fmaxf(m, sh_m[i][lane]);
-    if (y == 0) row_m[lane] = m;
-    const float base = m == -INFINITY ? 0.f : m;
-    double s = 0.0, s1 = 0.0, z = 0.0;
-    for (uint32_t t = y; t < c.tiles; t += kRowsY) {
-      const uint64_t at = uint64_t(t) * c.rows_cap + p;
-      const float tm = c.part_m[at], ts = c.part_s[at];
-      // a tile whose every column is left out has m = -inf and s = 0
-      s += double(ts) * (tm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(tm, c.cT) - __fmul_rn(base, c.cT))));
-      if (c.two) s1 += double(c.part_s1[at]) * (tm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(tm, c.c1) - __fmul_rn(base, c.c1))));
-      if (c.smooth) z += double(c.part_z[at]);
+    const uint32_t r = threadIdx.x % kRowsPerBlock, t0 = threadIdx.x / kRowsPerBlock;   // packed rows to the next multiple of 256 exist
+    float m = -INFINITY, s = 0.f, s1 = 0.f, z = 0.f;
+    for (uint32_t t = t0; t < c.tiles; t += 128) {
+      float tm[4], ts[4], t1[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = t + 32 * j < c.tiles;
+        const uint64_t at = uint64_t(in ? t + 32 * j : t) * c.rows_cap + p0 + r;
+        tm[j] = in ? c.part_m[at] : -INFINITY;
+        ts[j] = in ? c.part_s[at] : 0.f;
+        t1[j] = in && c.two ? c.part_s1[at] : 0.f;
+        z += in && c.smooth ? c.part_z[at] : 0.f;
+      }
+      const float nm = fmaxf(fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])), m), base = nm == -INFINITY ? 0.f : nm;
+      s *= exp2f(__fmul_rn(m, c.cT) - __fmul_rn(base, c.cT));          // an empty side has factor 2^-inf = 0
+      if (c.two) s1 *= exp2f(__fmul_rn(m, c.c1) - __fmul_rn(base, c.c1));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // columns all left out: m = -inf and s = 0; NaN goes through
+        s += ts[j] * (tm[j] == -INFINITY ? 1.f : exp2f(__fmul_rn(tm[j], c.cT) - __fmul_rn(base, c.cT)));
+        if (c.two) s1 += t1[j] * (tm[j] == -INFINITY ? 1.f : exp2f(__fmul_rn(tm[j], c.c1) - __fmul_rn(base, c.c1)));
+      }
+      m = nm;
     }
-    sh_s[y][lane] = s;
-    sh_s1[y][lane] = s1;
-    sh_z[y][lane] = z;
+    sh_m[t0][r] = m;
+    sh_s[t0][r] = s;
+    sh_s1[t0][r] = s1;
+    sh_z[t0][r] = z;
     __syncthreads();
   }
-  for (uint32_t q = y; q < 32; q += kRowsY) {
-    const uint32_t p = p0 + q;
-    if (p >= count) break;
+  {
+    const uint32_t p = p0 + y;
+    if (p >= count) return;
     const uint64_t n = uint64_t(c.src[p]);
-    const float mf = row_m[q];
-    const double M = mf == -INFINITY ? 0.0 : double(mf);
-    double denseT = 0.0, dense1 = 0.0, zsum = 0.0;
-    for (int i = 0; i < kRowsY; ++i) { denseT += sh_s[i][q]; dense1 += sh_s1[i][q]; zsum += sh_z[i][q]; }
-    if (!c.two) dense1 = denseT;
+    float mf = sh_m[lane][y];
+    for (uint32_t i = lane; i < c.slots; i += 32)
+      if (c.slot_idx[uint64_t(p) * c.slots + i] != INT_MAX) mf = fmaxf(mf, c.slot_z[uint64_t(p) * c.slots + i]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mf = fmaxf(mf, __shfl_xor_sync(0xFFFFFFFFu, mf, o));
+    const float base = mf == -INFINITY ? 0.f : mf, lm = sh_m[lane][y];
+    const double M = double(base);
+    const double denseT = warp_sum(double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(lm, c.cT) - __fmul_rn(base, c.cT)))));
+    const double dense1 = !c.two ? denseT : warp_sum(double(sh_s1[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(lm, c.c1) - __fmul_rn(base, c.c1)))));
+    const double zsum = c.smooth ? warp_sum(double(sh_z[lane][y])) : 0.0;
     const int64_t label = c.use_label ? c.labels[n] : c.ignore_label;
     const bool labelled = c.use_label && label != c.ignore_label;
     const int32_t* idx = c.slot_idx + uint64_t(p) * c.slots;
@@ -994,6 +1042,8 @@ __global__ void __launch_bounds__(32 * kRowsY) fls_head_rows_kernel(const __grid
 template <bool TWO>
 __global__ void __launch_bounds__(256) fls_head_rescale_kernel(const __grid_constant__ HeadCall c) {
   static_assert(kKeepCols == 256 * 8, "one thread, eight columns");
+  pdl_launch();
+  pdl_wait();
   const uint32_t row = blockIdx.x, count = c.state->count, col0 = blockIdx.y * kKeepCols;
   if (row >= (count + kHeadBK - 1) / kHeadBK * kHeadBK) return;
   float* z = c.keep_z + uint64_t(row) * c.keep_pitch + col0;
@@ -1034,25 +1084,48 @@ __global__ void __launch_bounds__(256) fls_head_rescale_kernel(const __grid_cons
   }
 }
 
-__global__ void __launch_bounds__(128) fls_head_grad_hidden_kernel(const __grid_constant__ HeadCall c) {
+// One block per row, four columns per thread; the split sums are added in order.
+__global__ void __launch_bounds__(256) fls_head_grad_hidden_kernel(const __grid_constant__ HeadCall c) {
+  pdl_launch();
+  pdl_wait();
   const uint64_t n = blockIdx.x;
   const int32_t p = c.pos[n];
   uint16_t* out = c.grad_hidden + n * c.grad_hidden_stride;
   const uint32_t splits = c.state->splits;
-  const bool vec = c.dim % 8 == 0 && aligned16(out);
-  for (uint32_t i = threadIdx.x * 8; i < c.dim; i += blockDim.x * 8) {
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (p >= 0)
+  const bool vec = c.dim % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 7) == 0;
+  for (uint32_t i = (blockIdx.y * 256 + threadIdx.x) * 4; i < c.dim; i += gridDim.y * 1024) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p >= 0) {
+      const float* x = c.dh + uint64_t(p) * c.dcap + i;
+      const uint64_t step = uint64_t(c.rows_cap) * c.dcap;
+#pragma unroll 8
       for (uint32_t s = 0; s < splits; ++s) {
-        const float4* x = reinterpret_cast<const float4*>(c.dh + (uint64_t(s) * c.rows_cap + p) * c.dcap + i);
-        const float4 a = x[0], b = x[1];
-        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        const float4 a = *reinterpret_cast<const float4*>(x + s * step);
+        v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
       }
-    if (vec)
-      *reinterpret_cast<uint4*>(out + i) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    else
-      for (uint32_t j = 0; j < 8 && i + j < c.dim; ++j) out[i + j] = bf16_bits(v[j]);
+    }
+    if (vec) *reinterpret_cast<uint2*>(out + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    else {
+      const float w[4] = {v.x, v.y, v.z, v.w};
+      for (uint32_t j = 0; j < 4 && i + j < c.dim; ++j) out[i + j] = bf16_bits(w[j]);
+    }
   }
+}
+
+// Kernels of a call after its first start while the one before ends (pdl_wait).
+template <typename... P, typename... A>
+cudaError_t launch(void (*k)(P...), dim3 grid, uint32_t block, uint32_t smem, bool first, cudaStream_t s, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = first ? 0 : 1;
+  return cudaLaunchKernelEx(&cfg, k, std::forward<A>(args)...);
 }
 
 template <int MODE, bool TWO, bool FLAG, bool KEEP = false>
@@ -1061,8 +1134,7 @@ cudaError_t launch_gemm(const HeadCall& c, const HeadMaps& m, const HeadPiece& p
   constexpr uint32_t kBytes = Smem<MODE, FLAG, KEEP>::kBytes;
   cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
   if (e != cudaSuccess) return e;
-  k<<<2 * c.clusters, kGemmThreads, kBytes, s>>>(m, c, p);
-  return cudaGetLastError();
+  return launch(k, dim3(2 * c.clusters), kGemmThreads, kBytes, false, s, m, c, p);
 }
 
 }  // namespace
@@ -1088,16 +1160,14 @@ cudaError_t head_clusters(uint32_t* out) {
 }
 
 cudaError_t launch_head_rows_map(const HeadCall& c, cudaStream_t s) {
-  fls_head_map_kernel<<<1, 1024, 0, s>>>(c);
-  return cudaGetLastError();
+  return launch(fls_head_map_kernel, dim3(uint32_t((c.rows + kRowChunk - 1) / kRowChunk)), kRowChunk, 0, true, s, c);
 }
 cudaError_t launch_head_pack(const HeadCall& c, cudaStream_t s) {
-  fls_head_pack_kernel<<<c.rows_cap, 128, 0, s>>>(c);
-  return cudaGetLastError();
+  if (c.rows <= kRowChunk) return launch(fls_head_pack_kernel<true>, dim3(c.rows_cap), 256, 0, true, s, c);
+  return launch(fls_head_pack_kernel<false>, dim3(c.rows_cap), 256, 0, false, s, c);
 }
 cudaError_t launch_head_pack_weight(const uint16_t* w, uint64_t stride, uint16_t* out, uint32_t vocab, uint32_t dim, uint32_t dp, cudaStream_t s) {
-  fls_head_pack_weight_kernel<<<vocab, 256, 0, s>>>(w, stride, out, dim, dp);
-  return cudaGetLastError();
+  return launch(fls_head_pack_weight_kernel, dim3(vocab), 256, 0, false, s, w, stride, out, dim, dp);
 }
 cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t s) {
   const HeadPiece p{0, c.vocab, 0, 0};
@@ -1111,8 +1181,7 @@ cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t
   return launch_gemm<kStats, false, false>(c, m, p, s);
 }
 cudaError_t launch_head_rows(const HeadCall& c, cudaStream_t s) {
-  fls_head_rows_kernel<<<c.rows_cap / 32, 32 * kRowsY, 0, s>>>(c);
-  return cudaGetLastError();
+  return launch(fls_head_rows_kernel, dim3(c.rows_cap / kRowsPerBlock), 256, 0, false, s, c);
 }
 cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
   if (c.planes == 2) return c.two ? launch_gemm<kDlogits, true, true>(c, m, p, s) : launch_gemm<kDlogits, false, true>(c, m, p, s);
@@ -1120,16 +1189,14 @@ cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const Head
 }
 cudaError_t launch_head_rescale(const HeadCall& c, cudaStream_t s) {
   const dim3 grid(c.rows_cap, c.keep_pitch / kKeepCols);
-  if (c.two) fls_head_rescale_kernel<true><<<grid, 256, 0, s>>>(c);
-  else fls_head_rescale_kernel<false><<<grid, 256, 0, s>>>(c);
-  return cudaGetLastError();
+  return c.two ? launch(fls_head_rescale_kernel<true>, grid, 256, 0, false, s, c) : launch(fls_head_rescale_kernel<false>, grid, 256, 0, false, s, c);
 }
 cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
   return launch_gemm<kGrads, false, false>(c, m, p, s);
 }
 cudaError_t launch_head_grad_hidden(const HeadCall& c, cudaStream_t s) {
-  fls_head_grad_hidden_kernel<<<uint32_t(c.rows), 128, 0, s>>>(c);
-  return cudaGetLastError();
+  // few rows: their columns spread over blocks of 1024
+  return launch(fls_head_grad_hidden_kernel, dim3(uint32_t(c.rows), c.rows <= 1024 ? (c.dim + 1023) / 1024 : 1), 256, 0, false, s, c);
 }
 
 }  // namespace fls
