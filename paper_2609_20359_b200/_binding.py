@@ -183,7 +183,7 @@ def _ptr_array(items: Sequence) -> C.Array:
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return int(stream) if isinstance(stream, int) else int(stream.cuda_stream)
 
 

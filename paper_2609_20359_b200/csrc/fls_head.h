@@ -87,7 +87,7 @@ cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const Head
 cudaError_t launch_head_rescale(const HeadCall& c, cudaStream_t s);
 cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s);
 cudaError_t launch_head_grad_hidden(const HeadCall& c, cudaStream_t s);
-// clusters of two CTAs that fit on the current device at once
+// Readies the kernels on the current device; clusters of two CTAs that fit on it at once.
 cudaError_t head_clusters(uint32_t* out);
 
 }  // namespace fls

@@ -1132,29 +1132,35 @@ template <int MODE, bool TWO, bool FLAG, bool KEEP = false>
 cudaError_t launch_gemm(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
   auto* k = fls_head_gemm_kernel<MODE, TWO, FLAG, KEEP>;
   constexpr uint32_t kBytes = Smem<MODE, FLAG, KEEP>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-  if (e != cudaSuccess) return e;
   return launch(k, dim3(2 * c.clusters), kGemmThreads, kBytes, false, s, m, c, p);
 }
 
 }  // namespace
 
+namespace {
+template <int MODE, bool TWO, bool FLAG, bool KEEP = false>
+cudaError_t allow_smem() {
+  return cudaFuncSetAttribute(fls_head_gemm_kernel<MODE, TWO, FLAG, KEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<MODE, FLAG, KEEP>::kBytes);
+}
+}  // namespace
+
 cudaError_t head_clusters(uint32_t* out) {
-  auto* k = fls_head_gemm_kernel<kStats, false, false, false>;      // the modes differ little in shared memory and not in CTAs per SM
-  constexpr uint32_t kSmemBytes = Smem<kStats, false, false>::kBytes;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  if (e != cudaSuccess) return e;
+  for (cudaError_t e : {allow_smem<kStats, false, false>(), allow_smem<kStats, false, true>(), allow_smem<kStats, true, false>(),
+                        allow_smem<kStats, false, false, true>(), allow_smem<kStats, false, true, true>(), allow_smem<kStats, true, false, true>(),
+                        allow_smem<kDlogits, false, false>(), allow_smem<kDlogits, true, false>(), allow_smem<kDlogits, false, true>(),
+                        allow_smem<kDlogits, true, true>(), allow_smem<kGrads, false, false>()})
+    if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(2);
   cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.dynamicSmemBytes = Smem<kStats, false, false>::kBytes;       // the variants differ little in it and not in CTAs per SM
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   int n = 0;
-  e = cudaOccupancyMaxActiveClusters(&n, k, &cfg);
+  const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, fls_head_gemm_kernel<kStats, false, false, false>, &cfg);
   *out = uint32_t(n > 0 ? n : 1);
   return e;
 }

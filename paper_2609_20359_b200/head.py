@@ -14,20 +14,24 @@ from . import _binding as fls
 
 def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: int, dtype: torch.dtype, device: torch.device):
     """Checks a 2-D tensor whose rows are contiguous; returns (address, elements between rows)."""
-    if t.dtype != dtype or t.device != device or t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows):
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != cols or (rows is not None and shape[0] != rows) or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor of shape [{'N' if rows is None else rows}, {cols}] on {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the elements of a row must be contiguous (stride {t.stride(1)})")
-    if t.shape[0] > 1 and t.stride(0) < cols:
-        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else cols)
+    row, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous (stride {one})")
+    if shape[0] <= 1:
+        row = cols
+    elif row < cols:
+        raise ValueError(f"{name}: rows overlap (stride {row})")
+    return t.data_ptr(), row
 
 
 def _dense(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, device: torch.device):
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -69,6 +73,7 @@ class Head:
         self.layout = fls.fls_head_query(self.handle)
         self.workspace = torch.empty(self.layout["workspace_bytes"], dtype=torch.uint8, device=self.device)
         self.workspace[:256].zero_()
+        self._args = fls.fls_head_io(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace.numel())   # of the call in preparation
 
     # ------------------------------------------------------------------ calls
     def xent(self, hidden, weight, labels, ignore_label: int = -100, label_smoothing: float = 0.0, z_loss: float = 0.0, stream=None):
@@ -114,18 +119,19 @@ class Head:
         return out
 
     def _io(self, hidden, weight, labels, ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream):
-        dev = self.device
-        h, hs = _matrix(hidden, "hidden", None, self.dim, torch.bfloat16, dev)
+        dev, dim, io = self.device, self.dim, self._args
+        io.hidden, io.hidden_stride = _matrix(hidden, "hidden", None, dim, torch.bfloat16, dev)
         n = hidden.shape[0]
-        w, ws = _matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16, dev)
-        gh, ghs = (None, 0) if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", n, self.dim, torch.bfloat16, dev)
-        gw, gws = (None, 0) if grad_weight is None else _matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype, dev)
-        out = _empty_on(stream, (2, n), torch.float32, dev)
-        loss = out.data_ptr()
-        io = fls.fls_head_io(n, h, w, _dense(labels, "labels", (n,), torch.int64, dev),
-                             _dense(row_weight, "row_weight", (n,), torch.float32, dev), loss, loss + 4 * n, gh, gw,
-                             self.workspace.data_ptr(), self.workspace.numel(), hs, ws, ghs, gws, ignore_label, int(accumulate), 0)
-        return io, (out[0], out[1])
+        io.rows = n
+        io.weight, io.weight_stride = _matrix(weight, "weight", self.vocab, dim, torch.bfloat16, dev)
+        io.labels = _dense(labels, "labels", (n,), torch.int64, dev)
+        io.row_weight = _dense(row_weight, "row_weight", (n,), torch.float32, dev)
+        io.grad_hidden, io.grad_hidden_stride = (None, 0) if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", n, dim, torch.bfloat16, dev)
+        io.grad_weight, io.grad_weight_stride = (None, 0) if grad_weight is None else _matrix(grad_weight, "grad_weight", self.vocab, dim, self.grad_torch_dtype, dev)
+        io.ignore_label, io.accumulate = ignore_label, accumulate
+        loss, lse = _empty_on(stream, (2, n), torch.float32, dev).unbind(0)
+        io.loss, io.lse = loss.data_ptr(), lse.data_ptr()
+        return io, (loss, lse)
 
     # ------------------------------------------------------------------ what the device wrote beside the outputs
     def _word(self, i: int) -> torch.Tensor:
