@@ -18,6 +18,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <type_traits>
 
 #include "fls.h"
 #include "fls_internal.h"
@@ -80,6 +81,25 @@ __device__ __forceinline__ float remote_f32(uint32_t a) {
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Two fp32 operations in one instruction.
+struct f2 { uint64_t v; };
+__device__ __forceinline__ f2 make_f2(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(f2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
   return r;
 }
 
@@ -269,44 +289,55 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
 
   // pass 1: maximum and sum of exponentials of what this thread reads
   float m = -INFINITY, s = 0.f;
-  auto batch = [&](const uint4* r, int cnt) {
+  const f2 c2 = make_f2(a.c, a.c);
+  auto batch = [&](const uint4* r, auto cnt) {
+    constexpr int n_vec = decltype(cnt)::value;
     float t = Vec<T>::top(r[0]);
 #pragma unroll
-    for (int j = 1; j < 4; ++j)
-      if (j < cnt) t = max_nan(t, Vec<T>::top(r[j]));
+    for (int j = 1; j < n_vec; ++j) t = max_nan(t, Vec<T>::top(r[j]));
     if (t > m || t != t) {                            // larger, or NaN, which stays
       s = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, t, a.c));
       m = t;
     }
     if (m == -INFINITY) return;
-    const bool huge = !(fabsf(m) < kHuge);
-    const float b = __fmul_rn(m, a.c);
-    float s0 = 0.f, s1 = 0.f;
+    if (!(fabsf(m) < kHuge)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < cnt) {
+      for (int j = 0; j < n_vec; ++j) {
         float x[VN];
         Vec<T>::unpack(r[j], x);
-        if (huge) {
 #pragma unroll
-          for (int e = 0; e < int(VN); ++e) s0 += ex2((x[e] - m) * a.c);
-        } else {
-#pragma unroll
-          for (int e = 0; e < int(VN); e += 2) { s0 += ex2(fmaf(x[e], a.c, -b)); s1 += ex2(fmaf(x[e + 1], a.c, -b)); }
-        }
+        for (int e = 0; e < int(VN); ++e) s += ex2((x[e] - m) * a.c);
       }
-    s += s0 + s1;
+      return;
+    }
+    const float b = -__fmul_rn(m, a.c);
+    const f2 b2 = make_f2(b, b);
+    f2 sum[2] = {make_f2(0.f, 0.f), make_f2(0.f, 0.f)};
+#pragma unroll
+    for (int j = 0; j < n_vec; ++j) {
+      float x[VN];
+      Vec<T>::unpack(r[j], x);
+#pragma unroll
+      for (int e = 0; e < int(VN); e += 2) {
+        float u, w;
+        split(fma2(make_f2(x[e], x[e + 1]), c2, b2), u, w);
+        sum[e / 2 % 2] = add2(sum[e / 2 % 2], make_f2(ex2(u), ex2(w)));
+      }
+    }
+    float u, w;
+    split(add2(sum[0], sum[1]), u, w);
+    s += u + w;
   };
   uint32_t i = threadIdx.x;
   for (; i + 3 * kTopThreads < p.n_vec; i += 4 * kTopThreads) {
     uint4 r[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) r[j] = p.vec[i + j * kTopThreads];
-    batch(r, 4);
+    batch(r, std::integral_constant<int, 4>());
   }
   for (; i < p.n_vec; i += kTopThreads) {
     const uint4 r = p.vec[i];
-    batch(&r, 1);
+    batch(&r, std::integral_constant<int, 1>());
   }
   const uint32_t key = order_key(m);                  // of the vectors only: the single elements are looked at below
   if (threadIdx.x < p.lead) add_one(Vec<T>::load(p.row + threadIdx.x), a.c, m, s);
@@ -339,7 +370,9 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   __syncthreads();
 
   // pass 2: the hot threads' logits again
+  const float low = key_value(thr);                   // NaN when only NaN may be chosen: the keys decide
   auto offer = [&](float x, uint32_t idx) {
+    if (x < low) return;
     const uint32_t k = order_key(x);
     if (k >= thr) {
       const uint32_t at = atomicAdd(&sh.n_cand, 1u);
@@ -350,8 +383,10 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   for (uint32_t w = threadIdx.x; w < items; w += kTopThreads) {
     const uint32_t h = w / per, v = (w - h * per) * kTopThreads + sh.hot[h];
     if (v < p.n_vec) {
+      const uint4 r = p.vec[v];
+      if (Vec<T>::top(r) < low) continue;
       float x[VN];
-      Vec<T>::unpack(p.vec[v], x);
+      Vec<T>::unpack(r, x);
 #pragma unroll
       for (int e = 0; e < int(VN); ++e) offer(x[e], p.vec0 + v * VN + e);
     }
@@ -371,6 +406,7 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   for (uint32_t q = threadIdx.x; q < cands; q += kTopThreads) {
     const uint64_t k = sh.cand[q];
     uint32_t r = 0;
+#pragma unroll 8
     for (uint32_t j = 0; j < cands; ++j) r += sh.cand[j] > k;
     if (r < a.top) { if (parts == 1) put(r, k); else sh.best[r] = k; }
   }
