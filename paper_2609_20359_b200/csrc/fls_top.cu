@@ -328,12 +328,27 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
     split(add2(sum[0], sum[1]), u, w);
     s += u + w;
   };
+  // Four vectors are added up while the next four are on their way: 128 KB in flight per SM.
+  constexpr uint32_t kStep = 4 * kTopThreads;
   uint32_t i = threadIdx.x;
-  for (; i + 3 * kTopThreads < p.n_vec; i += 4 * kTopThreads) {
-    uint4 r[4];
+  if (p.n_vec >= kStep) {
+    const uint32_t full = p.n_vec / kStep;
+    uint4 r[4], q[4];
+    auto fetch = [&](uint4* to, uint32_t k) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = p.vec[i + j * kTopThreads];
-    batch(r, std::integral_constant<int, 4>());
+      for (int j = 0; j < 4; ++j) to[j] = __ldg(p.vec + k * kStep + j * kTopThreads + threadIdx.x);
+    };
+    fetch(r, 0);
+#pragma unroll 1
+    for (uint32_t k = 0; k < full; k += 2) {
+      if (k + 1 < full) fetch(q, k + 1);
+      batch(r, std::integral_constant<int, 4>());
+      if (k + 1 < full) {
+        if (k + 2 < full) fetch(r, k + 2);
+        batch(q, std::integral_constant<int, 4>());
+      }
+    }
+    i += full * kStep;
   }
   for (; i < p.n_vec; i += kTopThreads) {
     const uint4 r = p.vec[i];
