@@ -1,13 +1,13 @@
 // fls_top_logits: the k largest logits of every row, ties to the lowest index, and the row's log sum exp.
 //
 // One pass over the logits, and a second look at few of them.  A row (or, when there are few rows, one of 2, 4 or 8 parts
-// of a row, the CTAs of a cluster) belongs to a CTA of 512 threads.  While a thread adds up exponentials it keeps the
-// largest logit it has seen.  The k-th largest of the 512 maxima is a lower bound of the k-th largest logit, and a close
-// one: only k threads can have seen a larger one, and of what they saw about 512 ln(512 / (512 - k)) logits are expected
-// to reach it (69 for k = 64).  So only the hot threads' logits, k / 512 of the row and still in L2, are read again.  The
-// candidates are then ranked by counting, on 64-bit keys (value, lowest index first) that are all different, which makes
-// the result independent of the order in which they were found.  Rows with so many equal logits that the candidates do
-// not fit are searched bit by bit instead (fls_top_exact below).
+// of a row, the CTAs of a cluster) belongs to a CTA of T threads.  While a thread adds up exponentials it keeps the largest
+// logit it has seen, overall and in each of up to nine stretches of what it reads.  The k-th largest of the T overall
+// maxima is a lower bound of the k-th largest logit, and a close one: about T ln(T / (T - k)) logits are expected to reach
+// it (68 for k = 64 and T = 512).  So only stretches whose maximum reaches it, about k of them and still in L2, are read
+// again.  The candidates are then ranked by counting, on 64-bit keys (value, lowest index first) that are all different,
+// which makes the result independent of the order in which they were found.  Rows with so many equal logits that the
+// stretches or candidates do not fit are searched bit by bit instead (fls_top_exact below).
 //
 // Bound by memory: 2 or 4 bytes per logit, read once.
 #include <cuda_bf16.h>
@@ -25,9 +25,8 @@
 
 namespace {
 
-constexpr int kTopThreads = 512;
-constexpr int kTopWarps = kTopThreads / 32;
 constexpr uint32_t kCap = 2048;              // candidates that are ranked directly
+static_assert(kCap >= 8 * FLS_HEAD_MAX_TOP, "the parts' results fit where the candidates were");
 constexpr uint32_t kNegInf = 0x007FFFFFu;    // order key of -inf; larger keys may be chosen
 
 struct TopArgs {
@@ -133,11 +132,14 @@ template <> struct Vec<uint16_t> {
   __device__ static __forceinline__ float load(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
 };
 
+constexpr uint32_t kStretches = 8;           // of whole steps (4 vectors per thread each), and one of what is left
+template <int kTopThreads>
 struct Shared {
-  uint64_t cand[kCap];
+  static constexpr int kTopWarps = kTopThreads / 32;
+  uint64_t cand[kCap];                       // later, in the cluster's first CTA, all parts' results
   uint64_t best[FLS_HEAD_MAX_TOP];           // this part's result, read by the cluster's first CTA
-  uint64_t merged[8 * FLS_HEAD_MAX_TOP];
-  uint32_t hot[kTopThreads];
+  float stretch[kStretches + 1][kTopThreads];
+  uint32_t hot[kTopThreads];                 // stretch * T + thread
   uint32_t scan[kTopWarps];
   float wm[kTopWarps], ws[kTopWarps];
   float m, s;
@@ -171,7 +173,7 @@ __device__ __forceinline__ void add_one(float x, float c, float& m, float& s) {
   m = n;
 }
 
-template <typename T, typename Body>
+template <int kTopThreads, typename T, typename Body>
 __device__ __forceinline__ void for_each(const Part<T>& p, Body&& body) {
   for (uint32_t i = threadIdx.x; i < p.n_vec; i += kTopThreads) {
     float x[Vec<T>::n];
@@ -185,14 +187,15 @@ __device__ __forceinline__ void for_each(const Part<T>& p, Body&& body) {
 
 // For rows with more than kCap candidates (many equal logits): the k-th largest key two bits at a time, then what is
 // above it, then the lowest indices of what equals it: 17 reads of the row, from L2.
-template <typename T>
-__device__ void fls_top_exact(const Part<T>& p, uint32_t top, Shared& sh) {
+template <int kTopThreads, typename T>
+__device__ void fls_top_exact(const Part<T>& p, uint32_t top, Shared<kTopThreads>& sh) {
+  constexpr int kTopWarps = kTopThreads / 32;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t thr = 0;
   for (int shift = 30; shift >= 0; shift -= 2) {
     uint32_t n1 = 0, n2 = 0, n3 = 0;
     const uint32_t t1 = thr | (1u << shift), t2 = thr | (2u << shift), t3 = thr | (3u << shift);
-    for_each(p, [&](float x, uint32_t) {
+    for_each<kTopThreads>(p, [&](float x, uint32_t) {
       const uint32_t k = order_key(x);
       if (k > kNegInf) { n1 += k >= t1; n2 += k >= t2; n3 += k >= t3; }
     });
@@ -210,7 +213,7 @@ __device__ void fls_top_exact(const Part<T>& p, uint32_t top, Shared& sh) {
   __syncthreads();
   if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
-  for_each(p, [&](float x, uint32_t idx) {
+  for_each<kTopThreads>(p, [&](float x, uint32_t idx) {
     const uint32_t k = order_key(x);
     if (k > kNegInf && k > thr) sh.cand[atomicAdd(&sh.n_cand, 1u)] = key64(k, idx);
   });
@@ -266,9 +269,10 @@ __device__ void fls_top_exact(const Part<T>& p, uint32_t top, Shared& sh) {
   __syncthreads();
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __grid_constant__ TopArgs a) {
-  __shared__ Shared sh;
+template <typename T, int kTopThreads>
+__global__ void __launch_bounds__(kTopThreads, kTopThreads == 512 ? 2 : 5) fls_top_logits_kernel(const __grid_constant__ TopArgs a) {
+  constexpr int kTopWarps = kTopThreads / 32;
+  __shared__ Shared<kTopThreads> sh;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t rank, parts;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -289,12 +293,14 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
 
   // pass 1: maximum and sum of exponentials of what this thread reads
   float m = -INFINITY, s = 0.f;
+  float seen = -INFINITY;                             // largest of the current stretch
   const f2 c2 = make_f2(a.c, a.c);
   auto batch = [&](const uint4* r, auto cnt) {
     constexpr int n_vec = decltype(cnt)::value;
     float t = Vec<T>::top(r[0]);
 #pragma unroll
     for (int j = 1; j < n_vec; ++j) t = max_nan(t, Vec<T>::top(r[j]));
+    seen = max_nan(seen, t);
     if (t > m || t != t) {                            // larger, or NaN, which stays
       s = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, t, a.c));
       m = t;
@@ -330,9 +336,17 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   };
   // Four vectors are added up while the next four are on their way: 128 KB in flight per SM.
   constexpr uint32_t kStep = 4 * kTopThreads;
-  uint32_t i = threadIdx.x;
-  if (p.n_vec >= kStep) {
-    const uint32_t full = p.n_vec / kStep;
+  const uint32_t full = p.n_vec / kStep;
+  uint32_t shift = 0;                                 // 2^shift steps per stretch
+  while ((full + (1u << shift) - 1) >> shift > kStretches) ++shift;
+  const uint32_t stretches = (full + (1u << shift) - 1) >> shift;
+  auto close = [&](uint32_t k) {                      // after step k
+    if (((k + 1) & ((1u << shift) - 1)) == 0 || k + 1 == full) {
+      sh.stretch[k >> shift][threadIdx.x] = seen;
+      seen = -INFINITY;
+    }
+  };
+  if (full) {
     uint4 r[4], q[4];
     auto fetch = [&](uint4* to, uint32_t k) {
 #pragma unroll
@@ -343,17 +357,19 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
     for (uint32_t k = 0; k < full; k += 2) {
       if (k + 1 < full) fetch(q, k + 1);
       batch(r, std::integral_constant<int, 4>());
+      close(k);
       if (k + 1 < full) {
         if (k + 2 < full) fetch(r, k + 2);
         batch(q, std::integral_constant<int, 4>());
+        close(k + 1);
       }
     }
-    i += full * kStep;
   }
-  for (; i < p.n_vec; i += kTopThreads) {
+  for (uint32_t i = full * kStep + threadIdx.x; i < p.n_vec; i += kTopThreads) {
     const uint4 r = p.vec[i];
     batch(&r, std::integral_constant<int, 1>());
   }
+  sh.stretch[stretches][threadIdx.x] = seen;          // what is left: fewer than 4 vectors per thread
   const uint32_t key = order_key(m);                  // of the vectors only: the single elements are looked at below
   if (threadIdx.x < p.lead) add_one(Vec<T>::load(p.row + threadIdx.x), a.c, m, s);
   if (threadIdx.x < p.trail) add_one(Vec<T>::load(p.row + p.trail0 + threadIdx.x), a.c, m, s);
@@ -381,11 +397,16 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
     if (__syncthreads_count(key >= t) >= int(a.top)) thr = t;
   }
   thr = max(thr, kNegInf + 1);
-  if (key >= thr) sh.hot[atomicAdd(&sh.n_hot, 1u)] = threadIdx.x;
+  const float low = key_value(thr);                   // NaN when only NaN may be chosen: the keys decide
+  if (key >= thr)
+    for (uint32_t g = 0; g <= stretches; ++g)
+      if (!(sh.stretch[g][threadIdx.x] < low)) {
+        const uint32_t at = atomicAdd(&sh.n_hot, 1u);
+        if (at < kTopThreads) sh.hot[at] = g * kTopThreads + threadIdx.x;
+      }
   __syncthreads();
 
-  // pass 2: the hot threads' logits again
-  const float low = key_value(thr);                   // NaN when only NaN may be chosen: the keys decide
+  // pass 2: the hot stretches again
   auto offer = [&](float x, uint32_t idx) {
     if (x < low) return;
     const uint32_t k = order_key(x);
@@ -394,10 +415,13 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
       if (at < kCap) sh.cand[at] = key64(k, idx);
     }
   };
-  const uint32_t per = (p.n_vec + kTopThreads - 1) / kTopThreads, items = sh.n_hot * per;
+  const bool too_hot = sh.n_hot > uint32_t(kTopThreads);
+  const uint32_t per = 4u << shift, items = too_hot ? 0 : sh.n_hot * per;
   for (uint32_t w = threadIdx.x; w < items; w += kTopThreads) {
-    const uint32_t h = w / per, v = (w - h * per) * kTopThreads + sh.hot[h];
-    if (v < p.n_vec) {
+    const uint32_t h = sh.hot[w / per], g = h / kTopThreads, t = h % kTopThreads;
+    const bool whole = g < stretches;                 // the last one may be short
+    const uint32_t v = ((whole ? g * per : full * 4) + w % per) * kTopThreads + t;
+    if (v < (whole ? full * kStep : p.n_vec)) {
       const uint4 r = p.vec[v];
       if (Vec<T>::top(r) < low) continue;
       float x[VN];
@@ -409,7 +433,7 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   if (threadIdx.x < p.lead) offer(Vec<T>::load(p.row + threadIdx.x), threadIdx.x);
   if (threadIdx.x < p.trail) offer(Vec<T>::load(p.row + p.trail0 + threadIdx.x), p.trail0 + threadIdx.x);
   __syncthreads();
-  if (sh.n_cand > kCap) fls_top_exact(p, a.top, sh);
+  if (too_hot || sh.n_cand > kCap) fls_top_exact<kTopThreads>(p, a.top, sh);
   const uint32_t cands = sh.n_cand;
 
   // rank by counting: the keys are all different
@@ -444,7 +468,7 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   if (rank == 0) {
     for (uint32_t q = threadIdx.x; q < parts * a.top; q += kTopThreads) {
       const uint32_t w = q / a.top;
-      sh.merged[q] = remote_u64(remote(&sh.best[q - w * a.top], w));
+      sh.cand[q] = remote_u64(remote(&sh.best[q - w * a.top], w));
     }
     if (threadIdx.x == 0) {
       float mm = -INFINITY;
@@ -460,10 +484,10 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
   cluster_sync();
   if (rank != 0) return;
   for (uint32_t q = threadIdx.x; q < parts * a.top; q += kTopThreads) {
-    const uint64_t k = sh.merged[q];
+    const uint64_t k = sh.cand[q];
     uint32_t r = 0;
     for (uint32_t w = 0; w < parts; ++w) {
-      const uint64_t* list = sh.merged + w * a.top;
+      const uint64_t* list = sh.cand + w * a.top;
       uint32_t lo = 0, len = a.top;                   // first entry not above k
       while (len) {
         const uint32_t half = len >> 1;
@@ -472,7 +496,7 @@ __global__ void __launch_bounds__(kTopThreads, 2) fls_top_logits_kernel(const __
       r += lo;
     }
     if (k == 0)                                       // empty entries follow all others
-      for (uint32_t j = 0; j < q; ++j) r += sh.merged[j] == 0;
+      for (uint32_t j = 0; j < q; ++j) r += sh.cand[j] == 0;
     if (r < a.top) put(r, k);
   }
 }
@@ -521,12 +545,16 @@ extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t
       if (a < b + s[j].bytes && b < a + s[i].bytes) return fail(FLS_EPTR, "%s overlaps %s", s[i].what, s[j].what);
     }
   TopArgs a{logits, stride, uint32_t(vocab), top, float(1.4426950408889634 / temperature), 1.0 / temperature, value, index, lse};
-  // Few rows: a row is shared by the CTAs of a cluster, as long as a thread still has a 16-byte vector or two to read.
+  // Few rows: a row is shared by the CTAs of a cluster, as long as a thread still has a 16-byte vector or two to read, and
+  // the CTAs are large (one row of 128256 bf16, k = 64: 12.6 us with 512 threads, 16.3 with 256).  Otherwise a CTA is small,
+  // five share an SM and some read while others rank (4096 rows of 128256 bf16: 204 us with 256 threads, 247 with 512;
+  // 4096 of 32000 fp32, k = 8: 104 and 147; 2000 of 5000 bf16: 23 and 45).
   uint32_t parts = 1;
-  while (parts < 8 && rows * parts * 2 <= 296 && vocab * elem >= uint64_t(parts) * 2 * kTopThreads * 16) parts *= 2;
+  while (parts < 8 && rows * parts * 2 <= 296 && vocab * elem >= uint64_t(parts) * 2 * 512 * 16) parts *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(uint32_t(rows) * parts);
-  cfg.blockDim = dim3(kTopThreads);
+  const int threads = parts > 1 ? 512 : 256;
+  cfg.blockDim = dim3(threads);
   cfg.stream = static_cast<cudaStream_t>(cuda_stream);
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeClusterDimension;
@@ -534,8 +562,11 @@ extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  const cudaError_t e = logit_dtype == FLS_GRAD_F32 ? cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<float>, a)
-                                                    : cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<uint16_t>, a);
+  const bool f32 = logit_dtype == FLS_GRAD_F32;
+  const cudaError_t e = threads == 512 ? (f32 ? cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<float, 512>, a)
+                                              : cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<uint16_t, 512>, a))
+                                       : (f32 ? cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<float, 256>, a)
+                                              : cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<uint16_t, 256>, a));
   if (e != cudaSuccess) return fail(FLS_ECUDA, "fls_top_logits: %s", cudaGetErrorString(e));
   return FLS_OK;
 }
