@@ -32,6 +32,7 @@ struct HeadCall {
   int32_t* src;              // [rows_cap]: row of a packed row
   uint16_t* hp;              // [rows_cap][dp]: packed hidden rows, zero up to the next multiple of 256 rows
   int32_t* slot_idx;         // [rows_cap][slots]: columns that get a value of their own, ascending, INT32_MAX = none
+  uint8_t* slot_start;       // [rows_cap][tiles]: the first of them in each 128 columns (only with a teacher's list)
   float* slot_t;             // [rows_cap][slots]: the teacher's logit of that column (-inf: label only)
   float* slot_z;             // [rows_cap][slots]: the logit of that column
   float* slot_g;             // [rows_cap][slots]: its gradient

@@ -34,7 +34,7 @@ constexpr uint64_t kMinPartialBytes = 48ull << 20;   // room for the split sums 
 
 // Byte offsets of the workspace.  Sizes are those of max_rows; a smaller call uses the front of each region.
 struct Regions {
-  uint64_t mask, counts, pos, src, hp, slot_idx, slot_t, slot_z, slot_g, part, coef, g, dh, wcopy, total;
+  uint64_t mask, counts, pos, src, hp, slot_idx, slot_start, slot_t, slot_z, slot_g, part, coef, g, dh, wcopy, total;
   uint64_t part_bytes, g_bytes, dh_bytes;
 };
 
@@ -51,6 +51,7 @@ Regions regions(const fls_head_desc& d) {
   r.src = take(cap * 4);
   r.hp = take(cap * dp * 2);
   r.slot_idx = take(cap * slots * 4);
+  if (d.top) r.slot_start = take(cap * tiles);
   r.slot_t = take(cap * slots * 4);
   r.slot_z = take(cap * slots * 4);
   r.slot_g = take(cap * slots * 4);
@@ -182,6 +183,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.src = reinterpret_cast<int32_t*>(ws + r.src);
   c.hp = reinterpret_cast<uint16_t*>(ws + r.hp);
   c.slot_idx = reinterpret_cast<int32_t*>(ws + r.slot_idx);
+  c.slot_start = reinterpret_cast<uint8_t*>(ws + r.slot_start);
   c.slot_t = reinterpret_cast<float*>(ws + r.slot_t);
   c.slot_z = reinterpret_cast<float*>(ws + r.slot_z);
   c.slot_g = reinterpret_cast<float*>(ws + r.slot_g);

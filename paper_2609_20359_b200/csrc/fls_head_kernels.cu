@@ -138,6 +138,45 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two fp32 operations in one instruction.
+struct f2 { uint64_t v; };
+__device__ __forceinline__ f2 make_f2(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(f2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// sum over 32 values of 2^(z c - b)
+__device__ __forceinline__ float sum_ex2(const float (&z)[32], float c, float b) {
+  const f2 c2 = make_f2(c, c), b2 = make_f2(-b, -b);
+  f2 t0 = make_f2(0.f, 0.f), t1 = t0;
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    float u, v, x, y;
+    split(fma2(make_f2(z[j], z[j + 1]), c2, b2), u, v);
+    split(fma2(make_f2(z[j + 2], z[j + 3]), c2, b2), x, y);
+    t0 = add2(t0, make_f2(ex2(u), ex2(v)));
+    t1 = add2(t1, make_f2(ex2(x), ex2(y)));
+  }
+  float u, v;
+  split(add2(t0, t1), u, v);
+  return u + v;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -242,25 +281,31 @@ struct Schedule {
 };
 
 // ------------------------------------------------------------------------------------------------ epilogues
-// First of this row's columns that is not below `col`.
-__device__ __forceinline__ uint32_t lower_slot(const int32_t* idx, uint32_t n, int32_t col) {
-  uint32_t lo = 0;
-  while (n) {
-    const uint32_t h = n >> 1;
-    if (idx[lo + h] < col) { lo += h + 1; n -= h + 1; } else n = h;
+// A row's own columns from some point on, ascending.  The one after the next is fetched ahead.
+struct Columns {
+  int32_t next = INT_MAX, after = INT_MAX;
+  const int32_t* idx;
+  uint32_t ptr, slots;
+  __device__ __forceinline__ int32_t at(uint32_t i) const { return i < slots ? idx[i] : INT_MAX; }
+  // start: the first of them not below the tile's first column
+  __device__ __forceinline__ void open(const int32_t* i, uint32_t n, uint32_t start) {
+    idx = i; slots = n; ptr = start;
+    next = at(start);
+    after = at(start + 1);
   }
-  return lo;
-}
+  __device__ __forceinline__ void advance() {
+    ++ptr;
+    next = after;
+    after = at(ptr + 1);
+  }
+};
 
 // Maximum and sum of exponentials of one row of a tile.  Columns with a value of their own (the label, the teacher's
 // list) are written down and left out of the sum, so that "everything else" is known without a cancelling difference.
 template <bool TWO, bool SMOOTH>
-struct StatsRow {
+struct StatsRow : Columns {
   float m = -INFINITY, s = 0.f, s1 = 0.f, sz = 0.f;
-  int32_t next = INT_MAX;
-  const int32_t* idx;
   float* zs;
-  uint32_t ptr, slots;
   __device__ __forceinline__ void chunk(float (&z)[32], int32_t col0, uint32_t vocab, float cT, float c1) {
     const bool edge = uint32_t(col0) + 32 > vocab;
     if constexpr (SMOOTH) {
@@ -286,14 +331,17 @@ struct StatsRow {
       const int32_t at = next;
       do {                                            // repeated columns share the value
         zs[ptr] = v;
-        ++ptr;
-        next = ptr < slots ? idx[ptr] : INT_MAX;
+        advance();
       } while (next == at);
     }
-    float x0 = z[0], x1 = z[1], x2 = z[2], x3 = z[3];
+    float x0 = max3(z[0], z[1], z[2]), x1 = max3(z[3], z[4], z[5]), x2 = max3(z[6], z[7], z[8]), x3 = max3(z[9], z[10], z[11]);
 #pragma unroll
-    for (int j = 4; j < 32; j += 4) { x0 = fmaxf(x0, z[j]); x1 = fmaxf(x1, z[j + 1]); x2 = fmaxf(x2, z[j + 2]); x3 = fmaxf(x3, z[j + 3]); }
-    const float cm = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
+    for (int j = 12; j < 28; j += 8) {
+      x0 = max3(x0, z[j], z[j + 1]); x1 = max3(x1, z[j + 2], z[j + 3]); x2 = max3(x2, z[j + 4], z[j + 5]); x3 = max3(x3, z[j + 6], z[j + 7]);
+    }
+    x0 = max3(x0, z[28], z[29]);
+    x1 = max3(x1, z[30], z[31]);
+    const float cm = fmaxf(max3(x0, x1, x2), x3);
     if (cm > m) {
       const float old = m;
       m = cm;
@@ -303,25 +351,8 @@ struct StatsRow {
       }
     }
     const float bT = m == -INFINITY ? 0.f : __fmul_rn(m, cT);
-    float t0 = 0.f, t1 = 0.f, t2 = 0.f, t3 = 0.f;
-#pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      t0 += ex2(fmaf(z[j], cT, -bT));
-      t1 += ex2(fmaf(z[j + 1], cT, -bT));
-      t2 += ex2(fmaf(z[j + 2], cT, -bT));
-      t3 += ex2(fmaf(z[j + 3], cT, -bT));
-    }
-    s += (t0 + t1) + (t2 + t3);
-    if constexpr (TWO) {
-      const float b1 = m == -INFINITY ? 0.f : __fmul_rn(m, c1);
-      t0 = t1 = 0.f;
-#pragma unroll
-      for (int j = 0; j < 32; j += 2) {
-        t0 += ex2(fmaf(z[j], c1, -b1));
-        t1 += ex2(fmaf(z[j + 1], c1, -b1));
-      }
-      s1 += t0 + t1;
-    }
+    s += sum_ex2(z, cT, bT);
+    if constexpr (TWO) s1 += sum_ex2(z, c1, m == -INFINITY ? 0.f : __fmul_rn(m, c1));
   }
 };
 
@@ -386,21 +417,24 @@ struct Stager {
 
 // dL/dz of one row of a tile: aT exp(z/T - lse_T) + a1 exp(z - lse_1) - b, then the columns with a value of their own.
 template <bool TWO, bool PLANES, int BUFS>
-struct DlogitsRow {
+struct DlogitsRow : Columns {
   float4 k;          // {lse_T log2(e), aT, lse_1 log2(e), a1}; without TWO {lse log2(e) , a, b, -}
-  int32_t next = INT_MAX;
-  const int32_t* idx;
   const float* val;
-  uint32_t ptr, slots;
   // the first (half 0) or second 32 of the 64 columns from col0 on; lo: buffer of the second term (PLANES)
   __device__ __forceinline__ void chunk(float (&v)[32], int32_t col0, uint32_t half, uint32_t vocab, float cT, float c1,
                                         const Stager<BUFS>& out, uint32_t hi, uint32_t lo) {
     const int32_t c0 = col0 + int32_t(half) * 32;
+    if constexpr (TWO) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const float z = v[j];
-      if constexpr (TWO) v[j] = fmaf(k.w, ex2(fmaf(z, c1, -k.z)), k.y * ex2(fmaf(z, cT, -k.x)));
-      else v[j] = fmaf(k.y, ex2(fmaf(z, cT, -k.x)), -k.z);
+      for (int j = 0; j < 32; ++j) v[j] = fmaf(k.w, ex2(fmaf(v[j], c1, -k.z)), k.y * ex2(fmaf(v[j], cT, -k.x)));
+    } else {
+      const f2 c2 = make_f2(cT, cT), l2 = make_f2(-k.x, -k.x), a2 = make_f2(k.y, k.y), b2 = make_f2(-k.z, -k.z);
+#pragma unroll
+      for (int j = 0; j < 32; j += 2) {
+        float x, y;
+        split(fma2(make_f2(v[j], v[j + 1]), c2, l2), x, y);
+        split(fma2(a2, make_f2(ex2(x), ex2(y)), b2), v[j], v[j + 1]);
+      }
     }
     if (uint32_t(c0) + 32 > vocab) {
 #pragma unroll
@@ -417,8 +451,7 @@ struct DlogitsRow {
       const float x = val[ptr];
       out.put_one(hi, uint32_t(next - col0), bf16_bits(x));
       if constexpr (PLANES) out.put_one(lo, uint32_t(next - col0), bf16_bits(x - bf16_round(x)));
-      ++ptr;
-      next = ptr < slots ? idx[ptr] : INT_MAX;
+      advance();
     }
   }
 };
@@ -464,6 +497,12 @@ __device__ __forceinline__ void store_row32(T* dst, const float (&v)[32], uint32
       }
     }
   }
+}
+
+// The first of a packed row's own columns that is not below column n (a multiple of 128).
+__device__ __forceinline__ uint32_t first_slot(const HeadCall& c, uint32_t row, uint32_t n) {
+  if (c.slots == 1) return c.slot_idx[row] < int32_t(n) ? 1 : 0;
+  return c.slot_start[uint64_t(row) * c.tiles + n / kHeadStatCols];
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
@@ -602,24 +641,14 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
       StatsRow<TWO, FLAG> st;
       DlogitsRow<TWO, FLAG, kBufs> dl;
       if constexpr (MODE == kStats) {
-        st.idx = c.slot_idx + uint64_t(row) * c.slots;
         st.zs = c.slot_z + uint64_t(row) * c.slots;
-        st.slots = c.slots;
-        st.ptr = c.slots;
-        if (row < count) {
-          st.ptr = lower_slot(st.idx, c.slots, int32_t(n0));
-          st.next = st.ptr < c.slots ? st.idx[st.ptr] : INT_MAX;
-        }
+        if (row < count) st.open(c.slot_idx + uint64_t(row) * c.slots, c.slots, first_slot(c, row, n0));
       } else if constexpr (MODE == kDlogits) {
-        dl.idx = c.slot_idx + uint64_t(row) * c.slots;
         dl.val = c.slot_g + uint64_t(row) * c.slots;
-        dl.slots = c.slots;
-        dl.ptr = c.slots;
         dl.k = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row < count) {
           dl.k = c.coef[row];
-          dl.ptr = lower_slot(dl.idx, c.slots, int32_t(piece.v0 + n0));
-          dl.next = dl.ptr < c.slots ? dl.idx[dl.ptr] : INT_MAX;
+          dl.open(c.slot_idx + uint64_t(row) * c.slots, c.slots, first_slot(c, row, piece.v0 + n0));
         }
       }
       if (!empty) {
@@ -776,6 +805,7 @@ __global__ void __launch_bounds__(kRowChunk) fls_head_map_kernel(const __grid_co
 template <bool ONE_CHUNK>
 __global__ void __launch_bounds__(256) fls_head_pack_kernel(const __grid_constant__ HeadCall c) {
   __shared__ int32_t s_idx[FLS_HEAD_MAX_TOP + 1];
+  __shared__ int32_t s_sorted[FLS_HEAD_MAX_TOP + 1];
   __shared__ float s_t[FLS_HEAD_MAX_TOP + 1];
   __shared__ uint32_t s_mask[kRowChunk / 32], s_before, s_count;
   const uint32_t i = blockIdx.x, chunk = i / kRowChunk;
@@ -846,6 +876,18 @@ __global__ void __launch_bounds__(256) fls_head_pack_kernel(const __grid_constan
     for (uint32_t j = 0; j < c.slots; ++j) rank += s_idx[j] < x || (s_idx[j] == x && j < k);
     c.slot_idx[uint64_t(p) * c.slots + rank] = x;
     c.slot_t[uint64_t(p) * c.slots + rank] = s_t[k];
+    s_sorted[rank] = x;
+  }
+  if (c.slots == 1) return;
+  __syncthreads();
+  for (uint32_t t = threadIdx.x; t < c.tiles; t += blockDim.x) {
+    const int32_t col = int32_t(t * kHeadStatCols);
+    uint32_t lo = 0, len = c.slots;
+    while (len) {
+      const uint32_t h = len >> 1;
+      if (s_sorted[lo + h] < col) { lo += h + 1; len -= h + 1; } else len = h;
+    }
+    c.slot_start[uint64_t(p) * c.tiles + t] = uint8_t(lo);
   }
 }
 
