@@ -13,7 +13,6 @@ constexpr int kHeadBM = 256;      // rows of C per CTA pair (128 per CTA)
 constexpr int kHeadBN = 256;      // columns of C per CTA pair; both CTAs hold all of them for their own rows
 constexpr int kHeadBK = 64;       // depth of one pipeline stage: 64 bf16 = one 128-byte swizzle row
 constexpr int kHeadStatCols = 128; // columns per partial sum of a row
-constexpr uint32_t kHeadKeepCols = 2048;
 constexpr int kHeadMaxSplits = 64;
 
 // Head of the workspace: words the device writes.
@@ -41,8 +40,8 @@ struct HeadCall {
   float* part_s1;            // same at temperature 1 (only when T != 1 and labels count)
   float* part_z;             // sum of the logits (only with label smoothing)
   float4* coef;              // [rows_cap]: see fls_head_rows_kernel
-  uint16_t* g;               // [planes][rows_cap][piece_cols]: d loss / d logits of one piece of the vocabulary
-  float* keep_z;             // [rows_cap][keep_pitch]: kept logits, in the bytes of g
+  uint16_t* g;               // d loss / d logits of one piece of the vocabulary, in panels of 64 columns (dz_panel)
+  float* keep_z;             // [panels of 32 columns][rows_cap][32]: kept logits, in the bytes of g
   float* dh;                 // [splits][rows_cap][dcap]: partial sums of the hidden gradient
   // problem
   const uint16_t* hidden; uint64_t hidden_stride;
@@ -62,7 +61,6 @@ struct HeadCall {
   uint32_t max_splits, clusters, group_m;
   uint32_t prefetch_weight;  // one row tile, and the weight is the caller's: fetched ahead of the packed rows
   uint32_t keep_v0;          // columns from here on keep their logits, vocab: none
-  uint32_t keep_pitch;       // kept columns, rounded up to kHeadKeepCols
   uint32_t split_cols;       // columns of the widest piece, 0 without gradients
   float c1, cT;              // log2(e), log2(e) / T
   double inv_temp, temp, smoothing, z_loss, distill_weight, label_weight;
@@ -76,7 +74,7 @@ struct HeadMaps { CUtensorMap a0, b0, a1, b1, store, store2; };
 struct HeadPiece {
   uint32_t v0, width;        // the columns of the vocabulary it works on
   uint32_t first;            // first piece: the hidden gradient's partial sums are stored, later ones added to
-  uint32_t kept;             // its dL/dz comes from kept logits and lies where they were
+  uint32_t panel_step;       // panels from one 64 columns of dL/dz to the next
 };
 
 cudaError_t launch_head_rows_map(const HeadCall& c, cudaStream_t s);
@@ -86,6 +84,7 @@ cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t
 cudaError_t launch_head_rows(const HeadCall& c, cudaStream_t s);
 cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s);
 cudaError_t launch_head_rescale(const HeadCall& c, cudaStream_t s);
+cudaError_t launch_head_own(const HeadCall& c, cudaStream_t s);
 cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s);
 cudaError_t launch_head_grad_hidden(const HeadCall& c, cudaStream_t s);
 // Readies the kernels on the current device; clusters of two CTAs that fit on it at once.

@@ -59,7 +59,7 @@ Regions regions(const fls_head_desc& d) {
   r.part = take(3 * r.part_bytes);          // maximum, sum, and one of: sum at temperature 1, sum of logits
   r.coef = take(cap * 16);
   if (d.grads) {
-    const uint64_t all = 4 * cap * up(d.vocab, kHeadKeepCols);       // every logit kept
+    const uint64_t all = 4 * cap * up(d.vocab, 256);                 // every logit kept
     r.g_bytes = std::min(all, std::max(d.piece_bytes ? d.piece_bytes : kDefaultPieceBytes, 2 * planes * cap * kMinPieceCols));
     r.g = take(r.g_bytes);
     r.dh_bytes = std::max(2 * cap * dcap * 4, kMinPartialBytes);
@@ -72,13 +72,12 @@ Regions regions(const fls_head_desc& d) {
 
 // How the vocabulary is taken apart.  The last columns keep the logits of the statistics pass, 4 bytes each, and get their
 // dL/dz from those; the columns before them are formed again, in pieces of 2 bytes per column and term, evened out.
-struct Pieces { uint32_t keep_v0, keep_pitch, cols; };
+struct Pieces { uint32_t keep_v0, cols; };
 Pieces pieces_of(const fls_head_desc& d, uint64_t g_bytes, uint64_t rows_cap, uint64_t planes) {
   Pieces p{};
-  const uint64_t keep = std::min(kMaxPieceCols, g_bytes / (4 * rows_cap) / kHeadKeepCols * kHeadKeepCols);
+  const uint64_t keep = std::min(kMaxPieceCols, g_bytes / (4 * rows_cap) / 256 * 256);
   const uint64_t v0 = keep >= d.vocab ? 0 : keep ? up(d.vocab - keep, 256) : d.vocab;
   p.keep_v0 = uint32_t(std::min(v0, d.vocab));
-  p.keep_pitch = uint32_t(up(d.vocab - p.keep_v0, kHeadKeepCols));
   if (p.keep_v0) {
     const uint64_t vr = up(p.keep_v0, 256);
     const uint64_t most = std::min({vr, kMaxPieceCols, std::max<uint64_t>(256, g_bytes / (2 * planes * rows_cap) / 256 * 256)});
@@ -98,6 +97,16 @@ bool encode(EncodeTiled f, CUtensorMap* m, const void* base, uint64_t cols, uint
   const cuuint64_t strides[1] = {stride * (f32 ? 4 : 2)};
   const cuuint32_t box[2] = {f32 ? 32u : 64u, box_rows}, step[2] = {1, 1};
   return f(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Panels of 128 bytes x rows, boxes of box_rows rows of one panel.
+bool encode_panels(EncodeTiled f, CUtensorMap* m, const void* base, uint64_t rows, uint64_t panels, uint32_t box_rows, bool f32 = false) {
+  const cuuint64_t dims[3] = {f32 ? 32u : 64u, rows, panels};
+  const cuuint64_t strides[2] = {128, rows * 128};
+  const cuuint32_t box[3] = {f32 ? 32u : 64u, box_rows, 1}, step[3] = {1, 1, 1};
+  return f(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -230,7 +239,6 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   if (grads) {
     const Pieces p = pieces_of(d, r.g_bytes, c.rows_cap, c.planes);
     c.keep_v0 = p.keep_v0;
-    c.keep_pitch = p.keep_pitch;
     c.piece_cols = p.cols;
     c.split_cols = std::max(p.cols, uint32_t(up(c.vocab - p.keep_v0, 256)));
     c.max_splits = uint32_t(std::min<uint64_t>(kHeadMaxSplits, r.dh_bytes / (uint64_t(c.rows_cap) * c.dcap * 4)));
@@ -256,14 +264,15 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
          encode(f, &grad.store2, c.dh, c.dcap, uint64_t(c.max_splits) * c.rows_cap, c.dcap, 32, true) &&
          (!c.want_gw || c.direct_store || encode(f, &grad.store, c.grad_weight, d.dim, d.vocab, c.grad_weight_stride, 32, c.grad_f32));
   kept = grad;
-  if (ok && keeps)
-    ok = encode(f, &stat.store, c.keep_z, c.keep_pitch, c.rows_cap, c.keep_pitch, 32, true) &&
-         encode(f, &kept.a0, c.g, 2ull * c.keep_pitch, c.rows_cap, 2ull * c.keep_pitch, 64) &&
-         encode(f, &kept.a1, c.g, 2ull * c.keep_pitch, c.rows_cap, 2ull * c.keep_pitch, 128);
+  if (ok && keeps) {
+    const uint64_t n = up(d.vocab - c.keep_v0, 256) / 32;
+    ok = encode_panels(f, &stat.store, c.keep_z, c.rows_cap, n, 32, true) && encode_panels(f, &kept.a0, c.g, c.rows_cap, n, 64) &&
+         encode_panels(f, &kept.a1, c.g, c.rows_cap, n, 128);
+  }
   if (ok && forms) {
-    const uint64_t n = uint64_t(c.planes) * c.rows_cap;
-    ok = encode(f, &fwd.store, c.g, c.piece_cols, n, c.piece_cols, 32) && encode(f, &grad.a0, c.g, c.piece_cols, n, c.piece_cols, 64) &&
-         encode(f, &grad.a1, c.g, c.piece_cols, n, c.piece_cols, 128);
+    const uint64_t n = uint64_t(c.planes) * c.piece_cols / 64;
+    ok = encode_panels(f, &fwd.store, c.g, c.rows_cap, n, 32) && encode_panels(f, &grad.a0, c.g, c.rows_cap, n, 64) &&
+         encode_panels(f, &grad.a1, c.g, c.rows_cap, n, 128);
   }
   if (!ok) return fail(FLS_ECUDA, "cuTensorMapEncodeTiled failed");
 
@@ -283,10 +292,11 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   if (grads) {
     if (keeps) {
       FLS_LAUNCH(launch_head_rescale(c, s));
-      FLS_LAUNCH(launch_head_grads(c, kept, HeadPiece{c.keep_v0, c.vocab - c.keep_v0, 1, 1}, s));
+      FLS_LAUNCH(launch_head_own(c, s));
+      FLS_LAUNCH(launch_head_grads(c, kept, HeadPiece{c.keep_v0, c.vocab - c.keep_v0, 1, 2}, s));
     }
     for (uint32_t v0 = 0; v0 < c.keep_v0; v0 += c.piece_cols) {
-      const HeadPiece p{v0, std::min(c.piece_cols, c.keep_v0 - v0), !keeps && v0 == 0, 0};
+      const HeadPiece p{v0, std::min(c.piece_cols, c.keep_v0 - v0), !keeps && v0 == 0, c.planes};
       FLS_LAUNCH(launch_head_dlogits(c, fwd, p, s));
       FLS_LAUNCH(launch_head_grads(c, grad, p, s));
     }

@@ -62,12 +62,12 @@ def test_workspace_and_pieces(fls, rows, vocab, dim, top, f32, piece):
     h = fls.fls_head_create(rows, vocab, dim, top, True, f32, False, piece)
     q = fls.fls_head_query(h)
     cap, planes = max(256, -(-rows // 256) * 256), 2 if f32 else 1
-    # the kept columns at the end (4 bytes each, whole blocks of 2048) and the pieces before them cover the vocabulary once
+    # the kept columns at the end (4 bytes each, whole tiles of 256) and the pieces before them cover the vocabulary once
     formed, most = vocab - q["kept_cols"], max(piece or 1 << 30, 2 * planes * cap * 512)
     assert 0 <= q["kept_cols"] <= vocab and (formed == 0 or formed % 256 == 0 or q["kept_cols"] == 0)
     assert q["piece_cols"] % 256 == 0 and q["piece_cols"] * q["pieces"] >= formed and (formed == 0) == (q["pieces"] == 0)
     assert q["pieces"] == 0 or formed > q["piece_cols"] * (q["pieces"] - 1)
-    assert 4 * cap * (-(-q["kept_cols"] // 2048) * 2048) <= most
+    assert 4 * cap * (-(-q["kept_cols"] // 256) * 256) <= most
     g = max(2 * planes * cap * q["piece_cols"], 4 * cap * q["kept_cols"])
     assert g <= most
     assert q["workspace_bytes"] >= g + 2 * cap * dim
