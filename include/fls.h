@@ -411,9 +411,10 @@ typedef struct {
                            and have any row stride; 0: the weight must start on a 16-byte boundary and its stride be a
                            multiple of 8 elements.  dim not a multiple of 8 implies 1                           */
   uint32_t reserved;    /* 0                                                                                    */
-  uint64_t piece_bytes; /* workspace for one piece of the vocabulary; 0: 1 GiB.  The logits of the last columns, as many
-                           as fit at 4 bytes each, are formed once, those before them twice, in pieces of 2 bytes per
-                           column (fp32 weight gradients: 4); a piece has at least 512 columns                  */
+  uint64_t piece_bytes; /* workspace for one piece of the vocabulary; 0: 1 GiB.  From d = 896 on, and with at most 2 d / 3
+                           rows, the logits of the last columns, as many as fit at 4 bytes each, are formed once; the
+                           others twice, in pieces of 2 bytes per column (fp32 weight gradients: 4); a piece has at
+                           least 512 columns                                                                    */
 } fls_head_desc;
 
 typedef struct {

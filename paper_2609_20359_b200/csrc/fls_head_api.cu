@@ -32,6 +32,13 @@ constexpr uint64_t kMinPieceCols = 512, kMaxPieceCols = 1ull << 28;
 constexpr uint64_t kDefaultPieceBytes = 1ull << 30;
 constexpr uint64_t kMinPartialBytes = 48ull << 20;   // room for the split sums of grad_hidden when there are few rows
 
+// Keeping a logit moves 8 bytes more than forming it again, which does 2 d operations or, with few rows, waits for the
+// weight (2 d bytes per column of all rows).  Measured equal at d = 896 and, below it, at about 2 d / 3 rows (us a step,
+// kept / formed again; 4096 x 50257: d = 256 658 / 496, 768 1030 / 1008, 896 1262 / 1262, 1024 1307 / 1355; 1024 x 128256,
+// d = 2048: 1591 / 1738; d = 768, 50257 columns: 128 rows 99 / 108, 512 184 / 186, 1024 320 / 309; d = 256: 128 rows
+// 74 / 75, 256 80 / 78).
+bool keeps_logits(uint64_t rows, uint64_t dim) { return dim >= 896 || 3 * rows <= 2 * dim; }
+
 // Byte offsets of the workspace.  Sizes are those of max_rows; a smaller call uses the front of each region.
 struct Regions {
   uint64_t mask, counts, pos, src, hp, slot_idx, slot_start, slot_t, slot_z, slot_g, part, coef, g, dh, wcopy, total;
@@ -59,7 +66,7 @@ Regions regions(const fls_head_desc& d) {
   r.part = take(3 * r.part_bytes);          // maximum, sum, and one of: sum at temperature 1, sum of logits
   r.coef = take(cap * 16);
   if (d.grads) {
-    const uint64_t all = 4 * cap * up(d.vocab, 256);                 // every logit kept
+    const uint64_t all = (keeps_logits(d.max_rows, d.dim) ? 4 : 2 * planes) * cap * up(d.vocab, 256);   // the whole vocabulary in one piece
     r.g_bytes = std::min(all, std::max(d.piece_bytes ? d.piece_bytes : kDefaultPieceBytes, 2 * planes * cap * kMinPieceCols));
     r.g = take(r.g_bytes);
     r.dh_bytes = std::max(2 * cap * dcap * 4, kMinPartialBytes);
@@ -73,9 +80,10 @@ Regions regions(const fls_head_desc& d) {
 // How the vocabulary is taken apart.  The last columns keep the logits of the statistics pass, 4 bytes each, and get their
 // dL/dz from those; the columns before them are formed again, in pieces of 2 bytes per column and term, evened out.
 struct Pieces { uint32_t keep_v0, cols; };
-Pieces pieces_of(const fls_head_desc& d, uint64_t g_bytes, uint64_t rows_cap, uint64_t planes) {
+Pieces pieces_of(const fls_head_desc& d, uint64_t g_bytes, uint64_t rows, uint64_t planes) {
+  const uint64_t rows_cap = up(std::max<uint64_t>(rows, 1), kHeadBM);
   Pieces p{};
-  const uint64_t keep = std::min(kMaxPieceCols, g_bytes / (4 * rows_cap) / 256 * 256);
+  const uint64_t keep = !keeps_logits(rows, d.dim) ? 0 : std::min(kMaxPieceCols, g_bytes / (4 * rows_cap) / 256 * 256);
   const uint64_t v0 = keep >= d.vocab ? 0 : keep ? up(d.vocab - keep, 256) : d.vocab;
   p.keep_v0 = uint32_t(std::min(v0, d.vocab));
   if (p.keep_v0) {
@@ -237,7 +245,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.direct_store = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 || c.grad_weight_stride * (c.grad_f32 ? 4 : 2) % 16 ||
                    (c.accumulate && !c.grad_f32);
   if (grads) {
-    const Pieces p = pieces_of(d, r.g_bytes, c.rows_cap, c.planes);
+    const Pieces p = pieces_of(d, r.g_bytes, c.rows, c.planes);
     c.keep_v0 = p.keep_v0;
     c.piece_cols = p.cols;
     c.split_cols = std::max(p.cols, uint32_t(up(c.vocab - p.keep_v0, 256)));
@@ -373,7 +381,7 @@ int fls_head_query(const fls_head* head, fls_head_layout* out) {
   out->workspace_bytes = head->reg.total;
   out->piece_cols = out->pieces = out->kept_cols = 0;
   if (d.grads) {
-    const Pieces p = pieces_of(d, head->reg.g_bytes, up(std::max<uint64_t>(d.max_rows, 1), kHeadBM), d.grad_dtype == FLS_GRAD_F32 ? 2 : 1);
+    const Pieces p = pieces_of(d, head->reg.g_bytes, d.max_rows, d.grad_dtype == FLS_GRAD_F32 ? 2 : 1);
     out->piece_cols = p.cols;
     out->pieces = p.cols ? (p.keep_v0 + p.cols - 1) / p.cols : 0;
     out->kept_cols = d.vocab - p.keep_v0;

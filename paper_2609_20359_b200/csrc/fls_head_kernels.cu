@@ -791,9 +791,13 @@ __device__ __forceinline__ bool row_active(const HeadCall& c, uint64_t n, bool w
     bad = y != c.ignore_label && (y < 0 || y >= int64_t(c.vocab));
     active = y != c.ignore_label;
   }
-  for (uint32_t k = 0; k < c.top && !active; ++k) {
-    const int32_t i = c.top_index[n * c.top + k];
-    active = i >= 0 && uint32_t(i) < c.vocab && c.top_logit[n * c.top + k] != -INFINITY;
+  for (uint32_t k0 = 0; k0 < c.top && !active; k0 += 8) {              // eight at a time: rows without any read all of them
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) {
+      const uint64_t at = n * c.top + min(k0 + j, c.top - 1);
+      const int32_t i = c.top_index[at];
+      active |= i >= 0 && uint32_t(i) < c.vocab && c.top_logit[at] != -INFINITY;
+    }
   }
   active = active && !bad;
   if (!active && write) {

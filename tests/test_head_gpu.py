@@ -79,6 +79,28 @@ def test_xent_larger(n, V, d):
     xent_case(n, V, d, ignored=range(0, n, 3) if n > 3 else ())
 
 
+# wide enough for kept logits: all of them, a part of them, none; one and two terms of dL/dz
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("n,V,d,piece", [(1, 300, 896, 0), (130, 777, 1000, 0), (300, 3000, 904, 1 << 22), (300, 3000, 904, 1)])
+def test_xent_kept_columns(n, V, d, piece, f32):
+    head = xent_case(n, V, d, f32=f32, piece=piece, eps=0.1, zeta=1e-3, ignored=(0,) if n > 1 else ())
+    assert (head.layout["kept_cols"] == V) == (piece == 0) and (head.layout["pieces"] == 0) == (piece == 0)
+
+
+def test_kept_and_formed_logits_give_the_same_bits():
+    from paper_2609_20359_b200.head import Head
+    n, V, d, k = 200, 2600, 1024, 9
+    h, w, y, g = make(n, V, d)
+    idx, t = teacher(n, V, k, g)
+    outs = []
+    for piece in (0, 1 << 20):
+        gh, gw = buffers(n, V, d, True)
+        head = Head(n, V, d, top=k, grad_dtype="f32", piece_bytes=piece)
+        outs.append((head.layout["kept_cols"], *head.distill_step(h, w, idx, t, gh, gw, labels=y, temperature=2.0, label_weight=0.4), gw))
+    assert outs[0][0] == V > outs[1][0]
+    assert all(torch.equal(a, b) for a, b in zip(outs[0][1:], outs[1][1:]))
+
+
 def test_smaller_calls_of_one_head():
     from paper_2609_20359_b200.head import Head
     head = Head(600, 1300, 128, piece_bytes=1 << 20)
@@ -385,6 +407,14 @@ def test_distill_sizes(n, V, d, k, tail):
     if tail and k == V:
         pytest.skip("no column outside the list: its class has probability zero")
     distill_case(n, V, d, k, 2.0, tail, 0.5)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T,wl", [(1.0, 0.0), (3.0, 0.5)])
+def test_distill_kept_columns(f32, tail, T, wl):
+    distill_case(140, 1500, 912, 40, T, tail, wl, f32=f32, ignored=(4, 6), empty=(6, 7))
+    distill_case(140, 1500, 912, 40, T, tail, wl, f32=f32, piece=1 << 20)
 
 
 @pytest.mark.parametrize("f32", [False, True])
