@@ -30,7 +30,7 @@ int cuda_fail(cudaError_t e, const char* what) { return fail(FLS_ECUDA, "%s: %s"
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
 constexpr uint64_t kMinPieceCols = 512, kMaxPieceCols = 1ull << 28;
 constexpr uint64_t kDefaultPieceBytes = 1ull << 30;
-constexpr uint64_t kMinPartialBytes = 48ull << 20;   // room for the split sums of grad_hidden when there are few rows
+constexpr uint64_t kPartialBytes = 256ull << 20;     // room for the split sums of grad_hidden: at least 2, at most 64 splits
 
 // Keeping a logit moves 8 bytes more than forming it again, which does 2 d operations or, with few rows, waits for the
 // weight (2 d bytes per column of all rows).  Measured equal at d = 896 and, below it, at about 2 d / 3 rows (us a step,
@@ -69,7 +69,7 @@ Regions regions(const fls_head_desc& d) {
     const uint64_t all = (keeps_logits(d.max_rows, d.dim) ? 4 : 2 * planes) * cap * up(d.vocab, 256);   // the whole vocabulary in one piece
     r.g_bytes = std::min(all, std::max(d.piece_bytes ? d.piece_bytes : kDefaultPieceBytes, 2 * planes * cap * kMinPieceCols));
     r.g = take(r.g_bytes);
-    r.dh_bytes = std::max(2 * cap * dcap * 4, kMinPartialBytes);
+    r.dh_bytes = std::max<uint64_t>(2, std::min<uint64_t>(kHeadMaxSplits, kPartialBytes / (cap * dcap * 4))) * cap * dcap * 4;
     r.dh = take(r.dh_bytes);
   }
   if (d.any_weight || d.dim % 8) r.wcopy = take(d.vocab * dp * 2);
