@@ -500,3 +500,16 @@ def test_no_rows():
     gw.fill_(2.0)
     head.xent_step(h, w, y, gh, gw, accumulate=True)
     assert bool((gw == 2.0).all())
+
+
+def test_example_trains():
+    """Loss, gradients into the plan's buffers, optimizer, averaging and distillation together."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "federated_head.py")
+    spec = importlib.util.spec_from_file_location("federated_head", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    history, taught = mod.main(quiet=True)
+    assert history[0] > math.log(mod.VOCAB) - 1 and history[-1] < 0.6 * history[0]
+    assert all(math.isfinite(x) for x in taught) and taught[-1] < 0.6 * taught[0]
