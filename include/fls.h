@@ -401,7 +401,7 @@ enum { FLS_TAIL_RENORM = 0, FLS_TAIL_CLASS = 1 };
 #define FLS_HEAD_MAX_TOP 128 /* longest teacher list */
 
 typedef struct {
-  uint64_t max_rows;    /* N of the largest call, <= 2^24                                                       */
+  uint64_t max_rows;    /* N of the largest call, <= 2^24, N V <= 2^47                                           */
   uint64_t vocab;       /* V, 1 .. 2^30                                                                         */
   uint32_t dim;         /* d, 1 .. 65536                                                                        */
   uint32_t top;         /* k: teacher entries per row of fls_head_distill, <= FLS_HEAD_MAX_TOP; 0: not used     */
@@ -461,9 +461,10 @@ int fls_head_destroy(fls_head* head);
 
 /* The losses, and the gradients for which a buffer is given, enqueued on cuda_stream; nothing is synchronised or
  * allocated.  A call with rows = 0 writes a zero grad_weight (or leaves it, with accumulate) and nothing else.
+ * Calls of one head, and calls with one workspace, must not overlap in time.
  * Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, gradients without desc.grads, smoothing outside
- * [0, 1), a negative or non-finite z_loss, weight or temperature, a stride below d), FLS_EPTR (null, host or overlapping
- * buffers), FLS_EALIGN (weight without desc.any_weight, float or index buffers off their element size, workspace),
+ * [0, 1), a negative or non-finite z_loss, weight or temperature, a stride below d), FLS_EPTR (null, host, another device's or
+ * overlapping buffers; a buffer is everything from its first to its last element), FLS_EALIGN (weight without desc.any_weight, float or index buffers off their element size, workspace),
  * FLS_ESIZE (workspace too small), FLS_ECUDA. */
 int fls_head_xent(fls_head* head, const fls_head_io* io, double label_smoothing, double z_loss, void* cuda_stream);
 int fls_head_distill(fls_head* head, const fls_head_io* io, const fls_distill_desc* distill, void* cuda_stream);
@@ -472,6 +473,11 @@ int fls_head_distill(fls_head* head, const fls_head_io* io, const fls_distill_de
  * (FLS_STATUS_WAIT_EXPIRED: a wait inside a kernel ran out, the call's results are incomplete) and the number of rows
  * that took part in the last call.  Clear the workspace's first 256 bytes before its first use.  Either may be NULL. */
 int fls_head_get_state(const void* workspace, const uint32_t** dev_status, const uint32_t** dev_count);
+
+/* For tests of the bounded waits: in the next call of this head nothing announces the arrival of the products' operands;
+ * every wait gives up after `polls` polls, FLS_STATUS_WAIT_EXPIRED appears in the status word, the outputs of that call are
+ * meaningless, and the device stays usable. */
+int fls_debug_expire_next_head_wait(fls_head* head, uint32_t polls);
 
 /* Number of kernels this head has launched so far. */
 int fls_head_get_launch_count(const fls_head* head, uint64_t* launches);

@@ -37,7 +37,7 @@ EXPORTS = [
     "fls_plan_tune", "fls_plan_set_recompute", "fls_plan_set_single_pass", "fls_plan_set_overlap", "fls_set_profiling", "fls_get_kernel_ms", "fls_get_launch_count", "fls_plan_destroy",
     "fls_last_error", "fls_reduce_norm_noalloc",
     "fls_head_create", "fls_head_query", "fls_head_destroy", "fls_head_xent", "fls_head_distill", "fls_head_get_state",
-    "fls_head_get_launch_count", "fls_top_logits",
+    "fls_head_get_launch_count", "fls_debug_expire_next_head_wait", "fls_top_logits",
 ]
 
 
@@ -154,6 +154,7 @@ def _load() -> C.CDLL:
     lib.fls_head_distill.argtypes = [P, C.POINTER(fls_head_io), C.POINTER(fls_distill_desc), P]
     lib.fls_head_get_state.argtypes = [P, C.POINTER(P), C.POINTER(P)]
     lib.fls_head_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
+    lib.fls_debug_expire_next_head_wait.argtypes = [P, C.c_uint32]
     lib.fls_top_logits.argtypes = [P, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint32, C.c_double, P, P, P, P]
     lib.fls_last_error.argtypes = []
     lib.fls_last_error.restype = C.c_char_p
@@ -453,6 +454,11 @@ def fls_head_get_launch_count(head: int) -> int:
     n = C.c_uint64()
     _check(lib.fls_head_get_launch_count(head, C.byref(n)))
     return n.value
+
+
+def fls_debug_expire_next_head_wait(head: int, polls: int) -> None:
+    """Test hook: the waits of this head's next call run out after `polls` polls."""
+    _check(lib.fls_debug_expire_next_head_wait(head, polls))
 
 
 def fls_top_logits(logits, logit_dtype: int, rows: int, vocab: int, stride: int, top: int, temperature: float, value, index, lse,

@@ -60,6 +60,8 @@ struct HeadCall {
   uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, bf16 accumulation): plain stores
   uint32_t max_splits, clusters, group_m;
   uint32_t prefetch_weight;  // one row tile, and the weight is the caller's: fetched ahead of the packed rows
+  uint32_t wait_limit;       // polls of a barrier before a role gives up
+  uint32_t hold_back;        // tests only: the operands' arrival is never announced
   uint32_t keep_v0;          // columns from here on keep their logits, vocab: none
   uint32_t split_cols;       // columns of the widest piece, 0 without gradients
   float c1, cT;              // log2(e), log2(e) / T

@@ -28,6 +28,7 @@ int fail(int code, const char* fmt, ...) {
 int cuda_fail(cudaError_t e, const char* what) { return fail(FLS_ECUDA, "%s: %s", what, cudaGetErrorString(e)); }
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
+constexpr uint32_t kWaitLimit = 1u << 20;            // polls, 4 us each, of a barrier before a role of the tensor-core kernel gives up
 constexpr uint64_t kMinPieceCols = 512, kMaxPieceCols = 1ull << 28;
 constexpr uint64_t kDefaultPieceBytes = 1ull << 30;
 constexpr uint64_t kPartialBytes = 256ull << 20;     // room for the split sums of grad_hidden: at least 2, at most 64 splits
@@ -127,6 +128,8 @@ struct Span {
 };
 
 int check_spans(const Span* s, int n) {
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); device = -1; }
   for (int i = 0; i < n; ++i) {
     if (!s[i].p) {
       if (s[i].bytes) return fail(FLS_EPTR, "%s is null", s[i].what);
@@ -140,6 +143,7 @@ int check_spans(const Span* s, int n) {
     if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e, "cudaPointerGetAttributes"); }
     if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged)
       return fail(FLS_EPTR, "%s is not device memory", s[i].what);
+    if (at.type == cudaMemoryTypeDevice && at.device != device) return fail(FLS_EPTR, "%s is on device %d, not the current one", s[i].what, at.device);
   }
   for (int i = 0; i < n; ++i)
     for (int j = 0; j < n; ++j) {
@@ -164,6 +168,7 @@ struct fls_head {
   uint32_t clusters = 0;
   EncodeTiled encode = nullptr;
   uint64_t launches = 0;
+  uint32_t expire_polls = 0;        // test hook: the next call's waits run out after so many polls
 };
 
 namespace {
@@ -238,6 +243,9 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.clusters = h->clusters;
   // hidden rows of one group of row tiles: 32 MB, a quarter of L2, beside the weight tiles that stream past them
   c.group_m = std::max<uint32_t>(1, uint32_t((32ull << 20) / (uint64_t(kHeadBM) * c.dp * 2)));
+  c.hold_back = h->expire_polls != 0;
+  c.wait_limit = h->expire_polls ? h->expire_polls : kWaitLimit;
+  h->expire_polls = 0;
   c.c1 = 1.4426950408889634f;
   c.cT = float(1.4426950408889634 * c.inv_temp);
   const bool grads = c.want_gh || c.want_gw;
@@ -363,6 +371,7 @@ int fls_head_create(const fls_head_desc* desc, fls_head** out) {
   if (desc->max_rows > (1ull << 24)) return fail(FLS_EINVAL, "max_rows > 2^24");
   if (desc->vocab < 1 || desc->vocab > (1ull << 30)) return fail(FLS_EINVAL, "vocab must be in 1 .. 2^30");
   if (desc->dim < 1 || desc->dim > 65536) return fail(FLS_EINVAL, "dim must be in 1 .. 65536");
+  if (up(desc->max_rows, 256) / 256 * (up(desc->vocab, 256) / 256) > (1ull << 31)) return fail(FLS_EINVAL, "max_rows * vocab > 2^47");
   if (desc->top > FLS_HEAD_MAX_TOP) return fail(FLS_EINVAL, "top > %d", FLS_HEAD_MAX_TOP);
   if (desc->grads > 1 || desc->any_weight > 1) return fail(FLS_EINVAL, "grads and any_weight must be 0 or 1");
   if (desc->grad_dtype != FLS_GRAD_BF16 && desc->grad_dtype != FLS_GRAD_F32) return fail(FLS_EINVAL, "unknown grad_dtype %u", desc->grad_dtype);
@@ -442,6 +451,12 @@ int fls_head_get_state(const void* workspace, const uint32_t** dev_status, const
   const HeadState* s = static_cast<const HeadState*>(workspace);
   if (dev_status) *dev_status = &s->status;
   if (dev_count) *dev_count = &s->count;
+  return FLS_OK;
+}
+
+int fls_debug_expire_next_head_wait(fls_head* head, uint32_t polls) {
+  if (!head || !polls) return fail(FLS_EINVAL, "null argument");
+  head->expire_polls = polls;
   return FLS_OK;
 }
 

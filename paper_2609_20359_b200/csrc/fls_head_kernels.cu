@@ -37,7 +37,6 @@ struct Smem {
   static_assert(kBytes <= 232448, "shared memory of one CTA");
 };
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;               // warp 0 TMA, 1 MMA, 2 TMEM, 4..11 epilogue
-constexpr uint32_t kWaitLimit = 1u << 22;                        // polls of an mbarrier before a role gives up
 
 // ------------------------------------------------------------------------------------------------ PTX
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
@@ -69,9 +68,9 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// False if the phase did not complete within kWaitLimit polls (each poll may sleep in hardware for a while).
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kWaitLimit; ++i) {
+// False if the phase did not complete within `limit` polls (each poll may sleep in hardware for a while).
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
+  for (uint32_t i = 0; i < limit; ++i) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -584,9 +583,9 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         const CUtensorMap* mb = w.grad_hidden ? &maps.b1 : &maps.b0;
         const int m = int(w.m0 + rank * 128), n = int(w.n0 + rank * 128);
         for (uint32_t i = 0; i < w.kbn; ++i) {
-          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1)) { ok = false; break; }
+          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1, c.wait_limit)) { ok = false; break; }
           const uint32_t bar = leader_addr(smem_u32(&bars->full[stage]));
-          if (rank == 0) mbar_expect(smem_u32(&bars->full[stage]), 2 * kStageBytes);
+          if (rank == 0 && !c.hold_back) mbar_expect(smem_u32(&bars->full[stage]), 2 * kStageBytes);
           const uint32_t sa = tile_base + stage * kStageBytes, sb = sa + kOperandBytes;
           const int k = int((w.kb0 + i) * kHeadBK);
           if constexpr (MODE == kGrads) {
@@ -620,11 +619,11 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         const bool a_mn = MODE == kGrads && !w.grad_hidden, b_mn = MODE == kGrads;
         const uint32_t idesc = instr_desc(a_mn, b_mn);
         const uint32_t ka = (a_mn ? 2048u : 32u) >> 4, kb = (b_mn ? 2048u : 32u) >> 4;   // 16 deep, in descriptor units
-        if (!mbar_wait(smem_u32(&bars->acc_empty[buf]), acc_phase ^ 1)) { ok = false; break; }
+        if (!mbar_wait(smem_u32(&bars->acc_empty[buf]), acc_phase ^ 1, c.wait_limit)) { ok = false; break; }
         fence_after();
         const uint32_t acc = tmem + buf * kHeadBN;
         for (uint32_t i = 0; i < w.kbn; ++i) {
-          if (!mbar_wait(smem_u32(&bars->full[stage]), phase)) { ok = false; break; }
+          if (!mbar_wait(smem_u32(&bars->full[stage]), phase, c.wait_limit)) { ok = false; break; }
           fence_after();
           const uint32_t sa = tile_base + stage * kStageBytes;
           const uint64_t da = smem_desc(sa), db = smem_desc(sa + kOperandBytes);
@@ -668,7 +667,7 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         }
       }
       if (!empty) {
-        ok = mbar_wait(smem_u32(&bars->acc_full[buf]), phase);
+        ok = mbar_wait(smem_u32(&bars->acc_full[buf]), phase, c.wait_limit);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         fence_after();
@@ -1078,7 +1077,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       double damp = 1.0;
       if (taught && c.tail_class) {
         const double qt = fmax(0.0, 1.0 - qsum), tail = denseT + outT;
-        if (qt > 0.0) {
+        if (qt > (tail > 0.0 ? 0.0 : 1e-6)) {          // a list that is the whole vocabulary: what is left of 1 is rounding
           kl += qt * (log(qt) - (log(tail) - log(totT)));
           damp = 1.0 - qt * totT / tail;
         }

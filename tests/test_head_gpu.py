@@ -489,6 +489,87 @@ def test_refusals_on_the_device():
         head.distill(h, w, torch.empty(n, 0, dtype=torch.int32, device=DEV), torch.empty(n, 0, device=DEV))
 
 
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("d", [64, 99])
+@pytest.mark.parametrize("f32", [False, True])
+def test_accumulate_at_any_alignment(f32, d, off):
+    from paper_2609_20359_b200.head import Head
+    n, V = 70, 600
+    h, w, y, _ = make(n, V, d)
+    dtype = torch.float32 if f32 else torch.bfloat16
+    gw = torch.empty(V * d + off, dtype=dtype, device=DEV)[off:].view(V, d)
+    gw.copy_(torch.randn(V, d, device=DEV))
+    before = gw.double()
+    live = torch.ones(n, dtype=torch.bool, device=DEV)
+    Head(n, V, d, grad_dtype="f32" if f32 else "bf16").xent_step(h, w, y, grad_weight=gw, accumulate=True)
+    ref = R.with_gradients(h, w, lambda z: (*R.xent_rows(z, y, live, 0.0, 0.0), live))
+    ref["grad_weight"] = ref["grad_weight"] + before
+    R.check_grads(ref, grad_weight=gw)
+
+
+def test_a_list_that_is_the_whole_vocabulary():
+    """Nothing is outside the list: the tail class is empty and both readings of the tail agree."""
+    from paper_2609_20359_b200.head import Head
+    n, V, d = 7, 64, 64
+    h, w, y, g = make(n, V, d)
+    idx, t = teacher(n, V, V, g, ragged=False)
+    head = Head(n, V, d, top=V)
+    out = []
+    for tl in (None, torch.logsumexp(t.double(), 1).float()):
+        gh, gw = buffers(n, V, d)
+        loss, _ = head.distill_step(h, w, idx, t, gh, gw, teacher_lse=tl)
+        out.append((loss.double(), gh.double()))
+    # teacher_lse is rounded to fp32: q is off by 2^-23 |lse|, the loss by that times its logarithms
+    assert bool(torch.isfinite(out[1][0]).all()) and bool(((out[0][0] - out[1][0]).abs() <= 1e-5 * (1 + out[0][0])).all())
+    assert bool(((out[0][1] - out[1][1]).abs() <= 2.0 ** -7 * out[0][1].abs() + 1e-5).all())
+
+
+def test_offsets_beyond_32_bits():
+    """A weight and its gradient of more than 2^31 elements; labels at both ends of the vocabulary."""
+    from paper_2609_20359_b200.head import Head
+    n, V, d = 4, 1_100_003, 2048
+    g = torch.Generator(device=DEV).manual_seed(0)
+    w = torch.empty(V, d, dtype=torch.bfloat16, device=DEV)
+    for lo in range(0, V, 1 << 17):
+        w[lo: lo + (1 << 17)] = torch.randn(min(1 << 17, V - lo), d, generator=g, device=DEV) / 30
+    h = torch.randn(n, d, generator=g, device=DEV).bfloat16()
+    y = torch.tensor([0, V - 1, V - 200, 1_050_000], device=DEV)
+    gh, gw = buffers(n, V, d)
+    loss, lse = Head(n, V, d).xent_step(h, w, y, gh, gw, row_weight=torch.ones(n, device=DEV))
+    z = torch.cat([h.double() @ w[lo: lo + (1 << 16)].double().t() for lo in range(0, V, 1 << 16)], 1)
+    p = torch.softmax(z, 1)
+    p[torch.arange(n), y] -= 1
+    want = torch.logsumexp(z, 1)
+    assert bool(((lse.double() - want).abs() <= 1e-5).all())
+    assert bool(((loss.double() - (want - z.gather(1, y[:, None])[:, 0])).abs() <= 2e-5).all())
+    for lo in (0, 524288, 1_048_576, V - 3000):
+        part = p[:, lo: lo + 3000].t() @ h.double()
+        bound = p[:, lo: lo + 3000].abs().t() @ h.double().abs() * (2.0 ** -8 + 2e-5) + 2.0 ** -8 * part.abs() + 1e-30
+        assert bool(((gw[lo: lo + 3000].double() - part).abs() <= bound).all()), lo
+    assert not bool(torch.isnan(gw[::997]).any())
+    dh = sum(p[:, lo: lo + (1 << 16)] @ w[lo: lo + (1 << 16)].double() for lo in range(0, V, 1 << 16))
+    size = sum(p[:, lo: lo + (1 << 16)].abs() @ w[lo: lo + (1 << 16)].double().abs() for lo in range(0, V, 1 << 16))
+    assert bool(((gh.double() - dh).abs() <= size * (2.0 ** -8 + 2e-5 + V / 16 * 2.0 ** -23) + 2.0 ** -8 * dh.abs()).all())
+
+
+def test_bounded_waits_run_out():
+    """Nothing announces the operands: every wait of the kernels gives up, the status word says so, the next call is right."""
+    from paper_2609_20359_b200 import _binding as fls
+    from paper_2609_20359_b200.head import Head
+    n, V, d = 300, 2000, 256
+    h, w, y, _ = make(n, V, d)
+    head = Head(n, V, d)
+    gh, gw = buffers(n, V, d)
+    want = [t.clone() for t in (*head.xent_step(h, w, y, gh, gw), gh, gw)]
+    assert head.status() == 0
+    fls.fls_debug_expire_next_head_wait(head.handle, 200)
+    head.xent_step(h, w, y, gh, gw)
+    assert head.status() == fls.FLS_STATUS_WAIT_EXPIRED
+    got = (*head.xent_step(h, w, y, gh, gw), gh, gw)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 def test_no_rows():
     from paper_2609_20359_b200.head import Head
     V, d = 300, 64

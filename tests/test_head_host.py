@@ -37,7 +37,7 @@ def test_struct_layouts_match_the_header(fls, tmp_path):
 
 
 @pytest.mark.parametrize("kw", [dict(vocab=0), dict(dim=0), dict(dim=65537), dict(top=129), dict(max_rows=(1 << 24) + 1), dict(grad_dtype=7),
-                                dict(vocab=(1 << 30) + 1), dict(piece_bytes=(1 << 40) + 1)])
+                                dict(vocab=(1 << 30) + 1), dict(max_rows=1 << 24, vocab=1 << 24), dict(piece_bytes=(1 << 40) + 1)])
 def test_create_refuses(fls, kw):
     base = dict(max_rows=16, vocab=1000, dim=64)
     with pytest.raises(fls.FlsError) as e:

@@ -153,6 +153,19 @@ def test_strides(off, extra):
 
 
 @pytest.mark.gpu
+def test_offsets_beyond_32_bits():
+    from paper_2609_20359_b200.head import TopLogits
+    n, V, k = 20000, 120001, 8
+    x = torch.zeros(n, V, dtype=torch.bfloat16, device=DEV)
+    x[-5:] = draw(5, V, torch.bfloat16)
+    x[9000] = draw(1, V, torch.bfloat16, 1)[0]
+    value, index, _ = TopLogits(n, V, k)(x)
+    for rows in (slice(n - 5, n), slice(9000, 9001), slice(0, 2)):
+        wv, wi, _ = reference(x[rows], k, 1.0)
+        assert torch.equal(index[rows], wi) and torch.equal(value[rows].double(), wv)
+
+
+@pytest.mark.gpu
 def test_feeds_distillation():
     """values, indices and lse of a teacher go into the loss as they are; a student equal to its teacher has KL 0."""
     from paper_2609_20359_b200.head import Head, TopLogits
