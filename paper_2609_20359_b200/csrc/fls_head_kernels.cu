@@ -936,6 +936,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
   __shared__ float sh_m[32][kRowsPerBlock], sh_s[32][kRowsPerBlock], sh_s1[32][kRowsPerBlock], sh_z[32][kRowsPerBlock];
   __shared__ double sh_q[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
   __shared__ int32_t sh_i[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
+  __shared__ float sh_t[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1], sh_zs[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
   const uint32_t lane = threadIdx.x & 31, y = threadIdx.x >> 5;
   pdl_launch();
   pdl_wait();
@@ -952,25 +953,20 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     if (lane == 0) c.state->splits = (best & 63) + 1;
   }
   if (p0 >= count) return;
-  // what this warp needs of its row is fetched before the sums, which take as long
   const uint32_t p = min(p0 + y, count - 1);
-  const uint64_t n = uint64_t(c.src[p]);
+  const uint64_t n = uint64_t(c.src[p]);               // used after the sums
   const int32_t* idx = c.slot_idx + uint64_t(p) * c.slots;
   const float* zs = c.slot_z + uint64_t(p) * c.slots;
   const float* ts = c.slot_t + uint64_t(p) * c.slots;
   float* gs = c.slot_g + uint64_t(p) * c.slots;
-  const int64_t label = c.use_label ? c.labels[n] : c.ignore_label;
-  const double w = c.row_weight ? double(c.row_weight[n]) : 1.0 / double(count);
-  float mf = -INFINITY;
-  for (uint32_t i = lane; i < c.slots; i += 32)
-    if (idx[i] != INT_MAX) mf = fmaxf(mf, zs[i]);
   {
     const uint32_t r = threadIdx.x % kRowsPerBlock, t0 = threadIdx.x / kRowsPerBlock;   // packed rows to the next multiple of 256 exist
     float m = -INFINITY, s = 0.f, s1 = 0.f, z = 0.f;
-    for (uint32_t t = t0; t < c.tiles; t += 128) {
-      float tm[4], ts[4], t1[4];
+    constexpr int B = 8;                               // loads in flight per thread
+    for (uint32_t t = t0; t < c.tiles; t += 32 * B) {
+      float tm[B], ts[B], t1[B];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < B; ++j) {
         const bool in = t + 32 * j < c.tiles;
         const uint64_t at = uint64_t(in ? t + 32 * j : t) * c.rows_cap + p0 + r;
         tm[j] = in ? c.part_m[at] : -INFINITY;
@@ -978,11 +974,14 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
         t1[j] = in && c.two ? c.part_s1[at] : 0.f;
         z += in && c.smooth ? c.part_z[at] : 0.f;
       }
-      const float nm = fmaxf(fmaxf(fmaxf(tm[0], tm[1]), fmaxf(tm[2], tm[3])), m), base = nm == -INFINITY ? 0.f : nm;
+      float nm = m;
+#pragma unroll
+      for (int j = 0; j < B; ++j) nm = fmaxf(nm, tm[j]);
+      const float base = nm == -INFINITY ? 0.f : nm;
       s *= exp2f(__fmul_rn(m, c.cT) - __fmul_rn(base, c.cT));          // an empty side has factor 2^-inf = 0
       if (c.two) s1 *= exp2f(__fmul_rn(m, c.c1) - __fmul_rn(base, c.c1));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < B; ++j) {
         // columns all left out: m = -inf and s = 0; NaN goes through
         s += ts[j] * (tm[j] == -INFINITY ? 1.f : exp2f(__fmul_rn(tm[j], c.cT) - __fmul_rn(base, c.cT)));
         if (c.two) s1 += t1[j] * (tm[j] == -INFINITY ? 1.f : exp2f(__fmul_rn(tm[j], c.c1) - __fmul_rn(base, c.c1)));
@@ -993,8 +992,19 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     sh_s[t0][r] = s;
     sh_s1[t0][r] = s1;
     sh_z[t0][r] = z;
-    __syncthreads();
   }
+  // what this warp needs of its row comes while the others finish
+  const int64_t label = c.use_label ? c.labels[n] : c.ignore_label;
+  const double w = c.row_weight ? double(c.row_weight[n]) : 1.0 / double(count);
+  float mf = -INFINITY;
+  for (uint32_t i = lane; i < c.slots; i += 32) {
+    const int32_t x = idx[i];
+    sh_i[y][i] = x;
+    sh_t[y][i] = ts[i];
+    sh_zs[y][i] = zs[i];
+    if (x != INT_MAX) mf = fmaxf(mf, zs[i]);
+  }
+  __syncthreads();
   {
     if (p0 + y >= count) return;
     mf = fmaxf(mf, sh_m[lane][y]);
@@ -1011,7 +1021,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     double tmax = -INFINITY;
     bool nan_t = false;
     for (uint32_t i = lane; i < c.slots; i += 32)
-      if (idx[i] != INT_MAX && ts[i] != -INFINITY) { tmax = fmax(tmax, double(ts[i])); nan_t |= isnan(ts[i]); }
+      if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) { tmax = fmax(tmax, double(sh_t[y][i])); nan_t |= isnan(sh_t[y][i]); }
     tmax = warp_max(tmax);
     const bool taught = __any_sync(0xFFFFFFFFu, nan_t) || tmax != -INFINITY;
     double norm = 0.0;
@@ -1020,7 +1030,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       else {
         double a = 0.0;
         for (uint32_t i = lane; i < c.slots; i += 32)
-          if (idx[i] != INT_MAX && ts[i] != -INFINITY) a += exp((double(ts[i]) - tmax) * c.inv_temp);
+          if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) a += exp((double(sh_t[y][i]) - tmax) * c.inv_temp);
         norm = tmax * c.inv_temp + log(warp_sum(a));
       }
     }
@@ -1028,20 +1038,19 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     double ownT = 0.0, own1 = 0.0, outT = 0.0, eT_label = 0.0, e1_label = 0.0, z_label = 0.0, qsum = 0.0;
     for (uint32_t i = lane; i < c.slots; i += 32) {
       double qi = 0.0;
-      const int32_t x = idx[i];
+      const int32_t x = sh_i[y][i];
       if (x != INT_MAX) {
-        if (ts[i] != -INFINITY) { qi = exp(double(ts[i]) * c.inv_temp - norm); qsum += qi; }
-        const bool first = i == 0 || idx[i - 1] != x;
+        if (sh_t[y][i] != -INFINITY) { qi = exp(double(sh_t[y][i]) * c.inv_temp - norm); qsum += qi; }
+        const bool first = i == 0 || sh_i[y][i - 1] != x;
         if (first) {
           bool listed = false;
-          for (uint32_t j = i; j < c.slots && idx[j] == x; ++j) listed |= ts[j] != -INFINITY;
-          const double eT = exp((double(zs[i]) - M) * c.inv_temp), e1 = c.two ? exp(double(zs[i]) - M) : eT;
-          if (labelled && int64_t(x) == label) { eT_label = eT; e1_label = e1; z_label = double(zs[i]); }
+          for (uint32_t j = i; j < c.slots && sh_i[y][j] == x; ++j) listed |= sh_t[y][j] != -INFINITY;
+          const double eT = exp((double(sh_zs[y][i]) - M) * c.inv_temp), e1 = c.two ? exp(double(sh_zs[y][i]) - M) : eT;
+          if (labelled && int64_t(x) == label) { eT_label = eT; e1_label = e1; z_label = double(sh_zs[y][i]); }
           else { ownT += eT; own1 += e1; }
           if (!listed) outT += eT;             // the label outside the teacher's list belongs to the tail
         }
       }
-      sh_i[y][i] = x;
       sh_q[y][i] = qi;
     }
     ownT = warp_sum(ownT); own1 = warp_sum(own1); outT = warp_sum(outT); qsum = warp_sum(qsum);
@@ -1069,9 +1078,9 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     } else {
       double kl = 0.0;
       for (uint32_t i = lane; i < c.slots; i += 32)
-        if (idx[i] != INT_MAX && ts[i] != -INFINITY) {
+        if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) {
           const double qi = sh_q[y][i];
-          if (qi != 0.0) kl += qi * ((double(ts[i]) * c.inv_temp - norm) - (double(zs[i]) * c.inv_temp - lseT));
+          if (qi != 0.0) kl += qi * ((double(sh_t[y][i]) * c.inv_temp - norm) - (double(sh_zs[y][i]) * c.inv_temp - lseT));
         }
       kl = warp_sum(kl);
       double damp = 1.0;
@@ -1094,11 +1103,11 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
         if (x == INT_MAX) continue;
         double qi = 0.0;
         bool listed = false;
-        for (uint32_t j = i + 1; j-- > 0 && sh_i[y][j] == x;) { qi += sh_q[y][j]; listed |= ts[j] != -INFINITY; }
-        for (uint32_t j = i + 1; j < c.slots && sh_i[y][j] == x; ++j) { qi += sh_q[y][j]; listed |= ts[j] != -INFINITY; }
-        const double pT = exp(double(zs[i]) * c.inv_temp - lseT);
+        for (uint32_t j = i + 1; j-- > 0 && sh_i[y][j] == x;) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
+        for (uint32_t j = i + 1; j < c.slots && sh_i[y][j] == x; ++j) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
+        const double pT = exp(double(sh_zs[y][i]) * c.inv_temp - lseT);
         double v = a * (pT * (listed ? 1.0 : damp) - qi);
-        if (labelled) v += b * (int64_t(x) == label ? -rest1 / tot1 : (c.two ? exp(double(zs[i]) - lse1) : pT));
+        if (labelled) v += b * (int64_t(x) == label ? -rest1 / tot1 : (c.two ? exp(double(sh_zs[y][i]) - lse1) : pT));
         gs[i] = float(v);
       }
     }
@@ -1173,26 +1182,43 @@ __global__ void __launch_bounds__(128) fls_head_own_kernel(const __grid_constant
   if (c.planes == 2) o[uint64_t(c.rows_cap) * 64] = bf16_bits(y - bf16_round(y));
 }
 
-// One block per row, four columns per thread; the split sums are added in order.
+// One row, 256 / G groups of four columns per block; G threads share a group's split sums (each adds every G-th, then the G
+// partial sums are added in order), so that with few rows and many splits the loads do not wait for one another.
+template <int G>
 __global__ void __launch_bounds__(256) fls_head_grad_hidden_kernel(const __grid_constant__ HeadCall c) {
+  __shared__ float4 part[G > 1 ? 256 : 1];
   pdl_launch();
   pdl_wait();
+  constexpr uint32_t kCols = 256 / G;
   const uint64_t n = blockIdx.x;
   const int32_t p = c.pos[n];
   uint16_t* out = c.grad_hidden + n * c.grad_hidden_stride;
-  const uint32_t splits = c.state->splits;
+  const uint32_t splits = c.state->splits, g = threadIdx.x / kCols;
   const bool vec = c.dim % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 7) == 0;
-  for (uint32_t i = (blockIdx.y * 256 + threadIdx.x) * 4; i < c.dim; i += gridDim.y * 1024) {
+  for (uint32_t i0 = blockIdx.y * kCols * 4; i0 < c.dim; i0 += gridDim.y * kCols * 4) {
+    const uint32_t i = i0 + threadIdx.x % kCols * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p >= 0) {
+    if (p >= 0 && i < c.dim) {
       const float* x = c.dh + uint64_t(p) * c.dcap + i;
       const uint64_t step = uint64_t(c.rows_cap) * c.dcap;
 #pragma unroll 8
-      for (uint32_t s = 0; s < splits; ++s) {
+      for (uint32_t s = g; s < splits; s += G) {
         const float4 a = *reinterpret_cast<const float4*>(x + s * step);
         v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
       }
     }
+    if constexpr (G > 1) {
+      __syncthreads();
+      part[threadIdx.x] = v;
+      __syncthreads();
+      if (g) continue;
+#pragma unroll
+      for (uint32_t q = 1; q < G; ++q) {
+        const float4 a = part[q * kCols + threadIdx.x];
+        v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+      }
+    }
+    if (i >= c.dim) continue;
     if (vec) *reinterpret_cast<uint2*>(out + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
     else {
       const float w[4] = {v.x, v.y, v.z, v.w};
@@ -1295,8 +1321,9 @@ cudaError_t launch_head_grads(const HeadCall& c, const HeadMaps& m, const HeadPi
   return launch_gemm<kGrads, false, false>(c, m, p, s);
 }
 cudaError_t launch_head_grad_hidden(const HeadCall& c, cudaStream_t s) {
-  // few rows: their columns spread over blocks of 1024
-  return launch(fls_head_grad_hidden_kernel, dim3(uint32_t(c.rows), c.rows <= 1024 ? (c.dim + 1023) / 1024 : 1), 256, 0, false, s, c);
+  // few rows have many splits and few blocks (128 x 50257 x 768, 24 splits: 10.5 us with one thread per four columns)
+  if (c.rows <= 512) return launch(fls_head_grad_hidden_kernel<8>, dim3(uint32_t(c.rows), (c.dim + 127) / 128), 256, 0, false, s, c);
+  return launch(fls_head_grad_hidden_kernel<1>, dim3(uint32_t(c.rows)), 256, 0, false, s, c);
 }
 
 }  // namespace fls
