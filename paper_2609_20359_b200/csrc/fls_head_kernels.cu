@@ -225,7 +225,7 @@ struct Unit {
 // works through units u, u + clusters, ...: first those of the hidden gradient (tiles_h * s of kb_h / s blocks), then
 // those of the weight gradient (tiles_w of kb_w blocks).  Time of the busiest cluster in blocks of depth, with kUnitCost
 // for what a unit costs besides its products (its epilogue's tail, the partial sums written and read again).
-constexpr uint32_t kUnitCost = 6;
+constexpr uint32_t kUnitCost = 12;
 __device__ __forceinline__ uint32_t head_makespan(uint32_t s, uint32_t tiles_h, uint32_t kb_h, uint32_t tiles_w, uint32_t kb_w, uint32_t clusters) {
   const uint32_t units_h = tiles_h * s, units = units_h + tiles_w;
   const uint32_t len_h = (kb_h + s - 1) / s + kUnitCost, len_w = kb_w + kUnitCost;
