@@ -533,6 +533,21 @@ struct alignas(8) Barriers {
   uint32_t gave_up;
 };
 
+// The products.  A CTA pair makes 256 x 256 tiles of C = A B^T with tcgen05.mma (cta_group::2, bf16, fp32 accumulator in
+// TMEM): each CTA brings 128 rows of A and 128 of B per 64 of depth by TMA, one thread of the leading CTA issues, eight
+// epilogue warps (a lane quarter and 128 columns each) read one accumulator while the other is being made.  The grid is
+// persistent, one pair per two SMs; a pair takes units u, u + pairs, ...
+//   What bounds it: one 64-deep block takes 577 to 588 cycles where the tensor pipe needs 512 (shared memory carries 64
+// bytes per cycle in by TMA and 64 out to the products, its limit; with half the loads left out 557), a unit another 500
+// cycles, about 1000 more while the epilogue reads TMEM beside the products, a launch about 12000 (7 us).  With d = 4096
+// the statistics of 1023 x 128256 run at 1.55 PFLOP/s from idle clocks (95 % of the measured library product); back to
+// back the board's power cap holds everything to 1.25 - 1.3 (library product 1.35 - 1.39), and then shape, stages and
+// split no longer show in time, only work left out does.
+//   Why these choices: a pair's tile of 256 x 256 needs 64 bytes per SM and cycle from L2 where two single CTAs would need
+// 96; clusters of four that share loads would leave 16 of 148 SMs idle (33 fit).  Tiles go out through shared memory and
+// TMA stores because a thread owns a row: as 32-byte stores of its own the kept logits of 3686 x 50257 took 293 us
+// instead of 243.  Operands whose depth is not contiguous in memory (dL/dz and hidden for the weight's gradient, the weight
+// for the hidden one) are read as they are, MN-major, so nothing is transposed; measured as fast as K-major (588 cycles).
 // TWO: two temperatures.  FLAG: label smoothing (kStats), dL/dz as two bf16 terms (kDlogits).  KEEP (kStats): the
 // logits of the columns from c.keep_v0 on stay in the workspace.
 template <int MODE, bool TWO, bool FLAG, bool KEEP>
@@ -1115,8 +1130,8 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
 }
 
 // dL/dz of the kept columns, in place: reads 4 bytes and writes 2 (two terms: 4) per element instead of forming the logit
-// again.  The same operations on the same fp32 logit as in the kDlogits epilogue: the same bits.  A block takes 128 rows
-// of 64 columns; eight threads of a warp share a row, so what is overwritten has been read.
+// again.  The same operations on the same fp32 logit as in the kDlogits epilogue: the same bits.  Bound by memory: 1024 x
+// 128256 in 122 us, 6.5 TB/s of its 6 bytes per element.  A block takes 128 rows of 64 columns; eight threads of a warp share a row, so what is overwritten has been read.
 constexpr uint32_t kRescaleRows = 128;
 template <bool TWO, bool PLANES>
 __global__ void __launch_bounds__(256) fls_head_rescale_kernel(const __grid_constant__ HeadCall c) {
@@ -1182,6 +1197,7 @@ __global__ void __launch_bounds__(128) fls_head_own_kernel(const __grid_constant
   if (c.planes == 2) o[uint64_t(c.rows_cap) * 64] = bf16_bits(y - bf16_round(y));
 }
 
+// Bound by memory: 4 bytes per column and split in, 2 out (1024 x 2048, 9 splits: 18 us cold, 4.1 TB/s).
 // One row, 256 / G groups of four columns per block; G threads share a group's split sums (each adds every G-th, then the G
 // partial sums are added in order), so that with few rows and many splits the loads do not wait for one another.
 template <int G>
