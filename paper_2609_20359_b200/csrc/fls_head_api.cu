@@ -233,7 +233,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.dim = d.dim;
   c.dp = uint32_t(up(d.dim, 8));
   c.dcap = uint32_t(up(d.dim, kHeadBN));
-  c.slots = c.top + 1;
+  c.slots = c.top + c.use_label;
   c.tiles = uint32_t(up(d.vocab, kHeadBN) / kHeadStatCols);
   c.grad_f32 = d.grad_dtype == FLS_GRAD_F32;
   c.accumulate = io->accumulate;

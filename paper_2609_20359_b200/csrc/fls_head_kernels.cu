@@ -589,44 +589,61 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
   const Schedule<MODE> plan(c, piece, count);
   bool ok = true;
 
+  // The two issuing threads do as little as they can per block: addresses advance, nothing is recomputed.
+  const uint32_t full0 = smem_u32(&bars->full[0]), empty0 = smem_u32(&bars->empty[0]);
   if (warp == 0) {
     if (lane == 0) {
+      const uint32_t full_leader = leader_addr(full0);
+      const bool leader = rank == 0 && !c.hold_back;
       uint32_t stage = 0, phase = 0;
+      // waits for the stage, announces both CTAs' bytes, and lets `load` fetch into it
+      auto block = [&](auto&& load) {
+        if (!mbar_wait(empty0 + stage * 8, phase ^ 1, c.wait_limit)) { ok = false; return; }
+        if (leader) mbar_expect(full0 + stage * 8, 2 * kStageBytes);
+        const uint32_t sa = tile_base + stage * kStageBytes;
+        load(sa, sa + kOperandBytes, full_leader + stage * 8);
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      };
       for (uint32_t u = cluster; u < plan.n_units && ok; u += n_clusters) {
         const Unit w = plan.at(u);
-        const CUtensorMap* ma = w.grad_hidden ? &maps.a1 : &maps.a0;
-        const CUtensorMap* mb = w.grad_hidden ? &maps.b1 : &maps.b0;
         const int m = int(w.m0 + rank * 128), n = int(w.n0 + rank * 128);
-        for (uint32_t i = 0; i < w.kbn; ++i) {
-          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1, c.wait_limit)) { ok = false; break; }
-          const uint32_t bar = leader_addr(smem_u32(&bars->full[stage]));
-          if (rank == 0 && !c.hold_back) mbar_expect(smem_u32(&bars->full[stage]), 2 * kStageBytes);
-          const uint32_t sa = tile_base + stage * kStageBytes, sb = sa + kOperandBytes;
-          const int k = int((w.kb0 + i) * kHeadBK);
-          if constexpr (MODE == kGrads) {
-            if (w.grad_hidden) {
-              tma_load3(sa, ma, m, dz_panel(piece, uint32_t(k), 0), bar); // dL/dz: 128 rows x 64 columns
-              tma_load(sb, mb, n, int(piece.v0) + k, bar);               // weight: 64 rows x 2 x 64 columns
-              tma_load(sb + 8192, mb, n + 64, int(piece.v0) + k, bar);
-            } else {
-              // fp32 weight gradients: the second half of the depth is the second plane of dL/dz against the same rows
-              const uint32_t second = i >= plan.kb ? 1u : 0u;
-              const int kr = int((i - second * plan.kb) * kHeadBK);
-              tma_load3(sa, ma, kr, dz_panel(piece, uint32_t(m), second), bar);   // dL/dz: 64 rows x 2 x 64 columns
-              tma_load3(sa + 8192, ma, kr, dz_panel(piece, uint32_t(m) + 64, second), bar);
-              tma_load(sb, mb, n, kr, bar);                              // hidden: 64 rows x 2 x 64 columns
-              tma_load(sb + 8192, mb, n + 64, kr, bar);
-            }
+        if constexpr (MODE == kGrads) {
+          if (w.grad_hidden) {
+            int panel = dz_panel(piece, w.kb0 * kHeadBK, 0), v = int(piece.v0 + w.kb0 * kHeadBK);
+            for (uint32_t i = 0; i < w.kbn && ok; ++i, panel += int(piece.panel_step), v += kHeadBK)
+              block([&](uint32_t sa, uint32_t sb, uint32_t bar) {
+                tma_load3(sa, &maps.a1, m, panel, bar);                  // dL/dz: 128 rows x 64 columns
+                tma_load(sb, &maps.b1, n, v, bar);                       // weight: 64 rows x 2 x 64 columns
+                tma_load(sb + 8192, &maps.b1, n + 64, v, bar);
+              });
           } else {
-            tma_load(sa, ma, k, m, bar);                                 // hidden: 128 rows x 64
-            tma_load(sb, mb, k, int(piece.v0) + n, bar);                 // weight: 128 rows x 64
+            // fp32 weight gradients: the depth twice, the second time with the second term of dL/dz
+            for (uint32_t second = 0; second < plan.planes; ++second) {
+              const int p0 = dz_panel(piece, uint32_t(m), second), p1 = dz_panel(piece, uint32_t(m) + 64, second);
+              int r = 0;
+              for (uint32_t i = 0; i < plan.kb && ok; ++i, r += kHeadBK)
+                block([&](uint32_t sa, uint32_t sb, uint32_t bar) {
+                  tma_load3(sa, &maps.a0, r, p0, bar);                   // dL/dz: 64 rows x 2 x 64 columns
+                  tma_load3(sa + 8192, &maps.a0, r, p1, bar);
+                  tma_load(sb, &maps.b0, n, r, bar);                     // hidden: 64 rows x 2 x 64 columns
+                  tma_load(sb + 8192, &maps.b0, n + 64, r, bar);
+                });
+            }
           }
-          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        } else {
+          const int v = int(piece.v0) + n;
+          int k = 0;
+          for (uint32_t i = 0; i < w.kbn && ok; ++i, k += kHeadBK)
+            block([&](uint32_t sa, uint32_t sb, uint32_t bar) {
+              tma_load(sa, &maps.a0, k, m, bar);                         // hidden: 128 rows x 64
+              tma_load(sb, &maps.b0, k, v, bar);                         // weight: 128 rows x 64
+            });
         }
       }
     }
   } else if (warp == 1) {
     if (rank == 0 && lane == 0) {
+      const uint64_t desc0 = smem_desc(tile_base);
       uint32_t stage = 0, phase = 0, buf = 0, acc_phase = 0;
       for (uint32_t u = cluster; u < plan.n_units && ok; u += n_clusters) {
         const Unit w = plan.at(u);
@@ -638,13 +655,12 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
         fence_after();
         const uint32_t acc = tmem + buf * kHeadBN;
         for (uint32_t i = 0; i < w.kbn; ++i) {
-          if (!mbar_wait(smem_u32(&bars->full[stage]), phase, c.wait_limit)) { ok = false; break; }
+          if (!mbar_wait(full0 + stage * 8, phase, c.wait_limit)) { ok = false; break; }
           fence_after();
-          const uint32_t sa = tile_base + stage * kStageBytes;
-          const uint64_t da = smem_desc(sa), db = smem_desc(sa + kOperandBytes);
+          const uint64_t da = desc0 + stage * (kStageBytes >> 4), db = da + (kOperandBytes >> 4);
 #pragma unroll
           for (uint32_t j = 0; j < kHeadBK / 16; ++j) mma_f16(acc, da + j * ka, db + j * kb, idesc, (i | j) != 0);
-          mma_commit(smem_u32(&bars->empty[stage]));
+          mma_commit(empty0 + stage * 8);
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
         if (!ok) break;
@@ -837,7 +853,7 @@ __global__ void __launch_bounds__(kRowChunk) fls_head_map_kernel(const __grid_co
 // take part and the next multiple of 256.  ONE_CHUNK: at most 256 rows; every block looks at all of them itself and the map
 // kernel is not needed.
 template <bool ONE_CHUNK>
-__global__ void __launch_bounds__(256) fls_head_pack_kernel(const __grid_constant__ HeadCall c) {
+__global__ void __launch_bounds__(ONE_CHUNK ? 256 : 128) fls_head_pack_kernel(const __grid_constant__ HeadCall c) {
   __shared__ int32_t s_idx[FLS_HEAD_MAX_TOP + 1];
   __shared__ int32_t s_sorted[FLS_HEAD_MAX_TOP + 1];
   __shared__ float s_t[FLS_HEAD_MAX_TOP + 1];
@@ -1301,7 +1317,7 @@ cudaError_t launch_head_rows_map(const HeadCall& c, cudaStream_t s) {
 }
 cudaError_t launch_head_pack(const HeadCall& c, cudaStream_t s) {
   if (c.rows <= kRowChunk) return launch(fls_head_pack_kernel<true>, dim3(c.rows_cap), 256, 0, true, s, c);
-  return launch(fls_head_pack_kernel<false>, dim3(c.rows_cap), 256, 0, false, s, c);
+  return launch(fls_head_pack_kernel<false>, dim3(c.rows_cap), 128, 0, false, s, c);
 }
 cudaError_t launch_head_pack_weight(const uint16_t* w, uint64_t stride, uint16_t* out, uint32_t vocab, uint32_t dim, uint32_t dp, cudaStream_t s) {
   return launch(fls_head_pack_weight_kernel, dim3(vocab), 256, 0, false, s, w, stride, out, dim, dp);
