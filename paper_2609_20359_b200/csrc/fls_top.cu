@@ -13,7 +13,7 @@
 // copy; with k = 128 249 us: the rest is the second look and the ranking, during which a CTA reads nothing new).  Ahead of
 // the sums two fp32 operations go into one instruction (270 us without) and four 16-byte vectors per thread are on their
 // way while four are added up (256 us with one thread maximum instead of stretches, 512 threads).  One row is latency:
-// 12.6 us for 128256 bf16 by eight CTAs, of which the load is a tenth; the 16 block-wide counts that find the bound, the
+// 11.5 us for 128256 bf16 by four CTAs, of which the load is a tenth; the 16 block-wide counts that find the bound, the
 // ranking and the two cluster barriers are the rest.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -550,15 +550,16 @@ extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t
       if (a < b + s[j].bytes && b < a + s[i].bytes) return fail(FLS_EPTR, "%s overlaps %s", s[i].what, s[j].what);
     }
   TopArgs a{logits, stride, uint32_t(vocab), top, float(1.4426950408889634 / temperature), 1.0 / temperature, value, index, lse};
-  // Few rows: a row is shared by the CTAs of a cluster, as long as a thread still has a 16-byte vector or two to read, and
-  // the CTAs are large (one row of 128256 bf16, k = 64: 12.6 us with 512 threads, 16.3 with 256).  Otherwise a CTA is small,
-  // five share an SM and some read while others rank (4096 rows of 128256 bf16: 204 us with 256 threads, 247 with 512;
-  // 4096 of 32000 fp32, k = 8: 104 and 147; 2000 of 5000 bf16: 23 and 45).
+  // Few rows: a row is shared by the CTAs of a cluster while there is an SM for each and a part has at least 64 KB (one row of
+  // 128256 bf16, k = 64, in 1, 2, 4, 8 parts: 13.0, 12.4, 11.5, 12.7 us; 20 rows of 32000 fp32: 8.7, 10.1, 10.3, 14.1).
   uint32_t parts = 1;
-  while (parts < 8 && rows * parts * 2 <= 296 && vocab * elem >= uint64_t(parts) * 2 * 512 * 16) parts *= 2;
+  while (parts < 8 && rows * parts * 2 <= 148 && vocab * elem >= uint64_t(parts) * 2 * (64 << 10)) parts *= 2;
+  // CTAs of 512 threads where an SM has one or two of them and the rows are not short, otherwise of 256, five to an SM, of
+  // which some read while others rank (512 / 256 threads, us: 1 x 128256 bf16 13.0 / 17.0, 200 rows 21.1 / 22.7, 500 rows
+  // 41.2 / 35.0, 4096 rows 247 / 204; 220 x 20000 bf16 9.8 / 11.0; 100 x 5000 bf16 6.9 / 6.4; 333 x 50257 fp32 24.6 / 19.4).
+  const int threads = parts > 1 || (rows <= 222 && vocab * elem >= (16 << 10)) ? 512 : 256;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(uint32_t(rows) * parts);
-  const int threads = parts > 1 ? 512 : 256;
   cfg.blockDim = dim3(threads);
   cfg.stream = static_cast<cudaStream_t>(cuda_stream);
   cudaLaunchAttribute at{};

@@ -106,6 +106,21 @@ def test_ties_and_orders(dtype, n, kind):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,V", [(1, 300001), (20, 70001), (30, 140003)])
+def test_rows_shared_by_a_cluster(dtype, n, V):
+    """Long rows of few are cut into 2, 4 or 8 parts: ties, masks and the sum have to hold across the cuts."""
+    check(draw(n, V, dtype), 77, 1.5)
+    x = torch.zeros(n, V, device=DEV)
+    x[:, ::3] = -math.inf
+    x[:, V // 2 - 20: V // 2 + 20] = 2.0
+    check(x.to(dtype), 64)
+    x[:] = -math.inf
+    x[:, -3:] = 1.0
+    check(x.to(dtype), 8)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("n", [2, 320])
 def test_masked_and_special_values(dtype, n):
     V, k = 30001, 16
