@@ -516,6 +516,12 @@ __device__ __forceinline__ void store_row32(T* dst, const float (&v)[32], uint32
   }
 }
 
+// Without row weights the mean's 1 / count stays out of dL/dz and goes onto the gradients in fp32: a label's entry is then
+// p - 1, whose leading term in bf16 is mostly exact, and not a number with 24 bits that 8 or 16 have to hold.
+__device__ __forceinline__ float mean_scale(const HeadCall& c, uint32_t count) {
+  return c.row_weight || !count ? 1.f : 1.f / float(count);
+}
+
 // The first of a packed row's own columns that is not below column n (a multiple of 128).
 __device__ __forceinline__ uint32_t first_slot(const HeadCall& c, uint32_t row, uint32_t n) {
   if (c.slots == 1) return c.slot_idx[row] < int32_t(n) ? 1 : 0;
@@ -673,6 +679,7 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
     const uint32_t lane_base = tmem + ((quarter * 32) << 16) + half * 128;
     Stager<kBufs> out(tile_base + kStages * kStageBytes + (warp - 4) * kBufs * kStoreBytes, lane);
     uint32_t buf = 0, phase = 0;
+    const float scale = mean_scale(c, count);
     for (uint32_t u = cluster; u < plan.n_units; u += n_clusters) {
       const Unit w = plan.at(u);
       const bool empty = w.kbn == 0;
@@ -728,6 +735,10 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
             if constexpr (FLAG) out.send3(&maps.store, int(row0), dz_panel(piece, n, 1), lo);
           }
         } else {
+          if (!w.grad_hidden) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= scale;
+          }
           if (w.grad_hidden) {
             // [split][rows_cap][dcap]; pieces after the first add to their split's sums, one after the other
             if (!empty || piece.first) {
@@ -1026,7 +1037,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
   }
   // what this warp needs of its row comes while the others finish
   const int64_t label = c.use_label ? c.labels[n] : c.ignore_label;
-  const double w = c.row_weight ? double(c.row_weight[n]) : 1.0 / double(count);
+  const double w = c.row_weight ? double(c.row_weight[n]) : 1.0;      // the mean's 1 / count: mean_scale
   float mf = -INFINITY;
   for (uint32_t i = lane; i < c.slots; i += 32) {
     const int32_t x = idx[i];
@@ -1251,6 +1262,8 @@ __global__ void __launch_bounds__(256) fls_head_grad_hidden_kernel(const __grid_
       }
     }
     if (i >= c.dim) continue;
+    const float scale = mean_scale(c, c.state->count);
+    v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
     if (vec) *reinterpret_cast<uint2*>(out + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
     else {
       const float w[4] = {v.x, v.y, v.z, v.w};
