@@ -34,6 +34,7 @@ struct HeadCall {
   uint8_t* slot_start;       // [rows_cap][tiles]: the first of them in each 128 columns (only with a teacher's list)
   float* slot_t;             // [rows_cap][slots]: the teacher's logit of that column (-inf: label only)
   float* slot_z;             // [rows_cap][slots]: the logit of that column
+  float* label_z;            // [rows_cap]: the label's logit, summed in double
   float* slot_g;             // [rows_cap][slots]: its gradient
   float* part_m;             // [tiles][rows_cap]: largest logit of 128 columns, slots left out
   float* part_s;             // [tiles][rows_cap]: sum of exp((z - m) / T)
@@ -45,6 +46,7 @@ struct HeadCall {
   float* dh;                 // [splits][rows_cap][dcap]: partial sums of the hidden gradient
   // problem
   const uint16_t* hidden; uint64_t hidden_stride;
+  const uint16_t* weight; uint64_t weight_stride;
   const int64_t* labels; int64_t ignore_label;
   const int32_t* top_index; const float* top_logit; const float* teacher_lse;
   const float* row_weight;

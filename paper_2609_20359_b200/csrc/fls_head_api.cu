@@ -42,7 +42,7 @@ bool keeps_logits(uint64_t rows, uint64_t dim) { return dim >= 896 || 3 * rows <
 
 // Byte offsets of the workspace.  Sizes are those of max_rows; a smaller call uses the front of each region.
 struct Regions {
-  uint64_t mask, counts, pos, src, hp, slot_idx, slot_start, slot_t, slot_z, slot_g, part, coef, g, dh, wcopy, total;
+  uint64_t mask, counts, pos, src, hp, slot_idx, slot_start, slot_t, slot_z, slot_g, label_z, part, coef, g, dh, wcopy, total;
   uint64_t part_bytes, g_bytes, dh_bytes;
 };
 
@@ -63,6 +63,7 @@ Regions regions(const fls_head_desc& d) {
   r.slot_t = take(cap * slots * 4);
   r.slot_z = take(cap * slots * 4);
   r.slot_g = take(cap * slots * 4);
+  r.label_z = take(cap * 4);
   r.part_bytes = cap * tiles * 4;
   r.part = take(3 * r.part_bytes);          // maximum, sum, and one of: sum at temperature 1, sum of logits
   r.coef = take(cap * 16);
@@ -209,6 +210,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.slot_t = reinterpret_cast<float*>(ws + r.slot_t);
   c.slot_z = reinterpret_cast<float*>(ws + r.slot_z);
   c.slot_g = reinterpret_cast<float*>(ws + r.slot_g);
+  c.label_z = reinterpret_cast<float*>(ws + r.label_z);
   c.part_m = reinterpret_cast<float*>(ws + r.part);
   c.part_s = reinterpret_cast<float*>(ws + r.part + r.part_bytes);
   c.part_s1 = c.part_z = reinterpret_cast<float*>(ws + r.part + 2 * r.part_bytes);
@@ -218,6 +220,8 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.dh = reinterpret_cast<float*>(ws + r.dh);
   c.hidden = static_cast<const uint16_t*>(io->hidden);
   c.hidden_stride = io->hidden_stride ? io->hidden_stride : d.dim;
+  c.weight = static_cast<const uint16_t*>(io->weight);
+  c.weight_stride = io->weight_stride ? io->weight_stride : d.dim;
   c.labels = io->labels;
   c.ignore_label = io->ignore_label;
   c.row_weight = io->row_weight;
