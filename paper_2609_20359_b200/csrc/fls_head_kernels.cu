@@ -1099,14 +1099,16 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) { tmax = fmax(tmax, double(sh_t[y][i])); nan_t |= isnan(sh_t[y][i]); }
     tmax = warp_max(tmax);
     const bool taught = __any_sync(0xFFFFFFFFu, nan_t) || tmax != -INFINITY;
-    double norm = 0.0;
+    // log q = (t - shift) / T - norm; the list's maximum goes first, so that entries at the type's lowest value keep log k
+    double norm = 0.0, shift = 0.0;
     if (taught) {
       if (c.tail_class) norm = double(c.teacher_lse[n]);
       else {
+        shift = tmax == -INFINITY ? 0.0 : tmax;
         double a = 0.0;
         for (uint32_t i = lane; i < c.slots; i += 32)
-          if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) a += exp((double(sh_t[y][i]) - tmax) * c.inv_temp);
-        norm = tmax * c.inv_temp + log(warp_sum(a));
+          if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) a += exp((double(sh_t[y][i]) - shift) * c.inv_temp);
+        norm = log(warp_sum(a));
       }
     }
     // own columns: their exponentials, with those of the label apart from the rest
@@ -1115,7 +1117,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       double qi = 0.0;
       const int32_t x = sh_i[y][i];
       if (x != INT_MAX) {
-        if (sh_t[y][i] != -INFINITY) { qi = exp(double(sh_t[y][i]) * c.inv_temp - norm); qsum += qi; }
+        if (sh_t[y][i] != -INFINITY) { qi = exp((double(sh_t[y][i]) - shift) * c.inv_temp - norm); qsum += qi; }
         const bool first = i == 0 || sh_i[y][i - 1] != x;
         if (first) {
           bool listed = false;
@@ -1155,7 +1157,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       for (uint32_t i = lane; i < c.slots; i += 32)
         if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) {
           const double qi = sh_q[y][i];
-          if (qi != 0.0) kl += qi * ((double(sh_t[y][i]) * c.inv_temp - norm) - (double(sh_zs[y][i]) * c.inv_temp - lseT));
+          if (qi != 0.0) kl += qi * (((double(sh_t[y][i]) - shift) * c.inv_temp - norm) - (double(sh_zs[y][i]) * c.inv_temp - lseT));
         }
       kl = warp_sum(kl);
       double damp = 1.0;

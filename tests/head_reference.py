@@ -27,9 +27,9 @@ def distill_rows(z, idx, top, y, T, wd, wl, tlse, ignore):
         lse = torch.logsumexp(zt, 0)
         loss = z.new_zeros(())
         if len(cols):
-            norm = torch.logsumexp(t, 0) if tlse is None else tlse[n].double()
-            q = torch.exp(t - norm)
-            part = torch.where(q > 0, q * ((t - norm) - (zt[cols] - lse)), 0.0).sum()
+            logq = torch.log_softmax(t, 0) if tlse is None else t - tlse[n].double()
+            q = torch.exp(logq)
+            part = torch.where(q > 0, q * (logq - (zt[cols] - lse)), 0.0).sum()
             if tlse is not None:
                 rest = max(0.0, 1.0 - float(q.sum()))
                 if rest > 0:

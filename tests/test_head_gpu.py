@@ -441,6 +441,32 @@ def test_distill_rows_without_a_teacher_may_hold_anything():
     assert not bool(gh[10:12].any()) and not bool(loss[10:12].any())
 
 
+def test_teacher_entries_at_the_lowest_value():
+    """Entries masked with the type's lowest value have probability zero, and a list of nothing else is uniform."""
+    from paper_2609_20359_b200.head import Head
+    n, V, d = 9, 300, 64
+    h, w, y, g = make(n, V, d)
+    idx, t = teacher(n, V, 6, g, ragged=False)
+    t[:, 2] = torch.finfo(torch.float32).min
+    t[4] = torch.finfo(torch.float32).min
+    gh, gw = buffers(n, V, d)
+    loss, lse = Head(n, V, d, top=6).distill_step(h, w, idx, t, gh, gw, temperature=0.5)
+    ref = R.with_gradients(h, w, lambda z: R.distill_rows(z, idx, t, y, 0.5, 1.0, 0.0, None, IGN))
+    R.check_rows(ref, loss, lse, 1.0, 0.5)
+    R.check_grads(ref, gh, gw)
+
+
+@pytest.mark.parametrize("n,V,d", [(1, 700, 64), (300, 3000, 1024)])
+def test_the_loss_alone_is_that_of_the_step(n, V, d):
+    from paper_2609_20359_b200.head import Head
+    h, w, y, _ = make(n, V, d)
+    gh, gw = buffers(n, V, d)
+    full, lean = Head(n, V, d), Head(n, V, d, grads=False)
+    step = full.xent_step(h, w, y, gh, gw, label_smoothing=0.1)
+    for head in (full, lean):
+        assert all(torch.equal(a, b) for a, b in zip(step, head.xent(h, w, y, label_smoothing=0.1)))
+
+
 def test_repeated_teacher_entries_add_up():
     """Two entries on one column count as two entries: in the gradient their probabilities add."""
     from paper_2609_20359_b200.head import Head
