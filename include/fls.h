@@ -377,9 +377,10 @@ int fls_plan_destroy(fls_plan* plan);
  * on request, the gradients of the weighted sum  L = sum_n w_n loss_n  with respect to h and W, without ever holding the
  * N x V logits (beyond a workspace of fixed size): a first pass keeps per row and per 128 columns the maximum and the sum
  * of exponentials, the gradient passes turn the logits of one piece of the vocabulary, formed again or for the last piece
- * still there, into dL/dz (bf16) in the workspace and multiply that by W and h.  Products are bf16 tensor-core products with fp32 accumulation; maxima, sums and losses are held in
- * fp32 / double; dL/dz is rounded to bf16 once before its products (with fp32 weight gradients it enters the product
- * with h as two bf16 terms, about 17 bits).  Results do not change from run to run.
+ * still there, into dL/dz (bf16) in the workspace and multiply that by W and h.  Products are bf16 tensor-core products
+ * with fp32 accumulation; the label's own logit is summed in double; maxima, sums and losses are held in fp32 / double;
+ * dL/dz is rounded to bf16 once before its products (with fp32 weight gradients it enters the product with h as two bf16
+ * terms, about 17 bits).  Results do not change from run to run.
  *
  * Cross entropy (fls_head_xent), label y, smoothing e, z loss c, lse = log sum_v exp(z_v):
  *   loss = (1-e) (lse - z_y) + e (lse - mean_v z_v) + c lse^2.

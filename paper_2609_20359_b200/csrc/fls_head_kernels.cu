@@ -6,7 +6,7 @@
 //     kStats    logits tile -> maximum and sum of exponentials per row and 128 columns
 //     kDlogits  logits tile -> dL/dz in bf16 (one piece of the vocabulary)
 //     kGrads    dL/dz of the piece -> rows of grad_weight, and partial sums of grad_hidden
-//   fls_head_rescale_kernel   dL/dz of the columns whose logits the statistics pass kept
+//   fls_head_rescale_kernel, fls_head_own_kernel   dL/dz of the columns whose logits the statistics pass kept
 //   fls_head_rows_kernel   joins the tile sums, losses, coefficients of dL/dz
 //   fls_head_grad_hidden_kernel   sums the partial sums, rounds, puts rows back in the caller's order
 #include <cuda_bf16.h>
