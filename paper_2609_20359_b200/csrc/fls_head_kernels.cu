@@ -1193,7 +1193,8 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
 
 // dL/dz of the kept columns, in place: reads 4 bytes and writes 2 (two terms: 4) per element instead of forming the logit
 // again.  The same operations on the same fp32 logit as in the kDlogits epilogue: the same bits.  Bound by memory: 1024 x
-// 128256 in 122 us, 6.5 TB/s of its 6 bytes per element.  A block takes 128 rows of 64 columns; eight threads of a warp share a row, so what is overwritten has been read.
+// 128256 in 122 us, 6.5 TB/s of its 6 bytes per element.  A block takes 128 rows of 64 columns; eight threads of a warp
+// share a row, so what is overwritten has been read.
 constexpr uint32_t kRescaleRows = 128;
 template <bool TWO, bool PLANES>
 __global__ void __launch_bounds__(256) fls_head_rescale_kernel(const __grid_constant__ HeadCall c) {
