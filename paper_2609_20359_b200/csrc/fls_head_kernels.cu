@@ -432,7 +432,8 @@ struct Stager {
   }
 };
 
-// dL/dz of one row of a tile: aT exp(z/T - lse_T) + a1 exp(z - lse_1) - b, then the columns with a value of their own.
+// dL/dz of one row of a tile: aT exp(z/T - lse_T) + a1 exp(z - lse_1) - b, then the columns with a value of their own
+// (lse_T: with the tail as a class that of the columns outside the list).
 template <bool TWO, bool PLANES, int BUFS>
 struct DlogitsRow : Columns {
   float4 k;          // {lse_T log2(e), aT, lse_1 log2(e), a1}; without TWO {lse log2(e) , a, b, -}
@@ -1112,7 +1113,8 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       }
     }
     // own columns: their exponentials, with those of the label apart from the rest
-    double ownT = 0.0, own1 = 0.0, outT = 0.0, eT_label = 0.0, e1_label = 0.0, z_label = 0.0, qsum = 0.0;
+    double ownT = 0.0, own1 = 0.0, eT_label = 0.0, e1_label = 0.0, z_label = 0.0, qsum = 0.0;
+    float out_z = -INFINITY;                               // the label's logit where it is not in the teacher's list
     for (uint32_t i = lane; i < c.slots; i += 32) {
       double qi = 0.0;
       const int32_t x = sh_i[y][i];
@@ -1125,20 +1127,34 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
           const double eT = exp((double(sh_zs[y][i]) - M) * c.inv_temp), e1 = c.two ? exp(double(sh_zs[y][i]) - M) : eT;
           if (labelled && int64_t(x) == label) { eT_label = eT; e1_label = e1; z_label = double(sh_zs[y][i]); }
           else { ownT += eT; own1 += e1; }
-          if (!listed) outT += eT;             // the label outside the teacher's list belongs to the tail
+          if (!listed) out_z = sh_zs[y][i];    // the label outside the teacher's list belongs to the tail
         }
       }
       sh_q[y][i] = qi;
     }
-    ownT = warp_sum(ownT); own1 = warp_sum(own1); outT = warp_sum(outT); qsum = warp_sum(qsum);
+    ownT = warp_sum(ownT); own1 = warp_sum(own1); qsum = warp_sum(qsum);
     eT_label = warp_sum(eT_label); e1_label = warp_sum(e1_label); z_label = warp_sum(z_label);
     __syncwarp();
     const double restT = denseT + ownT, rest1 = dense1 + own1;         // everything but the label
     const double totT = restT + eT_label, tot1 = rest1 + e1_label;
-    // Three logarithms, one per lane: of the sums (at least 1: the maximum's own term) at T and 1, and -log p_label where
-    // the label dominates and lse - z would cancel.
-    const double part = log1p(lane == 0 ? totT - 1.0 : lane == 1 ? tot1 - 1.0 : rest1 / e1_label);
+    // What is outside the list, relative to its own maximum: relative to the row's nothing of it is left where a student is sure.
+    const bool class_t = taught && c.tail_class;
+    double tail = 0.0, tail_m = 0.0;
+    if (class_t) {
+      float tm = fmaxf(lm, out_z);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xFFFFFFFFu, tm, o));
+      if (tm == -INFINITY) tm = 0.f;
+      tail_m = double(tm);
+      tail = double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(lm, c.cT) - __fmul_rn(tm, c.cT))));
+      if (out_z != -INFINITY) tail += exp((double(out_z) - tail_m) * c.inv_temp);
+      tail = warp_sum(tail);
+    }
+    // Four logarithms, one per lane: of the sums (at least 1: the maximum's own term) at T and 1, -log p_label where the
+    // label dominates and lse - z would cancel, and of the tail's sum (at least 1, or 0 where nothing is outside the list).
+    const double part = log1p(lane == 0 ? totT - 1.0 : lane == 1 ? tot1 - 1.0 : lane == 2 ? rest1 / e1_label : tail - 1.0);
     const double log_T = __shfl_sync(0xFFFFFFFFu, part, 0), log_1 = __shfl_sync(0xFFFFFFFFu, part, 1), log_p = __shfl_sync(0xFFFFFFFFu, part, 2);
+    const double lse_tail = tail_m * c.inv_temp + __shfl_sync(0xFFFFFFFFu, part, 3);
     const double lseT = M * c.inv_temp + log_T, lse1 = c.two ? M + log_1 : lseT;
     const double nll = !labelled ? 0.0 : (rest1 < e1_label ? log_p : (c.two ? lse1 - z_label : lseT - z_label * c.inv_temp));
 
@@ -1160,20 +1176,25 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
           if (qi != 0.0) kl += qi * (((double(sh_t[y][i]) - shift) * c.inv_temp - norm) - (double(sh_zs[y][i]) * c.inv_temp - lseT));
         }
       kl = warp_sum(kl);
-      double damp = 1.0;
-      if (taught && c.tail_class) {
-        const double qt = fmax(0.0, 1.0 - qsum), tail = denseT + outT;
-        if (qt > (tail > 0.0 ? 0.0 : 1e-6)) {          // a list that is the whole vocabulary: what is left of 1 is rounding
-          kl += qt * (log(qt) - (log(tail) - log(totT)));
-          damp = 1.0 - qt * totT / tail;
+      // Outside the list dL/dz = a p (1 - q'/p') = a r (p' - q'), r = p / p' = exp(z/T - lse_tail): neither factor exceeds 1
+      // however small p' is, where q'/p' would overflow and p vanish (in fp32 from 87 T between the list and the rest on).
+      const bool split_tail = class_t && lse_tail != -INFINITY;
+      double lse_out = lseT, p_out = 1.0, d_out = 1.0;      // p = p_out exp(z/T - lse_out), its distillation factor d_out for p_out
+      if (class_t) {
+        const double qt = qsum > 1.0 ? 0.0 : 1.0 - qsum;
+        if (qt > (split_tail ? 0.0 : 1e-6)) kl += qt * (log(qt) - (lse_tail - lseT));   // without a tail what is left of 1 is rounding
+        if (split_tail) {
+          lse_out = lse_tail;
+          p_out = exp(lse_tail - lseT);
+          d_out = p_out - qt;
         }
       }
       const double a = taught ? c.distill_weight * c.temp * w : 0.0, b = labelled ? c.label_weight * w : 0.0;
       if (lane == 0) {
         c.loss[n] = float((taught ? c.distill_weight * c.temp * c.temp * kl : 0.0) + (labelled ? c.label_weight * nll : 0.0));
         c.lse[n] = float(lseT);
-        if (c.two) c.coef[p] = make_float4(float(lseT * 1.4426950408889634), float(a * damp), float(lse1 * 1.4426950408889634), float(b));
-        else c.coef[p] = make_float4(float(lseT * 1.4426950408889634), float(a * damp + b), 0.f, 0.f);
+        if (c.two) c.coef[p] = make_float4(float(lse_out * 1.4426950408889634), float(a * d_out), float(lse1 * 1.4426950408889634), float(b));
+        else c.coef[p] = make_float4(float(lse_out * 1.4426950408889634), float(a * d_out + b * p_out), 0.f, 0.f);
       }
       for (uint32_t i = lane; i < c.slots; i += 32) {
         const int32_t x = sh_i[y][i];
@@ -1182,8 +1203,8 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
         bool listed = false;
         for (uint32_t j = i + 1; j-- > 0 && sh_i[y][j] == x;) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
         for (uint32_t j = i + 1; j < c.slots && sh_i[y][j] == x; ++j) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
-        const double pT = exp(double(sh_zs[y][i]) * c.inv_temp - lseT);
-        double v = a * (pT * (listed ? 1.0 : damp) - qi);
+        const double zT = double(sh_zs[y][i]) * c.inv_temp, pT = exp(zT - lseT);
+        double v = a * (listed ? pT - qi : exp(zT - lse_out) * d_out);
         if (labelled) v += b * (int64_t(x) == label ? -rest1 / tot1 : (c.two ? exp(double(sh_zs[y][i]) - lse1) : pT));
         gs[i] = float(v);
       }
