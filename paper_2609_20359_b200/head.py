@@ -51,8 +51,10 @@ class Head:
     grad_dtype: "bf16" or "f32", the type of weight gradients (as `Session`'s gradient buffers, whose units they may be
     written into).  grads=False: a workspace for losses only.  any_weight: accept weights of any alignment and stride.
 
-    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  The workspace is
-    used by one call at a time: calls of one Head belong on one stream, or on streams ordered by events.
+    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting; the constructor waits
+    until the workspace is cleared.  The workspace is used by one call at a time: calls of one Head belong on one stream, or on
+    streams ordered by events.  A Head may be dropped while its calls run (a stream given by its handle has to outlive it); a
+    captured graph has to be dropped first.
     """
 
     def __init__(self, max_rows: int, vocab: int, dim: int, top: int = 0, grad_dtype: str = "bf16", grads: bool = True,
@@ -73,13 +75,17 @@ class Head:
         self.layout = fls.fls_head_query(self.handle)
         self.workspace = torch.empty(self.layout["workspace_bytes"], dtype=torch.uint8, device=self.device)
         self.workspace[:256].zero_()
+        # The first call may be on any stream: the clear, and what used this memory before, must not come after it.
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()
+        self._streams = {fls._stream_handle(None)}             # those that torch's allocator knows to use the workspace
         self._args = fls.fls_head_io(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace.numel())   # of the call in preparation
 
     # ------------------------------------------------------------------ calls
     def xent(self, hidden, weight, labels, ignore_label: int = -100, label_smoothing: float = 0.0, z_loss: float = 0.0, stream=None):
         """(loss, lse) of every row, fp32."""
         io, out = self._io(hidden, weight, labels, ignore_label, None, None, None, False, stream)
-        fls.fls_head_xent(self.handle, io, label_smoothing, z_loss, stream)
+        fls.fls_head_xent(self.handle, io, label_smoothing, z_loss, self._use(stream))
         return out
 
     def xent_step(self, hidden, weight, labels, grad_hidden=None, grad_weight=None, row_weight=None, accumulate: bool = False,
@@ -87,7 +93,7 @@ class Head:
         """(loss, lse); the gradients of sum(row_weight * loss) (default: the mean over the rows that take part) are written
         to grad_hidden (bf16) and grad_weight, each optional; accumulate adds to grad_weight."""
         io, out = self._io(hidden, weight, labels, ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream)
-        fls.fls_head_xent(self.handle, io, label_smoothing, z_loss, stream)
+        fls.fls_head_xent(self.handle, io, label_smoothing, z_loss, self._use(stream))
         return out
 
     def distill(self, hidden, weight, top_index, top_logit, labels=None, teacher_lse=None, temperature: float = 1.0,
@@ -115,7 +121,7 @@ class Head:
                                  _dense(teacher_lse, "teacher_lse", (n,), torch.float32, self.device),
                                  fls.FLS_TAIL_RENORM if teacher_lse is None else fls.FLS_TAIL_CLASS, 0, temperature, distill_weight,
                                  label_weight)
-        fls.fls_head_distill(self.handle, io, t, stream)
+        fls.fls_head_distill(self.handle, io, t, self._use(stream))
         return out
 
     def _io(self, hidden, weight, labels, ignore_label, grad_hidden, grad_weight, row_weight, accumulate, stream):
@@ -132,6 +138,18 @@ class Head:
         loss, lse = _empty_on(stream, (2, n), torch.float32, dev).unbind(0)
         io.loss, io.lse = loss.data_ptr(), lse.data_ptr()
         return io, (loss, lse)
+
+    def _use(self, stream) -> int:
+        """The call's stream as a handle; the workspace's memory is not given to anyone else before its work is done."""
+        handle = fls._stream_handle(stream)
+        if handle not in self._streams:
+            if stream is None:
+                stream = torch.cuda.current_stream(self.device)
+            elif isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=self.device)
+            self.workspace.record_stream(stream)
+            self._streams.add(handle)
+        return handle
 
     # ------------------------------------------------------------------ what the device wrote beside the outputs
     def _word(self, i: int) -> torch.Tensor:
