@@ -490,7 +490,7 @@ int fls_head_get_launch_count(const fls_head* head, uint64_t* launches);
  * a row with fewer than `top` other logits ends with index -1 and value -inf, which fls_head_distill takes as absent.
  * NaN ranks above everything; +0 and -0 are equal.  No workspace; one kernel, enqueued on cuda_stream.
  * Errors: FLS_EINVAL (dtype, vocab outside 1 .. 2^30, rows > 2^24, top outside 1 .. FLS_HEAD_MAX_TOP, temperature,
- * stride < vocab), FLS_EPTR (null, host or overlapping buffers), FLS_EALIGN, FLS_ECUDA. */
+ * stride < vocab), FLS_EPTR (null, host, another device's or overlapping buffers), FLS_EALIGN, FLS_ECUDA. */
 int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t rows, uint64_t vocab, uint64_t stride, uint32_t top,
                    double temperature, float* value, int32_t* index, float* lse, void* cuda_stream);
 

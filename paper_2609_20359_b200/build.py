@@ -13,7 +13,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libfls.so")
 SOURCES = ["fls_api.cu", "fls_kernels.cu", "fls_noalloc.cu", "fls_head_api.cu", "fls_head_kernels.cu", "fls_top.cu",
-            "fls_layout.cpp", "fls_report.cpp"]
+           "fls_check.cpp", "fls_layout.cpp", "fls_report.cpp"]
 HEADERS = [os.path.join(CSRC, h) for h in ("fls_internal.h", "fls_kernels.h", "fls_head.h")] + [os.path.join(ROOT, "include", "fls.h")]
 
 

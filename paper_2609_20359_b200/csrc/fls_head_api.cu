@@ -4,8 +4,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <new>
 
@@ -16,16 +14,7 @@ using namespace fls;
 
 namespace {
 
-int fail(int code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  set_last_error(buf);
-  return code;
-}
-int cuda_fail(cudaError_t e, const char* what) { return fail(FLS_ECUDA, "%s: %s", what, cudaGetErrorString(e)); }
+int cuda_fail(cudaError_t e, const char* what) { return refuse(FLS_ECUDA, "%s: %s", what, cudaGetErrorString(e)); }
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
 constexpr uint32_t kWaitLimit = 1u << 20;            // polls, 4 us each, of a barrier before a role of the tensor-core kernel gives up
@@ -119,40 +108,6 @@ bool encode_panels(EncodeTiled f, CUtensorMap* m, const void* base, uint64_t row
   return f(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-struct Span {
-  const void* p;
-  uint64_t bytes, align;
-  bool output;
-  const char* what;
-};
-
-int check_spans(const Span* s, int n) {
-  int device = 0;
-  if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); device = -1; }
-  for (int i = 0; i < n; ++i) {
-    if (!s[i].p) {
-      if (s[i].bytes) return fail(FLS_EPTR, "%s is null", s[i].what);
-      continue;
-    }
-    if (reinterpret_cast<uintptr_t>(s[i].p) % s[i].align)
-      return fail(FLS_EALIGN, "%s must start on a %llu-byte boundary", s[i].what, (unsigned long long)s[i].align);
-    if (!s[i].bytes) continue;
-    cudaPointerAttributes at{};
-    const cudaError_t e = cudaPointerGetAttributes(&at, s[i].p);
-    if (e != cudaSuccess) { cudaGetLastError(); return cuda_fail(e, "cudaPointerGetAttributes"); }
-    if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged)
-      return fail(FLS_EPTR, "%s is not device memory", s[i].what);
-    if (at.type == cudaMemoryTypeDevice && at.device != device) return fail(FLS_EPTR, "%s is on device %d, not the current one", s[i].what, at.device);
-  }
-  for (int i = 0; i < n; ++i)
-    for (int j = 0; j < n; ++j) {
-      if (i == j || !s[i].output || (s[j].output && j < i) || !s[i].bytes || !s[j].bytes) continue;
-      const uintptr_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
-      if (a < b + s[j].bytes && b < a + s[i].bytes) return fail(FLS_EPTR, "%s overlaps %s", s[i].what, s[j].what);
-    }
-  return FLS_OK;
 }
 
 // Bytes from the first to the last element of a matrix with `stride` elements between rows.
@@ -294,7 +249,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
     ok = encode_panels(f, &fwd.store, c.g, c.rows_cap, n, 32) && encode_panels(f, &grad.a0, c.g, c.rows_cap, n, 64) &&
          encode_panels(f, &grad.a1, c.g, c.rows_cap, n, 128);
   }
-  if (!ok) return fail(FLS_ECUDA, "cuTensorMapEncodeTiled failed");
+  if (!ok) return refuse(FLS_ECUDA, "cuTensorMapEncodeTiled failed");
 
 #define FLS_LAUNCH(call)                                        \
   do {                                                          \
@@ -328,21 +283,21 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
 
 // Everything both losses check; `extra` / n_extra are the distillation's own buffers.
 int check_io(const fls_head* h, const fls_head_io* io, bool need_labels, const Span* extra, int n_extra) {
-  if (!h || !io) return fail(FLS_EINVAL, "null argument");
+  if (!h || !io) return refuse(FLS_EINVAL, "null argument");
   const fls_head_desc& d = h->desc;
-  if (io->reserved) return fail(FLS_EINVAL, "reserved must be 0");
-  if (io->rows > d.max_rows) return fail(FLS_EINVAL, "rows (%llu) > max_rows (%llu)", (unsigned long long)io->rows, (unsigned long long)d.max_rows);
-  if (io->accumulate > 1) return fail(FLS_EINVAL, "accumulate must be 0 or 1");
-  if ((io->grad_hidden || io->grad_weight) && !d.grads) return fail(FLS_EINVAL, "the head was created without grads");
+  if (io->reserved) return refuse(FLS_EINVAL, "reserved must be 0");
+  if (io->rows > d.max_rows) return refuse(FLS_EINVAL, "rows (%llu) > max_rows (%llu)", (unsigned long long)io->rows, (unsigned long long)d.max_rows);
+  if (io->accumulate > 1) return refuse(FLS_EINVAL, "accumulate must be 0 or 1");
+  if ((io->grad_hidden || io->grad_weight) && !d.grads) return refuse(FLS_EINVAL, "the head was created without grads");
   const uint64_t strides[4] = {io->hidden_stride, io->weight_stride, io->grad_hidden_stride, io->grad_weight_stride};
   static const char* const names[4] = {"hidden_stride", "weight_stride", "grad_hidden_stride", "grad_weight_stride"};
   for (int i = 0; i < 4; ++i) {
-    if (strides[i] && strides[i] < d.dim) return fail(FLS_EINVAL, "%s (%llu) < dim (%u)", names[i], (unsigned long long)strides[i], d.dim);
-    if (strides[i] >= (1ull << 36)) return fail(FLS_EINVAL, "%s out of range", names[i]);
+    if (strides[i] && strides[i] < d.dim) return refuse(FLS_EINVAL, "%s (%llu) < dim (%u)", names[i], (unsigned long long)strides[i], d.dim);
+    if (strides[i] >= (1ull << 36)) return refuse(FLS_EINVAL, "%s out of range", names[i]);
   }
   auto st = [&](int i) { return strides[i] ? strides[i] : uint64_t(d.dim); };
   if (!(d.any_weight || d.dim % 8) && (reinterpret_cast<uintptr_t>(io->weight) % 16 || st(1) % 8))
-    return fail(FLS_EALIGN, "weight must start on a 16-byte boundary with a stride of a multiple of 8 elements (or create the head with any_weight)");
+    return refuse(FLS_EALIGN, "weight must start on a 16-byte boundary with a stride of a multiple of 8 elements (or create the head with any_weight)");
   const uint64_t we = d.grad_dtype == FLS_GRAD_F32 ? 4 : 2;
   Span s[16] = {
       {io->hidden, span_bytes(io->rows, d.dim, st(0), 2), 2, false, "hidden"},
@@ -358,7 +313,7 @@ int check_io(const fls_head* h, const fls_head_io* io, bool need_labels, const S
   int n = 9;
   for (int i = 0; i < n_extra; ++i) s[n++] = extra[i];
   if (io->workspace && io->workspace_bytes < h->reg.total)
-    return fail(FLS_ESIZE, "workspace has %llu bytes, %llu needed", (unsigned long long)io->workspace_bytes, (unsigned long long)h->reg.total);
+    return refuse(FLS_ESIZE, "workspace has %llu bytes, %llu needed", (unsigned long long)io->workspace_bytes, (unsigned long long)h->reg.total);
   return check_spans(s, n);
 }
 
@@ -370,18 +325,18 @@ extern "C" {
 
 int fls_head_create(const fls_head_desc* desc, fls_head** out) {
   if (out) *out = nullptr;
-  if (!desc || !out) return fail(FLS_EINVAL, "null argument");
-  if (desc->reserved) return fail(FLS_EINVAL, "reserved must be 0");
-  if (desc->max_rows > (1ull << 24)) return fail(FLS_EINVAL, "max_rows > 2^24");
-  if (desc->vocab < 1 || desc->vocab > (1ull << 30)) return fail(FLS_EINVAL, "vocab must be in 1 .. 2^30");
-  if (desc->dim < 1 || desc->dim > 65536) return fail(FLS_EINVAL, "dim must be in 1 .. 65536");
-  if (up(desc->max_rows, 256) / 256 * (up(desc->vocab, 256) / 256) > (1ull << 31)) return fail(FLS_EINVAL, "max_rows * vocab > 2^47");
-  if (desc->top > FLS_HEAD_MAX_TOP) return fail(FLS_EINVAL, "top > %d", FLS_HEAD_MAX_TOP);
-  if (desc->grads > 1 || desc->any_weight > 1) return fail(FLS_EINVAL, "grads and any_weight must be 0 or 1");
-  if (desc->grad_dtype != FLS_GRAD_BF16 && desc->grad_dtype != FLS_GRAD_F32) return fail(FLS_EINVAL, "unknown grad_dtype %u", desc->grad_dtype);
-  if (desc->piece_bytes > (1ull << 40)) return fail(FLS_EINVAL, "piece_bytes > 2^40");
+  if (!desc || !out) return refuse(FLS_EINVAL, "null argument");
+  if (desc->reserved) return refuse(FLS_EINVAL, "reserved must be 0");
+  if (desc->max_rows > (1ull << 24)) return refuse(FLS_EINVAL, "max_rows > 2^24");
+  if (desc->vocab < 1 || desc->vocab > (1ull << 30)) return refuse(FLS_EINVAL, "vocab must be in 1 .. 2^30");
+  if (desc->dim < 1 || desc->dim > 65536) return refuse(FLS_EINVAL, "dim must be in 1 .. 65536");
+  if (up(desc->max_rows, 256) / 256 * (up(desc->vocab, 256) / 256) > (1ull << 31)) return refuse(FLS_EINVAL, "max_rows * vocab > 2^47");
+  if (desc->top > FLS_HEAD_MAX_TOP) return refuse(FLS_EINVAL, "top > %d", FLS_HEAD_MAX_TOP);
+  if (desc->grads > 1 || desc->any_weight > 1) return refuse(FLS_EINVAL, "grads and any_weight must be 0 or 1");
+  if (desc->grad_dtype != FLS_GRAD_BF16 && desc->grad_dtype != FLS_GRAD_F32) return refuse(FLS_EINVAL, "unknown grad_dtype %u", desc->grad_dtype);
+  if (desc->piece_bytes > (1ull << 40)) return refuse(FLS_EINVAL, "piece_bytes > 2^40");
   fls_head* h = new (std::nothrow) fls_head;
-  if (!h) return fail(FLS_ESTATE, "out of host memory");
+  if (!h) return refuse(FLS_ESTATE, "out of host memory");
   h->desc = *desc;
   h->reg = regions(*desc);
   *out = h;
@@ -389,7 +344,7 @@ int fls_head_create(const fls_head_desc* desc, fls_head** out) {
 }
 
 int fls_head_query(const fls_head* head, fls_head_layout* out) {
-  if (!head || !out) return fail(FLS_EINVAL, "null argument");
+  if (!head || !out) return refuse(FLS_EINVAL, "null argument");
   const fls_head_desc& d = head->desc;
   out->workspace_bytes = head->reg.total;
   out->piece_cols = out->pieces = out->kept_cols = 0;
@@ -408,8 +363,8 @@ int fls_head_destroy(fls_head* head) {
 }
 
 int fls_head_xent(fls_head* head, const fls_head_io* io, double label_smoothing, double z_loss, void* cuda_stream) {
-  if (!(label_smoothing >= 0.0 && label_smoothing < 1.0)) return fail(FLS_EINVAL, "label_smoothing must be in [0, 1)");
-  if (!weight_ok(z_loss)) return fail(FLS_EINVAL, "z_loss must be finite and >= 0");
+  if (!(label_smoothing >= 0.0 && label_smoothing < 1.0)) return refuse(FLS_EINVAL, "label_smoothing must be in [0, 1)");
+  if (!weight_ok(z_loss)) return refuse(FLS_EINVAL, "z_loss must be finite and >= 0");
   int rc = check_io(head, io, true, nullptr, 0);
   if (rc) return rc;
   HeadCall c{};
@@ -422,12 +377,12 @@ int fls_head_xent(fls_head* head, const fls_head_io* io, double label_smoothing,
 }
 
 int fls_head_distill(fls_head* head, const fls_head_io* io, const fls_distill_desc* t, void* cuda_stream) {
-  if (!head || !io || !t) return fail(FLS_EINVAL, "null argument");
-  if (t->reserved) return fail(FLS_EINVAL, "reserved must be 0");
-  if (head->desc.top == 0) return fail(FLS_EINVAL, "the head was created with top = 0");
-  if (t->tail != FLS_TAIL_RENORM && t->tail != FLS_TAIL_CLASS) return fail(FLS_EINVAL, "unknown tail %u", t->tail);
-  if (!(std::isfinite(t->temperature) && t->temperature > 0.0)) return fail(FLS_EINVAL, "temperature must be finite and > 0");
-  if (!weight_ok(t->distill_weight) || !weight_ok(t->label_weight)) return fail(FLS_EINVAL, "distill_weight and label_weight must be finite and >= 0");
+  if (!head || !io || !t) return refuse(FLS_EINVAL, "null argument");
+  if (t->reserved) return refuse(FLS_EINVAL, "reserved must be 0");
+  if (head->desc.top == 0) return refuse(FLS_EINVAL, "the head was created with top = 0");
+  if (t->tail != FLS_TAIL_RENORM && t->tail != FLS_TAIL_CLASS) return refuse(FLS_EINVAL, "unknown tail %u", t->tail);
+  if (!(std::isfinite(t->temperature) && t->temperature > 0.0)) return refuse(FLS_EINVAL, "temperature must be finite and > 0");
+  if (!weight_ok(t->distill_weight) || !weight_ok(t->label_weight)) return refuse(FLS_EINVAL, "distill_weight and label_weight must be finite and >= 0");
   const bool labels = t->label_weight > 0.0;
   const uint64_t n = io->rows, k = head->desc.top;
   const Span extra[3] = {{t->top_index, n * k * 4, 4, false, "top_index"},
@@ -451,7 +406,7 @@ int fls_head_distill(fls_head* head, const fls_head_io* io, const fls_distill_de
 }
 
 int fls_head_get_state(const void* workspace, const uint32_t** dev_status, const uint32_t** dev_count) {
-  if (!workspace) return fail(FLS_EPTR, "workspace is null");
+  if (!workspace) return refuse(FLS_EPTR, "workspace is null");
   const HeadState* s = static_cast<const HeadState*>(workspace);
   if (dev_status) *dev_status = &s->status;
   if (dev_count) *dev_count = &s->count;
@@ -459,13 +414,13 @@ int fls_head_get_state(const void* workspace, const uint32_t** dev_status, const
 }
 
 int fls_debug_expire_next_head_wait(fls_head* head, uint32_t polls) {
-  if (!head || !polls) return fail(FLS_EINVAL, "null argument");
+  if (!head || !polls) return refuse(FLS_EINVAL, "null argument");
   head->expire_polls = polls;
   return FLS_OK;
 }
 
 int fls_head_get_launch_count(const fls_head* head, uint64_t* launches) {
-  if (!head || !launches) return fail(FLS_EINVAL, "null argument");
+  if (!head || !launches) return refuse(FLS_EINVAL, "null argument");
   *launches = head->launches;
   return FLS_OK;
 }

@@ -60,6 +60,18 @@ std::string build_layout(const std::vector<uint64_t>& unit_numel, uint32_t S, ui
 
 // Sets the calling thread's message returned by fls_last_error() (defined beside it).
 void set_last_error(const char* msg);
+// Sets it from a format and returns `code`.
+int refuse(int code, const char* fmt, ...);
+
+// One buffer of a call: `bytes` from its first to its last element (0: not used; a null pointer then is right).
+struct Span {
+  const void* p;
+  uint64_t bytes, align;
+  bool output;
+  const char* what;
+};
+// Each non-null and aligned, device memory of the current device (or managed), outputs overlapping nothing.
+int check_spans(const Span* s, int n);
 
 // route: how fls_sync_step currently runs (0 store-and-reread, 1 recompute, 2 single pass), for the HBM byte count
 void comm_report(const Layout& lay, const fls_plan_desc& d, int route, const double* bw, fls_comm_costs* out);

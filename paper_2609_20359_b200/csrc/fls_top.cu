@@ -20,13 +20,13 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
 #include <cstdint>
-#include <cstdio>
 #include <type_traits>
 
 #include "fls.h"
 #include "fls_internal.h"
+
+using namespace fls;
 
 namespace {
 
@@ -506,49 +506,24 @@ __global__ void __launch_bounds__(kTopThreads, kTopThreads == 512 ? 2 : 5) fls_t
   }
 }
 
-int fail(int code, const char* fmt, ...) {
-  char buf[256];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  fls::set_last_error(buf);
-  return code;
-}
-
-int check_device(const void* p, uint64_t align, const char* what) {
-  if (!p) return fail(FLS_EPTR, "%s is null", what);
-  if (reinterpret_cast<uintptr_t>(p) % align) return fail(FLS_EALIGN, "%s must start on a %llu-byte boundary", what, (unsigned long long)align);
-  cudaPointerAttributes at{};
-  const cudaError_t e = cudaPointerGetAttributes(&at, p);
-  if (e != cudaSuccess) { cudaGetLastError(); return fail(FLS_ECUDA, "cudaPointerGetAttributes: %s", cudaGetErrorString(e)); }
-  if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged) return fail(FLS_EPTR, "%s is not device memory", what);
-  return FLS_OK;
-}
-
 }  // namespace
 
 extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t rows, uint64_t vocab, uint64_t stride, uint32_t top,
                               double temperature, float* value, int32_t* index, float* lse, void* cuda_stream) {
-  if (logit_dtype != FLS_GRAD_BF16 && logit_dtype != FLS_GRAD_F32) return fail(FLS_EINVAL, "unknown logit_dtype %u", logit_dtype);
-  if (vocab < 1 || vocab > (1ull << 30)) return fail(FLS_EINVAL, "vocab must be in 1 .. 2^30");
-  if (rows > (1ull << 24)) return fail(FLS_EINVAL, "rows > 2^24");
-  if (top < 1 || top > FLS_HEAD_MAX_TOP) return fail(FLS_EINVAL, "top must be in 1 .. %d", FLS_HEAD_MAX_TOP);
-  if (!(std::isfinite(temperature) && temperature > 0.0)) return fail(FLS_EINVAL, "temperature must be finite and > 0");
+  if (logit_dtype != FLS_GRAD_BF16 && logit_dtype != FLS_GRAD_F32) return refuse(FLS_EINVAL, "unknown logit_dtype %u", logit_dtype);
+  if (vocab < 1 || vocab > (1ull << 30)) return refuse(FLS_EINVAL, "vocab must be in 1 .. 2^30");
+  if (rows > (1ull << 24)) return refuse(FLS_EINVAL, "rows > 2^24");
+  if (top < 1 || top > FLS_HEAD_MAX_TOP) return refuse(FLS_EINVAL, "top must be in 1 .. %d", FLS_HEAD_MAX_TOP);
+  if (!(std::isfinite(temperature) && temperature > 0.0)) return refuse(FLS_EINVAL, "temperature must be finite and > 0");
   if (stride == 0) stride = vocab;
-  if (stride < vocab || stride >= (1ull << 36)) return fail(FLS_EINVAL, "stride out of range");
+  if (stride < vocab || stride >= (1ull << 36)) return refuse(FLS_EINVAL, "stride out of range");
   if (rows == 0) return FLS_OK;
   const uint64_t elem = logit_dtype == FLS_GRAD_F32 ? 4 : 2;
-  const struct { const void* p; uint64_t bytes, align; const char* what; } s[4] = {
-      {logits, ((rows - 1) * stride + vocab) * elem, elem, "logits"}, {value, rows * top * 4, 4, "value"},
-      {index, rows * top * 4, 4, "index"}, {lse, rows * 4, 4, "lse"}};
-  for (const auto& x : s)
-    if (int rc = check_device(x.p, x.align, x.what)) return rc;
-  for (int i = 1; i < 4; ++i)
-    for (int j = 0; j < i; ++j) {
-      const uintptr_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
-      if (a < b + s[j].bytes && b < a + s[i].bytes) return fail(FLS_EPTR, "%s overlaps %s", s[i].what, s[j].what);
-    }
+  const Span s[4] = {{logits, ((rows - 1) * stride + vocab) * elem, elem, false, "logits"},
+                     {value, rows * top * 4, 4, true, "value"},
+                     {index, rows * top * 4, 4, true, "index"},
+                     {lse, rows * 4, 4, true, "lse"}};
+  if (int rc = check_spans(s, 4)) return rc;
   TopArgs a{logits, stride, uint32_t(vocab), top, float(1.4426950408889634 / temperature), 1.0 / temperature, value, index, lse};
   // Few rows: a row is shared by the CTAs of a cluster while there is an SM for each and a part has at least 64 KB (one row of
   // 128256 bf16, k = 64, in 1, 2, 4, 8 parts: 13.0, 12.4, 11.5, 12.7 us; 20 rows of 32000 fp32: 8.7, 10.1, 10.3, 14.1).
@@ -573,6 +548,6 @@ extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t
                                               : cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<uint16_t, 512>, a))
                                        : (f32 ? cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<float, 256>, a)
                                               : cudaLaunchKernelEx(&cfg, fls_top_logits_kernel<uint16_t, 256>, a));
-  if (e != cudaSuccess) return fail(FLS_ECUDA, "fls_top_logits: %s", cudaGetErrorString(e));
+  if (e != cudaSuccess) return refuse(FLS_ECUDA, "fls_top_logits: %s", cudaGetErrorString(e));
   return FLS_OK;
 }

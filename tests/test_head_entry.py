@@ -1,0 +1,38 @@
+"""What the entry points of the head and of the top logits refuse and launch, seen on a CUDA runtime that only writes it down."""
+import pytest
+
+from tests import fake_cuda
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    return fake_cuda.build(tmp_path_factory.mktemp("fake"))
+
+
+def test_buffers_of_another_device_are_refused(fake):
+    """Each buffer in turn on a device that is not the current one, and on the host; then all where they belong."""
+    got = fake_cuda.run(fake, """
+def top(**kw):
+    at = lambda i, d=1: (d << 44) + (i + 1 << 24)
+    p = dict(logits=at(0), value=at(1), index=at(2), lse=at(3), **{})
+    p.update({k: at(["logits", "value", "index", "lse"].index(k), d) for k, d in kw.items()})
+    return fls.fls_top_logits(p["logits"], fls.FLS_GRAD_BF16, 3, 1000, 0, 5, 1.0, p["value"], p["index"], p["lse"], stream=0)
+
+result = {"top": [], "head": []}
+fake.fake_reset(1)
+for owner in (0, 2, 15):
+    result["top"] += [[code(top, **{k: owner}), fake.fake_launches()] for k in ("logits", "value", "index", "lse")]
+result["top ok"] = [code(top), fake.fake_launches()]
+head = fls.fls_head_create(64, 1000, 64)
+lay = fls.fls_head_query(head)
+fake.fake_reset(1)
+for owner in (0, 15):
+    for name in ("hidden", "weight", "labels", "loss", "lse", "grad_hidden", "grad_weight", "workspace"):
+        io = buffers(64, 1000, 64, lay, device=1)
+        setattr(io, name, getattr(io, name) % (1 << 44) + (owner << 44))
+        result["head"].append([code(fls.fls_head_xent, head, io, stream=0), fake.fake_launches()])
+result["head ok"] = [code(fls.fls_head_xent, head, buffers(64, 1000, 64, lay, device=1), stream=0), fake.fake_launches() > 0]
+result["EPTR"] = fls.FLS_EPTR
+""")
+    assert got["top"] == [[got["EPTR"], 0]] * 12 and got["top ok"] == [0, 1]
+    assert got["head"] == [[got["EPTR"], 0]] * 16 and got["head ok"] == [0, True]
