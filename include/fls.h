@@ -461,7 +461,8 @@ int fls_head_query(const fls_head* head, fls_head_layout* out);
 int fls_head_destroy(fls_head* head);
 
 /* The losses, and the gradients for which a buffer is given, enqueued on cuda_stream; nothing is synchronised or
- * allocated.  A call with rows = 0 writes a zero grad_weight (or leaves it, with accumulate) and nothing else.
+ * allocated.  A call with rows = 0 writes a zero grad_weight (or leaves it, with accumulate), the number of
+ * rows that took part, and nothing else.
  * Calls of one head, and calls with one workspace, must not overlap in time.
  * Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, gradients without desc.grads, smoothing outside
  * [0, 1), a negative or non-finite z_loss, weight or temperature, a stride below d), FLS_EPTR (null, host, another device's or

@@ -218,7 +218,10 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
     c.split_cols = std::max(p.cols, uint32_t(up(c.vocab - p.keep_v0, 256)));
     c.max_splits = uint32_t(std::min<uint64_t>(kHeadMaxSplits, r.dh_bytes / (uint64_t(c.rows_cap) * c.dcap * 4)));
   }
-  if (io->rows == 0 && (!c.want_gw || io->accumulate)) return FLS_OK;
+  if (io->rows == 0 && (!c.want_gw || io->accumulate)) {               // nothing to launch, but no rows took part
+    const cudaError_t e = cudaMemsetAsync(&c.state->count, 0, sizeof c.state->count, s);
+    return e == cudaSuccess ? FLS_OK : cuda_fail(e, "cudaMemsetAsync(rows that take part)");
+  }
 
   const uint16_t* w = static_cast<const uint16_t*>(io->weight);
   uint64_t w_stride = io->weight_stride ? io->weight_stride : d.dim, w_cols = d.dim;

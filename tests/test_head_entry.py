@@ -36,3 +36,37 @@ result["EPTR"] = fls.FLS_EPTR
 """)
     assert got["top"] == [[got["EPTR"], 0]] * 12 and got["top ok"] == [0, 1]
     assert got["head"] == [[got["EPTR"], 0]] * 16 and got["head ok"] == [0, True]
+
+
+def test_a_call_without_rows_counts_none(fake):
+    """The word behind rows_taking_part is cleared or rewritten by every call that has no rows."""
+    got = fake_cuda.run(fake, """
+head = fls.fls_head_create(64, 1000, 64)
+lay = fls.fls_head_query(head)
+result = []
+for grads, accumulate in ((False, 0), (True, 0), (True, 1)):
+    fake.fake_reset(0)
+    io = buffers(0, 1000, 64, lay, grads)
+    io.accumulate = accumulate
+    rc = code(fls.fls_head_xent, head, io, stream=0)
+    count = fls.fls_head_get_state(io.workspace)[1]
+    result.append([rc, fake.fake_launches() > 0, clears() == [[count, 4]]])
+""")
+    assert got == [[0, False, True], [0, True, False], [0, False, True]]
+
+
+@pytest.mark.gpu
+def test_rows_taking_part_after_a_call_without_rows():
+    import torch
+    from paper_2609_20359_b200.head import Head
+    dev, V, d = "cuda:0", 300, 64
+    h = torch.randn(5, d, device=dev).bfloat16()
+    w = torch.randn(V, d, device=dev).bfloat16()
+    y = torch.arange(5, device=dev)
+    gw = torch.zeros_like(w)
+    head = Head(8, V, d)
+    for kw in (dict(), dict(grad_weight=gw), dict(grad_weight=gw, accumulate=True)):
+        head.xent(h, w, y)
+        assert int(head.rows_taking_part()) == 5
+        head.xent_step(h[:0], w, y[:0], **kw)
+        assert int(head.rows_taking_part()) == 0
