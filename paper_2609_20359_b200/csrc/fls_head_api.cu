@@ -200,8 +200,9 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.want_gw = io->grad_weight != nullptr;
   c.planes = c.want_gw && c.grad_f32 ? 2 : 1;
   c.clusters = h->clusters;
-  // hidden rows of one group of row tiles: 32 MB, a quarter of L2, beside the weight tiles that stream past them
-  c.group_m = std::max<uint32_t>(1, uint32_t((32ull << 20) / (uint64_t(kHeadBM) * c.dp * 2)));
+  // hidden rows of one group of row tiles: 32 MB, a quarter of L2, beside the weight tiles that stream past them.  No more
+  // tiles than there are, so that a group's tiles of the vocabulary stay below the 2^31 that fls_head_create allows in all.
+  c.group_m = std::max<uint32_t>(1, std::min(c.rows_cap / uint32_t(kHeadBM), uint32_t((32ull << 20) / (uint64_t(kHeadBM) * c.dp * 2))));
   c.hold_back = h->expire_polls != 0;
   c.wait_limit = h->expire_polls ? h->expire_polls : kWaitLimit;
   h->expire_polls = 0;

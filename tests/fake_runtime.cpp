@@ -11,7 +11,7 @@
 
 namespace {
 struct Launch { uint64_t grid[3], block[3]; };
-Launch launches[64];
+Launch launches[1024];
 int n_launches = 0, n_clears = 0, device = 0;
 uint64_t cleared[64][2];
 fls::HeadCall first_call;
@@ -54,6 +54,7 @@ cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t* c, const void*, void**
   const dim3 g = c->gridDim, b = c->blockDim;
   if (!g.x || !g.y || !g.z || g.x > 0x7FFFFFFFu || g.y > 65535 || g.z > 65535 || b.x * b.y * b.z > 1024) return cudaErrorInvalidConfiguration;
   if (n_launches == 0 && args && b.x <= 256 && c->numAttrs == 0) std::memcpy(&first_call, args[0], sizeof first_call);
+  if (n_launches == 1024) return cudaErrorUnknown;
   launches[n_launches++] = {{g.x, g.y, g.z}, {b.x, b.y, b.z}};
   return cudaSuccess;
 }

@@ -70,3 +70,17 @@ def test_rows_taking_part_after_a_call_without_rows():
         assert int(head.rows_taking_part()) == 5
         head.xent_step(h[:0], w, y[:0], **kw)
         assert int(head.rows_taking_part()) == 0
+
+
+@pytest.mark.parametrize("rows,vocab,dim", [(300, 1 << 27, 8), (1 << 24, 1 << 23, 8), (256, 1 << 30, 16), (8192, 128256, 2048), (1, 1, 65536)])
+def test_groups_of_row_tiles_fit_32_bits(fake, rows, vocab, dim):
+    """The statistics' schedule counts tiles of a group in 32 bits: row tiles of the group times column tiles."""
+    got = fake_cuda.run(fake, f"""
+head = fls.fls_head_create({rows}, {vocab}, {dim}, grads=False)
+io = buffers({rows}, {vocab}, {dim}, fls.fls_head_query(head), False)
+fake.fake_reset(0)
+result = [code(fls.fls_head_xent, head, io, stream=0), fake.fake_group_m()]
+""")
+    assert got[0] == 0
+    assert 1 <= got[1] and got[1] * -(-vocab // 256) < 1 << 32
+    assert got[1] == max(1, min(-(-rows // 256), (32 << 20) // (256 * dim * 2)))
