@@ -1222,8 +1222,9 @@ __global__ void __launch_bounds__(256) fls_head_rescale_kernel(const __grid_cons
   pdl_launch();
   pdl_wait();
   const uint32_t count = c.state->count, live = (count + kHeadBK - 1) / kHeadBK * kHeadBK;
-  const uint32_t panel = blockIdx.x, row0 = blockIdx.y * kRescaleRows + threadIdx.x / 8, sub = threadIdx.x % 8;
-  if (blockIdx.y * kRescaleRows >= count) return;                      // live rows end in the same block
+  const uint32_t panels = (c.vocab - c.keep_v0 + 63) / 64, panel = blockIdx.x % panels, first = blockIdx.x / panels * kRescaleRows;
+  const uint32_t row0 = first + threadIdx.x / 8, sub = threadIdx.x % 8;
+  if (first >= count) return;                                          // live rows end in the same block
   const uint32_t n = c.keep_v0 + panel * 64 + sub * 8;
   const uint64_t pitch = uint64_t(c.rows_cap) * 32;                    // floats per panel of 32 columns
   float* base = c.keep_z + 2 * uint64_t(panel) * pitch;
@@ -1414,7 +1415,7 @@ cudaError_t launch_head_own(const HeadCall& c, cudaStream_t s) {
   return launch(fls_head_own_kernel, dim3(uint32_t((std::max<uint64_t>(c.rows, 1) * c.slots + 127) / 128)), 128, 0, false, s, c);
 }
 cudaError_t launch_head_rescale(const HeadCall& c, cudaStream_t s) {
-  const dim3 grid((c.vocab - c.keep_v0 + 63) / 64, (c.rows_cap + kRescaleRows - 1) / kRescaleRows);
+  const dim3 grid((c.vocab - c.keep_v0 + 63) / 64 * (c.rows_cap / kRescaleRows));      // either factor may exceed 65535
   if (c.planes == 2)
     return c.two ? launch(fls_head_rescale_kernel<true, true>, grid, 256, 0, false, s, c) : launch(fls_head_rescale_kernel<false, true>, grid, 256, 0, false, s, c);
   return c.two ? launch(fls_head_rescale_kernel<true, false>, grid, 256, 0, false, s, c) : launch(fls_head_rescale_kernel<false, false>, grid, 256, 0, false, s, c);

@@ -84,3 +84,23 @@ result = [code(fls.fls_head_xent, head, io, stream=0), fake.fake_group_m()]
     assert got[0] == 0
     assert 1 <= got[1] and got[1] * -(-vocab // 256) < 1 << 32
     assert got[1] == max(1, min(-(-rows // 256), (32 << 20) // (256 * dim * 2)))
+
+
+@pytest.mark.parametrize("rows,vocab,dim,top,f32,any_weight,piece", [
+    (1 << 24, 1000, 896, 0, 0, 0, 0), (1 << 24, 1000, 896, 128, 1, 0, 0), (8388480, 300, 1024, 0, 0, 0, 0),
+    (8388481, 300, 1024, 0, 0, 0, 0), (1, 1 << 30, 8, 0, 0, 1, 1 << 36), (256, 1 << 28, 1024, 0, 0, 0, 1 << 40),
+    (1, 2, 65536, 1, 1, 1, 0)])
+def test_launches_fit_the_device_at_the_largest_sizes(fake, rows, vocab, dim, top, f32, any_weight, piece):
+    """What fls_head_create accepts is launched: no grid beyond 65535 along y, none beyond 2^31 - 1 along x."""
+    got = fake_cuda.run(fake, f"""
+head = fls.fls_head_create({rows}, {vocab}, {dim}, {top}, True, {f32}, bool({any_weight}), {piece})
+io = buffers({rows}, {vocab}, {dim}, fls.fls_head_query(head), True, {f32})
+fake.fake_reset(0)
+result = [code(fls.fls_head_xent, head, io, stream=0)]
+if {top}:
+    fake.fake_reset(0)
+    t = fls.fls_distill_desc(1 << 43, (1 << 43) + (1 << 41), (1 << 43) + (1 << 42), fls.FLS_TAIL_CLASS, 0, 2.0, 0.5, 0.5)
+    result.append(code(fls.fls_head_distill, head, io, t, stream=0))
+result.append(fake.fake_launches())
+""")
+    assert not any(got[:-1]) and got[-1] >= 5
