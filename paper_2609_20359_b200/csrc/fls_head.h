@@ -56,7 +56,8 @@ struct HeadCall {
   uint64_t rows; uint32_t rows_cap;
   uint32_t vocab, dim, dp, dcap;
   uint32_t top, slots, tiles;
-  uint32_t piece_cols, planes;
+  uint32_t piece_cols;
+  uint32_t terms, planes;    // bf16 terms of dL/dz that a weight gradient of this head takes; those that this call stores
   uint32_t tail_class, use_label, two, smooth, grad_f32, accumulate;
   uint32_t want_gh, want_gw;
   uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, bf16 accumulation): plain stores

@@ -29,6 +29,9 @@ constexpr uint64_t kPartialBytes = 256ull << 20;     // room for the split sums 
 // 74 / 75, 256 80 / 78).
 bool keeps_logits(uint64_t rows, uint64_t dim) { return dim >= 896 || 3 * rows <= 2 * dim; }
 
+// bf16 terms of dL/dz that the weight's gradient takes.
+uint64_t terms_of(const fls_head_desc& d) { return d.grad_dtype == FLS_GRAD_F32 ? 2 : 1; }
+
 // Byte offsets of the workspace.  Sizes are those of max_rows; a smaller call uses the front of each region.
 struct Regions {
   uint64_t mask, counts, pos, src, hp, slot_idx, slot_start, slot_t, slot_z, slot_g, label_z, part, coef, g, dh, wcopy, total;
@@ -38,7 +41,7 @@ struct Regions {
 Regions regions(const fls_head_desc& d) {
   const uint64_t cap = up(std::max<uint64_t>(d.max_rows, 1), kHeadBM), dp = up(d.dim, 8), dcap = up(d.dim, kHeadBN);
   const uint64_t slots = uint64_t(d.top) + 1, tiles = up(d.vocab, kHeadBN) / kHeadStatCols;
-  const uint64_t planes = d.grad_dtype == FLS_GRAD_F32 ? 2 : 1;
+  const uint64_t planes = terms_of(d);
   Regions r{};
   uint64_t at = 256;
   auto take = [&](uint64_t bytes) { const uint64_t o = at; at += up(bytes, 256); return o; };
@@ -198,7 +201,8 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.accumulate = io->accumulate;
   c.want_gh = io->grad_hidden != nullptr && io->rows > 0;
   c.want_gw = io->grad_weight != nullptr;
-  c.planes = c.want_gw && c.grad_f32 ? 2 : 1;
+  c.terms = uint32_t(terms_of(d));
+  c.planes = c.want_gw ? c.terms : 1;
   c.clusters = h->clusters;
   // hidden rows of one group of row tiles: 32 MB, a quarter of L2, beside the weight tiles that stream past them.  No more
   // tiles than there are, so that a group's tiles of the vocabulary stay below the 2^31 that fls_head_create allows in all.
@@ -213,7 +217,7 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.direct_store = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 || c.grad_weight_stride * (c.grad_f32 ? 4 : 2) % 16 ||
                    (c.accumulate && !c.grad_f32);
   if (grads) {
-    const Pieces p = pieces_of(d, r.g_bytes, c.rows, c.planes);
+    const Pieces p = pieces_of(d, r.g_bytes, c.rows, terms_of(d));
     c.keep_v0 = p.keep_v0;
     c.piece_cols = p.cols;
     c.split_cols = std::max(p.cols, uint32_t(up(c.vocab - p.keep_v0, 256)));
@@ -353,7 +357,7 @@ int fls_head_query(const fls_head* head, fls_head_layout* out) {
   out->workspace_bytes = head->reg.total;
   out->piece_cols = out->pieces = out->kept_cols = 0;
   if (d.grads) {
-    const Pieces p = pieces_of(d, head->reg.g_bytes, d.max_rows, d.grad_dtype == FLS_GRAD_F32 ? 2 : 1);
+    const Pieces p = pieces_of(d, head->reg.g_bytes, d.max_rows, terms_of(d));
     out->piece_cols = p.cols;
     out->pieces = p.cols ? (p.keep_v0 + p.cols - 1) / p.cols : 0;
     out->kept_cols = d.vocab - p.keep_v0;

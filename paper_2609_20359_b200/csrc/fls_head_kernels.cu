@@ -1016,11 +1016,11 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
   pdl_launch();
   pdl_wait();
   const uint32_t count = c.state->count, p0 = blockIdx.x * kRowsPerBlock;
-  // How the gradient launches split their depth: good with and without the weight gradient, so that one gradient alone has
-  // the same bits as both together.
+  // How the gradient launches split their depth: good with and without the weight gradient, and from nothing that depends on
+  // which of the two is asked for (as are the pieces), so that one gradient alone has the same bits as both together.
   if (blockIdx.x == 0 && y == 7 && c.split_cols) {
     const uint32_t nt = (c.dim + kHeadBN - 1) / kHeadBN, th = (count + kHeadBM - 1) / kHeadBM * nt, kb_h = c.split_cols / kHeadBK;
-    const uint32_t tw = c.split_cols / kHeadBM * nt, kb_w = (count + kHeadBK - 1) / kHeadBK * c.planes;
+    const uint32_t tw = c.split_cols / kHeadBM * nt, kb_w = (count + kHeadBK - 1) / kHeadBK * c.terms;
     uint32_t best = 0xFFFFFFFFu;
     for (uint32_t s = lane + 1; s <= min(c.max_splits, kb_h); s += 32)
       best = min(best, min(head_makespan(s, th, kb_h, tw, kb_w, c.clusters) + head_makespan(s, th, kb_h, 0, 0, c.clusters), 0x3FFFFFFu) << 6 | (s - 1));
