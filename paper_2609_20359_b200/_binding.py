@@ -412,9 +412,6 @@ def fls_last_error() -> str:
     return lib.fls_last_error().decode()
 
 
-__all__ = [n for n in dir() if n.startswith(("fls_", "FLS_"))] + ["FlsError", "lib", "LIB_PATH", "EXPORTS"]
-
-
 # ---------------------------------------------------------------------------------------------- language-model head
 def fls_head_create(max_rows: int, vocab: int, dim: int, top: int = 0, grads: bool = True, grad_dtype: int = FLS_GRAD_BF16,
                     any_weight: bool = False, piece_bytes: int = 0) -> int:
@@ -465,3 +462,6 @@ def fls_top_logits(logits, logit_dtype: int, rows: int, vocab: int, stride: int,
                    stream=None) -> None:
     _check(lib.fls_top_logits(_ptr(logits), logit_dtype, rows, vocab, stride, top, temperature, _ptr(value), _ptr(index), _ptr(lse),
                               _stream_handle(stream)))
+
+
+__all__ = [n for n in dir() if n.startswith(("fls_", "FLS_"))] + ["FlsError", "lib", "LIB_PATH", "EXPORTS"]

@@ -38,6 +38,15 @@ result["EPTR"] = fls.FLS_EPTR
     assert got["head"] == [[got["EPTR"], 0]] * 16 and got["head ok"] == [0, True]
 
 
+def test_star_import_has_every_entry_point():
+    """`from ..._binding import *` gives all that the library exports and the structures its calls take."""
+    from paper_2609_20359_b200 import _binding as b
+    names = {}
+    exec("from paper_2609_20359_b200._binding import *", names)
+    assert [n for n in b.EXPORTS if n not in names] == []
+    assert all(n in names for n in ("fls_head_desc", "fls_head_io", "fls_distill_desc", "FLS_TAIL_CLASS", "FLS_HEAD_MAX_TOP"))
+
+
 def test_a_call_without_rows_counts_none(fake):
     """The word behind rows_taking_part is cleared or rewritten by every call that has no rows."""
     got = fake_cuda.run(fake, """
