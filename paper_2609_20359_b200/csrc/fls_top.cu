@@ -39,6 +39,7 @@ struct TopArgs {
   uint64_t stride;
   uint32_t vocab, top;
   float c;                 // log2(e) / T
+  float huge;              // logits from here on are not multiplied by c before the maximum is taken off
   double inv_temp;
   float* value;
   int32_t* index;
@@ -162,19 +163,19 @@ struct Part {
   uint32_t trail0;         // index in the row of the first trailing element
 };
 
-// (a - b) / T in powers of two.  Sums are kept relative to 2^(m c), rounded, wherever that is finite; beyond kHuge (masks
-// of the type's lowest value) the difference is taken first.
-constexpr float kHuge = 1e37f;
-__device__ __forceinline__ float log2_ratio(float a, float b, float c) {
-  if (fabsf(a) < kHuge && fabsf(b) < kHuge) return __fmul_rn(a, c) - __fmul_rn(b, c);
-  return (a - b) * c;
+// (x - y) / T in powers of two.  Sums are kept relative to 2^(m c), m c rounded, while that is off by less than 2^-8 (the log
+// sum exp by less than its own last digit); from |m c| = 2^16 on (masks; logits far beyond a model's) the difference is taken
+// first, since 2 to the power of a rounding error of m c soon has nothing to do with 1, and m c may have no fp32.
+__device__ __forceinline__ float log2_ratio(float x, float y, const TopArgs& a) {
+  if (fabsf(x) < a.huge && fabsf(y) < a.huge) return __fmul_rn(x, a.c) - __fmul_rn(y, a.c);
+  return (x - y) * a.c;
 }
 
 // Adds one value to a running maximum and sum of exponentials.
-__device__ __forceinline__ void add_one(float x, float c, float& m, float& s) {
+__device__ __forceinline__ void add_one(float x, const TopArgs& a, float& m, float& s) {
   const float n = max_nan(m, x);
   if (n == -INFINITY) return;
-  s = (m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, n, c))) + (x == -INFINITY ? 0.f : ex2(log2_ratio(x, n, c)));
+  s = (m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, n, a))) + (x == -INFINITY ? 0.f : ex2(log2_ratio(x, n, a)));
   m = n;
 }
 
@@ -307,11 +308,11 @@ __global__ void __launch_bounds__(kTopThreads, kTopThreads == 512 ? 2 : 5) fls_t
     for (int j = 1; j < n_vec; ++j) t = max_nan(t, Vec<T>::top(r[j]));
     seen = max_nan(seen, t);
     if (t > m || t != t) {                            // larger, or NaN, which stays
-      s = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, t, a.c));
+      s = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, t, a));
       m = t;
     }
     if (m == -INFINITY) return;
-    if (!(fabsf(m) < kHuge)) {
+    if (!(fabsf(m) < a.huge)) {
 #pragma unroll
       for (int j = 0; j < n_vec; ++j) {
         float x[VN];
@@ -376,8 +377,8 @@ __global__ void __launch_bounds__(kTopThreads, kTopThreads == 512 ? 2 : 5) fls_t
   }
   sh.stretch[stretches][threadIdx.x] = seen;          // what is left: fewer than 4 vectors per thread
   const uint32_t key = order_key(m);                  // of the vectors only: the single elements are looked at below
-  if (threadIdx.x < p.lead) add_one(Vec<T>::load(p.row + threadIdx.x), a.c, m, s);
-  if (threadIdx.x < p.trail) add_one(Vec<T>::load(p.row + p.trail0 + threadIdx.x), a.c, m, s);
+  if (threadIdx.x < p.lead) add_one(Vec<T>::load(p.row + threadIdx.x), a, m, s);
+  if (threadIdx.x < p.trail) add_one(Vec<T>::load(p.row + p.trail0 + threadIdx.x), a, m, s);
   if (threadIdx.x == 0) sh.n_hot = sh.n_cand = 0;
 
   // the block's maximum and sum
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kTopThreads, kTopThreads == 512 ? 2 : 5) fls_t
   bm = sh.wm[lane % kTopWarps];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) bm = max_nan(bm, __shfl_xor_sync(0xFFFFFFFFu, bm, o));
-  float bs = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, bm, a.c));
+  float bs = m == -INFINITY ? 0.f : s * ex2(log2_ratio(m, bm, a));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) bs += __shfl_xor_sync(0xFFFFFFFFu, bs, o);
   if (lane == 0) sh.ws[warp] = bs;
@@ -481,7 +482,7 @@ __global__ void __launch_bounds__(kTopThreads, kTopThreads == 512 ? 2 : 5) fls_t
       double ss = 0.0;
       for (uint32_t w = 0; w < parts; ++w) {
         const float pm = remote_f32(remote(&sh.m, w));
-        if (pm != -INFINITY) ss += double(remote_f32(remote(&sh.s, w))) * double(exp2f(log2_ratio(pm, mm, a.c)));
+        if (pm != -INFINITY) ss += double(remote_f32(remote(&sh.s, w))) * double(exp2f(log2_ratio(pm, mm, a)));
       }
       put_lse(mm, ss);
     }
@@ -524,7 +525,8 @@ extern "C" int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t
                      {index, rows * top * 4, 4, true, "index"},
                      {lse, rows * 4, 4, true, "lse"}};
   if (int rc = check_spans(s, 4)) return rc;
-  TopArgs a{logits, stride, uint32_t(vocab), top, float(1.4426950408889634 / temperature), 1.0 / temperature, value, index, lse};
+  const float c = float(std::min(1.4426950408889634 / temperature, 3e38));
+  TopArgs a{logits, stride, uint32_t(vocab), top, c, 65536.f / c, 1.0 / temperature, value, index, lse};
   // Few rows: a row is shared by the CTAs of a cluster while there is an SM for each and a part has at least 64 KB (one row of
   // 128256 bf16, k = 64, in 1, 2, 4, 8 parts: 13.0, 12.4, 11.5, 12.7 us; 20 rows of 32000 fp32: 8.7, 10.1, 10.3, 14.1).
   uint32_t parts = 1;
