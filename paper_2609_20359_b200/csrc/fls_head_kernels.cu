@@ -437,6 +437,7 @@ struct Stager {
 template <bool TWO, bool PLANES, int BUFS>
 struct DlogitsRow : Columns {
   float4 k;          // {lse_T log2(e), aT, lse_1 log2(e), a1}; without TWO {lse log2(e) , a, b, -}
+  bool live;         // one of the rows that take part; those after them are zero, whatever the weight holds
   const float* val;
   // the first (half 0) or second 32 of the 64 columns from col0 on; lo: buffer of the second term (PLANES)
   __device__ __forceinline__ void chunk(float (&v)[32], int32_t col0, uint32_t half, uint32_t vocab, float cT, float c1,
@@ -454,10 +455,10 @@ struct DlogitsRow : Columns {
         split(fma2(a2, make_f2(ex2(x), ex2(y)), b2), v[j], v[j + 1]);
       }
     }
-    if (uint32_t(c0) + 32 > vocab) {
+    if (!live || uint32_t(c0) + 32 > vocab) {
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (uint32_t(c0 + j) >= vocab) v[j] = 0.f;
+        if (!live || uint32_t(c0 + j) >= vocab) v[j] = 0.f;
     }
     out.put_bf16(hi, half, v);
     if constexpr (PLANES) {
@@ -700,7 +701,8 @@ fls_head_gemm_kernel(const __grid_constant__ HeadMaps maps, const __grid_constan
       } else if constexpr (MODE == kDlogits) {
         dl.val = c.slot_g + uint64_t(row) * c.slots;
         dl.k = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (row < count) {
+        dl.live = row < count;
+        if (dl.live) {
           dl.k = c.coef[row];
           dl.open(c.slot_idx + uint64_t(row) * c.slots, c.slots, first_slot(c, row, piece.v0 + n0));
         }
