@@ -168,8 +168,25 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// sum over 32 values of 2^(z c - b)
-__device__ __forceinline__ float sum_ex2(const float (&z)[32], float c, float b) {
+// Sums of exponentials are kept relative to 2^(m c), m c rounded (one instruction less per value), while that is off by less
+// than 2^-8, the log sum exp by less than its own last digit.  From |m c| = 2^16 on (columns masked through the weight with
+// -1e10 or the type's lowest value, in a stretch of nothing else) the difference to m is taken first: a rounding error of m c
+// is soon a power of two beyond fp32.
+constexpr float kFar = 65536.f;
+// (x - y) / T in powers of two, c = log2(e) / T
+__device__ __forceinline__ float log2_ratio(float x, float y, float c) {
+  const float a = __fmul_rn(x, c), b = __fmul_rn(y, c);
+  return fabsf(a) < kFar && fabsf(b) < kFar ? a - b : (x - y) * c;
+}
+// sum over 32 values of 2^((z - m) c)
+__device__ __forceinline__ float sum_ex2(const float (&z)[32], float c, float m) {
+  const float b = __fmul_rn(m, c);
+  if (!(fabsf(b) < kFar)) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) t += ex2((z[j] - m) * c);
+    return t;
+  }
   const f2 c2 = make_f2(c, c), b2 = make_f2(-b, -b);
   f2 t0 = make_f2(0.f, 0.f), t1 = t0;
 #pragma unroll
@@ -355,13 +372,13 @@ struct StatsRow : Columns {
       const float old = m;
       m = cm;
       if (old != -INFINITY) {
-        s *= ex2(__fmul_rn(old, cT) - __fmul_rn(m, cT));
-        if constexpr (TWO) s1 *= ex2(__fmul_rn(old, c1) - __fmul_rn(m, c1));
+        s *= ex2(log2_ratio(old, m, cT));
+        if constexpr (TWO) s1 *= ex2(log2_ratio(old, m, c1));
       }
     }
-    const float bT = m == -INFINITY ? 0.f : __fmul_rn(m, cT);
-    s += sum_ex2(z, cT, bT);
-    if constexpr (TWO) s1 += sum_ex2(z, c1, m == -INFINITY ? 0.f : __fmul_rn(m, c1));
+    const float base = m == -INFINITY ? 0.f : m;
+    s += sum_ex2(z, cT, base);
+    if constexpr (TWO) s1 += sum_ex2(z, c1, base);
   }
 };
 
@@ -1055,13 +1072,13 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
 #pragma unroll
       for (int j = 0; j < B; ++j) nm = fmaxf(nm, tm[j]);
       const float base = nm == -INFINITY ? 0.f : nm;
-      s *= exp2f(__fmul_rn(m, c.cT) - __fmul_rn(base, c.cT));          // an empty side has factor 2^-inf = 0
-      if (c.two) s1 *= exp2f(__fmul_rn(m, c.c1) - __fmul_rn(base, c.c1));
+      s *= exp2f(log2_ratio(m, base, c.cT));          // an empty side has factor 2^-inf = 0
+      if (c.two) s1 *= exp2f(log2_ratio(m, base, c.c1));
 #pragma unroll
       for (int j = 0; j < B; ++j) {
         // columns all left out: m = -inf and s = 0; NaN goes through
-        s += ts[j] * (tm[j] == -INFINITY ? 1.f : exp2f(__fmul_rn(tm[j], c.cT) - __fmul_rn(base, c.cT)));
-        if (c.two) s1 += t1[j] * (tm[j] == -INFINITY ? 1.f : exp2f(__fmul_rn(tm[j], c.c1) - __fmul_rn(base, c.c1)));
+        s += ts[j] * (tm[j] == -INFINITY ? 1.f : exp2f(log2_ratio(tm[j], base, c.cT)));
+        if (c.two) s1 += t1[j] * (tm[j] == -INFINITY ? 1.f : exp2f(log2_ratio(tm[j], base, c.c1)));
       }
       m = nm;
     }
@@ -1090,8 +1107,8 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     for (int o = 16; o > 0; o >>= 1) mf = fmaxf(mf, __shfl_xor_sync(0xFFFFFFFFu, mf, o));
     const float base = mf == -INFINITY ? 0.f : mf, lm = sh_m[lane][y];
     const double M = double(base);
-    const double denseT = warp_sum(double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(lm, c.cT) - __fmul_rn(base, c.cT)))));
-    const double dense1 = !c.two ? denseT : warp_sum(double(sh_s1[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(lm, c.c1) - __fmul_rn(base, c.c1)))));
+    const double denseT = warp_sum(double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(log2_ratio(lm, base, c.cT)))));
+    const double dense1 = !c.two ? denseT : warp_sum(double(sh_s1[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(log2_ratio(lm, base, c.c1)))));
     const double zsum = c.smooth ? warp_sum(double(sh_z[lane][y])) : 0.0;
     const bool labelled = c.use_label && label != c.ignore_label;
 
@@ -1148,7 +1165,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xFFFFFFFFu, tm, o));
       if (tm == -INFINITY) tm = 0.f;
       tail_m = double(tm);
-      tail = double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(__fmul_rn(lm, c.cT) - __fmul_rn(tm, c.cT))));
+      tail = double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(log2_ratio(lm, tm, c.cT))));
       if (out_z != -INFINITY) tail += exp((double(out_z) - tail_m) * c.inv_temp);
       tail = warp_sum(tail);
     }
@@ -1156,7 +1173,15 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     // label dominates and lse - z would cancel, and of the tail's sum (at least 1, or 0 where nothing is outside the list).
     const double part = log1p(lane == 0 ? totT - 1.0 : lane == 1 ? tot1 - 1.0 : lane == 2 ? rest1 / e1_label : tail - 1.0);
     const double log_T = __shfl_sync(0xFFFFFFFFu, part, 0), log_1 = __shfl_sync(0xFFFFFFFFu, part, 1), log_p = __shfl_sync(0xFFFFFFFFu, part, 2);
-    const double lse_tail = tail_m * c.inv_temp + __shfl_sync(0xFFFFFFFFu, part, 3);
+    const double log_tail = __shfl_sync(0xFFFFFFFFu, part, 3), lse_tail = tail_m * c.inv_temp + log_tail;
+    // A log sum exp of m / T + l, where its exponentials' exponents z cc - (.) are formed.  Far from zero it is rounded up, from
+    // the fp32 factor that z gets: no rounding makes a probability exceed 1.
+    auto exponent = [](double m, float cc, double t, double l) {
+      constexpr double kLog2e = 1.4426950408889634;
+      const double e = (m * t + l) * kLog2e;
+      return fabs(e) < double(kFar) ? float(e) : __double2float_ru(m * double(cc) + l * kLog2e);
+    };
+    const float exp_T = exponent(M, c.cT, c.inv_temp, log_T);
     const double lseT = M * c.inv_temp + log_T, lse1 = c.two ? M + log_1 : lseT;
     const double nll = !labelled ? 0.0 : (rest1 < e1_label ? log_p : (c.two ? lse1 - z_label : lseT - z_label * c.inv_temp));
 
@@ -1167,7 +1192,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
         if (c.smooth) loss += eps * (lseT - zsum / double(c.vocab));
         c.loss[n] = float(loss);
         c.lse[n] = float(lseT);
-        c.coef[p] = make_float4(float(lseT * 1.4426950408889634), float(w * (1.0 + zl)), float(w * eps / double(c.vocab)), 0.f);
+        c.coef[p] = make_float4(exp_T, float(w * (1.0 + zl)), float(w * eps / double(c.vocab)), 0.f);
         gs[0] = float(w * (-ql + zl * pl + eps - eps / double(c.vocab)));
       }
     } else {
@@ -1181,12 +1206,14 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       // Outside the list dL/dz = a p (1 - q'/p') = a r (p' - q'), r = p / p' = exp(z/T - lse_tail): neither factor exceeds 1
       // however small p' is, where q'/p' would overflow and p vanish (in fp32 from 87 T between the list and the rest on).
       const bool split_tail = class_t && lse_tail != -INFINITY;
+      float exp_out = exp_T;
       double lse_out = lseT, p_out = 1.0, d_out = 1.0;      // p = p_out exp(z/T - lse_out), its distillation factor d_out for p_out
       if (class_t) {
         const double qt = qsum > 1.0 ? 0.0 : 1.0 - qsum;
         if (qt > (split_tail ? 0.0 : 1e-6)) kl += qt * (log(qt) - (lse_tail - lseT));   // without a tail what is left of 1 is rounding
         if (split_tail) {
           lse_out = lse_tail;
+          exp_out = exponent(tail_m, c.cT, c.inv_temp, log_tail);
           p_out = exp(lse_tail - lseT);
           d_out = p_out - qt;
         }
@@ -1195,8 +1222,8 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       if (lane == 0) {
         c.loss[n] = float((taught ? c.distill_weight * c.temp * c.temp * kl : 0.0) + (labelled ? c.label_weight * nll : 0.0));
         c.lse[n] = float(lseT);
-        if (c.two) c.coef[p] = make_float4(float(lse_out * 1.4426950408889634), float(a * d_out), float(lse1 * 1.4426950408889634), float(b));
-        else c.coef[p] = make_float4(float(lse_out * 1.4426950408889634), float(a * d_out + b * p_out), 0.f, 0.f);
+        if (c.two) c.coef[p] = make_float4(exp_out, float(a * d_out), exponent(M, c.c1, 1.0, log_1), float(b));
+        else c.coef[p] = make_float4(exp_out, float(a * d_out + b * p_out), 0.f, 0.f);
       }
       for (uint32_t i = lane; i < c.slots; i += 32) {
         const int32_t x = sh_i[y][i];

@@ -1,4 +1,4 @@
-"""The head where logits are far from zero: columns masked through the weight."""
+"""The head where logits are far from zero: columns masked through the weight, and rows whose logits are all large."""
 import math
 
 import pytest
@@ -28,7 +28,7 @@ def masked(n, V, d, level, first, seed=0):
     return h.bfloat16(), w.bfloat16(), y, g
 
 
-LEVELS = [-1e4, -1e6, -math.inf]
+LEVELS = [-1e4, -1e6, -1e10, -1e30, float(torch.finfo(torch.bfloat16).min), -math.inf]
 
 
 # n and d: logits kept, and formed twice; one row tile that ends among the rows, two terms of dL/dz
@@ -72,3 +72,26 @@ def test_distillation_with_masked_columns(n, d, tail, T, wl, level):
     # p' - q' of the tail: both are below 1 and p' is known to e_p
     R.check_grads(ref, None, gw[:first], small=ref["e_p"] * T * float(h.float().abs().max()) if tail else 0.0)
     assert bool((gw[first:] == 0).all())
+
+
+@pytest.mark.parametrize("level", [1e5, -1e5, 1e9, -1e9, 1e12, -1e12, 1e30, -1e30])
+@pytest.mark.parametrize("n,d", [(40, 128), (300, 64)])
+def test_rows_far_from_zero(n, d, level):
+    """Every logit at one large magnitude.  They are equal there to fp32's last digit, so the loss is known to that only; it
+    and all gradients are finite, and dL/dz stays within what probabilities allow."""
+    from paper_2609_20359_b200.head import Head
+    V = 700
+    h, w, y, _ = masked(n, V, d, 0.0, V)
+    w[:, 0] = level
+    gh = torch.full((n, d), math.nan, dtype=torch.bfloat16, device=DEV)
+    gw = torch.full((V, d), math.nan, dtype=torch.bfloat16, device=DEV)
+    loss, lse = Head(n, V, d).xent_step(h, w, y, gh, gw, row_weight=torch.ones(n, device=DEV))
+    live = y >= 0
+    z = h.double() @ w.double().t()
+    ulp = 2.0 ** -20 * z.abs().max()
+    want = torch.where(live, torch.logsumexp(z, 1), 0.0)
+    assert bool(((lse.double() - want).abs() <= ulp).all())
+    assert bool(((loss.double() - torch.where(live, want - z.gather(1, y.clamp_min(0)[:, None])[:, 0], 0.0)).abs() <= ulp).all())
+    # |dL/dz| <= 1 in every element, bf16 sums
+    assert bool((gw.float().abs() <= 1.01 * h.float().abs().sum(0)).all())
+    assert bool((gh.float().abs() <= 1.01 * V * w.float().abs().max()).all())
