@@ -173,11 +173,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // -1e10 or the type's lowest value, in a stretch of nothing else) the difference to m is taken first: a rounding error of m c
 // is soon a power of two beyond fp32.
 constexpr float kFar = 65536.f;
-// (x - y) / T in powers of two, c = log2(e) / T
-__device__ __forceinline__ float log2_ratio(float x, float y, float c) {
-  const float a = __fmul_rn(x, c), b = __fmul_rn(y, c);
-  return fabsf(a) < kFar && fabsf(b) < kFar ? a - b : (x - y) * c;
-}
+// (x - m) / T in powers of two, c = log2(e) / T
+struct Log2Ratio {
+  float c, off, b;
+  __device__ __forceinline__ Log2Ratio(float m, float cc) : c(cc) {
+    b = __fmul_rn(m, c);
+    const bool far = !(fabsf(b) < kFar);
+    off = far ? m : 0.f;
+    if (far) b = 0.f;
+  }
+  __device__ __forceinline__ float operator()(float x) const { return __fmul_rn(x - off, c) - b; }
+};
 // sum over 32 values of 2^((z - m) c)
 __device__ __forceinline__ float sum_ex2(const float (&z)[32], float c, float m) {
   const float b = __fmul_rn(m, c);
@@ -372,8 +378,8 @@ struct StatsRow : Columns {
       const float old = m;
       m = cm;
       if (old != -INFINITY) {
-        s *= ex2(log2_ratio(old, m, cT));
-        if constexpr (TWO) s1 *= ex2(log2_ratio(old, m, c1));
+        s *= ex2(Log2Ratio(m, cT)(old));
+        if constexpr (TWO) s1 *= ex2(Log2Ratio(m, c1)(old));
       }
     }
     const float base = m == -INFINITY ? 0.f : m;
@@ -1025,12 +1031,22 @@ __device__ __forceinline__ double warp_max(double x) {
 // Eight packed rows per block.  First the partial sums of each row are joined: a warp reads four columns' worth of eight
 // neighbouring rows, whole 32-byte sectors.  Then a warp takes a row: its own columns are added to the sums and give loss
 // and gradient.  Sums over the row and logarithms are double: a few hundred operations beside 2 V d of the products.
+// TEACHER: distillation.  Cross entropy has one own column per row and gets code without the teacher's: a call of one row
+// waits for it to come from memory (1 x 50257 x 768: 27.1 us a call with it, 25.4 without).
+// Blocks start where the products' kernel ends first, and as many as fit there: few of them would share a few SMs while the
+// others idle.  kRowsSpread bytes of shared memory that nothing uses keep it at two per SM where all fit that way (step of
+// 128 x 50257 x 768 with five, three, two per SM: 90.6, 87.0, 85.0 us).
+constexpr uint32_t kRowsSpread = 85 * 1024;
 constexpr uint32_t kRowsPerBlock = 8;
+template <bool TEACHER>
 __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constant__ HeadCall c) {
   __shared__ float sh_m[32][kRowsPerBlock], sh_s[32][kRowsPerBlock], sh_s1[32][kRowsPerBlock], sh_z[32][kRowsPerBlock];
-  __shared__ double sh_q[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
-  __shared__ int32_t sh_i[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
-  __shared__ float sh_t[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1], sh_zs[kRowsPerBlock][FLS_HEAD_MAX_TOP + 1];
+  constexpr int kSlots = TEACHER ? FLS_HEAD_MAX_TOP + 1 : 1;
+  __shared__ double sh_q[kRowsPerBlock][kSlots];
+  __shared__ int32_t sh_i[kRowsPerBlock][kSlots];
+  __shared__ float sh_t[kRowsPerBlock][kSlots], sh_zs[kRowsPerBlock][kSlots];
+  const uint32_t slots = TEACHER ? c.slots : 1;
+  const bool two = TEACHER && c.two, smooth = !TEACHER && c.smooth;
   const uint32_t lane = threadIdx.x & 31, y = threadIdx.x >> 5;
   pdl_launch();
   pdl_wait();
@@ -1049,10 +1065,10 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
   if (p0 >= count) return;
   const uint32_t p = min(p0 + y, count - 1);
   const uint64_t n = uint64_t(c.src[p]);               // used after the sums
-  const int32_t* idx = c.slot_idx + uint64_t(p) * c.slots;
-  const float* zs = c.slot_z + uint64_t(p) * c.slots;
-  const float* ts = c.slot_t + uint64_t(p) * c.slots;
-  float* gs = c.slot_g + uint64_t(p) * c.slots;
+  const int32_t* idx = c.slot_idx + uint64_t(p) * slots;
+  const float* zs = c.slot_z + uint64_t(p) * slots;
+  const float* ts = c.slot_t + uint64_t(p) * slots;
+  float* gs = c.slot_g + uint64_t(p) * slots;
   {
     const uint32_t r = threadIdx.x % kRowsPerBlock, t0 = threadIdx.x / kRowsPerBlock;   // packed rows to the next multiple of 256 exist
     float m = -INFINITY, s = 0.f, s1 = 0.f, z = 0.f;
@@ -1065,20 +1081,21 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
         const uint64_t at = uint64_t(in ? t + 32 * j : t) * c.rows_cap + p0 + r;
         tm[j] = in ? c.part_m[at] : -INFINITY;
         ts[j] = in ? c.part_s[at] : 0.f;
-        t1[j] = in && c.two ? c.part_s1[at] : 0.f;
-        z += in && c.smooth ? c.part_z[at] : 0.f;
+        t1[j] = in && two ? c.part_s1[at] : 0.f;
+        z += in && smooth ? c.part_z[at] : 0.f;
       }
       float nm = m;
 #pragma unroll
       for (int j = 0; j < B; ++j) nm = fmaxf(nm, tm[j]);
       const float base = nm == -INFINITY ? 0.f : nm;
-      s *= exp2f(log2_ratio(m, base, c.cT));          // an empty side has factor 2^-inf = 0
-      if (c.two) s1 *= exp2f(log2_ratio(m, base, c.c1));
+      const Log2Ratio toT(base, c.cT), to1(base, c.c1);
+      s *= exp2f(toT(m));                              // an empty side has factor 2^-inf = 0
+      if (two) s1 *= exp2f(to1(m));
 #pragma unroll
       for (int j = 0; j < B; ++j) {
         // columns all left out: m = -inf and s = 0; NaN goes through
-        s += ts[j] * (tm[j] == -INFINITY ? 1.f : exp2f(log2_ratio(tm[j], base, c.cT)));
-        if (c.two) s1 += t1[j] * (tm[j] == -INFINITY ? 1.f : exp2f(log2_ratio(tm[j], base, c.c1)));
+        s += ts[j] * (tm[j] == -INFINITY ? 1.f : exp2f(toT(tm[j])));
+        if (two) s1 += t1[j] * (tm[j] == -INFINITY ? 1.f : exp2f(to1(tm[j])));
       }
       m = nm;
     }
@@ -1091,7 +1108,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
   const int64_t label = c.use_label ? c.labels[n] : c.ignore_label;
   const double w = c.row_weight ? double(c.row_weight[n]) : 1.0;      // the mean's 1 / count: mean_scale
   float mf = -INFINITY;
-  for (uint32_t i = lane; i < c.slots; i += 32) {
+  for (uint32_t i = lane; i < slots; i += 32) {
     const int32_t x = idx[i];
     sh_i[y][i] = x;
     const float z = c.use_label && int64_t(x) == label && label != c.ignore_label ? c.label_z[p] : zs[i];
@@ -1107,26 +1124,28 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     for (int o = 16; o > 0; o >>= 1) mf = fmaxf(mf, __shfl_xor_sync(0xFFFFFFFFu, mf, o));
     const float base = mf == -INFINITY ? 0.f : mf, lm = sh_m[lane][y];
     const double M = double(base);
-    const double denseT = warp_sum(double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(log2_ratio(lm, base, c.cT)))));
-    const double dense1 = !c.two ? denseT : warp_sum(double(sh_s1[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(log2_ratio(lm, base, c.c1)))));
-    const double zsum = c.smooth ? warp_sum(double(sh_z[lane][y])) : 0.0;
+    const double denseT = warp_sum(double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(Log2Ratio(base, c.cT)(lm)))));
+    const double dense1 = !two ? denseT : warp_sum(double(sh_s1[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(Log2Ratio(base, c.c1)(lm)))));
+    const double zsum = smooth ? warp_sum(double(sh_z[lane][y])) : 0.0;
     const bool labelled = c.use_label && label != c.ignore_label;
 
-    // the teacher's probabilities
-    double tmax = -INFINITY;
-    bool nan_t = false;
-    for (uint32_t i = lane; i < c.slots; i += 32)
-      if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) { tmax = fmax(tmax, double(sh_t[y][i])); nan_t |= isnan(sh_t[y][i]); }
-    tmax = warp_max(tmax);
-    const bool taught = __any_sync(0xFFFFFFFFu, nan_t) || tmax != -INFINITY;
-    // log q = (t - shift) / T - norm; the list's maximum goes first, so that entries at the type's lowest value keep log k
-    double norm = 0.0, shift = 0.0;
+    // the teacher's probabilities: log q = (t - shift) / T - norm; the list's maximum goes first, so that entries at the
+    // type's lowest value keep log k
+    bool taught = false;
+    double norm = 0.0, shift = 0.0, tmax = -INFINITY;
+    if constexpr (TEACHER) {
+      bool nan_t = false;
+      for (uint32_t i = lane; i < slots; i += 32)
+        if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) { tmax = fmax(tmax, double(sh_t[y][i])); nan_t |= isnan(sh_t[y][i]); }
+      tmax = warp_max(tmax);
+      taught = __any_sync(0xFFFFFFFFu, nan_t) || tmax != -INFINITY;
+    }
     if (taught) {
       if (c.tail_class) norm = double(c.teacher_lse[n]);
       else {
         shift = tmax == -INFINITY ? 0.0 : tmax;
         double a = 0.0;
-        for (uint32_t i = lane; i < c.slots; i += 32)
+        for (uint32_t i = lane; i < slots; i += 32)
           if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) a += exp((double(sh_t[y][i]) - shift) * c.inv_temp);
         norm = log(warp_sum(a));
       }
@@ -1134,16 +1153,16 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
     // own columns: their exponentials, with those of the label apart from the rest
     double ownT = 0.0, own1 = 0.0, eT_label = 0.0, e1_label = 0.0, z_label = 0.0, qsum = 0.0;
     float out_z = -INFINITY;                               // the label's logit where it is not in the teacher's list
-    for (uint32_t i = lane; i < c.slots; i += 32) {
+    for (uint32_t i = lane; i < slots; i += 32) {
       double qi = 0.0;
       const int32_t x = sh_i[y][i];
       if (x != INT_MAX) {
-        if (sh_t[y][i] != -INFINITY) { qi = exp((double(sh_t[y][i]) - shift) * c.inv_temp - norm); qsum += qi; }
+        if (TEACHER && sh_t[y][i] != -INFINITY) { qi = exp((double(sh_t[y][i]) - shift) * c.inv_temp - norm); qsum += qi; }
         const bool first = i == 0 || sh_i[y][i - 1] != x;
         if (first) {
           bool listed = false;
-          for (uint32_t j = i; j < c.slots && sh_i[y][j] == x; ++j) listed |= sh_t[y][j] != -INFINITY;
-          const double eT = exp((double(sh_zs[y][i]) - M) * c.inv_temp), e1 = c.two ? exp(double(sh_zs[y][i]) - M) : eT;
+          for (uint32_t j = i; j < slots && sh_i[y][j] == x; ++j) listed |= sh_t[y][j] != -INFINITY;
+          const double eT = exp((double(sh_zs[y][i]) - M) * c.inv_temp), e1 = two ? exp(double(sh_zs[y][i]) - M) : eT;
           if (labelled && int64_t(x) == label) { eT_label = eT; e1_label = e1; z_label = double(sh_zs[y][i]); }
           else { ownT += eT; own1 += e1; }
           if (!listed) out_z = sh_zs[y][i];    // the label outside the teacher's list belongs to the tail
@@ -1165,7 +1184,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xFFFFFFFFu, tm, o));
       if (tm == -INFINITY) tm = 0.f;
       tail_m = double(tm);
-      tail = double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(log2_ratio(lm, tm, c.cT))));
+      tail = double(sh_s[lane][y]) * (lm == -INFINITY ? 1.0 : double(exp2f(Log2Ratio(tm, c.cT)(lm))));
       if (out_z != -INFINITY) tail += exp((double(out_z) - tail_m) * c.inv_temp);
       tail = warp_sum(tail);
     }
@@ -1182,14 +1201,14 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       return fabs(e) < double(kFar) ? float(e) : __double2float_ru(m * double(cc) + l * kLog2e);
     };
     const float exp_T = exponent(M, c.cT, c.inv_temp, log_T);
-    const double lseT = M * c.inv_temp + log_T, lse1 = c.two ? M + log_1 : lseT;
-    const double nll = !labelled ? 0.0 : (rest1 < e1_label ? log_p : (c.two ? lse1 - z_label : lseT - z_label * c.inv_temp));
+    const double lseT = M * c.inv_temp + log_T, lse1 = two ? M + log_1 : lseT;
+    const double nll = !labelled ? 0.0 : (rest1 < e1_label ? log_p : (two ? lse1 - z_label : lseT - z_label * c.inv_temp));
 
-    if (c.top == 0) {
+    if constexpr (!TEACHER) {
       const double pl = e1_label / totT, ql = restT / totT, zl = 2.0 * c.z_loss * lseT, eps = c.smoothing;
       if (lane == 0) {
         double loss = (1.0 - eps) * nll + c.z_loss * lseT * lseT;
-        if (c.smooth) loss += eps * (lseT - zsum / double(c.vocab));
+        if (smooth) loss += eps * (lseT - zsum / double(c.vocab));
         c.loss[n] = float(loss);
         c.lse[n] = float(lseT);
         c.coef[p] = make_float4(exp_T, float(w * (1.0 + zl)), float(w * eps / double(c.vocab)), 0.f);
@@ -1197,7 +1216,7 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       }
     } else {
       double kl = 0.0;
-      for (uint32_t i = lane; i < c.slots; i += 32)
+      for (uint32_t i = lane; i < slots; i += 32)
         if (sh_i[y][i] != INT_MAX && sh_t[y][i] != -INFINITY) {
           const double qi = sh_q[y][i];
           if (qi != 0.0) kl += qi * (((double(sh_t[y][i]) - shift) * c.inv_temp - norm) - (double(sh_zs[y][i]) * c.inv_temp - lseT));
@@ -1222,19 +1241,19 @@ __global__ void __launch_bounds__(256) fls_head_rows_kernel(const __grid_constan
       if (lane == 0) {
         c.loss[n] = float((taught ? c.distill_weight * c.temp * c.temp * kl : 0.0) + (labelled ? c.label_weight * nll : 0.0));
         c.lse[n] = float(lseT);
-        if (c.two) c.coef[p] = make_float4(exp_out, float(a * d_out), exponent(M, c.c1, 1.0, log_1), float(b));
+        if (two) c.coef[p] = make_float4(exp_out, float(a * d_out), exponent(M, c.c1, 1.0, log_1), float(b));
         else c.coef[p] = make_float4(exp_out, float(a * d_out + b * p_out), 0.f, 0.f);
       }
-      for (uint32_t i = lane; i < c.slots; i += 32) {
+      for (uint32_t i = lane; i < slots; i += 32) {
         const int32_t x = sh_i[y][i];
         if (x == INT_MAX) continue;
         double qi = 0.0;
         bool listed = false;
         for (uint32_t j = i + 1; j-- > 0 && sh_i[y][j] == x;) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
-        for (uint32_t j = i + 1; j < c.slots && sh_i[y][j] == x; ++j) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
+        for (uint32_t j = i + 1; j < slots && sh_i[y][j] == x; ++j) { qi += sh_q[y][j]; listed |= sh_t[y][j] != -INFINITY; }
         const double zT = double(sh_zs[y][i]) * c.inv_temp, pT = exp(zT - lseT);
         double v = a * (listed ? pT - qi : exp(zT - lse_out) * d_out);
-        if (labelled) v += b * (int64_t(x) == label ? -rest1 / tot1 : (c.two ? exp(double(sh_zs[y][i]) - lse1) : pT));
+        if (labelled) v += b * (int64_t(x) == label ? -rest1 / tot1 : (two ? exp(double(sh_zs[y][i]) - lse1) : pT));
         gs[i] = float(v);
       }
     }
@@ -1395,7 +1414,9 @@ cudaError_t head_clusters(uint32_t* out) {
   for (cudaError_t e : {allow_smem<kStats, false, false>(), allow_smem<kStats, false, true>(), allow_smem<kStats, true, false>(),
                         allow_smem<kStats, false, false, true>(), allow_smem<kStats, false, true, true>(), allow_smem<kStats, true, false, true>(),
                         allow_smem<kDlogits, false, false>(), allow_smem<kDlogits, true, false>(), allow_smem<kDlogits, false, true>(),
-                        allow_smem<kDlogits, true, true>(), allow_smem<kGrads, false, false>()})
+                        allow_smem<kDlogits, true, true>(), allow_smem<kGrads, false, false>(),
+                        cudaFuncSetAttribute(fls_head_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSpread),
+                        cudaFuncSetAttribute(fls_head_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSpread)})
     if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(2);
@@ -1434,7 +1455,8 @@ cudaError_t launch_head_stats(const HeadCall& c, const HeadMaps& m, cudaStream_t
   return launch_gemm<kStats, false, false>(c, m, p, s);
 }
 cudaError_t launch_head_rows(const HeadCall& c, cudaStream_t s) {
-  return launch(fls_head_rows_kernel, dim3(c.rows_cap / kRowsPerBlock), 256, 0, false, s, c);
+  const uint32_t blocks = c.rows_cap / kRowsPerBlock, smem = blocks <= 4 * c.clusters ? kRowsSpread : 0;      // a cluster is two SMs
+  return launch(c.top ? fls_head_rows_kernel<true> : fls_head_rows_kernel<false>, dim3(blocks), 256, smem, false, s, c);
 }
 cudaError_t launch_head_dlogits(const HeadCall& c, const HeadMaps& m, const HeadPiece& p, cudaStream_t s) {
   if (c.planes == 2) return c.two ? launch_gemm<kDlogits, true, true>(c, m, p, s) : launch_gemm<kDlogits, false, true>(c, m, p, s);
