@@ -60,7 +60,7 @@ struct HeadCall {
   uint32_t terms, planes;    // bf16 terms of dL/dz that a weight gradient of this head takes; those that this call stores
   uint32_t tail_class, use_label, two, smooth, grad_f32, accumulate;
   uint32_t want_gh, want_gw;
-  uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, bf16 accumulation): plain stores
+  uint32_t direct_store;     // grad_weight cannot be a TMA store's target (alignment, length of a row, bf16 accumulation): plain stores
   uint32_t max_splits, clusters, group_m;
   uint32_t prefetch_weight;  // one row tile, and the weight is the caller's: fetched ahead of the packed rows
   uint32_t wait_limit;       // polls of a barrier before a role gives up

@@ -214,7 +214,10 @@ int run(fls_head* h, const fls_head_io* io, HeadCall& c, void* cuda_stream) {
   c.cT = float(1.4426950408889634 * c.inv_temp);
   const bool grads = c.want_gh || c.want_gw;
   c.keep_v0 = c.vocab;
-  c.direct_store = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 || c.grad_weight_stride * (c.grad_f32 ? 4 : 2) % 16 ||
+  // A TMA store ends on a 16-byte boundary: with a row of any other length it writes into what follows the row (zeros, seen
+  // in the first column after rows of 23 fp32, stride 24).
+  const uint32_t we = c.grad_f32 ? 4 : 2;
+  c.direct_store = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 || c.grad_weight_stride * we % 16 || uint64_t(c.dim) * we % 16 ||
                    (c.accumulate && !c.grad_f32);
   if (grads) {
     const Pieces p = pieces_of(d, r.g_bytes, c.rows, terms_of(d));

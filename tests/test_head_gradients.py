@@ -40,3 +40,25 @@ def test_one_gradient_alone_has_the_bits_of_both(rows, n, V, d, piece, f32):
     head.xent_step(h, w, y, grad_hidden=alone[0])
     head.xent_step(h, w, y, grad_weight=alone[1])
     assert torch.equal(alone[0], both[0]) and torch.equal(alone[1], both[1])
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("d,stride", [(1, 8), (23, 24), (34, 40), (67, 72), (100, 104), (125, 128), (126, 136), (71, 96), (64, 72), (1021, 1024)])
+def test_nothing_between_the_rows_is_written(d, stride, accumulate, f32):
+    """Gradients in views whose rows start on 16-byte boundaries and end anywhere."""
+    from paper_2609_20359_b200.head import Head
+    n, V = 40, 300
+    h, w, y = make(n, V, d)
+    dtype = torch.float32 if f32 else torch.bfloat16
+    bh = torch.full((n + 1, stride), 5.0, dtype=torch.bfloat16, device=DEV)
+    bw = torch.full((V + 1, stride), 5.0, dtype=dtype, device=DEV)
+    gh, gw = bh[:n, :d], bw[:V, :d]
+    want_h, want_w = torch.empty(n, d, dtype=torch.bfloat16, device=DEV), torch.full((V, d), 5.0, dtype=dtype, device=DEV)
+    head = Head(n, V, d, grad_dtype="f32" if f32 else "bf16", any_weight=True)
+    head.xent_step(h, w, y, gh, gw, accumulate=accumulate)
+    head.xent_step(h, w, y, want_h, want_w, accumulate=accumulate)
+    assert torch.equal(gh, want_h) and torch.equal(gw, want_w)
+    gh.fill_(5.0)
+    gw.fill_(5.0)
+    assert bool((bh == 5.0).all()) and bool((bw == 5.0).all())
