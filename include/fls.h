@@ -395,7 +395,7 @@ int fls_plan_destroy(fls_plan* plan);
  * of the products, get loss 0, lse 0 and a zero gradient, and their hidden state may hold anything, NaN included.  A
  * label outside [0, V) other than ignore_label is not an error the host could see: that row's loss is NaN and it takes
  * no other part.  Teacher entries with an index outside [0, V) or a logit of -inf are absent; entries of one row should
- * be distinct (repeated ones count as separate entries). */
+ * be distinct (repeated ones count as separate entries).  Logits beyond 1e38 T in magnitude have no log sum exp in fp32. */
 typedef struct fls_head fls_head; /* opaque, created by fls_head_create, freed by fls_head_destroy */
 
 enum { FLS_TAIL_RENORM = 0, FLS_TAIL_CLASS = 1 };

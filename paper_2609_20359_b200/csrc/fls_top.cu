@@ -9,8 +9,9 @@
 // which makes the result independent of the order in which they were found.  Rows with so many equal logits that the
 // stretches or candidates do not fit are searched bit by bit instead (fls_top_exact below).
 //
-// Bound by memory, 2 or 4 bytes per logit read once: 4096 x 128256 bf16, k = 64 in 205 us, 5.1 TB/s (79 % of the measured
-// copy; with k = 128 249 us: the rest is the second look and the ranking, during which a CTA reads nothing new).  Ahead of
+// Bound by memory, 2 or 4 bytes per logit read once: 4096 x 128256 bf16, k = 64 in 206 us alone, 5.1 TB/s (79 % of the measured
+// copy), 214 to 219 us among others (76 %); with k = 128 249 us.  The rest is the second look, for which 180 MB come from memory
+// again, and the ranking, during which a CTA reads nothing new.  Ahead of
 // the sums two fp32 operations go into one instruction (270 us without) and four 16-byte vectors per thread are on their
 // way while four are added up (256 us with one thread maximum instead of stretches, 512 threads).  One row is latency:
 // 11.5 us for 128256 bf16 by four CTAs, of which the load is a tenth; the 16 block-wide counts that find the bound, the

@@ -4,6 +4,8 @@ import math
 import pytest
 import torch
 
+from tests import head_reference as R
+
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
@@ -62,3 +64,20 @@ def test_nothing_between_the_rows_is_written(d, stride, accumulate, f32):
     gh.fill_(5.0)
     gw.fill_(5.0)
     assert bool((bh == 5.0).all()) and bool((bw == 5.0).all())
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("n,V,d", [(1, 700, 64), (2, 3000, 256), (1, 12, 1000)])
+def test_probabilities_that_cancel(n, V, d, f32):
+    """With smoothing p - eps / V may nearly vanish; its error is that of p then, not of the difference."""
+    from paper_2609_20359_b200.head import Head
+    eps = 0.5
+    h, w, y = make(n, V, d)
+    gh = torch.full((n, d), math.nan, dtype=torch.bfloat16, device=DEV)
+    gw = torch.full((V, d), math.nan, dtype=torch.float32 if f32 else torch.bfloat16, device=DEV)
+    Head(n, V, d, grad_dtype="f32" if f32 else "bf16").xent_step(h, w, y, gh, gw, label_smoothing=eps)
+    live = torch.ones(n, dtype=torch.bool, device=DEV)
+    ref = R.with_gradients(h, w, lambda z: (*R.xent_rows(z, y, live, eps, 0.0), live))
+    p = ref["dz"].abs() + eps / (V * n)                # what the difference is taken of, with the mean's 1 / n
+    R.check_grads(ref, gh, None, small=ref["e_p"] * p @ w.double().abs())
+    R.check_grads(ref, None, gw, small=ref["e_p"] * p.t() @ h.double().abs())
