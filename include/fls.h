@@ -495,6 +495,149 @@ int fls_head_get_launch_count(const fls_head* head, uint64_t* launches);
 int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t rows, uint64_t vocab, uint64_t stride, uint32_t top,
                    double temperature, float* value, int32_t* index, float* lse, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * The input end of a language model: rows of the embedding table (V x d, bf16: a view of fls_buffers.param_bf16, or any
+ * other buffer) by token, and the gradient of that table, written into a unit of a plan's gradient buffer.
+ *
+ *   lookup:    out_n = scale * W[t_n]                                                 one rounding to out's type
+ *   gradient:  G[v]  = scale * sum over n with t_n = v of D_n  (+ G[v], accumulate)   fp32 sums, one rounding to G's type
+ * Positions with t_n == ignore_token take no part: their row of out is zero, their row of D may hold anything, NaN included.
+ * A token outside [0, V) other than ignore_token is not an error the host could see: its row of out is NaN, and it takes no
+ * part in the gradient.  Without accumulate every row of G is written, zeros where v is no token; with it only the rows of
+ * tokens are touched (tied tables: after fls_head_xent has written the head's gradient; several micro-batches).  The sums
+ * are made in an order that depends on the tokens alone, so results do not change from run to run. */
+typedef struct fls_embed fls_embed; /* opaque, created by fls_embed_create, freed by fls_embed_destroy */
+
+typedef struct {
+  uint64_t max_tokens;  /* N of the largest call, <= 2^24                                             */
+  uint64_t vocab;       /* V, 1 .. 2^30                                                               */
+  uint32_t dim;         /* d, 1 .. 65536                                                              */
+  uint32_t grads;       /* 1: the workspace has room for fls_embed_grad; 0: lookups only              */
+  uint32_t act_dtype;   /* FLS_GRAD_BF16 or FLS_GRAD_F32: element type of out and grad_out            */
+  uint32_t grad_dtype;  /* element type of grad_weight, as the plan's gradients                       */
+  uint64_t reserved;    /* 0                                                                          */
+} fls_embed_desc;
+
+typedef struct { uint64_t workspace_bytes; } fls_embed_layout;
+
+/* One call's data.  All buffers are device memory of the current device; strides count elements between rows, 0 means dense,
+ * < 2^31.  Any element alignment and stride (rows that start on 16-byte boundaries on both sides are faster). */
+typedef struct {
+  uint64_t tokens;              /* N, 0 .. max_tokens                                                 */
+  const int64_t* token;         /* N                                                                  */
+  const void* weight;           /* lookup: V x d, bf16                                                */
+  void* out;                    /* lookup: N x d, act_dtype, output                                   */
+  const void* grad_out;         /* gradient: N x d, act_dtype                                         */
+  void* grad_weight;            /* gradient: V x d, grad_dtype, output                                */
+  void* workspace;              /* gradient: 256-byte aligned; holds nothing between calls            */
+  uint64_t workspace_bytes;
+  uint64_t weight_stride, out_stride, grad_out_stride, grad_weight_stride;
+  int64_t ignore_token;
+  double scale;
+  uint32_t accumulate;          /* 1: grad_weight is added to                                         */
+  uint32_t reserved;            /* 0                                                                  */
+} fls_embed_io;
+
+/* Host only.  Errors: FLS_EINVAL (null argument, a size outside its range, an unknown dtype, reserved not 0). */
+int fls_embed_create(const fls_embed_desc* desc, fls_embed** out);
+int fls_embed_query(const fls_embed* embed, fls_embed_layout* out);
+int fls_embed_destroy(fls_embed* embed);
+
+/* Enqueued on cuda_stream; nothing is synchronised or allocated.  A lookup without tokens does nothing; a gradient without
+ * tokens writes a zero grad_weight (or leaves it, with accumulate).  Lookups may overlap in time; gradients with one
+ * workspace must not.  Errors, before anything is enqueued: FLS_EINVAL (tokens > max_tokens, a gradient without desc.grads, a
+ * stride below d, scale not finite in fp32), FLS_EPTR (null, host, another device's or overlapping buffers), FLS_EALIGN
+ * (buffers off their element size, workspace), FLS_ESIZE (workspace too small), FLS_ECUDA. */
+int fls_embed_lookup(fls_embed* embed, const fls_embed_io* io, void* cuda_stream);
+int fls_embed_grad(fls_embed* embed, const fls_embed_io* io, void* cuda_stream);
+
+/* Number of kernels this embedding has launched so far. */
+int fls_embed_get_launch_count(const fls_embed* embed, uint64_t* launches);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * The norms between the blocks of a language model and in front of its head: layer norm and root mean square norm of rows of
+ * d values, with the residual addition before it on request, and the backward pass.
+ *
+ *   s = x, or with a residual s = x + r, rounded to x's type and written to total;
+ *   FLS_NORM_LAYER: mu = mean(s), var = mean((s - mu)^2);   FLS_NORM_RMS: mu = 0, var = mean(s^2);
+ *   rho = 1 / sqrt(var + eps);   y = (s - mu) rho w + b    (w: ones where weight is null, b: zeros where bias is null)
+ * and, for the gradient dy of y (and dt of total, added, where grad_total is given), with xh = (s - mu) rho and g = dy w:
+ *   grad_x = rho (g - mean(g) - xh mean(g xh)) + dt        (root mean square: without mean(g))
+ *   grad_weight = sum over rows of dy xh,   grad_bias = sum over rows of dy    (+ what is there, with accumulate)
+ * grad_x is the gradient of s: with a residual, of x and of r alike.  Statistics, sums and products are fp32, every output is
+ * rounded once; a row whose sum of squares leaves fp32's range (values beyond about 1e19) has no statistics in fp32.  The
+ * backward pass takes mean and rstd as fp32, so that (s - mu) carries the rounding of mu, 2^-24 |mu|.  Results do not change
+ * from run to run.  A row without finite statistics gives NaN in itself, and in grad_weight and grad_bias, alone. */
+typedef struct fls_norm fls_norm; /* opaque, created by fls_norm_create, freed by fls_norm_destroy */
+
+enum { FLS_NORM_LAYER = 0, FLS_NORM_RMS = 1 };
+
+typedef struct {
+  uint64_t max_rows;      /* N of the largest call, <= 2^24                                                     */
+  uint32_t dim;           /* d, 1 .. 65536                                                                      */
+  uint32_t kind;          /* FLS_NORM_*                                                                         */
+  uint32_t x_dtype;       /* FLS_GRAD_BF16 or FLS_GRAD_F32: x, residual, total, grad_total, grad_x              */
+  uint32_t y_dtype;       /* y, grad_y                                                                          */
+  uint32_t weight_dtype;  /* weight, bias                                                                       */
+  uint32_t grad_dtype;    /* grad_weight, grad_bias, as the plan's gradients                                    */
+  uint32_t grads;         /* 1: the workspace has room for fls_norm_backward; 0: forward passes only            */
+  uint32_t reserved;      /* 0                                                                                  */
+  double eps;             /* 0 .. 1e30                                                                          */
+} fls_norm_desc;
+
+typedef struct { uint64_t workspace_bytes; } fls_norm_layout;
+
+/* One call's data.  All buffers are device memory of the current device; strides count elements between rows, 0 means dense,
+ * < 2^31; weight, bias and their gradients are dense.  Any element alignment (16-byte aligned rows are faster). */
+typedef struct {
+  uint64_t rows;                /* N, 0 .. max_rows                                                             */
+  const void* x;                /* N x d                                                                        */
+  const void* residual;         /* N x d, or NULL                                                               */
+  const void* weight;           /* d, or NULL                                                                   */
+  const void* bias;             /* d, or NULL                                                                   */
+  void* y;                      /* N x d, output                                                                */
+  void* total;                  /* N x d, output, with a residual; may be x or residual itself (same stride)    */
+  float* mean;                  /* N, output, or NULL (layer norm only)                                         */
+  float* rstd;                  /* N, output, or NULL                                                           */
+  uint64_t x_stride, residual_stride, y_stride, total_stride;
+  uint64_t reserved;            /* 0                                                                            */
+} fls_norm_io;
+
+typedef struct {
+  uint64_t rows;                /* N, 0 .. max_rows                                                             */
+  const void* x;                /* N x d: what was normalised (total, with a residual)                          */
+  const void* weight;           /* d, or NULL                                                                   */
+  const float* mean;            /* N (layer norm; NULL otherwise)                                               */
+  const float* rstd;            /* N                                                                            */
+  const void* grad_y;           /* N x d                                                                        */
+  const void* grad_total;       /* N x d, or NULL: added to grad_x                                              */
+  void* grad_x;                 /* N x d, output; may be grad_total itself (same stride); NULL: not computed    */
+  void* grad_weight;            /* d, output; NULL: not computed                                                */
+  void* grad_bias;              /* d, output; NULL: not computed                                                */
+  void* workspace;              /* 256-byte aligned; holds nothing between calls                                */
+  uint64_t workspace_bytes;
+  uint64_t x_stride, grad_y_stride, grad_total_stride, grad_x_stride;
+  uint32_t accumulate;          /* 1: grad_weight and grad_bias are added to                                    */
+  uint32_t reserved;            /* 0                                                                            */
+} fls_norm_grad_io;
+
+/* Host only.  Errors: FLS_EINVAL (null argument, a size outside its range, an unknown dtype or kind, reserved not 0). */
+int fls_norm_create(const fls_norm_desc* desc, fls_norm** out);
+int fls_norm_query(const fls_norm* norm, fls_norm_layout* out);
+int fls_norm_destroy(fls_norm* norm);
+
+/* Enqueued on cuda_stream; nothing is synchronised or allocated.  Without rows the forward pass does nothing and the backward
+ * pass writes zeros to grad_weight and grad_bias (or leaves them, with accumulate).  Forward passes may overlap in time;
+ * backward passes with one workspace must not.  Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, a backward
+ * pass without desc.grads, a stride below d, residual without total or the reverse, grad_total without grad_x, a mean for a
+ * root mean square norm), FLS_EPTR (null, host, another device's or overlapping buffers), FLS_EALIGN (buffers off their
+ * element size, workspace), FLS_ESIZE (workspace too small), FLS_ECUDA. */
+int fls_norm_forward(fls_norm* norm, const fls_norm_io* io, void* cuda_stream);
+int fls_norm_backward(fls_norm* norm, const fls_norm_grad_io* io, void* cuda_stream);
+
+/* Number of kernels this norm has launched so far. */
+int fls_norm_get_launch_count(const fls_norm* norm, uint64_t* launches);
+
 /* Message of the last error on the calling thread ("" if none).  Host string owned by the library. */
 const char* fls_last_error(void);
 

@@ -27,6 +27,7 @@ FLS_BUFFER_ALIGN = 32
 FLS_NOALLOC_MAX_ELEMS = 1 << 29
 FLS_TAIL_RENORM, FLS_TAIL_CLASS = 0, 1
 FLS_HEAD_MAX_TOP = 128
+FLS_NORM_LAYER, FLS_NORM_RMS = 0, 1
 
 EXPORTS = [
     "fls_plan_create", "fls_plan_query", "fls_plan_bind", "fls_sync_step", "fls_sync_step_host", "fls_fedavg",
@@ -38,6 +39,8 @@ EXPORTS = [
     "fls_last_error", "fls_reduce_norm_noalloc",
     "fls_head_create", "fls_head_query", "fls_head_destroy", "fls_head_xent", "fls_head_distill", "fls_head_get_state",
     "fls_head_get_launch_count", "fls_debug_expire_next_head_wait", "fls_top_logits",
+    "fls_embed_create", "fls_embed_query", "fls_embed_destroy", "fls_embed_lookup", "fls_embed_grad", "fls_embed_get_launch_count",
+    "fls_norm_create", "fls_norm_query", "fls_norm_destroy", "fls_norm_forward", "fls_norm_backward", "fls_norm_get_launch_count",
 ]
 
 
@@ -108,6 +111,44 @@ class fls_distill_desc(C.Structure):
                 ("label_weight", C.c_double)]
 
 
+class fls_embed_desc(C.Structure):
+    _fields_ = [("max_tokens", C.c_uint64), ("vocab", C.c_uint64), ("dim", C.c_uint32), ("grads", C.c_uint32),
+                ("act_dtype", C.c_uint32), ("grad_dtype", C.c_uint32), ("reserved", C.c_uint64)]
+
+
+class fls_embed_layout(C.Structure):
+    _fields_ = [("workspace_bytes", C.c_uint64)]
+
+
+class fls_embed_io(C.Structure):
+    _fields_ = [("tokens", C.c_uint64), ("token", C.c_void_p), ("weight", C.c_void_p), ("out", C.c_void_p), ("grad_out", C.c_void_p),
+                ("grad_weight", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("weight_stride", C.c_uint64), ("out_stride", C.c_uint64), ("grad_out_stride", C.c_uint64),
+                ("grad_weight_stride", C.c_uint64), ("ignore_token", C.c_int64), ("scale", C.c_double), ("accumulate", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
+class fls_norm_desc(C.Structure):
+    _fields_ = [("max_rows", C.c_uint64)] + [(n, C.c_uint32) for n in ("dim", "kind", "x_dtype", "y_dtype", "weight_dtype", "grad_dtype",
+                                                                       "grads", "reserved")] + [("eps", C.c_double)]
+
+
+class fls_norm_layout(C.Structure):
+    _fields_ = [("workspace_bytes", C.c_uint64)]
+
+
+class fls_norm_io(C.Structure):
+    _fields_ = [("rows", C.c_uint64)] + [(n, C.c_void_p) for n in ("x", "residual", "weight", "bias", "y", "total", "mean", "rstd")] + \
+               [(n, C.c_uint64) for n in ("x_stride", "residual_stride", "y_stride", "total_stride", "reserved")]
+
+
+class fls_norm_grad_io(C.Structure):
+    _fields_ = [("rows", C.c_uint64)] + [(n, C.c_void_p) for n in ("x", "weight", "mean", "rstd", "grad_y", "grad_total", "grad_x",
+                                                                   "grad_weight", "grad_bias", "workspace")] + \
+               [(n, C.c_uint64) for n in ("workspace_bytes", "x_stride", "grad_y_stride", "grad_total_stride", "grad_x_stride")] + \
+               [("accumulate", C.c_uint32), ("reserved", C.c_uint32)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} not found: build it with `python -m paper_2609_20359_b200.build` "
@@ -156,6 +197,18 @@ def _load() -> C.CDLL:
     lib.fls_head_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
     lib.fls_debug_expire_next_head_wait.argtypes = [P, C.c_uint32]
     lib.fls_top_logits.argtypes = [P, C.c_uint32, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint32, C.c_double, P, P, P, P]
+    lib.fls_embed_create.argtypes = [C.POINTER(fls_embed_desc), C.POINTER(P)]
+    lib.fls_embed_query.argtypes = [P, C.POINTER(fls_embed_layout)]
+    lib.fls_embed_destroy.argtypes = [P]
+    lib.fls_embed_lookup.argtypes = [P, C.POINTER(fls_embed_io), P]
+    lib.fls_embed_grad.argtypes = [P, C.POINTER(fls_embed_io), P]
+    lib.fls_embed_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
+    lib.fls_norm_create.argtypes = [C.POINTER(fls_norm_desc), C.POINTER(P)]
+    lib.fls_norm_query.argtypes = [P, C.POINTER(fls_norm_layout)]
+    lib.fls_norm_destroy.argtypes = [P]
+    lib.fls_norm_forward.argtypes = [P, C.POINTER(fls_norm_io), P]
+    lib.fls_norm_backward.argtypes = [P, C.POINTER(fls_norm_grad_io), P]
+    lib.fls_norm_get_launch_count.argtypes = [P, C.POINTER(C.c_uint64)]
     lib.fls_last_error.argtypes = []
     lib.fls_last_error.restype = C.c_char_p
     for name in EXPORTS:
@@ -462,6 +515,75 @@ def fls_top_logits(logits, logit_dtype: int, rows: int, vocab: int, stride: int,
                    stream=None) -> None:
     _check(lib.fls_top_logits(_ptr(logits), logit_dtype, rows, vocab, stride, top, temperature, _ptr(value), _ptr(index), _ptr(lse),
                               _stream_handle(stream)))
+
+
+# ---------------------------------------------------------------------------------------------- embedding
+def fls_embed_create(max_tokens: int, vocab: int, dim: int, grads: bool = True, act_dtype: int = FLS_GRAD_BF16,
+                     grad_dtype: int = FLS_GRAD_BF16) -> int:
+    """Returns the opaque embedding handle."""
+    d = fls_embed_desc(max_tokens, vocab, dim, int(grads), act_dtype, grad_dtype, 0)
+    out = C.c_void_p()
+    _check(lib.fls_embed_create(C.byref(d), C.byref(out)))
+    return out.value
+
+
+def fls_embed_query(embed: int) -> dict:
+    lay = fls_embed_layout()
+    _check(lib.fls_embed_query(embed, C.byref(lay)))
+    return {n: getattr(lay, n) for n, _ in fls_embed_layout._fields_}
+
+
+def fls_embed_destroy(embed: int) -> None:
+    _check(lib.fls_embed_destroy(embed))
+
+
+def fls_embed_lookup(embed: int, io: fls_embed_io, stream=None) -> None:
+    _check(lib.fls_embed_lookup(embed, C.byref(io), _stream_handle(stream)))
+
+
+def fls_embed_grad(embed: int, io: fls_embed_io, stream=None) -> None:
+    _check(lib.fls_embed_grad(embed, C.byref(io), _stream_handle(stream)))
+
+
+def fls_embed_get_launch_count(embed: int) -> int:
+    n = C.c_uint64()
+    _check(lib.fls_embed_get_launch_count(embed, C.byref(n)))
+    return n.value
+
+
+# ---------------------------------------------------------------------------------------------- norm
+def fls_norm_create(max_rows: int, dim: int, kind: int = FLS_NORM_LAYER, eps: float = 1e-5, x_dtype: int = FLS_GRAD_BF16,
+                    y_dtype: int = FLS_GRAD_BF16, weight_dtype: int = FLS_GRAD_BF16, grad_dtype: int = FLS_GRAD_BF16,
+                    grads: bool = True) -> int:
+    """Returns the opaque norm handle."""
+    d = fls_norm_desc(max_rows, dim, kind, x_dtype, y_dtype, weight_dtype, grad_dtype, int(grads), 0, eps)
+    out = C.c_void_p()
+    _check(lib.fls_norm_create(C.byref(d), C.byref(out)))
+    return out.value
+
+
+def fls_norm_query(norm: int) -> dict:
+    lay = fls_norm_layout()
+    _check(lib.fls_norm_query(norm, C.byref(lay)))
+    return {n: getattr(lay, n) for n, _ in fls_norm_layout._fields_}
+
+
+def fls_norm_destroy(norm: int) -> None:
+    _check(lib.fls_norm_destroy(norm))
+
+
+def fls_norm_forward(norm: int, io: fls_norm_io, stream=None) -> None:
+    _check(lib.fls_norm_forward(norm, C.byref(io), _stream_handle(stream)))
+
+
+def fls_norm_backward(norm: int, io: fls_norm_grad_io, stream=None) -> None:
+    _check(lib.fls_norm_backward(norm, C.byref(io), _stream_handle(stream)))
+
+
+def fls_norm_get_launch_count(norm: int) -> int:
+    n = C.c_uint64()
+    _check(lib.fls_norm_get_launch_count(norm, C.byref(n)))
+    return n.value
 
 
 __all__ = [n for n in dir() if n.startswith(("fls_", "FLS_"))] + ["FlsError", "lib", "LIB_PATH", "EXPORTS"]

@@ -1,0 +1,81 @@
+"""Embedding: the input end of a language model on libfls (device memory and streams only).
+
+All arithmetic happens in libfls through the fls_embed_* calls; this class owns one handle and its workspace, and checks the
+tensors it is given.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _binding as fls
+from .head import _dense, _empty_on, _matrix
+from .workspace import Workspace, device_of, dtype_of
+
+
+class Embedding:
+    """Rows of a [vocab, dim] bf16 table by token, and the gradient of that table.
+
+    max_tokens, vocab, dim: N of the largest call, V and d.  act_dtype: "bf16" or "f32", the type of looked-up rows and of
+    their gradients.  grad_dtype: the type of the table's gradient (as `Session`'s gradient buffers, whose units it may be
+    written into).  grads=False: lookups only.
+
+    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  Gradients use the
+    workspace, one call at a time: those of one Embedding belong on one stream, or on streams ordered by events.  An Embedding
+    may be dropped while its calls run (a stream given by its handle has to outlive it); a captured graph has to be dropped
+    first.
+    """
+
+    def __init__(self, max_tokens: int, vocab: int, dim: int, act_dtype: str = "bf16", grad_dtype: str = "bf16", grads: bool = True,
+                 device: str = "cuda:0"):
+        self.handle = None
+        self.device = device_of(device)
+        self.act_torch_dtype, act = dtype_of(act_dtype, "act_dtype")
+        self.grad_torch_dtype, grad = dtype_of(grad_dtype, "grad_dtype")
+        self.max_tokens, self.vocab, self.dim, self.grads = max_tokens, vocab, dim, grads
+        self.handle = fls.fls_embed_create(max_tokens, vocab, dim, grads, act, grad)
+        self.workspace = Workspace(fls.fls_embed_query(self.handle)["workspace_bytes"], self.device)
+        mem = self.workspace.memory
+        self._args = fls.fls_embed_io(workspace=mem.data_ptr(), workspace_bytes=mem.numel())   # of the call in preparation
+
+    def lookup(self, tokens, weight, out=None, scale: float = 1.0, ignore_token: int = -100, stream=None):
+        """scale * weight[tokens], [N, dim]: zeros where a token is ignore_token, NaN where it is outside the table."""
+        io, dev = self._args, self.device
+        n = self._tokens(tokens)
+        io.weight, io.weight_stride = _matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16, dev)
+        if out is None:
+            out = _empty_on(stream, (n, self.dim), self.act_torch_dtype, dev)
+            io.out, io.out_stride = out.data_ptr(), 0
+        else:
+            io.out, io.out_stride = _matrix(out, "out", n, self.dim, self.act_torch_dtype, dev)
+        io.scale, io.ignore_token, io.accumulate = scale, ignore_token, 0
+        fls.fls_embed_lookup(self.handle, io, stream)
+        return out
+
+    def grad(self, tokens, grad_out, grad_weight, scale: float = 1.0, accumulate: bool = False, ignore_token: int = -100,
+             stream=None) -> None:
+        """grad_weight [vocab, dim] becomes (accumulate: is added) scale times the sums of the rows of grad_out by token."""
+        io, dev = self._args, self.device
+        n = self._tokens(tokens)
+        io.grad_out, io.grad_out_stride = _matrix(grad_out, "grad_out", n, self.dim, self.act_torch_dtype, dev)
+        io.grad_weight, io.grad_weight_stride = _matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype, dev)
+        io.scale, io.ignore_token, io.accumulate = scale, ignore_token, accumulate
+        fls.fls_embed_grad(self.handle, io, self.workspace.use(stream))
+
+    def _tokens(self, tokens) -> int:
+        if tokens.dim() != 1:
+            raise ValueError(f"tokens must be one-dimensional, got {tuple(tokens.shape)}")
+        n = tokens.shape[0]
+        self._args.token = _dense(tokens, "tokens", (n,), torch.int64, self.device)
+        self._args.tokens = n
+        return n
+
+    def close(self) -> None:
+        if self.handle is not None:
+            fls.fls_embed_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
