@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 #include <new>
 
 #include "fls.h"
@@ -64,6 +65,366 @@ __device__ __forceinline__ float2 block_sum(float2 v, float2* shared) {
   return v;
 }
 
+// ------------------------------------------------------------------------------------------------ rows in registers
+// A row belongs to `tpr` neighbouring threads, each with K cells of eight columns: neighbouring columns where every row starts
+// on a 16-byte boundary and holds whole cells (VEC), otherwise columns 32 apart, moved one by one.
+template <bool VEC>
+__device__ __forceinline__ uint32_t column(uint32_t tpr, uint32_t t, int k, int j) {
+  return VEC ? (k * tpr + t) * 8 + j : (k * (tpr / 32) + t / 32) * 256 + t % 32 + 32 * j;
+}
+
+template <typename T, bool VEC> struct Cell;
+template <typename T> struct Cell<T, true> {
+  typename Elem<T>::Raw raw;
+  __device__ __forceinline__ void load(const T* row, uint32_t col, uint32_t dim) {
+    raw = typename Elem<T>::Raw{};
+    if (col < dim) raw = Elem<T>::load_raw(row + col);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const { Elem<T>::unpack(raw, x); }
+  __device__ static __forceinline__ void store(T* row, uint32_t col, uint32_t dim, const float (&x)[8]) {
+    if (col < dim) Elem<T>::store8(row + col, x);
+  }
+  // What was computed from the cell is computed again after this, not kept in registers.
+  __device__ __forceinline__ void forget() {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
+#pragma unroll
+    for (int i = 0; i < int(sizeof raw / 4); ++i) asm volatile("" : "+r"(w[i]));
+  }
+};
+template <typename T> struct Cell<T, false> {
+  float x_[8];
+  __device__ __forceinline__ void load(const T* row, uint32_t col, uint32_t dim) {
+    row += col;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x_[j] = col + 32 * j < dim ? Elem<T>::get(row + 32 * j) : 0.f;
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = x_[j];
+  }
+  __device__ static __forceinline__ void store(T* row, uint32_t col, uint32_t dim, const float (&x)[8]) {
+    row += col;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (col + 32 * j < dim) Elem<T>::put(row + 32 * j, x[j]);
+  }
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) asm volatile("" : "+f"(x_[j]));
+  }
+};
+
+// Eight values of the weight or the bias; `other` where there is none.  VEC asks for a 16-byte boundary of theirs too.
+template <bool VEC>
+__device__ __forceinline__ void weight_cell(const NormCall& c, const void* p, float other, uint32_t col, float (&x)[8]) {
+  if (!p) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = other;
+  } else if (c.weight_f32) {
+    Cell<float, VEC> w;
+    w.load(static_cast<const float*>(p), col, c.dim);
+    w.get(x);
+  } else {
+    Cell<uint16_t, VEC> w;
+    w.load(static_cast<const uint16_t*>(p), col, c.dim);
+    w.get(x);
+  }
+}
+
+// Sum over the threads of a row; all of the CTA's rows at once where a row has several warps.
+template <int V>
+__device__ __forceinline__ void row_sum(float (&v)[V], uint32_t tpr, float (*shared)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int o = 16; o; o /= 2) v[i] += __shfl_xor_sync(~0u, v[i], o);
+  if (tpr == 32) return;
+  const uint32_t warps = tpr / 32, warp = threadIdx.x / 32, first = warp / warps * warps;
+  if (threadIdx.x % 32 == 0)
+#pragma unroll
+    for (int i = 0; i < V; ++i) shared[warp][i] = v[i];
+  __syncthreads();
+  // every thread adds the warps' sums in the same order
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    float s = shared[first][i];
+    for (uint32_t w = 1; w < warps; ++w) s += shared[first + w][i];
+    v[i] = s;
+  }
+}
+
+template <typename X, typename Y, bool VEC, int K, int THREADS>
+__global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
+  __shared__ float shared1[32][1], shared2[32][2];
+  const uint32_t t = threadIdx.x % tpr;
+  const uint64_t n = uint64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
+  const bool live = n < c.rows;                             // the others keep the barriers company
+  const uint64_t row = live ? n : c.rows - 1;
+  float x[K][8];
+  {
+    Cell<X, VEC> in[K], add[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) in[k].load(static_cast<const X*>(c.x) + row * c.x_stride, column<VEC>(tpr, t, k, 0), c.dim);
+    if (c.residual)
+#pragma unroll
+      for (int k = 0; k < K; ++k) add[k].load(static_cast<const X*>(c.residual) + row * c.residual_stride, column<VEC>(tpr, t, k, 0), c.dim);
+#pragma unroll
+    for (int k = 0; k < K; ++k) in[k].get(x[k]);
+    if (c.residual) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float r[8];
+        add[k].get(r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[k][j] = Elem<X>::round(x[k][j] + r[j]);
+        if (live) Cell<X, VEC>::store(static_cast<X*>(c.total) + row * c.total_stride, column<VEC>(tpr, t, k, 0), c.dim, x[k]);
+      }
+    }
+  }
+  float w[8], b[8];
+  if (K == 1) {                                             // few rows: everything on its way at once
+    weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, 0, 0), w);
+    weight_cell<VEC>(c, c.bias, 0.f, column<VEC>(tpr, t, 0, 0), b);
+  }
+  float m = 0.f;
+  if (!c.rms) {
+    float v[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[0] += x[k][j];
+    row_sum<1>(v, tpr, shared1);
+    m = v[0] * c.inv_dim;
+  }
+  float v[2] = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[k][j] = column<VEC>(tpr, t, k, j) < c.dim ? x[k][j] - m : 0.f;
+      v[0] += x[k][j];
+      v[1] = fmaf(x[k][j], x[k][j], v[1]);
+    }
+  row_sum<2>(v, tpr, shared2);
+  const float e = c.rms ? 0.f : v[0] * c.inv_dim, var = fmaf(-e, e, v[1] * c.inv_dim);
+  const float rstd = 1.f / sqrtf(var + c.eps);
+  if (!live) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (column<VEC>(tpr, t, k, 0) >= c.dim) break;
+    if (K > 1) {
+      weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, k, 0), w);
+      weight_cell<VEC>(c, c.bias, 0.f, column<VEC>(tpr, t, k, 0), b);
+    }
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = fmaf((x[k][j] - e) * rstd, w[j], b[j]);
+    Cell<Y, VEC>::store(static_cast<Y*>(c.y) + row * c.y_stride, column<VEC>(tpr, t, k, 0), c.dim, y);
+  }
+  if (t == 0) {
+    if (c.mean) c.mean[n] = m + e;
+    if (c.rstd) c.rstd[n] = rstd;
+  }
+}
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 shared16(uint32_t from) {
+  uint4 x;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(from) : "memory");
+  return x;
+}
+
+// All gradients in one look at the rows.  A CTA has blockDim / tpr groups, a group a stretch of rows, one at a time; a thread
+// keeps its columns' sums for weight and bias in registers, adds them to the other groups' at the end and leaves the CTA's in
+// the workspace.  VEC: STAGES rows are on their way at once, copied asynchronously into shared memory; every thread copies
+// and reads its own 16-byte pieces, so that nobody waits for anybody's copies but his own.
+template <typename X, typename Y, bool VEC, int K, int STAGES, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
+  constexpr int kX = sizeof(X) / 2, kY = sizeof(Y) / 2;     // 16-byte pieces of a cell
+  extern __shared__ __align__(16) float smem[];             // rows on their way, then the groups' sums
+  __shared__ float2 sums[2][32];
+  const uint32_t t = threadIdx.x % tpr, group = threadIdx.x / tpr, groups = blockDim.x / tpr, warps = tpr / 32, lane = threadIdx.x % 32;
+  const uint64_t all = uint64_t(gridDim.x) * groups, g = uint64_t(blockIdx.x) * groups + group;
+  const uint64_t begin = c.rows * g / all;
+  const uint32_t count = uint32_t(c.rows * (g + 1) / all - begin);
+  const bool with_total = c.grad_total != nullptr;
+  const uint32_t pieces = K * (kX + kY + (with_total ? kX : 0));
+  const uint32_t mine = uint32_t(__cvta_generic_to_shared(smem)) + threadIdx.x * 16, step = blockDim.x * 16;
+  const X* px = static_cast<const X*>(c.x) + begin * c.x_stride;
+  const Y* py = static_cast<const Y*>(c.grad_y) + begin * c.grad_y_stride;
+  const X* pt = static_cast<const X*>(c.grad_total) + begin * c.grad_total_stride;
+  X* pd = static_cast<X*>(c.grad_x) + begin * c.grad_x_stride;
+  pdl_launch();
+
+  uint32_t to = mine, sent = 0;
+  auto send = [&] {                                         // the next row's copies
+    if (VEC && sent < count) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint32_t col = column<VEC>(tpr, t, k, 0);
+        const bool there = col < c.dim;
+        const uint32_t at = there ? col : 0;
+        uint32_t q = to + k * (kX + kY) * step;
+#pragma unroll
+        for (int i = 0; i < kX; ++i, q += step) copy16(q, reinterpret_cast<const uint4*>(px + at) + i, there);
+#pragma unroll
+        for (int i = 0; i < kY; ++i, q += step) copy16(q, reinterpret_cast<const uint4*>(py + at) + i, there);
+        if (with_total) {
+          q = to + (K * (kX + kY) + k * kX) * step;
+#pragma unroll
+          for (int i = 0; i < kX; ++i, q += step) copy16(q, reinterpret_cast<const uint4*>(pt + at) + i, there);
+        }
+      }
+      px += c.x_stride;
+      py += c.grad_y_stride;
+      pt += c.grad_total_stride;
+      ++sent;
+      to = sent % STAGES ? to + pieces * step : mine;
+    }
+    if (VEC) asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (VEC)
+    for (int i = 0; i + 1 < STAGES; ++i) send();
+
+  float w[K][8], dw[K][8], db[K][8];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, k, 0), w[k]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[k][j] = db[k][j] = 0.f;
+  }
+  float means = 0.f, rstds = 0.f;                           // of 32 rows, one per lane
+  uint32_t from = mine;
+  for (uint32_t i = 0; i < count; ++i) {
+    if (i % 32 == 0 && i + lane < count) {
+      if (!c.rms) means = c.mean_in[begin + i + lane];
+      rstds = c.rstd_in[begin + i + lane];
+    }
+    Cell<X, VEC> x[K], dt[K];
+    Cell<Y, VEC> dy[K];
+    if constexpr (VEC) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES > 1 ? STAGES - 2 : 0) : "memory");
+      uint32_t q = from;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        uint4* rx = reinterpret_cast<uint4*>(&x[k].raw);
+        uint4* ry = reinterpret_cast<uint4*>(&dy[k].raw);
+#pragma unroll
+        for (int p = 0; p < kX; ++p, q += step) rx[p] = shared16(q);
+#pragma unroll
+        for (int p = 0; p < kY; ++p, q += step) ry[p] = shared16(q);
+      }
+      if (with_total)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          uint4* rt = reinterpret_cast<uint4*>(&dt[k].raw);
+#pragma unroll
+          for (int p = 0; p < kX; ++p, q += step) rt[p] = shared16(q);
+        }
+      from = (i + 1) % STAGES ? from + pieces * step : mine;
+      send();                                               // into the place that the row before this one had
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        x[k].load(px, column<VEC>(tpr, t, k, 0), c.dim);
+        dy[k].load(py, column<VEC>(tpr, t, k, 0), c.dim);
+        if (with_total) dt[k].load(pt, column<VEC>(tpr, t, k, 0), c.dim);
+      }
+      px += c.x_stride;
+      py += c.grad_y_stride;
+      pt += c.grad_total_stride;
+    }
+    const float mean = __shfl_sync(~0u, means, i % 32), rstd = __shfl_sync(~0u, rstds, i % 32);
+    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float xs[8], ys[8];
+      x[k].get(xs);
+      dy[k].get(ys);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float xhat = (xs[j] - mean) * rstd, gy = ys[j] * w[k][j];
+        v.x += gy;
+        v.y = fmaf(gy, xhat, v.y);
+        dw[k][j] = fmaf(ys[j], xhat, dw[k][j]);
+        db[k][j] += ys[j];
+      }
+    }
+    if (!c.grad_x) continue;
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+      v.x += __shfl_xor_sync(~0u, v.x, o);
+      v.y += __shfl_xor_sync(~0u, v.y, o);
+    }
+    if (warps > 1) {
+      float2* sh = sums[i % 2] + group * warps;             // the next row's go elsewhere while these are read
+      if (lane == 0) sh[t / 32] = v;
+      asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
+      v = sh[0];
+#pragma unroll 1
+      for (uint32_t k = 1; k < warps; ++k) {
+        const float2 a = sh[k];
+        v.x += a.x;
+        v.y += a.y;
+      }
+    }
+    const float c1 = c.rms ? 0.f : v.x * c.inv_dim, c2 = v.y * c.inv_dim;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      x[k].forget();
+      dy[k].forget();
+      float xs[8], ys[8], dx[8];
+      x[k].get(xs);
+      dy[k].get(ys);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float xhat = (xs[j] - mean) * rstd;
+        dx[j] = (fmaf(-xhat, c2, ys[j] * w[k][j]) - c1) * rstd;
+      }
+      if (with_total) {
+        dt[k].get(xs);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dx[j] += xs[j];
+      }
+      Cell<X, VEC>::store(pd, column<VEC>(tpr, t, k, 0), c.dim, dx);
+    }
+    pd += c.grad_x_stride;
+  }
+  if (!c.grad_weight && !c.grad_bias) return;
+  // the groups' sums, in their order
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  if (group) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        smem[((group - 1) * 16 * K + k * 16 + j) * tpr + t] = dw[k][j];
+        smem[((group - 1) * 16 * K + k * 16 + 8 + j) * tpr + t] = db[k][j];
+      }
+  }
+  __syncthreads();
+  if (group) return;
+#pragma unroll 1
+  for (uint32_t o = 0; o + 1 < groups; ++o)
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dw[k][j] += smem[(o * 16 * K + k * 16 + j) * tpr + t];
+        db[k][j] += smem[(o * 16 * K + k * 16 + 8 + j) * tpr + t];
+      }
+  float* part = c.part + uint64_t(2 * blockIdx.x) * c.dp;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    Cell<float, VEC>::store(part, column<VEC>(tpr, t, k, 0), c.dim, dw[k]);
+    Cell<float, VEC>::store(part + c.dp, column<VEC>(tpr, t, k, 0), c.dim, db[k]);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rows of any length
 // A row per CTA, read again for each step.
 template <typename X, typename Y>
 __global__ void __launch_bounds__(256) fls_norm_rows_kernel(const __grid_constant__ NormCall c) {
@@ -157,31 +518,37 @@ __global__ void __launch_bounds__(256) fls_norm_columns_kernel(const __grid_cons
   c.part[uint64_t(2 * blockIdx.y + 1) * c.dp + j] = sum.y;
 }
 
-// The parts' sums, in their order inside each of eight groups, then of the groups.
-__global__ void __launch_bounds__(256) fls_norm_join_kernel(const __grid_constant__ NormCall c) {
-  __shared__ float shared[8][kColTile];
+// The parts' sums, in their order inside each of 32 groups, then of the groups.
+__global__ void __launch_bounds__(1024) fls_norm_join_kernel(const __grid_constant__ NormCall c) {
+  __shared__ float shared[32][kColTile + 1];
   const uint32_t lane = threadIdx.x % 32, group = threadIdx.x / 32, j = blockIdx.x * kColTile + lane, which = blockIdx.y;
   void* out = which ? c.grad_bias : c.grad_weight;
   pdl_wait();
   if (!out) return;
   float sum = 0.f;
-  for (uint32_t p = group; p < c.parts && j < c.dim; p += 8) sum += c.part[uint64_t(2 * p + which) * c.dp + j];
+#pragma unroll 10
+  for (uint32_t p = group; p < c.parts; p += 32)
+    if (j < c.dim) sum += c.part[uint64_t(2 * p + which) * c.dp + j];
   shared[group][lane] = sum;
   __syncthreads();
-  if (group || j >= c.dim) return;
-  for (int g = 1; g < 8; ++g) sum += shared[g][lane];
+  sum = shared[lane][group];                                // column `group`, group `lane`
+#pragma unroll
+  for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+  const uint32_t col = blockIdx.x * kColTile + group;
+  if (lane || col >= c.dim) return;
   if (c.grad_f32) {
-    float* o = static_cast<float*>(out) + j;
+    float* o = static_cast<float*>(out) + col;
     *o = c.accumulate ? *o + sum : sum;
   } else {
-    uint16_t* o = static_cast<uint16_t*>(out) + j;
+    uint16_t* o = static_cast<uint16_t*>(out) + col;
     Elem<uint16_t>::put(o, c.accumulate ? Elem<uint16_t>::get(o) + sum : sum);
   }
 }
 
 template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
+cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, uint32_t smem, bool dependent, cudaStream_t s, const A&... args) {
   cudaLaunchConfig_t cfg{};
+  cfg.dynamicSmemBytes = smem;
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.stream = s;
@@ -227,23 +594,72 @@ namespace {
     ++h->launches;                                                                                  \
   } while (0)
 
+bool aligned(const void* p, uint64_t stride, uint64_t elem) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * elem % 16 == 0; }
+
+template <typename X, typename Y, bool VEC>
+cudaError_t forward_rows(const NormCall& c, cudaStream_t s) {
+  const uint32_t cells = (c.dim + 7) / 8;
+  int k = 4;
+  if (c.rows * cells <= 148 * 1024) k = 1;
+  while (k < 4 && cells > uint32_t(k) * 1024) ++k;
+  if (k == 4)
+    while (k > 1 && cells <= 32u * (k - 1)) --k;            // short rows: no empty cells
+  const uint32_t tpr = (cells + 32 * k - 1) / (32 * k) * 32, rows = std::max(1u, 256 / tpr);
+  const dim3 grid(uint32_t((c.rows + rows - 1) / rows));
+#define FLS_K(K) (tpr > 256 ? launch(fls_norm_forward_kernel<X, Y, VEC, K, 1024>, grid, tpr * rows, 0, false, s, c, tpr) \
+                            : launch(fls_norm_forward_kernel<X, Y, VEC, K, 256>, grid, tpr * rows, 0, false, s, c, tpr))
+  return k == 1 ? FLS_K(1) : k == 2 ? FLS_K(2) : k == 3 ? FLS_K(3) : FLS_K(4);
+#undef FLS_K
+}
+
 template <typename X, typename Y>
-int run_forward(fls_norm* h, const NormCall& c, cudaStream_t s) {
-  FLS_LAUNCH(launch(fls_norm_rows_kernel<X, Y>, dim3(uint32_t(std::min<uint64_t>(c.rows, 148 * 64))), 256, false, s, c));
+int run_forward(fls_norm* h, NormCall& c, cudaStream_t s) {
+  if (c.dim <= 32768) {
+    const bool vec = c.dim % 8 == 0 && aligned(c.weight, 0, 0) && aligned(c.bias, 0, 0) && aligned(c.x, c.x_stride, sizeof(X)) && aligned(c.y, c.y_stride, sizeof(Y)) &&
+                     (!c.residual || (aligned(c.residual, c.residual_stride, sizeof(X)) && aligned(c.total, c.total_stride, sizeof(X))));
+    FLS_LAUNCH((vec ? forward_rows<X, Y, true>(c, s) : forward_rows<X, Y, false>(c, s)));
+    return FLS_OK;
+  }
+  FLS_LAUNCH(launch(fls_norm_rows_kernel<X, Y>, dim3(uint32_t(std::min<uint64_t>(c.rows, 148 * 64))), 256, 0, false, s, c));
   return FLS_OK;
+}
+
+template <typename X, typename Y, bool VEC, int K, int STAGES, int THREADS>
+cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
+  const uint32_t cells = (c.dim + 7) / 8, tpr = (cells + 32 * K - 1) / (32 * K) * 32, groups = THREADS / tpr, threads = tpr * groups;
+  c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(148, (c.rows + groups - 1) / groups)));
+  const uint32_t pieces = K * (sizeof(X) * (c.grad_total ? 2 : 1) + sizeof(Y)) / 2;
+  const uint32_t smem = std::max(VEC ? STAGES * pieces * threads * 16 : 0, (groups - 1) * tpr * 16 * K * 4);
+  auto kernel = fls_norm_backward_kernel<X, Y, VEC, K, STAGES, THREADS>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 << 10);
+  if (e != cudaSuccess) return e;
+  return launch(kernel, dim3(c.parts), threads, smem, false, s, c, tpr);
+}
+
+template <typename X, typename Y, bool VEC>
+cudaError_t backward_of(NormCall& c, cudaStream_t s) {
+  return c.dim <= 6144 ? backward_rows<X, Y, VEC, 1, 3, 768>(c, s) : backward_rows<X, Y, VEC, 2, 2, 512>(c, s);
 }
 
 template <typename X, typename Y>
 int run_backward(fls_norm* h, NormCall& c, cudaStream_t s) {
   const uint32_t tiles = (c.dim + kColTile - 1) / kColTile;
   bool dependent = false;
-  c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kMaxParts, (c.rows + 7) / 8, std::max<uint32_t>(1, 148 * 16 / tiles)})));
-  if (c.grad_x && c.rows) {
-    FLS_LAUNCH(launch(fls_norm_coef_kernel<X, Y>, dim3(uint32_t(std::min<uint64_t>(c.rows, 148 * 64))), 256, false, s, c));
-    dependent = true;
+  if (c.dim <= 8192) {
+    const bool vec = c.dim % 8 == 0 && aligned(c.weight, 0, 0) &&
+                     (!c.rows || (aligned(c.x, c.x_stride, sizeof(X)) && aligned(c.grad_y, c.grad_y_stride, sizeof(Y)) &&
+                                 (!c.grad_x || aligned(c.grad_x, c.grad_x_stride, sizeof(X))) &&
+                                 (!c.grad_total || aligned(c.grad_total, c.grad_total_stride, sizeof(X)))));
+    FLS_LAUNCH((vec ? backward_of<X, Y, true>(c, s) : backward_of<X, Y, false>(c, s)));
+  } else {
+    c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kMaxParts, (c.rows + 7) / 8, std::max<uint32_t>(1, 148 * 16 / tiles)})));
+    if (c.grad_x && c.rows) {
+      FLS_LAUNCH(launch(fls_norm_coef_kernel<X, Y>, dim3(uint32_t(std::min<uint64_t>(c.rows, 148 * 64))), 256, 0, false, s, c));
+      dependent = true;
+    }
+    FLS_LAUNCH(launch(fls_norm_columns_kernel<X, Y>, dim3(tiles, c.parts), 256, 0, dependent, s, c));
   }
-  FLS_LAUNCH(launch(fls_norm_columns_kernel<X, Y>, dim3(tiles, c.parts), 256, dependent, s, c));
-  if (c.grad_weight || c.grad_bias) FLS_LAUNCH(launch(fls_norm_join_kernel, dim3(tiles, 2), 256, true, s, c));
+  if (c.grad_weight || c.grad_bias) FLS_LAUNCH(launch(fls_norm_join_kernel, dim3(tiles, 2), 1024, 0, true, s, c));
   return FLS_OK;
 }
 
