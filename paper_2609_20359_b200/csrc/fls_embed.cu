@@ -39,6 +39,7 @@ struct EmbedCall {
   void* grad_weight; uint64_t grad_weight_stride;
   float scale;
   uint32_t accumulate;
+  uint32_t grad_size, zero_vec;   // bytes of an element; rows of grad_weight start on 16-byte boundaries
   uint32_t chunk, chunks;
   uint2* pairs[2];                // (key, position)
   uint32_t* counts;               // [radix][tiles]
@@ -197,6 +198,10 @@ __global__ void __launch_bounds__(kSortThreads) fls_embed_scatter_kernel(const _
 
 // ------------------------------------------------------------------------------------------------ rows without a token
 constexpr uint32_t kFillRows = 8192;                       // rows of one look at the tokens
+#ifndef FLS_FILL
+#define FLS_FILL 147
+#endif
+constexpr uint32_t kFillCtas = FLS_FILL;
 
 __device__ __forceinline__ uint32_t first_at_least(const uint2* pairs, uint32_t n, uint64_t key) {
   uint32_t lo = 0, len = n;
@@ -207,7 +212,19 @@ __device__ __forceinline__ uint32_t first_at_least(const uint2* pairs, uint32_t 
   return lo;
 }
 
-template <typename G, bool VEC>
+// Zeros to the rows v0 .. v1 - 1 whose bit in `there` is not set, a warp each.
+__device__ __forceinline__ void fill_rows(const EmbedCall& c, const uint32_t* there, uint64_t v0, uint64_t v1) {
+  const uint32_t lane = threadIdx.x % 32, warps = blockDim.x / 32;
+  for (uint64_t v = v0 + threadIdx.x / 32; v < v1; v += warps) {
+    const uint32_t r = uint32_t(v - v0);
+    if (there[r / 32] >> (r % 32) & 1) continue;
+    char* row = static_cast<char*>(c.grad_weight) + v * c.grad_weight_stride * c.grad_size;
+    const uint32_t bytes = c.dim * c.grad_size, whole = c.zero_vec ? bytes / 16 * 16 : 0;
+    for (uint32_t j = lane * 16; j < whole; j += 512) __stcs(reinterpret_cast<uint4*>(row + j), make_uint4(0, 0, 0, 0));
+    for (uint32_t j = whole + lane * 2; j < bytes; j += 64) *reinterpret_cast<uint16_t*>(row + j) = 0;
+  }
+}
+
 __global__ void __launch_bounds__(256) fls_embed_fill_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs, uint64_t rows_per_cta) {
   __shared__ uint32_t there[kFillRows / 32], range[2];
   pdl_launch();
@@ -217,23 +234,140 @@ __global__ void __launch_bounds__(256) fls_embed_fill_kernel(const __grid_consta
     const uint64_t v1 = min(end, v0 + kFillRows);
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kFillRows / 32; i += 256) there[i] = 0;
-    if (threadIdx.x < 2 && c.tokens) range[threadIdx.x] = first_at_least(pairs, uint32_t(c.tokens), threadIdx.x ? v1 : v0);
-    else if (threadIdx.x < 2) range[threadIdx.x] = 0;
+    if (threadIdx.x < 2) range[threadIdx.x] = c.tokens ? first_at_least(pairs, uint32_t(c.tokens), threadIdx.x ? v1 : v0) : 0;
     __syncthreads();
     for (uint32_t p = range[0] + threadIdx.x; p < range[1]; p += 256) {
       const uint32_t r = pairs[p].x - uint32_t(v0);
       atomicOr(&there[r / 32], 1u << (r % 32));
     }
     __syncthreads();
-    const float zero[8] = {};
-    for (uint64_t v = v0 + threadIdx.x / 32; v < v1; v += 8) {
-      const uint32_t r = uint32_t(v - v0);
-      if (there[r / 32] >> (r % 32) & 1) continue;
-      G* row = static_cast<G*>(c.grad_weight) + v * c.grad_weight_stride;
-      const uint32_t whole = VEC ? c.dim / 8 * 8 : 0;
-      for (uint32_t j = threadIdx.x % 32 * 8; j < whole; j += kSlab) Elem<G>::store8(row + j, zero);
-      for (uint32_t j = whole + threadIdx.x % 32; j < c.dim; j += 32) Elem<G>::put(row + j, 0.f);
+    fill_rows(c, there, v0, v1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sort of up to 2^17 tokens
+// The first cluster of the grid sorts while the others write zeros to the rows without a token, which they find for
+// themselves by looking through the tokens.  A warp of the sort owns up to 16 * 32 neighbouring positions; per pass it ranks
+// them among its own by digit, the CTA adds its warps up, and the CTAs of the cluster read each other's digit counts from
+// distributed shared memory.
+constexpr int kClusterThreads = 1024, kClusterRounds = 16;
+constexpr uint32_t kCluster = 8;
+constexpr uint32_t kOneCta = kClusterThreads * kClusterRounds;
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote_u32(const uint32_t* p, uint32_t rank) {
+  uint32_t a, x;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(a) : "memory");
+  return x;
+}
+
+struct SortShared {
+  uint16_t count[kClusterThreads / 32][kMaxRadix];   // of a warp, then of the warps before it
+  uint32_t total[kMaxRadix];                         // of the CTA, read by the cluster
+  uint32_t base[kMaxRadix];                          // where the CTA's first item of a digit goes
+  uint32_t scan[kMaxRadix / 32];
+};
+
+template <int ROUNDS>
+__device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, uint32_t bits, uint32_t passes, uint32_t ctas) {
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, rank = blockIdx.x, n = uint32_t(c.tokens);
+  const uint32_t per = (bits + passes - 1) / passes;
+  const uint32_t first = (rank * (kClusterThreads / 32) + warp) * (ROUNDS * 32) + lane;
+  for (uint32_t pass = 0; pass < passes; ++pass) {
+    const uint32_t shift = pass * per, radix = 1u << min(per, bits - shift);
+    uint2 item[ROUNDS];
+    uint32_t at[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const uint32_t i = first + r * 32;
+      item[r] = i >= n ? make_uint2(0, 0) : pass ? __ldcg(&c.pairs[(pass - 1) & 1][i]) : make_uint2(key_of(c, i), i);
     }
+    for (uint32_t d = threadIdx.x; d < kClusterThreads / 32 * kMaxRadix / 2; d += kClusterThreads) reinterpret_cast<uint32_t*>(sh.count)[d] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const bool in = first + r * 32 < n;
+      if (__any_sync(~0u, in)) {
+        const uint32_t d = in ? (item[r].x >> shift) & (radix - 1) : kMaxRadix;      // not a digit: apart from all others
+        const uint32_t same = __match_any_sync(~0u, d);
+        at[r] = in ? sh.count[warp][d] + __popc(same & ((1u << lane) - 1)) : 0;
+        __syncwarp();
+        if (in && (same >> lane) == 1) sh.count[warp][d] = uint16_t(at[r] + 1);      // the last of them
+        __syncwarp();
+      }
+    }
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < radix; d += kClusterThreads) {
+      uint32_t sum = 0;
+#pragma unroll 8
+      for (int w = 0; w < kClusterThreads / 32; ++w) {
+        const uint32_t k = sh.count[w][d];
+        sh.count[w][d] = uint16_t(sum);
+        sum += k;
+      }
+      sh.total[d] = sum;
+    }
+    if (ctas > 1) cluster_sync(); else __syncthreads();
+    uint32_t before = 0, all = 0, x = 0;
+    if (threadIdx.x < kMaxRadix) {
+      if (threadIdx.x < radix)
+        for (uint32_t q = 0; q < ctas; ++q) {
+          const uint32_t k = ctas > 1 ? remote_u32(&sh.total[threadIdx.x], q) : sh.total[threadIdx.x];
+          all += k;
+          if (q < rank) before += k;
+        }
+      x = all;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const uint32_t y = __shfl_up_sync(~0u, x, o);
+        if (lane >= o) x += y;
+      }
+      if (lane == 31) sh.scan[warp] = x;
+    }
+    __syncthreads();
+    if (threadIdx.x < radix) {
+      for (uint32_t w = 0; w < warp; ++w) before += sh.scan[w];
+      sh.base[threadIdx.x] = before + x - all;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      if (first + r * 32 >= n) continue;
+      const uint32_t d = (item[r].x >> shift) & (radix - 1);
+      c.pairs[pass & 1][sh.base[d] + sh.count[warp][d] + at[r]] = item[r];
+    }
+    if (ctas > 1) cluster_sync(); else __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(kClusterThreads, 1)
+    fls_embed_sort_kernel(const __grid_constant__ EmbedCall c, uint32_t bits, uint32_t passes, uint32_t ctas, uint64_t rows_per_cta) {
+  __shared__ union { SortShared sort; uint32_t there[kFillRows / 32]; } sh;
+  pdl_launch();
+  if (blockIdx.x < ctas) {
+    const uint32_t rounds = uint32_t((c.tokens + ctas * kClusterThreads - 1) / (ctas * kClusterThreads));
+    if (rounds <= 1) sort_tokens<1>(c, sh.sort, bits, passes, ctas);
+    else if (rounds <= 4) sort_tokens<4>(c, sh.sort, bits, passes, ctas);
+    else if (rounds <= 8) sort_tokens<8>(c, sh.sort, bits, passes, ctas);
+    else sort_tokens<16>(c, sh.sort, bits, passes, ctas);
+    return;
+  }
+  const uint64_t begin = (blockIdx.x - ctas) * rows_per_cta, end = min(c.vocab, begin + rows_per_cta);
+  for (uint64_t v0 = begin; v0 < end; v0 += kFillRows) {
+    const uint64_t v1 = min(end, v0 + kFillRows);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kFillRows / 32; i += kClusterThreads) sh.there[i] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < uint32_t(c.tokens); i += kClusterThreads) {
+      const uint32_t v = key_of(c, i);
+      if (v >= v0 && v < v1) atomicOr(&sh.there[(v - uint32_t(v0)) / 32], 1u << ((v - uint32_t(v0)) % 32));
+    }
+    __syncthreads();
+    fill_rows(c, sh.there, v0, v1);
   }
 }
 
@@ -371,17 +505,24 @@ __global__ void __launch_bounds__(256) fls_embed_join_kernel(const __grid_consta
 
 // ------------------------------------------------------------------------------------------------ host
 template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
+cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, uint32_t cluster, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.stream = s;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = dependent ? 1 : 0;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute at[2] = {};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = dependent ? 1 : 0;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
+  return launch_clusters(kernel, grid, 1, threads, dependent, s, args...);
 }
 
 struct Regions { uint64_t pairs[2], counts, part, total; };
@@ -474,12 +615,22 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
   const uint64_t n = c.tokens;
   uint32_t bits = 1, at = 0;
   const uint2* sorted = nullptr;
-  bool dependent = false;
-  if (n) {
-    while (c.vocab >> bits) ++bits;                       // of keys 0 .. V
-    const uint32_t passes = (bits + 8) / 9, per = (bits + passes - 1) / passes;
+  while (c.vocab >> bits) ++bits;                         // of keys 0 .. V
+  const uint32_t passes = (bits + 8) / 9, per = (bits + passes - 1) / passes;
+  if (n && n <= uint64_t(kOneCta) * kCluster) {
+    const uint32_t ctas = n <= kOneCta ? 1 : kCluster;
+    uint64_t per_cta = 0;
+    uint32_t fill = 0;
+    if (!c.accumulate) {
+      per_cta = std::max<uint64_t>(1, (c.vocab + kFillCtas - 1) / kFillCtas);
+      fill = uint32_t(up((c.vocab + per_cta - 1) / per_cta, ctas));
+    }
+    FLS_LAUNCH(launch_clusters(fls_embed_sort_kernel, ctas + fill, ctas, kClusterThreads, false, s, c, bits, passes, ctas, per_cta));
+    sorted = c.pairs[(passes - 1) & 1];
+  } else {
+    bool dependent = false;
     c.tiles = uint32_t((n + kSortTile - 1) / kSortTile);
-    for (uint32_t p = 0; p < passes; ++p) {
+    for (uint32_t p = 0; n && p < passes; ++p) {
       const SortPass sp{p * per, std::min(per, bits - p * per), p == 0, at};
       FLS_LAUNCH(launch(fls_embed_count_kernel, c.tiles, kSortThreads, dependent, s, c, sp));
       dependent = true;
@@ -488,11 +639,11 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
       at ^= 1;
     }
     sorted = c.pairs[at];
-  }
-  if (!c.accumulate) {
-    const uint64_t per_cta = std::max<uint64_t>(1, (c.vocab + 148 * 8 - 1) / (148 * 8));
-    const uint32_t ctas = uint32_t((c.vocab + per_cta - 1) / per_cta);
-    FLS_LAUNCH((launch(fls_embed_fill_kernel<G, VEC>, ctas, 256, dependent, s, c, sorted, per_cta)));
+    if (!c.accumulate) {
+      const uint64_t per_cta = std::max<uint64_t>(1, (c.vocab + 148 * 8 - 1) / (148 * 8));
+      const uint32_t ctas = uint32_t((c.vocab + per_cta - 1) / per_cta);
+      FLS_LAUNCH((launch(fls_embed_fill_kernel, ctas, 256, dependent, s, c, sorted, per_cta)));
+    }
   }
   if (n) {
     c.chunk = chunk_of(n);
@@ -573,7 +724,9 @@ int fls_embed_grad(fls_embed* e, const fls_embed_io* io, void* cuda_stream) {
   for (int i = 0; i < 2; ++i) c.pairs[i] = reinterpret_cast<uint2*>(ws + e->reg.pairs[i]);
   c.counts = reinterpret_cast<uint32_t*>(ws + e->reg.counts);
   c.part = reinterpret_cast<float*>(ws + e->reg.part);
-  const bool vec = cells(c.grad_weight, c.grad_weight_stride, gs) && (!n || cells(c.grad_out, c.grad_out_stride, es));
+  c.grad_size = uint32_t(gs);
+  c.zero_vec = cells(c.grad_weight, c.grad_weight_stride, gs);
+  const bool vec = c.zero_vec && (!n || cells(c.grad_out, c.grad_out_stride, es));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (d.act_dtype == FLS_GRAD_F32) {
     if (d.grad_dtype == FLS_GRAD_F32) return vec ? run_grad<float, float, true>(e, c, st) : run_grad<float, float, false>(e, c, st);
