@@ -24,6 +24,22 @@ constexpr int kSortThreads = 256, kSortRounds = 16;
 constexpr uint32_t kSortTile = kSortThreads * kSortRounds;   // positions per CTA of the sort
 constexpr uint32_t kMaxRadix = 512;
 constexpr uint32_t kMaxChunks = 2048;
+#ifndef FLS_WARPS
+#define FLS_WARPS 2400
+#endif
+#ifndef FLS_ONE
+#define FLS_ONE 2048
+#endif
+#ifndef FLS_SCAN
+#define FLS_SCAN 16384
+#endif
+#ifndef FLS_F
+#define FLS_F 512
+#endif
+#ifndef FLS_JOINMB
+#define FLS_JOINMB 16ull
+#endif
+constexpr uint64_t kWarpsWanted = FLS_WARPS;
 constexpr uint32_t kSlab = 256;                              // columns of a warp: eight per lane
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
@@ -46,6 +62,10 @@ struct EmbedCall {
   uint32_t tiles;
   float* part;                    // [2 * chunks][dp]: of the token a chunk begins with, of the one it ends with
 };
+
+// Rows begin .. end - 1 of grad_weight, per_cta to each of `ctas` CTAs, of which a kernel sets those without a token to zero.
+// wait: the CTAs take the tokens from the sort; otherwise they look through them and wait for nothing.
+struct FillShare { uint64_t begin, end, per_cta; uint32_t ctas, wait; };
 
 // V stands for a position that takes no part: ignored, or outside the table.
 __device__ __forceinline__ uint32_t key_of(const EmbedCall& c, uint64_t i) {
@@ -96,6 +116,19 @@ __global__ void __launch_bounds__(256) fls_embed_lookup_kernel(const __grid_cons
 
 // ------------------------------------------------------------------------------------------------ sort
 // One pass sorts by `bits` bits of the key from `shift` on; the first takes its keys from the tokens.
+// The lanes with the same digit of `bits` bits among those that take part.  (Ballots: a match instruction takes the longer the
+// more different digits a warp holds.)
+__device__ __forceinline__ uint32_t same_digit(bool in, uint32_t d, uint32_t bits) {
+  uint32_t same = __ballot_sync(~0u, in);
+#pragma unroll
+  for (int b = 0; b < 9; ++b)
+    if (b < bits) {
+      const uint32_t set = __ballot_sync(~0u, d >> b & 1);
+      same &= d >> b & 1 ? set : ~set;
+    }
+  return same;
+}
+
 struct SortPass { uint32_t shift, bits, first, from; };
 
 __device__ __forceinline__ uint2 sort_item(const EmbedCall& c, const SortPass& p, uint64_t i) {
@@ -172,8 +205,7 @@ __global__ void __launch_bounds__(kSortThreads) fls_embed_scatter_kernel(const _
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const bool in = first + r * 32 + lane < c.tokens;
-    const uint32_t d = in ? (item[r].x >> p.shift) & (radix - 1) : kMaxRadix;     // not a digit: apart from all others
-    const uint32_t same = __match_any_sync(~0u, d);
+    const uint32_t d = (item[r].x >> p.shift) & (radix - 1), same = same_digit(in, d, p.bits);
     rank[r] = in ? count[warp][d] + __popc(same & ((1u << lane) - 1)) : 0;
     __syncwarp();
     if (in && (same >> lane) == 1) count[warp][d] = rank[r] + 1;                  // the last of them
@@ -198,61 +230,85 @@ __global__ void __launch_bounds__(kSortThreads) fls_embed_scatter_kernel(const _
 
 // ------------------------------------------------------------------------------------------------ rows without a token
 constexpr uint32_t kFillRows = 8192;                       // rows of one look at the tokens
-#ifndef FLS_FILL
-#define FLS_FILL 147
-#endif
-constexpr uint32_t kFillCtas = FLS_FILL;
 
+// The first of n sorted pairs whose key is at least `key`, found by a warp that looks at 32 places at once.
 __device__ __forceinline__ uint32_t first_at_least(const uint2* pairs, uint32_t n, uint64_t key) {
-  uint32_t lo = 0, len = n;
+  const uint32_t lane = threadIdx.x % 32;
+  uint32_t lo = 0, len = n;                                 // the place is in lo .. lo + len
   while (len) {
-    const uint32_t half = len / 2;
-    if (pairs[lo + half].x < key) { lo += half + 1; len -= half + 1; } else len = half;
+    const uint32_t step = (len + 31) / 32, p = lo + lane * step;
+    const uint32_t below = __popc(__ballot_sync(~0u, p < lo + len && pairs[p].x < key));   // a prefix of the lanes
+    if (!below) return lo;
+    const uint32_t end = lo + len;
+    lo += (below - 1) * step + 1;
+    len = min(step - 1, end - lo);
   }
   return lo;
 }
 
+struct FillShared { uint32_t there[kFillRows / 32]; };
+
 // Zeros to the rows v0 .. v1 - 1 whose bit in `there` is not set, a warp each.
-__device__ __forceinline__ void fill_rows(const EmbedCall& c, const uint32_t* there, uint64_t v0, uint64_t v1) {
+__device__ __forceinline__ void fill_rows(const EmbedCall& c, const FillShared& sh, uint64_t v0, uint64_t v1) {
   const uint32_t lane = threadIdx.x % 32, warps = blockDim.x / 32;
+  const uint32_t bytes = c.dim * c.grad_size, whole = c.zero_vec ? bytes / 16 * 16 : 0;
   for (uint64_t v = v0 + threadIdx.x / 32; v < v1; v += warps) {
     const uint32_t r = uint32_t(v - v0);
-    if (there[r / 32] >> (r % 32) & 1) continue;
+    if (sh.there[r / 32] >> (r % 32) & 1) continue;
     char* row = static_cast<char*>(c.grad_weight) + v * c.grad_weight_stride * c.grad_size;
-    const uint32_t bytes = c.dim * c.grad_size, whole = c.zero_vec ? bytes / 16 * 16 : 0;
+#pragma unroll 4
     for (uint32_t j = lane * 16; j < whole; j += 512) __stcs(reinterpret_cast<uint4*>(row + j), make_uint4(0, 0, 0, 0));
     for (uint32_t j = whole + lane * 2; j < bytes; j += 64) *reinterpret_cast<uint16_t*>(row + j) = 0;
   }
 }
 
-__global__ void __launch_bounds__(256) fls_embed_fill_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs, uint64_t rows_per_cta) {
-  __shared__ uint32_t there[kFillRows / 32], range[2];
-  pdl_launch();
-  pdl_wait();
-  const uint64_t begin = blockIdx.x * rows_per_cta, end = min(c.vocab, begin + rows_per_cta);
+// The rows without a token among those of one CTA of a kernel: CTA `index` of `share.ctas`.  The tokens that fall there are
+// those that the sort has put side by side, or, beside the sort itself (pairs null), found by looking through all.
+__device__ __forceinline__ void fill_part(const EmbedCall& c, const FillShare& share, uint32_t index, const uint2* pairs, FillShared& sh) {
+  const uint64_t begin = share.begin + index * share.per_cta, end = min(share.end, begin + share.per_cta);
   for (uint64_t v0 = begin; v0 < end; v0 += kFillRows) {
     const uint64_t v1 = min(end, v0 + kFillRows);
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kFillRows / 32; i += 256) there[i] = 0;
-    if (threadIdx.x < 2) range[threadIdx.x] = c.tokens ? first_at_least(pairs, uint32_t(c.tokens), threadIdx.x ? v1 : v0) : 0;
+    for (uint32_t i = threadIdx.x; i < kFillRows / 32; i += blockDim.x) sh.there[i] = 0;
     __syncthreads();
-    for (uint32_t p = range[0] + threadIdx.x; p < range[1]; p += 256) {
-      const uint32_t r = pairs[p].x - uint32_t(v0);
-      atomicOr(&there[r / 32], 1u << (r % 32));
+    if (pairs) {
+      const uint32_t last = first_at_least(pairs, uint32_t(c.tokens), v1);
+      for (uint32_t p = first_at_least(pairs, uint32_t(c.tokens), v0) + threadIdx.x; p < last; p += blockDim.x) {
+        const uint32_t r = pairs[p].x - uint32_t(v0);
+        atomicOr(&sh.there[r / 32], 1u << (r % 32));
+      }
+    } else {
+      for (uint32_t base = threadIdx.x; base < uint32_t(c.tokens); base += 8 * blockDim.x) {
+        uint32_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const uint32_t i = base + u * blockDim.x;
+          v[u] = i < uint32_t(c.tokens) ? key_of(c, i) : uint32_t(c.vocab);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (v[u] >= v0 && v[u] < v1) atomicOr(&sh.there[(v[u] - uint32_t(v0)) / 32], 1u << ((v[u] - uint32_t(v0)) % 32));
+      }
     }
     __syncthreads();
-    fill_rows(c, there, v0, v1);
+    fill_rows(c, sh, v0, v1);
   }
 }
 
+__global__ void __launch_bounds__(256) fls_embed_fill_kernel(const __grid_constant__ EmbedCall c, const FillShare share, const uint2* pairs) {
+  __shared__ FillShared sh;
+  pdl_launch();
+  pdl_wait();
+  fill_part(c, share, blockIdx.x, pairs, sh);
+}
+
 // ------------------------------------------------------------------------------------------------ sort of up to 2^17 tokens
-// The first cluster of the grid sorts while the others write zeros to the rows without a token, which they find for
-// themselves by looking through the tokens.  A warp of the sort owns up to 16 * 32 neighbouring positions; per pass it ranks
+// By the CTAs of one cluster.  A warp owns up to 16 * 32 neighbouring positions; per pass it ranks
 // them among its own by digit, the CTA adds its warps up, and the CTAs of the cluster read each other's digit counts from
 // distributed shared memory.
 constexpr int kClusterThreads = 1024, kClusterRounds = 16;
 constexpr uint32_t kCluster = 8;
-constexpr uint32_t kOneCta = kClusterThreads * kClusterRounds;
+constexpr uint32_t kSortAtOnce = kCluster * kClusterThreads * kClusterRounds;
 
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -265,6 +321,12 @@ __device__ __forceinline__ uint32_t remote_u32(const uint32_t* p, uint32_t rank)
   return x;
 }
 
+__device__ __forceinline__ void remote_store(const uint2* p, uint32_t rank, uint2 x) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(uint32_t(__cvta_generic_to_shared(p))), "r"(rank));
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(x.x), "r"(x.y) : "memory");
+}
+
 struct SortShared {
   uint16_t count[kClusterThreads / 32][kMaxRadix];   // of a warp, then of the warps before it
   uint32_t total[kMaxRadix];                         // of the CTA, read by the cluster
@@ -273,7 +335,7 @@ struct SortShared {
 };
 
 template <int ROUNDS>
-__device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, uint32_t bits, uint32_t passes, uint32_t ctas) {
+__device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, uint2* items, uint32_t bits, uint32_t passes, uint32_t ctas) {
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, rank = blockIdx.x, n = uint32_t(c.tokens);
   const uint32_t per = (bits + passes - 1) / passes;
   const uint32_t first = (rank * (kClusterThreads / 32) + warp) * (ROUNDS * 32) + lane;
@@ -284,7 +346,7 @@ __device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, 
 #pragma unroll
     for (int r = 0; r < ROUNDS; ++r) {
       const uint32_t i = first + r * 32;
-      item[r] = i >= n ? make_uint2(0, 0) : pass ? __ldcg(&c.pairs[(pass - 1) & 1][i]) : make_uint2(key_of(c, i), i);
+      item[r] = i >= n ? make_uint2(0, 0) : pass ? items[(warp * ROUNDS + r) * 32 + lane] : make_uint2(key_of(c, i), i);
     }
     for (uint32_t d = threadIdx.x; d < kClusterThreads / 32 * kMaxRadix / 2; d += kClusterThreads) reinterpret_cast<uint32_t*>(sh.count)[d] = 0;
     __syncthreads();
@@ -292,8 +354,7 @@ __device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, 
     for (int r = 0; r < ROUNDS; ++r) {
       const bool in = first + r * 32 < n;
       if (__any_sync(~0u, in)) {
-        const uint32_t d = in ? (item[r].x >> shift) & (radix - 1) : kMaxRadix;      // not a digit: apart from all others
-        const uint32_t same = __match_any_sync(~0u, d);
+        const uint32_t d = (item[r].x >> shift) & (radix - 1), same = same_digit(in, d, per);
         at[r] = in ? sh.count[warp][d] + __popc(same & ((1u << lane) - 1)) : 0;
         __syncwarp();
         if (in && (same >> lane) == 1) sh.count[warp][d] = uint16_t(at[r] + 1);      // the last of them
@@ -302,12 +363,14 @@ __device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, 
     }
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < radix; d += kClusterThreads) {
+      uint16_t k[kClusterThreads / 32];
+#pragma unroll
+      for (int w = 0; w < kClusterThreads / 32; ++w) k[w] = sh.count[w][d];
       uint32_t sum = 0;
-#pragma unroll 8
+#pragma unroll
       for (int w = 0; w < kClusterThreads / 32; ++w) {
-        const uint32_t k = sh.count[w][d];
         sh.count[w][d] = uint16_t(sum);
-        sum += k;
+        sum += k[w];
       }
       sh.total[d] = sum;
     }
@@ -315,11 +378,20 @@ __device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, 
     uint32_t before = 0, all = 0, x = 0;
     if (threadIdx.x < kMaxRadix) {
       if (threadIdx.x < radix)
-        for (uint32_t q = 0; q < ctas; ++q) {
-          const uint32_t k = ctas > 1 ? remote_u32(&sh.total[threadIdx.x], q) : sh.total[threadIdx.x];
-          all += k;
-          if (q < rank) before += k;
+      {
+        if (ctas == 1) {
+          all = sh.total[threadIdx.x];
+        } else {
+          uint32_t k[kCluster];
+#pragma unroll
+          for (uint32_t q = 0; q < kCluster; ++q) k[q] = remote_u32(&sh.total[threadIdx.x], q);
+#pragma unroll
+          for (uint32_t q = 0; q < kCluster; ++q) {
+            all += k[q];
+            if (q < rank) before += k[q];
+          }
         }
+      }
       x = all;
 #pragma unroll
       for (int o = 1; o < 32; o *= 2) {
@@ -338,146 +410,212 @@ __device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, 
     for (int r = 0; r < ROUNDS; ++r) {
       if (first + r * 32 >= n) continue;
       const uint32_t d = (item[r].x >> shift) & (radix - 1);
-      c.pairs[pass & 1][sh.base[d] + sh.count[warp][d] + at[r]] = item[r];
+      const uint32_t to = sh.base[d] + sh.count[warp][d] + at[r];
+      if (pass + 1 == passes) c.pairs[0][to] = item[r];
+      else if (ctas == 1) items[to] = item[r];
+      else remote_store(items + to % (ROUNDS * kClusterThreads), to / (ROUNDS * kClusterThreads), item[r]);
     }
     if (ctas > 1) cluster_sync(); else __syncthreads();
   }
 }
 
 __global__ void __launch_bounds__(kClusterThreads, 1)
-    fls_embed_sort_kernel(const __grid_constant__ EmbedCall c, uint32_t bits, uint32_t passes, uint32_t ctas, uint64_t rows_per_cta) {
-  __shared__ union { SortShared sort; uint32_t there[kFillRows / 32]; } sh;
+    fls_embed_sort_kernel(const __grid_constant__ EmbedCall c, uint32_t bits, uint32_t passes) {
+  __shared__ SortShared sh;
+  extern __shared__ uint2 items[];                          // of the CTA, between two passes
   pdl_launch();
-  if (blockIdx.x < ctas) {
-    const uint32_t rounds = uint32_t((c.tokens + ctas * kClusterThreads - 1) / (ctas * kClusterThreads));
-    if (rounds <= 1) sort_tokens<1>(c, sh.sort, bits, passes, ctas);
-    else if (rounds <= 4) sort_tokens<4>(c, sh.sort, bits, passes, ctas);
-    else if (rounds <= 8) sort_tokens<8>(c, sh.sort, bits, passes, ctas);
-    else sort_tokens<16>(c, sh.sort, bits, passes, ctas);
-    return;
-  }
-  const uint64_t begin = (blockIdx.x - ctas) * rows_per_cta, end = min(c.vocab, begin + rows_per_cta);
-  for (uint64_t v0 = begin; v0 < end; v0 += kFillRows) {
-    const uint64_t v1 = min(end, v0 + kFillRows);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kFillRows / 32; i += kClusterThreads) sh.there[i] = 0;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < uint32_t(c.tokens); i += kClusterThreads) {
-      const uint32_t v = key_of(c, i);
-      if (v >= v0 && v < v1) atomicOr(&sh.there[(v - uint32_t(v0)) / 32], 1u << ((v - uint32_t(v0)) % 32));
-    }
-    __syncthreads();
-    fill_rows(c, sh.there, v0, v1);
-  }
+  const uint32_t ctas = gridDim.x, rounds = uint32_t((c.tokens + ctas * kClusterThreads - 1) / (ctas * kClusterThreads));
+  if (rounds <= 1) sort_tokens<1>(c, sh, items, bits, passes, ctas);
+  else if (rounds <= 2) sort_tokens<2>(c, sh, items, bits, passes, ctas);
+  else if (rounds <= 4) sort_tokens<4>(c, sh, items, bits, passes, ctas);
+  else if (rounds <= 8) sort_tokens<8>(c, sh, items, bits, passes, ctas);
+  else sort_tokens<16>(c, sh, items, bits, passes, ctas);
 }
 
 // ------------------------------------------------------------------------------------------------ sums
-// The eight columns of a lane: neighbours (VEC) or 32 apart.
-template <bool VEC>
-__device__ __forceinline__ uint32_t column(uint32_t slab, uint32_t lane, int j) {
-  return slab * kSlab + (VEC ? lane * 8 + j : lane + 32 * j);
-}
+// The eight columns of a lane are neighbours where every row starts on a 16-byte boundary and holds whole cells (VEC),
+// otherwise 32 apart.
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_columns(const T* row, uint32_t slab, uint32_t lane, uint32_t dim, float (&x)[8]) {
-  const uint32_t col = column<VEC>(slab, lane, 0);
-  if (VEC && col + 8 <= dim) {
-    load8(row + col, x);
-    return;
+// The columns of one row as they lie in memory.
+template <typename T, bool VEC> struct Piece;
+template <typename T> struct Piece<T, true> {
+  typename Elem<T>::Raw raw;
+  __device__ __forceinline__ void load(const T* row, uint32_t col, uint32_t dim) {
+    raw = typename Elem<T>::Raw{};
+    if (col < dim) raw = Elem<T>::load_raw(row + col);
   }
+  __device__ __forceinline__ void get(float (&x)[8]) const { Elem<T>::unpack(raw, x); }
+};
+template <typename T> struct Piece<T, false> {
+  float x_[8];
+  __device__ __forceinline__ void load(const T* row, uint32_t col, uint32_t dim) {
+    row += col;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t k = column<VEC>(slab, lane, j);
-    x[j] = k < dim ? Elem<T>::get(row + k) : 0.f;
+    for (int j = 0; j < 8; ++j) x_[j] = col + 32 * j < dim ? Elem<T>::get(row + 32 * j) : 0.f;
   }
-}
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = x_[j];
+  }
+};
 
+// old: what is there, with accumulate.
 template <typename G, bool VEC>
-__device__ __forceinline__ void write_row(const EmbedCall& c, uint32_t key, uint32_t slab, uint32_t lane, const float (&sum)[8]) {
+__device__ __forceinline__ void write_row(const EmbedCall& c, uint32_t key, uint32_t col, const float (&sum)[8], const Piece<G, VEC>& old) {
+  if (col >= c.dim) return;
   G* row = static_cast<G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride;
   float x[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = sum[j] * c.scale;
   if (c.accumulate) {
-    float old[8];
-    load_columns<G, VEC>(row, slab, lane, c.dim, old);
+    float o[8];
+    old.get(o);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] += old[j];
+    for (int j = 0; j < 8; ++j) x[j] += o[j];
   }
-  const uint32_t col = column<VEC>(slab, lane, 0);
-  if (VEC && col + 8 <= c.dim) {
+  if constexpr (VEC) {
     Elem<G>::store8(row + col, x);
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t k = column<VEC>(slab, lane, j);
-    if (k < c.dim) Elem<G>::put(row + k, x[j]);
+    for (int j = 0; j < 8; ++j)
+      if (col + 32 * j < c.dim) Elem<G>::put(row + col + 32 * j, x[j]);
   }
 }
 
+// Partial sums of a warp's 256 columns: eight neighbours per lane.
+__device__ __forceinline__ void write_part(const EmbedCall& c, uint32_t row, uint32_t slab, uint32_t lane, const float (&sum)[8]) {
+  Elem<float>::store8(c.part + uint64_t(row) * c.dp + slab * kSlab + lane * 8, sum);
+}
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ uint4 shared16(uint32_t from) {
+  uint4 x;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(from) : "memory");
+  return x;
+}
+
+// A warp takes a chunk and 256 columns.  VEC: kAhead rows, and what is there of the rows that they finish, are on their way at
+// once, copied asynchronously into shared memory, where a lane reads only what it copied itself.
+constexpr int kAhead = 8;
+
 template <typename T, typename G, bool VEC>
-__global__ void __launch_bounds__(256) fls_embed_sum_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs) {
-  const uint32_t lane = threadIdx.x % 32, chunk = blockIdx.x * 8 + threadIdx.x / 32, slab = blockIdx.y;
+__global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs, const FillShare share) {
+  constexpr int kT = sizeof(T) / 2, kG = sizeof(G) / 2;     // 16-byte pieces of a lane's columns
+  extern __shared__ uint4 rows[];
+  __shared__ FillShared sh;
   pdl_launch();
+  // first two CTAs of zeros for every SM, then the sums, then the other zeros
+  const uint32_t ahead = min(share.ctas, 296u), sums = gridDim.x - share.ctas;
+  if (blockIdx.x < ahead || blockIdx.x >= ahead + sums) {
+    if (share.wait) pdl_wait();
+    fill_part(c, share, blockIdx.x < ahead ? blockIdx.x : blockIdx.x - sums, share.wait ? pairs : nullptr, sh);
+    return;
+  }
   pdl_wait();
+  const uint32_t block = blockIdx.x - ahead;
+  const uint32_t lane = threadIdx.x % 32, slabs = c.dp / kSlab, unit = block * 8 + threadIdx.x / 32;
+  const uint32_t chunk = unit / slabs, slab = unit - chunk * slabs;
   if (chunk >= c.chunks) return;
   const uint32_t n = uint32_t(c.tokens), none = uint32_t(c.vocab);
-  const uint32_t begin = chunk * c.chunk, end = min(n, begin + c.chunk);
+  const uint32_t begin = chunk * c.chunk, end = min(n, begin + c.chunk), col = slab * kSlab + (VEC ? lane * 8 : lane);
+  const uint32_t pieces = kT + (c.accumulate ? kG : 0), step = 256 * 16;
+  const uint32_t place = uint32_t(__cvta_generic_to_shared(rows)) + threadIdx.x * 16;
   float sum[8] = {};
-  uint32_t now = pairs[begin].x;
-  if (now == none) return;
-  bool from_left = begin > 0 && pairs[begin - 1].x == now;
-  for (uint32_t p0 = begin; p0 < end; p0 += 8) {
-    uint2 pair[8];
-    float x[8][8];
+  const uint32_t first = pairs[begin].x, left = begin ? pairs[begin - 1].x : none, right = end < n ? pairs[end].x : none;
+  if (first == none) return;
+  bool from_left = left == first;
+  uint32_t now = first;
+  for (uint32_t base = begin; base < end; base += 64) {
+    // 64 positions, two per lane, and the key behind each
+    const uint32_t here = min(64u, end - base);
+    const uint2 lo = lane < here ? pairs[base + lane] : make_uint2(none, 0), hi = lane + 32 < here ? pairs[base + lane + 32] : make_uint2(none, 0);
+    const uint32_t behind = base + here < end ? pairs[base + here].x : right;
+    uint32_t lo_next = __shfl_down_sync(~0u, lo.x, 1), hi_next = __shfl_down_sync(~0u, hi.x, 1);
+    const uint32_t hi_first = __shfl_sync(~0u, hi.x, 0);
+    if (lane == 31) lo_next = hi_first;
+    if (lane + 1 >= here) lo_next = behind;
+    if (lane + 33 >= here) hi_next = behind;
+    auto key_at = [&](uint32_t i) { return __shfl_sync(~0u, i < 32 ? lo.x : hi.x, i); };
+    auto row_at = [&](uint32_t i) { return __shfl_sync(~0u, i < 32 ? lo.y : hi.y, i); };
+    auto next_at = [&](uint32_t i) { return __shfl_sync(~0u, i < 32 ? lo_next : hi_next, i); };
+    auto send = [&](uint32_t i) {
+      if (i < here) {
+        const uint32_t key = key_at(i), row = row_at(i), next = next_at(i);
+        if (key != none && col < c.dim) {
+          uint32_t to = place + i % kAhead * pieces * step;
+          const uint4* x = reinterpret_cast<const uint4*>(static_cast<const T*>(c.grad_out) + row * c.grad_out_stride + col);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      pair[u] = p0 + u < end ? pairs[p0 + u] : make_uint2(none, 0);
-      if (pair[u].x != none) load_columns<T, VEC>(static_cast<const T*>(c.grad_out) + pair[u].y * c.grad_out_stride, slab, lane, c.dim, x[u]);
-    }
+          for (int p = 0; p < kT; ++p, to += step) copy16(to, x + p);
+          if (c.accumulate && key != next) {
+            const uint4* g = reinterpret_cast<const uint4*>(static_cast<const G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride + col);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      if (p0 + u >= end) break;
-      if (pair[u].x != now) {
+            for (int p = 0; p < kG; ++p, to += step) copy16(to, g + p);
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if constexpr (VEC)
+      for (int i = 0; i + 1 < kAhead; ++i) send(i);
+    for (uint32_t i = 0; i < here; ++i) {
+      const uint32_t key = key_at(i), next = next_at(i);
+      if (key == none) return;                              // nothing follows
+      Piece<T, VEC> x;
+      Piece<G, VEC> old;
+      uint32_t from = place + i % kAhead * pieces * step;
+      if constexpr (VEC) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
+#pragma unroll
+        for (int p = 0; p < kT; ++p, from += step) reinterpret_cast<uint4*>(&x.raw)[p] = shared16(from);
+      } else {
+        x.load(static_cast<const T*>(c.grad_out) + row_at(i) * c.grad_out_stride, col, c.dim);
+        if (c.accumulate && key != next) old.load(static_cast<const G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride, col, c.dim);
+      }
+      float v[8];
+      x.get(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[j];
+      now = key;
+      if (key != next) {
         if (from_left) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) c.part[uint64_t(2 * chunk) * c.dp + column<VEC>(slab, lane, j)] = sum[j];
+          write_part(c, 2 * chunk, slab, lane, sum);
         } else {
-          write_row<G, VEC>(c, now, slab, lane, sum);
+          if constexpr (VEC)
+            if (c.accumulate)
+#pragma unroll
+              for (int p = 0; p < kG; ++p, from += step) reinterpret_cast<uint4*>(&old.raw)[p] = shared16(from);
+          write_row<G, VEC>(c, key, col, sum, old);
         }
         from_left = false;
-        now = pair[u].x;
-        if (now == none) return;                            // nothing follows
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.f;
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += x[u][j];
+      if constexpr (VEC) send(i + kAhead - 1);              // into the place that the row before this one had
     }
+    if constexpr (VEC) asm volatile("cp.async.wait_all;" ::: "memory");
   }
-  const bool to_right = end < n && pairs[end].x == now;
-  if (!from_left && !to_right) {
-    write_row<G, VEC>(c, now, slab, lane, sum);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) c.part[uint64_t(2 * chunk + (from_left ? 0 : 1)) * c.dp + column<VEC>(slab, lane, j)] = sum[j];
+  if (right != none && right == now) write_part(c, 2 * chunk + (from_left ? 0 : 1), slab, lane, sum);
 }
 
-// A CTA for every chunk whose last token begins in it and goes on in the next: the sums of that token, in order of the chunks
-// inside each of eight warps, then of the warps.
+// A CTA for every chunk whose last token begins in it and goes on in the next: the sums of that token.  Up to eight are added
+// up in order, a warp for every 256 columns; more of them in order inside each of eight warps, then of the warps.
 template <typename G, bool VEC>
-__global__ void __launch_bounds__(256) fls_embed_join_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs) {
-  __shared__ float sums[8][kSlab];
-  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, chunk = blockIdx.x, slab = blockIdx.y;
-  const uint32_t n = uint32_t(c.tokens), none = uint32_t(c.vocab);
+__global__ void __launch_bounds__(256, 4) fls_embed_join_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs, const FillShare share) {
+  __shared__ union { float sums[8][kSlab]; FillShared fill; } sh;
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, slabs = c.dp / kSlab;
+  if (blockIdx.x < share.ctas) {
+    if (share.wait) pdl_wait();
+    fill_part(c, share, blockIdx.x, share.wait ? pairs : nullptr, sh.fill);
+    return;
+  }
   pdl_wait();
+  const uint32_t chunk = blockIdx.x - share.ctas, n = uint32_t(c.tokens), none = uint32_t(c.vocab);
   const uint32_t begin = chunk * c.chunk, end = begin + c.chunk;
   if (end >= n) return;
-  const uint32_t key = pairs[end].x;
-  if (key == none || pairs[end - 1].x != key) return;
-  if (pairs[begin].x == key && begin > 0 && pairs[begin - 1].x == key) return;   // began before this chunk
+  const uint32_t key = pairs[end].x, last = pairs[end - 1].x, first = pairs[begin].x, left = begin ? pairs[begin - 1].x : none;
+  if (key == none || last != key || (first == key && left == key)) return;       // nothing goes on, or began before this chunk
   uint32_t more = 0;                                                             // chunks after this one that begin with the token
   for (;;) {
     const uint64_t p = uint64_t(end) + uint64_t(more + threadIdx.x) * c.chunk;
@@ -485,30 +623,50 @@ __global__ void __launch_bounds__(256) fls_embed_join_kernel(const __grid_consta
     more += got;
     if (got < 256) break;
   }
-  float sum[8] = {};
-  for (uint32_t k = warp; k <= more; k += 8) {
-    const float* row = c.part + uint64_t(k ? 2 * (chunk + k) : 2 * chunk + 1) * c.dp;
+  // the sums are in rows 2 chunk + 1, 2 chunk + 2, 2 chunk + 4, ... 2 (chunk + more)
+  const bool few = more < 8;
+  const uint32_t per = few ? more + 1 : (more + 8) / 8, k0 = few ? 0 : warp * per, k1 = min(more + 1, k0 + per);
+  for (uint32_t slab = few ? warp : 0; slab < slabs; slab += few ? 8 : 1) {
+    const uint32_t col = slab * kSlab + (VEC ? lane * 8 : lane);
+    const float* part = c.part + slab * kSlab + lane * 8;
+    Piece<G, VEC> old;
+    if (c.accumulate && (few || warp == 0)) old.load(static_cast<const G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride, col, c.dim);
+    float sum[8] = {};
+    for (uint32_t k = k0; k < k1; k += 4) {
+      typename Elem<float>::Raw x[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += row[column<VEC>(slab, lane, j)];
+      for (int u = 0; u < 4; ++u)
+        if (k + u < k1) x[u] = Elem<float>::load_raw(part + uint64_t(k + u ? 2 * (chunk + k + u) : 2 * chunk + 1) * c.dp);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (k + u < k1) {
+          float v[8];
+          Elem<float>::unpack(x[u], v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[j] += v[j];
+        }
+    }
+    if (!few) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sh.sums[warp][lane + 32 * j] = sum[j];
+      __syncthreads();
+      if (warp) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        for (int w = 1; w < 8; ++w) sum[j] += sh.sums[w][lane + 32 * j];
+    }
+    write_row<G, VEC>(c, key, col, sum, old);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sums[warp][lane + 32 * j] = sum[j];
-  __syncthreads();
-  if (warp) return;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    sum[j] = sums[0][lane + 32 * j];
-    for (int w = 1; w < 8; ++w) sum[j] += sums[w][lane + 32 * j];
-  }
-  write_row<G, VEC>(c, key, slab, lane, sum);
 }
 
 // ------------------------------------------------------------------------------------------------ host
 template <typename... P, typename... A>
-cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, uint32_t cluster, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
+cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, uint32_t cluster, uint32_t threads, uint32_t smem, bool dependent, cudaStream_t s, const A&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute at[2] = {};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -522,14 +680,15 @@ cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, uint32_t cluster, u
 }
 template <typename... P, typename... A>
 cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
-  return launch_clusters(kernel, grid, 1, threads, dependent, s, args...);
+  return launch_clusters(kernel, grid, 1, threads, 0, dependent, s, args...);
 }
 
 struct Regions { uint64_t pairs[2], counts, part, total; };
 
-uint32_t chunk_of(uint64_t tokens) {
+// Positions per chunk: few chunks leave few sums to join, many keep the memory busy.
+uint32_t chunk_of(uint64_t tokens, uint32_t slabs) {
   uint32_t c = 8;
-  while (uint64_t(c) * kMaxChunks < tokens) c *= 2;
+  while (uint64_t(c) * kMaxChunks < tokens || (c < 64 && tokens * slabs >= uint64_t(2 * c) * kWarpsWanted)) c *= 2;
   return c;
 }
 
@@ -617,16 +776,37 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
   const uint2* sorted = nullptr;
   while (c.vocab >> bits) ++bits;                         // of keys 0 .. V
   const uint32_t passes = (bits + 8) / 9, per = (bits + passes - 1) / passes;
-  if (n && n <= uint64_t(kOneCta) * kCluster) {
-    const uint32_t ctas = n <= kOneCta ? 1 : kCluster;
-    uint64_t per_cta = 0;
-    uint32_t fill = 0;
-    if (!c.accumulate) {
-      per_cta = std::max<uint64_t>(1, (c.vocab + kFillCtas - 1) / kFillCtas);
-      fill = uint32_t(up((c.vocab + per_cta - 1) / per_cta, ctas));
+  c.chunk = chunk_of(n, c.dp / kSlab);
+  c.chunks = uint32_t((n + c.chunk - 1) / c.chunk);
+  const uint32_t sums = uint32_t((uint64_t(c.chunks) * (c.dp / kSlab) + 7) / 8);
+  // The zeros are written beside the sort and the sums, and some beside the joins, so that the memory is never idle.
+  FillShare beside_sums{}, beside_joins{};
+  uint64_t done = 0;
+  auto share = [&](uint64_t bytes, uint32_t ctas) {
+    FillShare f{};
+    if (c.accumulate) return f;
+    const uint64_t row = uint64_t(c.dim) * c.grad_size, rows = std::min(c.vocab - done, bytes / row);
+    if (!rows) return f;
+    f.begin = done;
+    f.end = done += rows;
+    f.per_cta = (rows + ctas - 1) / ctas;
+    f.ctas = uint32_t((rows + f.per_cta - 1) / f.per_cta);
+    f.wait = n > FLS_SCAN;
+    return f;
+  };
+  if (n && n <= kSortAtOnce) {
+    const uint32_t ctas = n <= FLS_ONE ? 1 : kCluster;
+    if (c.chunks > 1) beside_joins = share(std::min<uint64_t>(c.vocab * c.dim * c.grad_size / 8, FLS_JOINMB << 20), 148);
+    beside_sums = share(~0ull, uint32_t(std::clamp<uint64_t>(c.vocab * c.dim * c.grad_size / (FLS_F << 10), 296, 148 * 16)));
+    const uint32_t rounds = uint32_t((n + ctas * kClusterThreads - 1) / (ctas * kClusterThreads));
+    uint32_t room = kClusterThreads * 8;                    // as many rounds as the kernel is made for
+    while (room < rounds * kClusterThreads * 8) room *= 2;
+    if (room > 8 << 10) {
+      const cudaError_t err = cudaFuncSetAttribute(fls_embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 << 10);
+      if (err != cudaSuccess) return refuse(FLS_ECUDA, "embedding kernel: %s", cudaGetErrorString(err));
     }
-    FLS_LAUNCH(launch_clusters(fls_embed_sort_kernel, ctas + fill, ctas, kClusterThreads, false, s, c, bits, passes, ctas, per_cta));
-    sorted = c.pairs[(passes - 1) & 1];
+    FLS_LAUNCH(launch_clusters(fls_embed_sort_kernel, ctas, ctas, kClusterThreads, room, false, s, c, bits, passes));
+    sorted = c.pairs[0];
   } else {
     bool dependent = false;
     c.tiles = uint32_t((n + kSortTile - 1) / kSortTile);
@@ -638,19 +818,20 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
       FLS_LAUNCH(launch(fls_embed_scatter_kernel, c.tiles, kSortThreads, true, s, c, sp));
       at ^= 1;
     }
-    sorted = c.pairs[at];
-    if (!c.accumulate) {
-      const uint64_t per_cta = std::max<uint64_t>(1, (c.vocab + 148 * 8 - 1) / (148 * 8));
-      const uint32_t ctas = uint32_t((c.vocab + per_cta - 1) / per_cta);
-      FLS_LAUNCH((launch(fls_embed_fill_kernel, ctas, 256, dependent, s, c, sorted, per_cta)));
-    }
+    sorted = n ? c.pairs[at] : nullptr;
+    const FillShare all = share(~0ull, 148 * 8);
+    if (all.ctas) FLS_LAUNCH(launch(fls_embed_fill_kernel, all.ctas, 256, dependent, s, c, all, sorted));
   }
   if (n) {
-    c.chunk = chunk_of(n);
-    c.chunks = uint32_t((n + c.chunk - 1) / c.chunk);
-    const uint32_t slabs = (c.dim + kSlab - 1) / kSlab;
-    FLS_LAUNCH((launch(fls_embed_sum_kernel<T, G, VEC>, dim3((c.chunks + 7) / 8, slabs), 256, true, s, c, sorted)));
-    if (c.chunks > 1) FLS_LAUNCH((launch(fls_embed_join_kernel<G, VEC>, dim3(c.chunks - 1, slabs), 256, true, s, c, sorted)));
+    auto kernel = fls_embed_sum_kernel<T, G, VEC>;
+    const uint32_t smem = VEC ? kAhead * 256 * 16 * (sizeof(T) / 2 + (c.accumulate ? sizeof(G) / 2 : 0)) : 0;
+    if (smem > 32 << 10) {
+      const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 << 10);
+      if (err != cudaSuccess) return refuse(FLS_ECUDA, "embedding kernel: %s", cudaGetErrorString(err));
+    }
+    FLS_LAUNCH(launch_clusters(kernel, sums + beside_sums.ctas, 1, 256, smem, true, s, c, sorted, beside_sums));
+    if (c.chunks > 1 || beside_joins.ctas)
+      FLS_LAUNCH((launch(fls_embed_join_kernel<G, VEC>, beside_joins.ctas + c.chunks - 1, 256, true, s, c, sorted, beside_joins)));
   }
   return FLS_OK;
 }
@@ -726,7 +907,7 @@ int fls_embed_grad(fls_embed* e, const fls_embed_io* io, void* cuda_stream) {
   c.part = reinterpret_cast<float*>(ws + e->reg.part);
   c.grad_size = uint32_t(gs);
   c.zero_vec = cells(c.grad_weight, c.grad_weight_stride, gs);
-  const bool vec = c.zero_vec && (!n || cells(c.grad_out, c.grad_out_stride, es));
+  const bool vec = d.dim % 8 == 0 && c.zero_vec && (!n || cells(c.grad_out, c.grad_out_stride, es));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (d.act_dtype == FLS_GRAD_F32) {
     if (d.grad_dtype == FLS_GRAD_F32) return vec ? run_grad<float, float, true>(e, c, st) : run_grad<float, float, false>(e, c, st);
