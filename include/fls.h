@@ -521,7 +521,8 @@ typedef struct {
 typedef struct { uint64_t workspace_bytes; } fls_embed_layout;
 
 /* One call's data.  All buffers are device memory of the current device; strides count elements between rows, 0 means dense,
- * < 2^31.  Any element alignment and stride (rows that start on 16-byte boundaries on both sides are faster). */
+ * < 2^31.  Any element alignment and stride (faster where d is a multiple of eight and all rows start on boundaries of eight
+ * elements: 16 bytes of bf16, 32 of fp32). */
 typedef struct {
   uint64_t tokens;              /* N, 0 .. max_tokens                                                 */
   const int64_t* token;         /* N                                                                  */
@@ -588,7 +589,8 @@ typedef struct {
 typedef struct { uint64_t workspace_bytes; } fls_norm_layout;
 
 /* One call's data.  All buffers are device memory of the current device; strides count elements between rows, 0 means dense,
- * < 2^31; weight, bias and their gradients are dense.  Any element alignment (16-byte aligned rows are faster). */
+ * < 2^31; weight, bias and their gradients are dense.  Any element alignment (faster where d is a multiple of eight and all
+ * rows, weight and bias start on boundaries of eight elements: 16 bytes of bf16, 32 of fp32). */
 typedef struct {
   uint64_t rows;                /* N, 0 .. max_rows                                                             */
   const void* x;                /* N x d                                                                        */

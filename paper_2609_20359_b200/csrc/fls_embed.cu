@@ -24,22 +24,17 @@ constexpr int kSortThreads = 256, kSortRounds = 16;
 constexpr uint32_t kSortTile = kSortThreads * kSortRounds;   // positions per CTA of the sort
 constexpr uint32_t kMaxRadix = 512;
 constexpr uint32_t kMaxChunks = 2048;
-#ifndef FLS_WARPS
-#define FLS_WARPS 2400
-#endif
-#ifndef FLS_ONE
-#define FLS_ONE 2048
-#endif
-#ifndef FLS_SCAN
-#define FLS_SCAN 16384
-#endif
-#ifndef FLS_F
-#define FLS_F 512
-#endif
-#ifndef FLS_JOINMB
-#define FLS_JOINMB 16ull
-#endif
-constexpr uint64_t kWarpsWanted = FLS_WARPS;
+// Warps of the sums' kernel below which a chunk is not made longer: 16 on every SM.  (1200 / 2400 / 4800, us: 16384 tokens x 768
+// 42 / 42 / 45; 65536 x 768 87 / 87 / 85; 8191 x 2048 273 / 271 / 274.)
+constexpr uint64_t kWarpsWanted = 2400;
+// Tokens that one CTA sorts, in fewer steps than the cluster of eight; from there on its scattered stores are what takes time (us a
+// call that adds, one CTA / cluster: 1024 12.4 / 12.7, 2048 14.6 / 15.8, 4096 18.4 / 15.6).
+constexpr uint64_t kOneCta = 2048;
+// Tokens up to which the CTAs that write zeros look through all of them (4 us for 8192) rather than wait for the sort (11 us);
+// 8192 x 768 29 us against 33, 16384 39 against 47.
+constexpr uint64_t kLookThrough = 16384;
+constexpr uint64_t kZerosPerCta = 256 << 10;     // bytes: 8191 x 2048 fp32 in 179 us, with 1 MB 189; at least two CTAs per SM
+constexpr uint64_t kZerosBesideJoins = 16 << 20; // bytes, at most an eighth: what the memory takes during the joins' 5 us
 constexpr uint32_t kSlab = 256;                              // columns of a warp: eight per lane
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
@@ -74,7 +69,7 @@ __device__ __forceinline__ uint32_t key_of(const EmbedCall& c, uint64_t i) {
 }
 
 // ------------------------------------------------------------------------------------------------ lookup
-// A warp takes a row and 1024 of its columns.  VEC: cells of eight columns start on 16-byte boundaries on both sides.
+// A warp takes a row and 1024 of its columns.  VEC: rows are whole cells of eight columns and start on boundaries of eight elements on both sides.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) fls_embed_lookup_kernel(const __grid_constant__ EmbedCall c) {
   const uint64_t n = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32;
@@ -92,20 +87,17 @@ __global__ void __launch_bounds__(256) fls_embed_lookup_kernel(const __grid_cons
     for (int k = 0; k < 4; ++k) {
       const uint32_t col = col0 + k * kSlab + lane * 8;
       raw[k] = make_uint4(0, 0, 0, 0);
-      if (live && col + 8 <= c.dim) raw[k] = Elem<uint16_t>::load_raw(w + col);
+      if (live && col < c.dim) raw[k] = Elem<uint16_t>::load_raw(w + col);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const uint32_t col = col0 + k * kSlab + lane * 8;
-      if (col + 8 <= c.dim) {
-        float x[8];
-        Elem<uint16_t>::unpack(raw[k], x);
+      if (col >= c.dim) break;
+      float x[8];
+      Elem<uint16_t>::unpack(raw[k], x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = live ? x[j] * c.scale : other;
-        Elem<T>::store8(out + col, x);
-      } else {
-        for (uint32_t j = col; j < c.dim; ++j) Elem<T>::put(out + j, live ? Elem<uint16_t>::get(w + j) * c.scale : other);
-      }
+      for (int j = 0; j < 8; ++j) x[j] = live ? x[j] * c.scale : other;
+      Elem<T>::store8(out + col, x);
     }
   } else {
     const uint32_t end = min(c.dim, col0 + 1024);
@@ -433,7 +425,7 @@ __global__ void __launch_bounds__(kClusterThreads, 1)
 }
 
 // ------------------------------------------------------------------------------------------------ sums
-// The eight columns of a lane are neighbours where every row starts on a 16-byte boundary and holds whole cells (VEC),
+// The eight columns of a lane are neighbours where every row starts on a boundary of eight elements and holds whole cells (VEC),
 // otherwise 32 apart.
 
 // The columns of one row as they lie in memory.
@@ -487,22 +479,12 @@ __device__ __forceinline__ void write_part(const EmbedCall& c, uint32_t row, uin
   Elem<float>::store8(c.part + uint64_t(row) * c.dp + slab * kSlab + lane * 8, sum);
 }
 
-__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ uint4 shared16(uint32_t from) {
-  uint4 x;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(from) : "memory");
-  return x;
-}
-
 // A warp takes a chunk and 256 columns.  VEC: kAhead rows, and what is there of the rows that they finish, are on their way at
-// once, copied asynchronously into shared memory, where a lane reads only what it copied itself.
+// once, copied asynchronously into shared memory.
 constexpr int kAhead = 8;
 
 template <typename T, typename G, bool VEC>
 __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs, const FillShare share) {
-  constexpr int kT = sizeof(T) / 2, kG = sizeof(G) / 2;     // 16-byte pieces of a lane's columns
   extern __shared__ uint4 rows[];
   __shared__ FillShared sh;
   pdl_launch();
@@ -520,8 +502,8 @@ __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_cons
   if (chunk >= c.chunks) return;
   const uint32_t n = uint32_t(c.tokens), none = uint32_t(c.vocab);
   const uint32_t begin = chunk * c.chunk, end = min(n, begin + c.chunk), col = slab * kSlab + (VEC ? lane * 8 : lane);
-  const uint32_t pieces = kT + (c.accumulate ? kG : 0), step = 256 * 16;
-  const uint32_t place = uint32_t(__cvta_generic_to_shared(rows)) + threadIdx.x * 16;
+  const uint32_t row_bytes = Staged<T>::bytes + (c.accumulate ? Staged<G>::bytes : 0);
+  const uint32_t place = uint32_t(__cvta_generic_to_shared(rows)) + threadIdx.x / 32 * (kAhead * row_bytes);
   float sum[8] = {};
   const uint32_t first = pairs[begin].x, left = begin ? pairs[begin - 1].x : none, right = end < n ? pairs[end].x : none;
   if (first == none) return;
@@ -543,16 +525,11 @@ __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_cons
     auto send = [&](uint32_t i) {
       if (i < here) {
         const uint32_t key = key_at(i), row = row_at(i), next = next_at(i);
-        if (key != none && col < c.dim) {
-          uint32_t to = place + i % kAhead * pieces * step;
-          const uint4* x = reinterpret_cast<const uint4*>(static_cast<const T*>(c.grad_out) + row * c.grad_out_stride + col);
-#pragma unroll
-          for (int p = 0; p < kT; ++p, to += step) copy16(to, x + p);
-          if (c.accumulate && key != next) {
-            const uint4* g = reinterpret_cast<const uint4*>(static_cast<const G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride + col);
-#pragma unroll
-            for (int p = 0; p < kG; ++p, to += step) copy16(to, g + p);
-          }
+        if (key != none) {
+          const uint32_t to = place + i % kAhead * row_bytes;
+          Staged<T>::copy(to, static_cast<const T*>(c.grad_out) + row * c.grad_out_stride, slab * kSlab, lane, c.dim);
+          if (c.accumulate && key != next)
+            Staged<G>::copy(to + Staged<T>::bytes, static_cast<const G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride, slab * kSlab, lane, c.dim);
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -564,11 +541,13 @@ __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_cons
       if (key == none) return;                              // nothing follows
       Piece<T, VEC> x;
       Piece<G, VEC> old;
-      uint32_t from = place + i % kAhead * pieces * step;
+      const uint32_t from = place + i % kAhead * row_bytes;
       if constexpr (VEC) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory");
-#pragma unroll
-        for (int p = 0; p < kT; ++p, from += step) reinterpret_cast<uint4*>(&x.raw)[p] = shared16(from);
+        __syncwarp();
+        Staged<T>::read(from, lane, x.raw);
+        if (c.accumulate && key != next) Staged<G>::read(from + Staged<T>::bytes, lane, old.raw);
+        __syncwarp();
       } else {
         x.load(static_cast<const T*>(c.grad_out) + row_at(i) * c.grad_out_stride, col, c.dim);
         if (c.accumulate && key != next) old.load(static_cast<const G*>(c.grad_weight) + uint64_t(key) * c.grad_weight_stride, col, c.dim);
@@ -582,10 +561,6 @@ __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_cons
         if (from_left) {
           write_part(c, 2 * chunk, slab, lane, sum);
         } else {
-          if constexpr (VEC)
-            if (c.accumulate)
-#pragma unroll
-              for (int p = 0; p < kG; ++p, from += step) reinterpret_cast<uint4*>(&old.raw)[p] = shared16(from);
           write_row<G, VEC>(c, key, col, sum, old);
         }
         from_left = false;
@@ -661,28 +636,6 @@ __global__ void __launch_bounds__(256, 4) fls_embed_join_kernel(const __grid_con
 }
 
 // ------------------------------------------------------------------------------------------------ host
-template <typename... P, typename... A>
-cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, uint32_t cluster, uint32_t threads, uint32_t smem, bool dependent, cudaStream_t s, const A&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute at[2] = {};
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = dependent ? 1 : 0;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = cluster;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-}
-template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, bool dependent, cudaStream_t s, const A&... args) {
-  return launch_clusters(kernel, grid, 1, threads, 0, dependent, s, args...);
-}
-
 struct Regions { uint64_t pairs[2], counts, part, total; };
 
 // Positions per chunk: few chunks leave few sums to join, many keep the memory busy.
@@ -709,8 +662,6 @@ Regions regions(const fls_embed_desc& d) {
 
 bool known(uint32_t dtype) { return dtype == FLS_GRAD_BF16 || dtype == FLS_GRAD_F32; }
 uint64_t size_of(uint32_t dtype) { return dtype == FLS_GRAD_F32 ? 4 : 2; }
-// Whether every row starts on a 16-byte boundary.
-bool cells(const void* p, uint64_t stride, uint64_t elem) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * elem % 16 == 0; }
 uint64_t span_bytes(uint64_t rows, uint64_t cols, uint64_t stride, uint64_t elem) { return rows ? ((rows - 1) * stride + cols) * elem : 0; }
 
 }  // namespace
@@ -791,18 +742,19 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
     f.end = done += rows;
     f.per_cta = (rows + ctas - 1) / ctas;
     f.ctas = uint32_t((rows + f.per_cta - 1) / f.per_cta);
-    f.wait = n > FLS_SCAN;
+    f.wait = n > kLookThrough;
     return f;
   };
   if (n && n <= kSortAtOnce) {
-    const uint32_t ctas = n <= FLS_ONE ? 1 : kCluster;
-    if (c.chunks > 1) beside_joins = share(std::min<uint64_t>(c.vocab * c.dim * c.grad_size / 8, FLS_JOINMB << 20), 148);
-    beside_sums = share(~0ull, uint32_t(std::clamp<uint64_t>(c.vocab * c.dim * c.grad_size / (FLS_F << 10), 296, 148 * 16)));
+    const uint32_t ctas = n <= kOneCta ? 1 : kCluster;
+    if (c.chunks > 1) beside_joins = share(std::min<uint64_t>(c.vocab * c.dim * c.grad_size / 8, kZerosBesideJoins), 148);
+    beside_sums = share(~0ull, uint32_t(std::clamp<uint64_t>(c.vocab * c.dim * c.grad_size / kZerosPerCta, 296, 148 * 16)));
     const uint32_t rounds = uint32_t((n + ctas * kClusterThreads - 1) / (ctas * kClusterThreads));
     uint32_t room = kClusterThreads * 8;                    // as many rounds as the kernel is made for
     while (room < rounds * kClusterThreads * 8) room *= 2;
     if (room > 8 << 10) {
-      const cudaError_t err = cudaFuncSetAttribute(fls_embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 << 10);
+      static std::atomic<uint64_t> done{0};
+      const cudaError_t err = allow_shared(reinterpret_cast<const void*>(fls_embed_sort_kernel), 128 << 10, done);
       if (err != cudaSuccess) return refuse(FLS_ECUDA, "embedding kernel: %s", cudaGetErrorString(err));
     }
     FLS_LAUNCH(launch_clusters(fls_embed_sort_kernel, ctas, ctas, kClusterThreads, room, false, s, c, bits, passes));
@@ -812,26 +764,27 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
     c.tiles = uint32_t((n + kSortTile - 1) / kSortTile);
     for (uint32_t p = 0; n && p < passes; ++p) {
       const SortPass sp{p * per, std::min(per, bits - p * per), p == 0, at};
-      FLS_LAUNCH(launch(fls_embed_count_kernel, c.tiles, kSortThreads, dependent, s, c, sp));
+      FLS_LAUNCH(launch(fls_embed_count_kernel, c.tiles, kSortThreads, 0, dependent, s, c, sp));
       dependent = true;
-      FLS_LAUNCH(launch(fls_embed_scan_kernel, 1, 1024, true, s, c, sp));
-      FLS_LAUNCH(launch(fls_embed_scatter_kernel, c.tiles, kSortThreads, true, s, c, sp));
+      FLS_LAUNCH(launch(fls_embed_scan_kernel, 1, 1024, 0, true, s, c, sp));
+      FLS_LAUNCH(launch(fls_embed_scatter_kernel, c.tiles, kSortThreads, 0, true, s, c, sp));
       at ^= 1;
     }
     sorted = n ? c.pairs[at] : nullptr;
     const FillShare all = share(~0ull, 148 * 8);
-    if (all.ctas) FLS_LAUNCH(launch(fls_embed_fill_kernel, all.ctas, 256, dependent, s, c, all, sorted));
+    if (all.ctas) FLS_LAUNCH(launch(fls_embed_fill_kernel, all.ctas, 256, 0, dependent, s, c, all, sorted));
   }
   if (n) {
     auto kernel = fls_embed_sum_kernel<T, G, VEC>;
-    const uint32_t smem = VEC ? kAhead * 256 * 16 * (sizeof(T) / 2 + (c.accumulate ? sizeof(G) / 2 : 0)) : 0;
+    const uint32_t smem = VEC ? kAhead * 8 * (Staged<T>::bytes + (c.accumulate ? Staged<G>::bytes : 0)) : 0;
     if (smem > 32 << 10) {
-      const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 << 10);
+      static std::atomic<uint64_t> done{0};
+      const cudaError_t err = allow_shared(reinterpret_cast<const void*>(kernel), 128 << 10, done);
       if (err != cudaSuccess) return refuse(FLS_ECUDA, "embedding kernel: %s", cudaGetErrorString(err));
     }
-    FLS_LAUNCH(launch_clusters(kernel, sums + beside_sums.ctas, 1, 256, smem, true, s, c, sorted, beside_sums));
+    FLS_LAUNCH(launch(kernel, sums + beside_sums.ctas, 256, smem, true, s, c, sorted, beside_sums));
     if (c.chunks > 1 || beside_joins.ctas)
-      FLS_LAUNCH((launch(fls_embed_join_kernel<G, VEC>, beside_joins.ctas + c.chunks - 1, 256, true, s, c, sorted, beside_joins)));
+      FLS_LAUNCH((launch(fls_embed_join_kernel<G, VEC>, beside_joins.ctas + c.chunks - 1, 256, 0, true, s, c, sorted, beside_joins)));
   }
   return FLS_OK;
 }
@@ -880,10 +833,10 @@ int fls_embed_lookup(fls_embed* e, const fls_embed_io* io, void* cuda_stream) {
   if (int rc = check_spans(s, 3)) return rc;
   if (!n) return FLS_OK;
   const dim3 grid(uint32_t((n + 7) / 8), (d.dim + 1023) / 1024);
-  const bool vec = cells(c.weight, c.weight_stride, 2) && cells(c.out, c.out_stride, es), f32 = d.act_dtype == FLS_GRAD_F32;
+  const bool vec = d.dim % 8 == 0 && in_cells(c.weight, c.weight_stride, 2) && in_cells(c.out, c.out_stride, es), f32 = d.act_dtype == FLS_GRAD_F32;
   auto kernel = f32 ? (vec ? fls_embed_lookup_kernel<float, true> : fls_embed_lookup_kernel<float, false>)
                     : (vec ? fls_embed_lookup_kernel<uint16_t, true> : fls_embed_lookup_kernel<uint16_t, false>);
-  FLS_LAUNCH(launch(kernel, grid, 256, false, static_cast<cudaStream_t>(cuda_stream), c));
+  FLS_LAUNCH(launch(kernel, grid, 256, 0, false, static_cast<cudaStream_t>(cuda_stream), c));
   return FLS_OK;
 }
 
@@ -906,8 +859,8 @@ int fls_embed_grad(fls_embed* e, const fls_embed_io* io, void* cuda_stream) {
   c.counts = reinterpret_cast<uint32_t*>(ws + e->reg.counts);
   c.part = reinterpret_cast<float*>(ws + e->reg.part);
   c.grad_size = uint32_t(gs);
-  c.zero_vec = cells(c.grad_weight, c.grad_weight_stride, gs);
-  const bool vec = d.dim % 8 == 0 && c.zero_vec && (!n || cells(c.grad_out, c.grad_out_stride, es));
+  c.zero_vec = reinterpret_cast<uintptr_t>(c.grad_weight) % 16 == 0 && c.grad_weight_stride * gs % 16 == 0;
+  const bool vec = d.dim % 8 == 0 && in_cells(c.grad_weight, c.grad_weight_stride, gs) && (!n || in_cells(c.grad_out, c.grad_out_stride, es));
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (d.act_dtype == FLS_GRAD_F32) {
     if (d.grad_dtype == FLS_GRAD_F32) return vec ? run_grad<float, float, true>(e, c, st) : run_grad<float, float, false>(e, c, st);

@@ -18,6 +18,9 @@
 using namespace fls;
 
 namespace {
+#ifndef FLS_STAGES
+#define FLS_STAGES 3
+#endif
 
 constexpr uint32_t kColTile = 32;          // columns of a CTA of the weight gradients' kernel
 constexpr uint32_t kMaxParts = 296;        // parts of the rows whose sums are joined
@@ -67,7 +70,7 @@ __device__ __forceinline__ float2 block_sum(float2 v, float2* shared) {
 
 // ------------------------------------------------------------------------------------------------ rows in registers
 // A row belongs to `tpr` neighbouring threads, each with K cells of eight columns: neighbouring columns where every row starts
-// on a 16-byte boundary and holds whole cells (VEC), otherwise columns 32 apart, moved one by one.
+// on a boundary of eight elements and holds whole cells (VEC), otherwise columns 32 apart, moved one by one.
 template <bool VEC>
 __device__ __forceinline__ uint32_t column(uint32_t tpr, uint32_t t, int k, int j) {
   return VEC ? (k * tpr + t) * 8 + j : (k * (tpr / 32) + t / 32) * 256 + t % 32 + 32 * j;
@@ -114,7 +117,7 @@ template <typename T> struct Cell<T, false> {
   }
 };
 
-// Eight values of the weight or the bias; `other` where there is none.  VEC asks for a 16-byte boundary of theirs too.
+// Eight values of the weight or the bias; `other` where there is none.  VEC asks for a boundary of eight of theirs too.
 template <bool VEC>
 __device__ __forceinline__ void weight_cell(const NormCall& c, const void* p, float other, uint32_t col, float (&x)[8]) {
   if (!p) {
@@ -227,22 +230,11 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
   }
 }
 
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ uint4 shared16(uint32_t from) {
-  uint4 x;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(from) : "memory");
-  return x;
-}
-
 // All gradients in one look at the rows.  A CTA has blockDim / tpr groups, a group a stretch of rows, one at a time; a thread
 // keeps its columns' sums for weight and bias in registers, adds them to the other groups' at the end and leaves the CTA's in
-// the workspace.  VEC: STAGES rows are on their way at once, copied asynchronously into shared memory; every thread copies
-// and reads its own 16-byte pieces, so that nobody waits for anybody's copies but his own.
+// the workspace.  VEC: STAGES rows are on their way at once, copied asynchronously into shared memory, every warp for itself.
 template <typename X, typename Y, bool VEC, int K, int STAGES, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
-  constexpr int kX = sizeof(X) / 2, kY = sizeof(Y) / 2;     // 16-byte pieces of a cell
   extern __shared__ __align__(16) float smem[];             // rows on their way, then the groups' sums
   __shared__ float2 sums[2][32];
   const uint32_t t = threadIdx.x % tpr, group = threadIdx.x / tpr, groups = blockDim.x / tpr, warps = tpr / 32, lane = threadIdx.x % 32;
@@ -250,8 +242,8 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
   const uint64_t begin = c.rows * g / all;
   const uint32_t count = uint32_t(c.rows * (g + 1) / all - begin);
   const bool with_total = c.grad_total != nullptr;
-  const uint32_t pieces = K * (kX + kY + (with_total ? kX : 0));
-  const uint32_t mine = uint32_t(__cvta_generic_to_shared(smem)) + threadIdx.x * 16, step = blockDim.x * 16;
+  const uint32_t row_bytes = K * (Staged<X>::bytes + Staged<Y>::bytes + (with_total ? Staged<X>::bytes : 0));
+  const uint32_t mine = uint32_t(__cvta_generic_to_shared(smem)) + threadIdx.x / 32 * (STAGES * row_bytes);
   const X* px = static_cast<const X*>(c.x) + begin * c.x_stride;
   const Y* py = static_cast<const Y*>(c.grad_y) + begin * c.grad_y_stride;
   const X* pt = static_cast<const X*>(c.grad_total) + begin * c.grad_total_stride;
@@ -263,25 +255,17 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
     if (VEC && sent < count) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const uint32_t col = column<VEC>(tpr, t, k, 0);
-        const bool there = col < c.dim;
-        const uint32_t at = there ? col : 0;
-        uint32_t q = to + k * (kX + kY) * step;
-#pragma unroll
-        for (int i = 0; i < kX; ++i, q += step) copy16(q, reinterpret_cast<const uint4*>(px + at) + i, there);
-#pragma unroll
-        for (int i = 0; i < kY; ++i, q += step) copy16(q, reinterpret_cast<const uint4*>(py + at) + i, there);
-        if (with_total) {
-          q = to + (K * (kX + kY) + k * kX) * step;
-#pragma unroll
-          for (int i = 0; i < kX; ++i, q += step) copy16(q, reinterpret_cast<const uint4*>(pt + at) + i, there);
-        }
+        const uint32_t first = column<VEC>(tpr, t - lane, k, 0);
+        uint32_t q = to + k * (Staged<X>::bytes + Staged<Y>::bytes);
+        Staged<X>::copy(q, px, first, lane, c.dim);
+        Staged<Y>::copy(q + Staged<X>::bytes, py, first, lane, c.dim);
+        if (with_total) Staged<X>::copy(to + K * (Staged<X>::bytes + Staged<Y>::bytes) + k * Staged<X>::bytes, pt, first, lane, c.dim);
       }
       px += c.x_stride;
       py += c.grad_y_stride;
       pt += c.grad_total_stride;
       ++sent;
-      to = sent % STAGES ? to + pieces * step : mine;
+      to = sent % STAGES ? to + row_bytes : mine;
     }
     if (VEC) asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -306,24 +290,16 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
     Cell<Y, VEC> dy[K];
     if constexpr (VEC) {
       asm volatile("cp.async.wait_group %0;" ::"n"(STAGES > 1 ? STAGES - 2 : 0) : "memory");
-      uint32_t q = from;
+      __syncwarp();
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        uint4* rx = reinterpret_cast<uint4*>(&x[k].raw);
-        uint4* ry = reinterpret_cast<uint4*>(&dy[k].raw);
-#pragma unroll
-        for (int p = 0; p < kX; ++p, q += step) rx[p] = shared16(q);
-#pragma unroll
-        for (int p = 0; p < kY; ++p, q += step) ry[p] = shared16(q);
+        const uint32_t q = from + k * (Staged<X>::bytes + Staged<Y>::bytes);
+        Staged<X>::read(q, lane, x[k].raw);
+        Staged<Y>::read(q + Staged<X>::bytes, lane, dy[k].raw);
+        if (with_total) Staged<X>::read(from + K * (Staged<X>::bytes + Staged<Y>::bytes) + k * Staged<X>::bytes, lane, dt[k].raw);
       }
-      if (with_total)
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          uint4* rt = reinterpret_cast<uint4*>(&dt[k].raw);
-#pragma unroll
-          for (int p = 0; p < kX; ++p, q += step) rt[p] = shared16(q);
-        }
-      from = (i + 1) % STAGES ? from + pieces * step : mine;
+      __syncwarp();
+      from = (i + 1) % STAGES ? from + row_bytes : mine;
       send();                                               // into the place that the row before this one had
     } else {
 #pragma unroll
@@ -545,21 +521,6 @@ __global__ void __launch_bounds__(1024) fls_norm_join_kernel(const __grid_consta
   }
 }
 
-template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, uint32_t threads, uint32_t smem, bool dependent, cudaStream_t s, const A&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.dynamicSmemBytes = smem;
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.stream = s;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = dependent ? 1 : 0;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-}
-
 struct Regions { uint64_t coef, part, total; };
 Regions regions(const fls_norm_desc& d) {
   Regions r{};
@@ -594,8 +555,6 @@ namespace {
     ++h->launches;                                                                                  \
   } while (0)
 
-bool aligned(const void* p, uint64_t stride, uint64_t elem) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * elem % 16 == 0; }
-
 template <typename X, typename Y, bool VEC>
 cudaError_t forward_rows(const NormCall& c, cudaStream_t s) {
   const uint32_t cells = (c.dim + 7) / 8;
@@ -614,9 +573,10 @@ cudaError_t forward_rows(const NormCall& c, cudaStream_t s) {
 
 template <typename X, typename Y>
 int run_forward(fls_norm* h, NormCall& c, cudaStream_t s) {
+  const uint64_t ws = c.weight_f32 ? 4 : 2;
   if (c.dim <= 32768) {
-    const bool vec = c.dim % 8 == 0 && aligned(c.weight, 0, 0) && aligned(c.bias, 0, 0) && aligned(c.x, c.x_stride, sizeof(X)) && aligned(c.y, c.y_stride, sizeof(Y)) &&
-                     (!c.residual || (aligned(c.residual, c.residual_stride, sizeof(X)) && aligned(c.total, c.total_stride, sizeof(X))));
+    const bool vec = c.dim % 8 == 0 && in_cells(c.weight, 0, ws) && in_cells(c.bias, 0, ws) && in_cells(c.x, c.x_stride, sizeof(X)) && in_cells(c.y, c.y_stride, sizeof(Y)) &&
+                     (!c.residual || (in_cells(c.residual, c.residual_stride, sizeof(X)) && in_cells(c.total, c.total_stride, sizeof(X))));
     FLS_LAUNCH((vec ? forward_rows<X, Y, true>(c, s) : forward_rows<X, Y, false>(c, s)));
     return FLS_OK;
   }
@@ -628,28 +588,30 @@ template <typename X, typename Y, bool VEC, int K, int STAGES, int THREADS>
 cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
   const uint32_t cells = (c.dim + 7) / 8, tpr = (cells + 32 * K - 1) / (32 * K) * 32, groups = THREADS / tpr, threads = tpr * groups;
   c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(148, (c.rows + groups - 1) / groups)));
-  const uint32_t pieces = K * (sizeof(X) * (c.grad_total ? 2 : 1) + sizeof(Y)) / 2;
-  const uint32_t smem = std::max(VEC ? STAGES * pieces * threads * 16 : 0, (groups - 1) * tpr * 16 * K * 4);
+  const uint32_t row_bytes = K * (Staged<X>::bytes * (c.grad_total ? 2 : 1) + Staged<Y>::bytes);
+  const uint32_t smem = std::max(VEC ? STAGES * row_bytes * (threads / 32) : 0, (groups - 1) * tpr * 16 * K * 4);
   auto kernel = fls_norm_backward_kernel<X, Y, VEC, K, STAGES, THREADS>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 << 10);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_shared(reinterpret_cast<const void*>(kernel), 226 << 10, done);
   if (e != cudaSuccess) return e;
   return launch(kernel, dim3(c.parts), threads, smem, false, s, c, tpr);
 }
 
 template <typename X, typename Y, bool VEC>
 cudaError_t backward_of(NormCall& c, cudaStream_t s) {
-  return c.dim <= 6144 ? backward_rows<X, Y, VEC, 1, 3, 768>(c, s) : backward_rows<X, Y, VEC, 2, 2, 512>(c, s);
+  return c.dim <= 6144 ? backward_rows<X, Y, VEC, 1, FLS_STAGES, 768>(c, s) : backward_rows<X, Y, VEC, 2, 2, 512>(c, s);
 }
 
 template <typename X, typename Y>
 int run_backward(fls_norm* h, NormCall& c, cudaStream_t s) {
   const uint32_t tiles = (c.dim + kColTile - 1) / kColTile;
   bool dependent = false;
+  const uint64_t ws = c.weight_f32 ? 4 : 2;
   if (c.dim <= 8192) {
-    const bool vec = c.dim % 8 == 0 && aligned(c.weight, 0, 0) &&
-                     (!c.rows || (aligned(c.x, c.x_stride, sizeof(X)) && aligned(c.grad_y, c.grad_y_stride, sizeof(Y)) &&
-                                 (!c.grad_x || aligned(c.grad_x, c.grad_x_stride, sizeof(X))) &&
-                                 (!c.grad_total || aligned(c.grad_total, c.grad_total_stride, sizeof(X)))));
+    const bool vec = c.dim % 8 == 0 && in_cells(c.weight, 0, ws) &&
+                     (!c.rows || (in_cells(c.x, c.x_stride, sizeof(X)) && in_cells(c.grad_y, c.grad_y_stride, sizeof(Y)) &&
+                                 (!c.grad_x || in_cells(c.grad_x, c.grad_x_stride, sizeof(X))) &&
+                                 (!c.grad_total || in_cells(c.grad_total, c.grad_total_stride, sizeof(X)))));
     FLS_LAUNCH((vec ? backward_of<X, Y, true>(c, s) : backward_of<X, Y, false>(c, s)));
   } else {
     c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>({kMaxParts, (c.rows + 7) / 8, std::max<uint32_t>(1, 148 * 16 / tiles)})));

@@ -43,7 +43,10 @@ class Embedding:
         n = self._tokens(tokens)
         io.weight, io.weight_stride = _matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16, dev)
         if out is None:
-            out = _empty_on(stream, (n, self.dim), self.act_torch_dtype, dev)
+            if stream is None and self.act_torch_dtype is torch.bfloat16:
+                out = weight.new_empty((n, self.dim))
+            else:
+                out = _empty_on(stream, (n, self.dim), self.act_torch_dtype, dev)
             io.out, io.out_stride = out.data_ptr(), 0
         else:
             io.out, io.out_stride = _matrix(out, "out", n, self.dim, self.act_torch_dtype, dev)
