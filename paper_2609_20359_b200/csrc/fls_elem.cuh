@@ -13,6 +13,44 @@ namespace fls {
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Two fp32 operations in one instruction.
+struct f2 { uint64_t v; };
+__device__ __forceinline__ f2 make_f2(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ f2 make_f2(float a) { return make_f2(a, a); }
+__device__ __forceinline__ void split(f2 x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ float sum2(f2 x) {
+  float a, b;
+  split(x, a, b);
+  return a + b;
+}
+__device__ __forceinline__ void pairs_of(const float (&x)[8], f2 (&y)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = make_f2(x[2 * i], x[2 * i + 1]);
+}
+__device__ __forceinline__ void singles_of(const f2 (&x)[4], float (&y)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split(x[i], y[2 * i], y[2 * i + 1]);
+}
+
 template <typename T> struct Elem;
 template <> struct Elem<uint16_t> {
   __device__ static __forceinline__ float get(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }

@@ -83,15 +83,15 @@ template <typename T> struct Cell<T, true> {
     raw = typename Elem<T>::Raw{};
     if (col < dim) raw = Elem<T>::load_raw(row + col);
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const { Elem<T>::unpack(raw, x); }
-  __device__ static __forceinline__ void store(T* row, uint32_t col, uint32_t dim, const float (&x)[8]) {
-    if (col < dim) Elem<T>::store8(row + col, x);
+  __device__ __forceinline__ void get(f2 (&x)[4]) const {
+    float y[8];
+    Elem<T>::unpack(raw, y);
+    pairs_of(y, x);
   }
-  // What was computed from the cell is computed again after this, not kept in registers.
-  __device__ __forceinline__ void forget() {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
-#pragma unroll
-    for (int i = 0; i < int(sizeof raw / 4); ++i) asm volatile("" : "+r"(w[i]));
+  __device__ static __forceinline__ void store(T* row, uint32_t col, uint32_t dim, const f2 (&x2)[4]) {
+    float x[8];
+    singles_of(x2, x);
+    if (col < dim) Elem<T>::store8(row + col, x);
   }
 };
 template <typename T> struct Cell<T, false> {
@@ -101,28 +101,23 @@ template <typename T> struct Cell<T, false> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x_[j] = col + 32 * j < dim ? Elem<T>::get(row + 32 * j) : 0.f;
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x_[j];
-  }
-  __device__ static __forceinline__ void store(T* row, uint32_t col, uint32_t dim, const float (&x)[8]) {
+  __device__ __forceinline__ void get(f2 (&x)[4]) const { pairs_of(x_, x); }
+  __device__ static __forceinline__ void store(T* row, uint32_t col, uint32_t dim, const f2 (&x2)[4]) {
+    float x[8];
+    singles_of(x2, x);
     row += col;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (col + 32 * j < dim) Elem<T>::put(row + 32 * j, x[j]);
   }
-  __device__ __forceinline__ void forget() {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) asm volatile("" : "+f"(x_[j]));
-  }
 };
 
 // Eight values of the weight or the bias; `other` where there is none.  VEC asks for a boundary of eight of theirs too.
 template <bool VEC>
-__device__ __forceinline__ void weight_cell(const NormCall& c, const void* p, float other, uint32_t col, float (&x)[8]) {
+__device__ __forceinline__ void weight_cell(const NormCall& c, const void* p, float other, uint32_t col, f2 (&x)[4]) {
   if (!p) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = other;
+    for (int i = 0; i < 4; ++i) x[i] = make_f2(other);
   } else if (c.weight_f32) {
     Cell<float, VEC> w;
     w.load(static_cast<const float*>(p), col, c.dim);
@@ -134,36 +129,42 @@ __device__ __forceinline__ void weight_cell(const NormCall& c, const void* p, fl
   }
 }
 
-// Sum over the threads of a row; all of the CTA's rows at once where a row has several warps.
-template <int V>
-__device__ __forceinline__ void row_sum(float (&v)[V], uint32_t tpr, float (*shared)[V]) {
+// Sum over a warp of one or two values; the second step on, two values are in one half of the warp each.
+__device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
-  for (int i = 0; i < V; ++i)
+  for (int o = 16; o; o /= 2) x += __shfl_xor_sync(~0u, x, o);
+  return x;
+}
+// x's sum in lanes 0 .. 15, y's in lanes 16 .. 31.
+__device__ __forceinline__ float warp_sum(float x, float y, uint32_t lane) {
+  const float other = __shfl_xor_sync(~0u, lane < 16 ? y : x, 16);
+  float v = (lane < 16 ? x : y) + other;
 #pragma unroll
-    for (int o = 16; o; o /= 2) v[i] += __shfl_xor_sync(~0u, v[i], o);
-  if (tpr == 32) return;
-  const uint32_t warps = tpr / 32, warp = threadIdx.x / 32, first = warp / warps * warps;
-  if (threadIdx.x % 32 == 0)
-#pragma unroll
-    for (int i = 0; i < V; ++i) shared[warp][i] = v[i];
-  __syncthreads();
-  // every thread adds the warps' sums in the same order
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    float s = shared[first][i];
-    for (uint32_t w = 1; w < warps; ++w) s += shared[first + w][i];
-    v[i] = s;
+  for (int o = 8; o; o /= 2) v += __shfl_xor_sync(~0u, v, o);
+  return v;
+}
+
+// Sums over the `warps` warps of a row of what each has left in `shared`, a value of x and one of y.
+__device__ __forceinline__ float2 warps_sum(const float2* shared, uint32_t warps, uint32_t lane) {
+  float2 v = lane < warps ? shared[lane] : make_float2(0.f, 0.f);
+  for (uint32_t o = 1; o < warps; o *= 2) {
+    v.x += __shfl_xor_sync(~0u, v.x, o);
+    v.y += __shfl_xor_sync(~0u, v.y, o);
   }
+  // lanes that hold no sum of all take it from lane 0
+  v.x = __shfl_sync(~0u, v.x, 0);
+  v.y = __shfl_sync(~0u, v.y, 0);
+  return v;
 }
 
 template <typename X, typename Y, bool VEC, int K, int THREADS>
 __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
-  __shared__ float shared1[32][1], shared2[32][2];
-  const uint32_t t = threadIdx.x % tpr;
+  __shared__ float2 shared1[32], shared2[32];
+  const uint32_t t = threadIdx.x % tpr, lane = threadIdx.x % 32, warps = tpr / 32, mine = threadIdx.x / 32, first = mine / warps * warps;
   const uint64_t n = uint64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
   const bool live = n < c.rows;                             // the others keep the barriers company
   const uint64_t row = live ? n : c.rows - 1;
-  float x[K][8];
+  f2 x[K][4];
   {
     Cell<X, VEC> in[K], add[K];
 #pragma unroll
@@ -176,42 +177,76 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
     if (c.residual) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        float r[8];
+        f2 r[4];
+        float s[8];
         add[k].get(r);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[k][j] = Elem<X>::round(x[k][j] + r[j]);
+        for (int i = 0; i < 4; ++i) r[i] = add2(x[k][i], r[i]);
+        singles_of(r, s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = Elem<X>::round(s[j]);
+        pairs_of(s, x[k]);
         if (live) Cell<X, VEC>::store(static_cast<X*>(c.total) + row * c.total_stride, column<VEC>(tpr, t, k, 0), c.dim, x[k]);
       }
     }
   }
-  float w[8], b[8];
+  f2 w[4], b[4];
   if (K == 1) {                                             // few rows: everything on its way at once
     weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, 0, 0), w);
     weight_cell<VEC>(c, c.bias, 0.f, column<VEC>(tpr, t, 0, 0), b);
   }
   float m = 0.f;
   if (!c.rms) {
-    float v[1] = {0.f};
+    f2 a = make_f2(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[0] += x[k][j];
-    row_sum<1>(v, tpr, shared1);
-    m = v[0] * c.inv_dim;
+      for (int i = 0; i < 4; ++i) a = add2(a, x[k][i]);
+    m = warp_sum(sum2(a));
+    if (warps > 1) {
+      if (lane == 0) shared1[mine] = make_float2(m, 0.f);
+      __syncthreads();
+      m = warps_sum(shared1 + first, warps, lane).x;
+    }
+    m *= c.inv_dim;
+    const f2 less = make_f2(-m);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (VEC) {
+        const f2 off = column<VEC>(tpr, t, k, 0) < c.dim ? less : make_f2(0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[k][i] = add2(x[k][i], off);
+      } else {
+        float s[8];
+        singles_of(x[k], s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = column<VEC>(tpr, t, k, j) < c.dim ? s[j] - m : 0.f;
+        pairs_of(s, x[k]);
+      }
+    }
   }
-  float v[2] = {0.f, 0.f};
+  f2 ones = make_f2(0.f), squares = make_f2(0.f);
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[k][j] = column<VEC>(tpr, t, k, j) < c.dim ? x[k][j] - m : 0.f;
-      v[0] += x[k][j];
-      v[1] = fmaf(x[k][j], x[k][j], v[1]);
+    for (int i = 0; i < 4; ++i) {
+      if (!c.rms) ones = add2(ones, x[k][i]);
+      squares = fma2(x[k][i], x[k][i], squares);
     }
-  row_sum<2>(v, tpr, shared2);
-  const float e = c.rms ? 0.f : v[0] * c.inv_dim, var = fmaf(-e, e, v[1] * c.inv_dim);
+  float2 v;
+  const float half = warp_sum(sum2(ones), sum2(squares), lane);
+  if (warps > 1) {
+    if (lane == 0) shared2[mine].x = half;
+    if (lane == 16) shared2[mine].y = half;
+    __syncthreads();
+    v = warps_sum(shared2 + first, warps, lane);
+  } else {
+    v = make_float2(__shfl_sync(~0u, half, 0), __shfl_sync(~0u, half, 16));
+  }
+  const float e = c.rms ? 0.f : v.x * c.inv_dim, var = fmaf(-e, e, v.y * c.inv_dim);
   const float rstd = 1.f / sqrtf(var + c.eps);
   if (!live) return;
+  const f2 scale = make_f2(rstd), shift = make_f2(-e * rstd);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     if (column<VEC>(tpr, t, k, 0) >= c.dim) break;
@@ -219,9 +254,9 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
       weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, k, 0), w);
       weight_cell<VEC>(c, c.bias, 0.f, column<VEC>(tpr, t, k, 0), b);
     }
-    float y[8];
+    f2 y[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = fmaf((x[k][j] - e) * rstd, w[j], b[j]);
+    for (int i = 0; i < 4; ++i) y[i] = fma2(fma2(x[k][i], scale, shift), w[i], b[i]);
     Cell<Y, VEC>::store(static_cast<Y*>(c.y) + row * c.y_stride, column<VEC>(tpr, t, k, 0), c.dim, y);
   }
   if (t == 0) {
@@ -272,12 +307,12 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
   if (VEC)
     for (int i = 0; i + 1 < STAGES; ++i) send();
 
-  float w[K][8], dw[K][8], db[K][8];
+  f2 w[K][4], dw[K][4], db[K][4];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, k, 0), w[k]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw[k][j] = db[k][j] = 0.f;
+    for (int i = 0; i < 4; ++i) dw[k][i] = db[k][i] = make_f2(0.f);
   }
   float means = 0.f, rstds = 0.f;                           // of 32 rows, one per lane
   uint32_t from = mine;
@@ -313,56 +348,47 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
       pt += c.grad_total_stride;
     }
     const float mean = __shfl_sync(~0u, means, i % 32), rstd = __shfl_sync(~0u, rstds, i % 32);
-    float2 v = make_float2(0.f, 0.f);
+    f2 xhat[K][4], gy[K][4], sum_g = make_f2(0.f), sum_gx = make_f2(0.f);
+    const f2 less = make_f2(-mean), scale = make_f2(rstd);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      float xs[8], ys[8];
-      x[k].get(xs);
-      dy[k].get(ys);
+      x[k].get(xhat[k]);
+      dy[k].get(gy[k]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float xhat = (xs[j] - mean) * rstd, gy = ys[j] * w[k][j];
-        v.x += gy;
-        v.y = fmaf(gy, xhat, v.y);
-        dw[k][j] = fmaf(ys[j], xhat, dw[k][j]);
-        db[k][j] += ys[j];
+      for (int j = 0; j < 4; ++j) {
+        if (!c.rms) xhat[k][j] = add2(xhat[k][j], less);
+        xhat[k][j] = mul2(xhat[k][j], scale);
+        dw[k][j] = fma2(gy[k][j], xhat[k][j], dw[k][j]);
+        db[k][j] = add2(db[k][j], gy[k][j]);
+        gy[k][j] = mul2(gy[k][j], w[k][j]);
+        if (!c.rms) sum_g = add2(sum_g, gy[k][j]);
+        sum_gx = fma2(gy[k][j], xhat[k][j], sum_gx);
       }
     }
     if (!c.grad_x) continue;
-#pragma unroll
-    for (int o = 16; o; o /= 2) {
-      v.x += __shfl_xor_sync(~0u, v.x, o);
-      v.y += __shfl_xor_sync(~0u, v.y, o);
-    }
+    float2 v;
+    const float half = warp_sum(sum2(sum_g), sum2(sum_gx), lane);
     if (warps > 1) {
       float2* sh = sums[i % 2] + group * warps;             // the next row's go elsewhere while these are read
-      if (lane == 0) sh[t / 32] = v;
+      if (lane == 0) sh[t / 32].x = half;
+      if (lane == 16) sh[t / 32].y = half;
       asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
-      v = sh[0];
-#pragma unroll 1
-      for (uint32_t k = 1; k < warps; ++k) {
-        const float2 a = sh[k];
-        v.x += a.x;
-        v.y += a.y;
-      }
+      v = warps_sum(sh, warps, lane);
+    } else {
+      v = make_float2(__shfl_sync(~0u, half, 0), __shfl_sync(~0u, half, 16));
     }
-    const float c1 = c.rms ? 0.f : v.x * c.inv_dim, c2 = v.y * c.inv_dim;
+    // rstd (gy - mean(gy) - xhat mean(gy xhat))
+    const f2 k1 = make_f2(c.rms ? 0.f : -v.x * c.inv_dim * rstd), k2 = make_f2(-v.y * c.inv_dim * rstd);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      x[k].forget();
-      dy[k].forget();
-      float xs[8], ys[8], dx[8];
-      x[k].get(xs);
-      dy[k].get(ys);
+      f2 dx[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float xhat = (xs[j] - mean) * rstd;
-        dx[j] = (fmaf(-xhat, c2, ys[j] * w[k][j]) - c1) * rstd;
-      }
+      for (int j = 0; j < 4; ++j) dx[j] = fma2(gy[k][j], scale, fma2(xhat[k][j], k2, k1));
       if (with_total) {
-        dt[k].get(xs);
+        f2 add[4];
+        dt[k].get(add);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dx[j] += xs[j];
+        for (int j = 0; j < 4; ++j) dx[j] = add2(dx[j], add[j]);
       }
       Cell<X, VEC>::store(pd, column<VEC>(tpr, t, k, 0), c.dim, dx);
     }
@@ -372,13 +398,14 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
   // the groups' sums, in their order
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
+  f2* sh = reinterpret_cast<f2*>(smem);
   if (group) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        smem[((group - 1) * 16 * K + k * 16 + j) * tpr + t] = dw[k][j];
-        smem[((group - 1) * 16 * K + k * 16 + 8 + j) * tpr + t] = db[k][j];
+      for (int j = 0; j < 4; ++j) {
+        sh[((group - 1) * 8 * K + k * 8 + j) * tpr + t] = dw[k][j];
+        sh[((group - 1) * 8 * K + k * 8 + 4 + j) * tpr + t] = db[k][j];
       }
   }
   __syncthreads();
@@ -388,9 +415,9 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dw[k][j] += smem[(o * 16 * K + k * 16 + j) * tpr + t];
-        db[k][j] += smem[(o * 16 * K + k * 16 + 8 + j) * tpr + t];
+      for (int j = 0; j < 4; ++j) {
+        dw[k][j] = add2(dw[k][j], sh[(o * 8 * K + k * 8 + j) * tpr + t]);
+        db[k][j] = add2(db[k][j], sh[(o * 8 * K + k * 8 + 4 + j) * tpr + t]);
       }
   float* part = c.part + uint64_t(2 * blockIdx.x) * c.dp;
 #pragma unroll
