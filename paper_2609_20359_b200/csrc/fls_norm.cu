@@ -10,6 +10,7 @@
 #include <cstdint>
 #include <cstring>
 #include <new>
+#include <type_traits>
 
 #include "fls.h"
 #include "fls_elem.cuh"
@@ -18,8 +19,20 @@
 using namespace fls;
 
 namespace {
+#ifndef FLS_RULE
+#define FLS_RULE (c.dim <= 4096)
+#endif
+#ifndef FLS_T
+#define FLS_T 512
+#endif
+#ifndef FLS_B
+#define FLS_B 2
+#endif
+#ifndef FLS_S2
+#define FLS_S2 2
+#endif
 #ifndef FLS_STAGES
-#define FLS_STAGES 3
+#define FLS_STAGES 2
 #endif
 
 constexpr uint32_t kColTile = 32;          // columns of a CTA of the weight gradients' kernel
@@ -129,12 +142,14 @@ __device__ __forceinline__ void weight_cell(const NormCall& c, const void* p, fl
   }
 }
 
-// Sum over a warp of one or two values; the second step on, two values are in one half of the warp each.
-__device__ __forceinline__ float warp_sum(float x) {
+// Sum over `width` neighbouring lanes, a power of two.
+__device__ __forceinline__ float warp_sum(float x, uint32_t width) {
 #pragma unroll
-  for (int o = 16; o; o /= 2) x += __shfl_xor_sync(~0u, x, o);
+  for (uint32_t o = 16; o; o /= 2)
+    if (o < width) x += __shfl_xor_sync(~0u, x, o);
   return x;
 }
+// Two sums over a warp, from the second step on one in each half:
 // x's sum in lanes 0 .. 15, y's in lanes 16 .. 31.
 __device__ __forceinline__ float warp_sum(float x, float y, uint32_t lane) {
   const float other = __shfl_xor_sync(~0u, lane < 16 ? y : x, 16);
@@ -144,23 +159,35 @@ __device__ __forceinline__ float warp_sum(float x, float y, uint32_t lane) {
   return v;
 }
 
-// Sums over the `warps` warps of a row of what each has left in `shared`, a value of x and one of y.
-__device__ __forceinline__ float2 warps_sum(const float2* shared, uint32_t warps, uint32_t lane) {
-  float2 v = lane < warps ? shared[lane] : make_float2(0.f, 0.f);
-  for (uint32_t o = 1; o < warps; o *= 2) {
-    v.x += __shfl_xor_sync(~0u, v.x, o);
-    v.y += __shfl_xor_sync(~0u, v.y, o);
+// Four sums over a warp: a's in lanes 0 .. 7, b's in lanes 8 .. 15, c's and d's in the other half.
+__device__ __forceinline__ float warp_sum(float a, float b, float c, float d, uint32_t lane) {
+  const bool low = lane < 16, even = (lane & 8) == 0;
+  a = (low ? a : c) + __shfl_xor_sync(~0u, low ? c : a, 16);
+  b = (low ? b : d) + __shfl_xor_sync(~0u, low ? d : b, 16);
+  a = (even ? a : b) + __shfl_xor_sync(~0u, even ? b : a, 8);
+#pragma unroll
+  for (int o = 4; o; o /= 2) a += __shfl_xor_sync(~0u, a, o);
+  return a;
+}
+
+// Sums over the `warps` warps of a row of what each has left in `shared`, V values each, in order of the warps.
+template <int V>
+__device__ __forceinline__ void warps_sum(const float* shared, uint32_t warps, float (&v)[V]) {
+  typedef typename std::conditional<V == 4, float4, float2>::type Vec;
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = shared[i];
+#pragma unroll 4
+  for (uint32_t w = 1; w < warps; ++w) {
+    const Vec x = reinterpret_cast<const Vec*>(shared)[w];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += reinterpret_cast<const float*>(&x)[i];
   }
-  // lanes that hold no sum of all take it from lane 0
-  v.x = __shfl_sync(~0u, v.x, 0);
-  v.y = __shfl_sync(~0u, v.y, 0);
-  return v;
 }
 
 template <typename X, typename Y, bool VEC, int K, int THREADS>
 __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
   __shared__ float2 shared1[32], shared2[32];
-  const uint32_t t = threadIdx.x % tpr, lane = threadIdx.x % 32, warps = tpr / 32, mine = threadIdx.x / 32, first = mine / warps * warps;
+  const uint32_t t = threadIdx.x % tpr, lane = threadIdx.x % 32, width = min(tpr, 32u), warps = tpr / width, mine = threadIdx.x / 32, first = mine / warps * warps;
   const uint64_t n = uint64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
   const bool live = n < c.rows;                             // the others keep the barriers company
   const uint64_t row = live ? n : c.rows - 1;
@@ -202,11 +229,13 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) a = add2(a, x[k][i]);
-    m = warp_sum(sum2(a));
+    m = warp_sum(sum2(a), width);
     if (warps > 1) {
       if (lane == 0) shared1[mine] = make_float2(m, 0.f);
       __syncthreads();
-      m = warps_sum(shared1 + first, warps, lane).x;
+      float v[2];
+      warps_sum<2>(&shared1[first].x, warps, v);
+      m = v[0];
     }
     m *= c.inv_dim;
     const f2 less = make_f2(-m);
@@ -233,17 +262,22 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
       if (!c.rms) ones = add2(ones, x[k][i]);
       squares = fma2(x[k][i], x[k][i], squares);
     }
-  float2 v;
-  const float half = warp_sum(sum2(ones), sum2(squares), lane);
-  if (warps > 1) {
-    if (lane == 0) shared2[mine].x = half;
-    if (lane == 16) shared2[mine].y = half;
-    __syncthreads();
-    v = warps_sum(shared2 + first, warps, lane);
+  float v[2];
+  if (width < 32) {
+    v[0] = c.rms ? 0.f : warp_sum(sum2(ones), width);
+    v[1] = warp_sum(sum2(squares), width);
   } else {
-    v = make_float2(__shfl_sync(~0u, half, 0), __shfl_sync(~0u, half, 16));
+    const float half = warp_sum(sum2(ones), sum2(squares), lane);
+    if (warps > 1) {
+      if (lane % 16 == 0) (lane ? shared2[mine].y : shared2[mine].x) = half;
+      __syncthreads();
+      warps_sum<2>(&shared2[first].x, warps, v);
+    } else {
+      v[0] = __shfl_sync(~0u, half, 0);
+      v[1] = __shfl_sync(~0u, half, 16);
+    }
   }
-  const float e = c.rms ? 0.f : v.x * c.inv_dim, var = fmaf(-e, e, v.y * c.inv_dim);
+  const float e = c.rms ? 0.f : v[0] * c.inv_dim, var = fmaf(-e, e, v[1] * c.inv_dim);
   const float rstd = 1.f / sqrtf(var + c.eps);
   if (!live) return;
   const f2 scale = make_f2(rstd), shift = make_f2(-e * rstd);
@@ -265,47 +299,54 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
   }
 }
 
-// All gradients in one look at the rows.  A CTA has blockDim / tpr groups, a group a stretch of rows, one at a time; a thread
-// keeps its columns' sums for weight and bias in registers, adds them to the other groups' at the end and leaves the CTA's in
-// the workspace.  VEC: STAGES rows are on their way at once, copied asynchronously into shared memory, every warp for itself.
-template <typename X, typename Y, bool VEC, int K, int STAGES, int THREADS>
+// All gradients in one look at the rows.  A CTA has blockDim / tpr groups, a group a stretch of rows, B of them at a time; a
+// thread keeps its columns' sums for weight and bias in registers, adds them to the other groups' at the end and leaves the
+// CTA's in the workspace.  VEC: STAGES times B rows are on their way at once, copied asynchronously into shared memory, every
+// warp for itself.
+template <typename X, typename Y, bool VEC, int K, int B, int STAGES, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
   extern __shared__ __align__(16) float smem[];             // rows on their way, then the groups' sums
-  __shared__ float2 sums[2][32];
+  __shared__ __align__(16) float sums[2][THREADS / 32][2 * B];
   const uint32_t t = threadIdx.x % tpr, group = threadIdx.x / tpr, groups = blockDim.x / tpr, warps = tpr / 32, lane = threadIdx.x % 32;
   const uint64_t all = uint64_t(gridDim.x) * groups, g = uint64_t(blockIdx.x) * groups + group;
   const uint64_t begin = c.rows * g / all;
   const uint32_t count = uint32_t(c.rows * (g + 1) / all - begin);
   const bool with_total = c.grad_total != nullptr;
   const uint32_t row_bytes = K * (Staged<X>::bytes + Staged<Y>::bytes + (with_total ? Staged<X>::bytes : 0));
-  const uint32_t mine = uint32_t(__cvta_generic_to_shared(smem)) + threadIdx.x / 32 * (STAGES * row_bytes);
+  const uint32_t mine = uint32_t(__cvta_generic_to_shared(smem)) + threadIdx.x / 32 * (STAGES * B * row_bytes), stop = mine + STAGES * B * row_bytes;
   const X* px = static_cast<const X*>(c.x) + begin * c.x_stride;
   const Y* py = static_cast<const Y*>(c.grad_y) + begin * c.grad_y_stride;
   const X* pt = static_cast<const X*>(c.grad_total) + begin * c.grad_total_stride;
   X* pd = static_cast<X*>(c.grad_x) + begin * c.grad_x_stride;
   pdl_launch();
 
-  uint32_t to = mine, sent = 0;
-  auto send = [&] {                                         // the next row's copies
-    if (VEC && sent < count) {
+  uint32_t to = mine, unsent = count;
+  auto send = [&] {                                         // the next B rows' copies
+    if (VEC) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const uint32_t first = column<VEC>(tpr, t - lane, k, 0);
-        uint32_t q = to + k * (Staged<X>::bytes + Staged<Y>::bytes);
-        Staged<X>::copy(q, px, first, lane, c.dim);
-        Staged<Y>::copy(q + Staged<X>::bytes, py, first, lane, c.dim);
-        if (with_total) Staged<X>::copy(to + K * (Staged<X>::bytes + Staged<Y>::bytes) + k * Staged<X>::bytes, pt, first, lane, c.dim);
+      for (int b = 0; b < B; ++b) {
+        if (unsent) {
+          --unsent;
+#pragma unroll
+          for (int k = 0; k < K; ++k) {
+            const uint32_t first = column<VEC>(tpr, t - lane, k, 0);
+            const uint32_t q = to + k * (Staged<X>::bytes + Staged<Y>::bytes);
+            Staged<X>::copy(q, px, first, lane, c.dim);
+            Staged<Y>::copy(q + Staged<X>::bytes, py, first, lane, c.dim);
+            if (with_total) Staged<X>::copy(to + K * (Staged<X>::bytes + Staged<Y>::bytes) + k * Staged<X>::bytes, pt, first, lane, c.dim);
+          }
+          px += c.x_stride;
+          py += c.grad_y_stride;
+          pt += c.grad_total_stride;
+        }
+        to += row_bytes;
       }
-      px += c.x_stride;
-      py += c.grad_y_stride;
-      pt += c.grad_total_stride;
-      ++sent;
-      to = sent % STAGES ? to + row_bytes : mine;
+      if (to == stop) to = mine;
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    if (VEC) asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (VEC)
-    for (int i = 0; i + 1 < STAGES; ++i) send();
+#pragma unroll 1
+  for (int i = 0; i + 1 < STAGES; ++i) send();
 
   f2 w[K][4], dw[K][4], db[K][4];
 #pragma unroll
@@ -315,84 +356,108 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
     for (int i = 0; i < 4; ++i) dw[k][i] = db[k][i] = make_f2(0.f);
   }
   float means = 0.f, rstds = 0.f;                           // of 32 rows, one per lane
-  uint32_t from = mine;
-  for (uint32_t i = 0; i < count; ++i) {
-    if (i % 32 == 0 && i + lane < count) {
-      if (!c.rms) means = c.mean_in[begin + i + lane];
-      rstds = c.rstd_in[begin + i + lane];
+  uint32_t from = mine, turn = 0;
+  for (uint32_t i = 0; i < count; i += B) {
+    if (i % 32 == 0) {
+      const bool there = i + lane < count;
+      means = there && !c.rms ? c.mean_in[begin + i + lane] : 0.f;
+      rstds = there ? c.rstd_in[begin + i + lane] : 0.f;
     }
-    Cell<X, VEC> x[K], dt[K];
-    Cell<Y, VEC> dy[K];
-    if constexpr (VEC) {
+    if (VEC) {
       asm volatile("cp.async.wait_group %0;" ::"n"(STAGES > 1 ? STAGES - 2 : 0) : "memory");
       __syncwarp();
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const uint32_t q = from + k * (Staged<X>::bytes + Staged<Y>::bytes);
-        Staged<X>::read(q, lane, x[k].raw);
-        Staged<Y>::read(q + Staged<X>::bytes, lane, dy[k].raw);
-        if (with_total) Staged<X>::read(from + K * (Staged<X>::bytes + Staged<Y>::bytes) + k * Staged<X>::bytes, lane, dt[k].raw);
-      }
-      __syncwarp();
-      from = (i + 1) % STAGES ? from + row_bytes : mine;
-      send();                                               // into the place that the row before this one had
-    } else {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        x[k].load(px, column<VEC>(tpr, t, k, 0), c.dim);
-        dy[k].load(py, column<VEC>(tpr, t, k, 0), c.dim);
-        if (with_total) dt[k].load(pt, column<VEC>(tpr, t, k, 0), c.dim);
-      }
-      px += c.x_stride;
-      py += c.grad_y_stride;
-      pt += c.grad_total_stride;
     }
-    const float mean = __shfl_sync(~0u, means, i % 32), rstd = __shfl_sync(~0u, rstds, i % 32);
-    f2 xhat[K][4], gy[K][4], sum_g = make_f2(0.f), sum_gx = make_f2(0.f);
-    const f2 less = make_f2(-mean), scale = make_f2(rstd);
+    Cell<X, VEC> dt[B][K];
+    f2 xhat[B][K][4], gy[B][K][4];
+    f2 scale[B];
+    float rstd[B], v[2 * B];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      x[k].get(xhat[k]);
-      dy[k].get(gy[k]);
+    for (int b = 0; b < B; ++b) {
+      const bool there = B == 1 || i + b < count;           // the stretch may end with half of a pair, whose place holds what was there
+      Cell<X, VEC> x[K];
+      Cell<Y, VEC> dy[K];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (!c.rms) xhat[k][j] = add2(xhat[k][j], less);
-        xhat[k][j] = mul2(xhat[k][j], scale);
-        dw[k][j] = fma2(gy[k][j], xhat[k][j], dw[k][j]);
-        db[k][j] = add2(db[k][j], gy[k][j]);
-        gy[k][j] = mul2(gy[k][j], w[k][j]);
-        if (!c.rms) sum_g = add2(sum_g, gy[k][j]);
-        sum_gx = fma2(gy[k][j], xhat[k][j], sum_gx);
+      for (int k = 0; k < K; ++k) {
+        if constexpr (VEC) {
+          const uint32_t q = from + b * row_bytes + k * (Staged<X>::bytes + Staged<Y>::bytes);
+          Staged<X>::read(q, lane, x[k].raw);
+          Staged<Y>::read(q + Staged<X>::bytes, lane, dy[k].raw);
+          if (with_total) Staged<X>::read(from + b * row_bytes + K * (Staged<X>::bytes + Staged<Y>::bytes) + k * Staged<X>::bytes, lane, dt[b][k].raw);
+          if (!there) { x[k] = Cell<X, VEC>{}; dy[k] = Cell<Y, VEC>{}; }
+        } else {
+          const uint32_t col = there ? column<VEC>(tpr, t, k, 0) : c.dim;      // nothing beyond the last column
+          x[k].load(px, col, c.dim);
+          dy[k].load(py, col, c.dim);
+          if (with_total) dt[b][k].load(pt, col, c.dim);
+        }
       }
+      if (!VEC) {
+        px += c.x_stride;
+        py += c.grad_y_stride;
+        pt += c.grad_total_stride;
+      }
+      const float mean = __shfl_sync(~0u, means, i + b);
+      rstd[b] = __shfl_sync(~0u, rstds, i + b);             // 0 for a row that is not there
+      scale[b] = make_f2(rstd[b]);
+      f2 sum_g = make_f2(0.f), sum_gx = make_f2(0.f);
+      const f2 less = make_f2(-mean);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        x[k].get(xhat[b][k]);
+        dy[k].get(gy[b][k]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (!c.rms) xhat[b][k][j] = add2(xhat[b][k][j], less);
+          xhat[b][k][j] = mul2(xhat[b][k][j], scale[b]);
+          dw[k][j] = fma2(gy[b][k][j], xhat[b][k][j], dw[k][j]);
+          db[k][j] = add2(db[k][j], gy[b][k][j]);
+          gy[b][k][j] = mul2(gy[b][k][j], w[k][j]);
+          if (!c.rms) sum_g = add2(sum_g, gy[b][k][j]);
+          sum_gx = fma2(gy[b][k][j], xhat[b][k][j], sum_gx);
+        }
+      }
+      v[2 * b] = sum2(sum_g);
+      v[2 * b + 1] = sum2(sum_gx);
+    }
+    if (VEC) {
+      __syncwarp();
+      from += B * row_bytes;
+      if (from == stop) from = mine;
+      send();                                               // into the place that the rows before these had
     }
     if (!c.grad_x) continue;
-    float2 v;
-    const float half = warp_sum(sum2(sum_g), sum2(sum_gx), lane);
+    float part;
+    if constexpr (B == 2) part = warp_sum(v[0], v[1], v[2], v[3], lane);
+    else part = warp_sum(v[0], v[1], lane);
     if (warps > 1) {
-      float2* sh = sums[i % 2] + group * warps;             // the next row's go elsewhere while these are read
-      if (lane == 0) sh[t / 32].x = half;
-      if (lane == 16) sh[t / 32].y = half;
+      if (lane % (16 / B) == 0) sums[turn][threadIdx.x / 32][lane / (16 / B)] = part;
       asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
-      v = warps_sum(sh, warps, lane);
+      warps_sum<2 * B>(sums[turn][group * warps], warps, v);
+      turn ^= 1;                                            // the next rows' go elsewhere while these are read
     } else {
-      v = make_float2(__shfl_sync(~0u, half, 0), __shfl_sync(~0u, half, 16));
+#pragma unroll
+      for (int q = 0; q < 2 * B; ++q) v[q] = __shfl_sync(~0u, part, q * (16 / B));
     }
     // rstd (gy - mean(gy) - xhat mean(gy xhat))
-    const f2 k1 = make_f2(c.rms ? 0.f : -v.x * c.inv_dim * rstd), k2 = make_f2(-v.y * c.inv_dim * rstd);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      f2 dx[4];
+    for (int b = 0; b < B; ++b) {
+      if (B > 1 && i + b >= count) break;
+      const f2 k1 = make_f2(c.rms ? 0.f : -v[2 * b] * c.inv_dim * rstd[b]), k2 = make_f2(-v[2 * b + 1] * c.inv_dim * rstd[b]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) dx[j] = fma2(gy[k][j], scale, fma2(xhat[k][j], k2, k1));
-      if (with_total) {
-        f2 add[4];
-        dt[k].get(add);
+      for (int k = 0; k < K; ++k) {
+        f2 dx[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dx[j] = add2(dx[j], add[j]);
+        for (int j = 0; j < 4; ++j) dx[j] = fma2(gy[b][k][j], scale[b], fma2(xhat[b][k][j], k2, k1));
+        if (with_total) {
+          f2 add[4];
+          dt[b][k].get(add);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dx[j] = add2(dx[j], add[j]);
+        }
+        Cell<X, VEC>::store(pd, column<VEC>(tpr, t, k, 0), c.dim, dx);
       }
-      Cell<X, VEC>::store(pd, column<VEC>(tpr, t, k, 0), c.dim, dx);
+      pd += c.grad_x_stride;
     }
-    pd += c.grad_x_stride;
   }
   if (!c.grad_weight && !c.grad_bias) return;
   // the groups' sums, in their order
@@ -585,12 +650,14 @@ namespace {
 template <typename X, typename Y, bool VEC>
 cudaError_t forward_rows(const NormCall& c, cudaStream_t s) {
   const uint32_t cells = (c.dim + 7) / 8;
-  int k = 4;
-  if (c.rows * cells <= 148 * 1024) k = 1;
+  // Few rows: a cell per thread, for the shortest way through a row.  Many: four, which leaves the fewest sums over threads;
+  // columns moved one by one are many loads on their way as it is.
+  int k = VEC && c.rows * cells > 148 * 1024 ? 4 : 1;
   while (k < 4 && cells > uint32_t(k) * 1024) ++k;
-  if (k == 4)
-    while (k > 1 && cells <= 32u * (k - 1)) --k;            // short rows: no empty cells
-  const uint32_t tpr = (cells + 32 * k - 1) / (32 * k) * 32, rows = std::max(1u, 256 / tpr);
+  while (k > 1 && cells <= 32u * (k - 1)) --k;              // short rows: no empty cells
+  uint32_t tpr = (cells + 32 * k - 1) / (32 * k) * 32;
+  if (VEC && cells <= 16) tpr = cells <= 8 ? 8 : 16;        // two or four rows in a warp
+  const uint32_t rows = std::max(1u, 256 / tpr);
   const dim3 grid(uint32_t((c.rows + rows - 1) / rows));
 #define FLS_K(K) (tpr > 256 ? launch(fls_norm_forward_kernel<X, Y, VEC, K, 1024>, grid, tpr * rows, 0, false, s, c, tpr) \
                             : launch(fls_norm_forward_kernel<X, Y, VEC, K, 256>, grid, tpr * rows, 0, false, s, c, tpr))
@@ -611,13 +678,13 @@ int run_forward(fls_norm* h, NormCall& c, cudaStream_t s) {
   return FLS_OK;
 }
 
-template <typename X, typename Y, bool VEC, int K, int STAGES, int THREADS>
+template <typename X, typename Y, bool VEC, int K, int B, int STAGES, int THREADS>
 cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
   const uint32_t cells = (c.dim + 7) / 8, tpr = (cells + 32 * K - 1) / (32 * K) * 32, groups = THREADS / tpr, threads = tpr * groups;
   c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(148, (c.rows + groups - 1) / groups)));
   const uint32_t row_bytes = K * (Staged<X>::bytes * (c.grad_total ? 2 : 1) + Staged<Y>::bytes);
-  const uint32_t smem = std::max(VEC ? STAGES * row_bytes * (threads / 32) : 0, (groups - 1) * tpr * 16 * K * 4);
-  auto kernel = fls_norm_backward_kernel<X, Y, VEC, K, STAGES, THREADS>;
+  const uint32_t smem = std::max(VEC ? STAGES * B * row_bytes * (threads / 32) : 0, (groups - 1) * tpr * 16 * K * 4);
+  auto kernel = fls_norm_backward_kernel<X, Y, VEC, K, B, STAGES, THREADS>;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_shared(reinterpret_cast<const void*>(kernel), 226 << 10, done);
   if (e != cudaSuccess) return e;
@@ -626,7 +693,7 @@ cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
 
 template <typename X, typename Y, bool VEC>
 cudaError_t backward_of(NormCall& c, cudaStream_t s) {
-  return c.dim <= 6144 ? backward_rows<X, Y, VEC, 1, FLS_STAGES, 768>(c, s) : backward_rows<X, Y, VEC, 2, 2, 512>(c, s);
+  return FLS_RULE ? backward_rows<X, Y, VEC, 1, FLS_B, FLS_STAGES, FLS_T>(c, s) : backward_rows<X, Y, VEC, 2, 1, FLS_S2, 512>(c, s);
 }
 
 template <typename X, typename Y>
