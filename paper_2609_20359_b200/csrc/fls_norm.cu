@@ -19,21 +19,6 @@
 using namespace fls;
 
 namespace {
-#ifndef FLS_RULE
-#define FLS_RULE (c.dim <= 4096)
-#endif
-#ifndef FLS_T
-#define FLS_T 512
-#endif
-#ifndef FLS_B
-#define FLS_B 2
-#endif
-#ifndef FLS_S2
-#define FLS_S2 2
-#endif
-#ifndef FLS_STAGES
-#define FLS_STAGES 2
-#endif
 
 constexpr uint32_t kColTile = 32;          // columns of a CTA of the weight gradients' kernel
 constexpr uint32_t kMaxParts = 296;        // parts of the rows whose sums are joined
@@ -184,40 +169,30 @@ __device__ __forceinline__ void warps_sum(const float* shared, uint32_t warps, f
   }
 }
 
-template <typename X, typename Y, bool VEC, int K, int THREADS>
-__global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
-  __shared__ float2 shared1[32], shared2[32];
-  const uint32_t t = threadIdx.x % tpr, lane = threadIdx.x % 32, width = min(tpr, 32u), warps = tpr / width, mine = threadIdx.x / 32, first = mine / warps * warps;
-  const uint64_t n = uint64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
-  const bool live = n < c.rows;                             // the others keep the barriers company
-  const uint64_t row = live ? n : c.rows - 1;
-  f2 x[K][4];
-  {
-    Cell<X, VEC> in[K], add[K];
+// One row from its cells on: the residual's addition, statistics and the result.  The row's threads meet in `meet`; shared1 and
+// shared2 hold a value of each of the CTA's warps.  live: false for threads that only keep the others' barriers company.
+template <typename X, typename Y, bool VEC, int K, typename Meet>
+__device__ __forceinline__ void norm_row(const NormCall& c, const Cell<X, VEC> (&in)[K], const Cell<X, VEC> (&add)[K], uint64_t n, bool live,
+                                         uint32_t tpr, uint32_t t, float2* shared1, float2* shared2, Meet meet) {
+  const uint32_t lane = threadIdx.x % 32, width = min(tpr, 32u), warps = tpr / width, mine = threadIdx.x / 32, first = mine / warps * warps;
+  f2 x[K][4], w[4], b[4];
 #pragma unroll
-    for (int k = 0; k < K; ++k) in[k].load(static_cast<const X*>(c.x) + row * c.x_stride, column<VEC>(tpr, t, k, 0), c.dim);
-    if (c.residual)
+  for (int k = 0; k < K; ++k) in[k].get(x[k]);
+  if (c.residual) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) add[k].load(static_cast<const X*>(c.residual) + row * c.residual_stride, column<VEC>(tpr, t, k, 0), c.dim);
+    for (int k = 0; k < K; ++k) {
+      f2 r[4];
+      float s[8];
+      add[k].get(r);
 #pragma unroll
-    for (int k = 0; k < K; ++k) in[k].get(x[k]);
-    if (c.residual) {
+      for (int i = 0; i < 4; ++i) r[i] = add2(x[k][i], r[i]);
+      singles_of(r, s);
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        f2 r[4];
-        float s[8];
-        add[k].get(r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = add2(x[k][i], r[i]);
-        singles_of(r, s);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = Elem<X>::round(s[j]);
-        pairs_of(s, x[k]);
-        if (live) Cell<X, VEC>::store(static_cast<X*>(c.total) + row * c.total_stride, column<VEC>(tpr, t, k, 0), c.dim, x[k]);
-      }
+      for (int j = 0; j < 8; ++j) s[j] = Elem<X>::round(s[j]);
+      pairs_of(s, x[k]);
+      if (live) Cell<X, VEC>::store(static_cast<X*>(c.total) + n * c.total_stride, column<VEC>(tpr, t, k, 0), c.dim, x[k]);
     }
   }
-  f2 w[4], b[4];
   if (K == 1) {                                             // few rows: everything on its way at once
     weight_cell<VEC>(c, c.weight, 1.f, column<VEC>(tpr, t, 0, 0), w);
     weight_cell<VEC>(c, c.bias, 0.f, column<VEC>(tpr, t, 0, 0), b);
@@ -232,7 +207,7 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
     m = warp_sum(sum2(a), width);
     if (warps > 1) {
       if (lane == 0) shared1[mine] = make_float2(m, 0.f);
-      __syncthreads();
+      meet();
       float v[2];
       warps_sum<2>(&shared1[first].x, warps, v);
       m = v[0];
@@ -270,7 +245,7 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
     const float half = warp_sum(sum2(ones), sum2(squares), lane);
     if (warps > 1) {
       if (lane % 16 == 0) (lane ? shared2[mine].y : shared2[mine].x) = half;
-      __syncthreads();
+      meet();
       warps_sum<2>(&shared2[first].x, warps, v);
     } else {
       v[0] = __shfl_sync(~0u, half, 0);
@@ -291,12 +266,34 @@ __global__ void __launch_bounds__(THREADS) fls_norm_forward_kernel(const __grid_
     f2 y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = fma2(fma2(x[k][i], scale, shift), w[i], b[i]);
-    Cell<Y, VEC>::store(static_cast<Y*>(c.y) + row * c.y_stride, column<VEC>(tpr, t, k, 0), c.dim, y);
+    Cell<Y, VEC>::store(static_cast<Y*>(c.y) + n * c.y_stride, column<VEC>(tpr, t, k, 0), c.dim, y);
   }
   if (t == 0) {
     if (c.mean) c.mean[n] = m + e;
     if (c.rstd) c.rstd[n] = rstd;
   }
+}
+
+// CTAs of an SM that the registers are divided among (us of 16384 x 2048 bf16, K = 4, with 3 / 4: 32.6 / 29.4; 65536 x 512, K = 2,
+// with 4 / 5: 46.3 / 43.5; 65536 x 256, K = 1, with 5 / 6: 29.4 / 27.8).
+constexpr int ctas_per_sm(bool vec, int k, int size, int threads) {
+  return threads != 256 ? 1 : !vec ? (k == 1 ? 5 : 1) : size == 4 ? 1 : k == 1 ? 6 : k == 2 ? 5 : 4;
+}
+
+template <typename X, typename Y, bool VEC, int K, int THREADS>
+__global__ void __launch_bounds__(THREADS, ctas_per_sm(VEC, K, sizeof(X), THREADS)) fls_norm_forward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
+  __shared__ float2 shared1[32], shared2[32];
+  const uint32_t t = threadIdx.x % tpr;
+  const uint64_t n = uint64_t(blockIdx.x) * (blockDim.x / tpr) + threadIdx.x / tpr;
+  const bool live = n < c.rows;
+  const uint64_t row = live ? n : c.rows - 1;
+  Cell<X, VEC> in[K], add[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) in[k].load(static_cast<const X*>(c.x) + row * c.x_stride, column<VEC>(tpr, t, k, 0), c.dim);
+  if (c.residual)
+#pragma unroll
+    for (int k = 0; k < K; ++k) add[k].load(static_cast<const X*>(c.residual) + row * c.residual_stride, column<VEC>(tpr, t, k, 0), c.dim);
+  norm_row<X, Y, VEC, K>(c, in, add, row, live, tpr, t, shared1, shared2, [] { __syncthreads(); });
 }
 
 // All gradients in one look at the rows.  A CTA has blockDim / tpr groups, a group a stretch of rows, B of them at a time; a
@@ -693,7 +690,10 @@ cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
 
 template <typename X, typename Y, bool VEC>
 cudaError_t backward_of(NormCall& c, cudaStream_t s) {
-  return FLS_RULE ? backward_rows<X, Y, VEC, 1, FLS_B, FLS_STAGES, FLS_T>(c, s) : backward_rows<X, Y, VEC, 2, 1, FLS_S2, 512>(c, s);
+  // One row of two cells per thread, or two rows of one cell: the latter leaves more threads for short rows (us, two cells / two rows:
+  // 32768 x 768 fp32 54.8 / 48.1, 8192 x 4096 bf16 52.9 / 55.3); columns moved one by one want the former (8192 x 1001 33.4 / 39.5).
+  // One row of one cell and 768 threads: 51.7 and 77.7.
+  return VEC && c.dim <= 4096 ? backward_rows<X, Y, VEC, 1, 2, 2, 512>(c, s) : backward_rows<X, Y, VEC, 2, 1, 2, 512>(c, s);
 }
 
 template <typename X, typename Y>

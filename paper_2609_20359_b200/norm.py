@@ -75,8 +75,8 @@ class Norm:
                 raise ValueError("grad_x and grad_total without input_grad")
             io.grad_x, io.grad_x_stride = None, 0
         elif grad_x is None:
-            grad_x = x.new_empty((n, dim)) if stream is None else _empty_on(stream, (n, dim), xt, dev)
-            io.grad_x, io.grad_x_stride = grad_x.data_ptr(), 0
+            grad_x = torch.empty_like(x) if stream is None else _empty_on(stream, (n, dim), xt, dev)
+            io.grad_x, io.grad_x_stride = grad_x.data_ptr(), 0       # dense, whatever x's stride
         else:
             io.grad_x, io.grad_x_stride = _matrix(grad_x, "grad_x", n, dim, xt, dev)
         io.grad_total, io.grad_total_stride = (None, 0) if grad_total is None else _matrix(grad_total, "grad_total", n, dim, xt, dev)
@@ -98,12 +98,12 @@ class Norm:
         else:
             io.residual, io.residual_stride = _matrix(residual, "residual", n, dim, xt, dev)
             if total is None:
-                total = x.new_empty((n, dim)) if stream is None else _empty_on(stream, (n, dim), xt, dev)
+                total = torch.empty_like(x) if stream is None else _empty_on(stream, (n, dim), xt, dev)
                 io.total, io.total_stride = total.data_ptr(), 0
             else:
                 io.total, io.total_stride = _matrix(total, "total", n, dim, xt, dev)
         if y is None:
-            y = x.new_empty((n, dim)) if stream is None and xt is self.y_torch_dtype else _empty_on(stream, (n, dim), self.y_torch_dtype, dev)
+            y = torch.empty_like(x) if stream is None and xt is self.y_torch_dtype else _empty_on(stream, (n, dim), self.y_torch_dtype, dev)
             io.y, io.y_stride = y.data_ptr(), 0
         else:
             io.y, io.y_stride = _matrix(y, "y", n, dim, self.y_torch_dtype, dev)
