@@ -8,8 +8,7 @@ from __future__ import annotations
 import torch
 
 from . import _binding as fls
-from .head import _dense, _empty_on, _matrix
-from .workspace import Workspace, device_of, dtype_of
+from .workspace import Workspace, device_of, dtype_of, matrix, vector
 
 
 class Embedding:
@@ -39,36 +38,29 @@ class Embedding:
 
     def lookup(self, tokens, weight, out=None, scale: float = 1.0, ignore_token: int = -100, stream=None):
         """scale * weight[tokens], [N, dim]: zeros where a token is ignore_token, NaN where it is outside the table."""
-        io, dev = self._args, self.device
-        n = self._tokens(tokens)
-        io.weight, io.weight_stride = _matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16, dev)
+        io, n = self._args, self._tokens(tokens)
+        io.weight, io.weight_stride = matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16)
         if out is None:
-            if stream is None and self.act_torch_dtype is torch.bfloat16:
-                out = weight.new_empty((n, self.dim))
-            else:
-                out = _empty_on(stream, (n, self.dim), self.act_torch_dtype, dev)
+            out = self.workspace.new(stream, (n, self.dim), self.act_torch_dtype)
             io.out, io.out_stride = out.data_ptr(), 0
         else:
-            io.out, io.out_stride = _matrix(out, "out", n, self.dim, self.act_torch_dtype, dev)
+            io.out, io.out_stride = matrix(out, "out", n, self.dim, self.act_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, 0
-        fls.fls_embed_lookup(self.handle, io, stream)
+        fls.fls_embed_lookup(self.handle, io, self.workspace.stream(stream))
         return out
 
     def grad(self, tokens, grad_out, grad_weight, scale: float = 1.0, accumulate: bool = False, ignore_token: int = -100,
              stream=None) -> None:
         """grad_weight [vocab, dim] becomes (accumulate: is added) scale times the sums of the rows of grad_out by token."""
-        io, dev = self._args, self.device
-        n = self._tokens(tokens)
-        io.grad_out, io.grad_out_stride = _matrix(grad_out, "grad_out", n, self.dim, self.act_torch_dtype, dev)
-        io.grad_weight, io.grad_weight_stride = _matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype, dev)
+        io, n = self._args, self._tokens(tokens)
+        io.grad_out, io.grad_out_stride = matrix(grad_out, "grad_out", n, self.dim, self.act_torch_dtype)
+        io.grad_weight, io.grad_weight_stride = matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, accumulate
         fls.fls_embed_grad(self.handle, io, self.workspace.use(stream))
 
     def _tokens(self, tokens) -> int:
-        if tokens.dim() != 1:
-            raise ValueError(f"tokens must be one-dimensional, got {tuple(tokens.shape)}")
-        n = tokens.shape[0]
-        self._args.token = _dense(tokens, "tokens", (n,), torch.int64, self.device)
+        n = tokens.numel()
+        self._args.token = vector(tokens, "tokens", n, torch.int64)
         self._args.tokens = n
         return n
 

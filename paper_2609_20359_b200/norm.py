@@ -8,8 +8,7 @@ from __future__ import annotations
 import torch
 
 from . import _binding as fls
-from .head import _dense, _empty_on, _matrix
-from .workspace import Workspace, device_of, dtype_of
+from .workspace import Workspace, device_of, dtype_of, matrix, vector
 
 
 class Norm:
@@ -58,65 +57,62 @@ class Norm:
         """grad_x, the gradient of what was normalised (`x`: total, after add_forward), plus grad_total if given; the gradients of
         weight and bias go to grad_weight and grad_bias, each optional, accumulate adds to them.  `grad_x` may be grad_total
         itself; input_grad=False leaves it out."""
-        io, dev, dim = self._grad_io, self.device, self.dim
-        xt = self.x_torch_dtype
-        io.x, io.x_stride = _matrix(x, "x", None, dim, xt, dev)
+        io, dim, xt, gt = self._grad_io, self.dim, self.x_torch_dtype, self.grad_torch_dtype
+        io.x, io.x_stride = matrix(x, "x", None, dim, xt)
         n = io.rows = x.shape[0]
-        io.weight = _dense(weight, "weight", (dim,), self.weight_torch_dtype, dev)
+        io.weight = vector(weight, "weight", dim, self.weight_torch_dtype)
         if (mean is None) != (self.kind == "rms"):
             raise ValueError("mean belongs to layer norms, and to all of them")
-        io.mean = _dense(mean, "mean", (n,), torch.float32, dev)
+        io.mean = vector(mean, "mean", n, torch.float32)
         if rstd is None:
             raise ValueError("rstd is needed")
-        io.rstd = _dense(rstd, "rstd", (n,), torch.float32, dev)
-        io.grad_y, io.grad_y_stride = _matrix(grad_y, "grad_y", n, dim, self.y_torch_dtype, dev)
+        io.rstd = vector(rstd, "rstd", n, torch.float32)
+        io.grad_y, io.grad_y_stride = matrix(grad_y, "grad_y", n, dim, self.y_torch_dtype)
         if not input_grad:
             if grad_x is not None or grad_total is not None:
                 raise ValueError("grad_x and grad_total without input_grad")
             io.grad_x, io.grad_x_stride = None, 0
         elif grad_x is None:
-            grad_x = torch.empty_like(x) if stream is None else _empty_on(stream, (n, dim), xt, dev)
-            io.grad_x, io.grad_x_stride = grad_x.data_ptr(), 0       # dense, whatever x's stride
+            grad_x = self.workspace.new(stream, (n, dim), xt)
+            io.grad_x, io.grad_x_stride = grad_x.data_ptr(), 0
         else:
-            io.grad_x, io.grad_x_stride = _matrix(grad_x, "grad_x", n, dim, xt, dev)
-        io.grad_total, io.grad_total_stride = (None, 0) if grad_total is None else _matrix(grad_total, "grad_total", n, dim, xt, dev)
-        io.grad_weight = _dense(grad_weight, "grad_weight", (dim,), self.grad_torch_dtype, dev)
-        io.grad_bias = _dense(grad_bias, "grad_bias", (dim,), self.grad_torch_dtype, dev)
+            io.grad_x, io.grad_x_stride = matrix(grad_x, "grad_x", n, dim, xt)
+        io.grad_total, io.grad_total_stride = (None, 0) if grad_total is None else matrix(grad_total, "grad_total", n, dim, xt)
+        io.grad_weight = vector(grad_weight, "grad_weight", dim, gt)
+        io.grad_bias = vector(grad_bias, "grad_bias", dim, gt)
         io.accumulate = accumulate
         fls.fls_norm_backward(self.handle, io, self.workspace.use(stream))
         return grad_x
 
     def _forward(self, x, residual, weight, bias, y, total, stats, stream):
-        io, dev, dim, xt = self._io, self.device, self.dim, self.x_torch_dtype
-        io.x, io.x_stride = _matrix(x, "x", None, dim, xt, dev)
+        io, dim, xt, yt, new = self._io, self.dim, self.x_torch_dtype, self.y_torch_dtype, self.workspace.new
+        io.x, io.x_stride = matrix(x, "x", None, dim, xt)
         n = io.rows = x.shape[0]
-        io.weight = _dense(weight, "weight", (dim,), self.weight_torch_dtype, dev)
-        io.bias = _dense(bias, "bias", (dim,), self.weight_torch_dtype, dev)
+        io.weight = vector(weight, "weight", dim, self.weight_torch_dtype)
+        io.bias = vector(bias, "bias", dim, self.weight_torch_dtype)
         if residual is None:
             io.residual = io.total = None
             io.residual_stride = io.total_stride = 0
         else:
-            io.residual, io.residual_stride = _matrix(residual, "residual", n, dim, xt, dev)
+            io.residual, io.residual_stride = matrix(residual, "residual", n, dim, xt)
             if total is None:
-                total = torch.empty_like(x) if stream is None else _empty_on(stream, (n, dim), xt, dev)
+                total = new(stream, (n, dim), xt)
                 io.total, io.total_stride = total.data_ptr(), 0
             else:
-                io.total, io.total_stride = _matrix(total, "total", n, dim, xt, dev)
+                io.total, io.total_stride = matrix(total, "total", n, dim, xt)
         if y is None:
-            y = torch.empty_like(x) if stream is None and xt is self.y_torch_dtype else _empty_on(stream, (n, dim), self.y_torch_dtype, dev)
+            y = new(stream, (n, dim), yt)
             io.y, io.y_stride = y.data_ptr(), 0
         else:
-            io.y, io.y_stride = _matrix(y, "y", n, dim, self.y_torch_dtype, dev)
-        mean = rstd = None
-        io.mean = io.rstd = None
+            io.y, io.y_stride = matrix(y, "y", n, dim, yt)
+        mean = rstd = io.mean = io.rstd = None
         if stats:
             if self.kind == "layer":
-                mean, rstd = _empty_on(stream, (2, n), torch.float32, dev).unbind(0)
+                mean = new(stream, n, torch.float32)
                 io.mean = mean.data_ptr()
-            else:
-                rstd = _empty_on(stream, (n,), torch.float32, dev)
+            rstd = new(stream, n, torch.float32)
             io.rstd = rstd.data_ptr()
-        fls.fls_norm_forward(self.handle, io, stream)
+        fls.fls_norm_forward(self.handle, io, self.workspace.stream(stream))
         return y, total, mean, rstd
 
     def close(self) -> None:

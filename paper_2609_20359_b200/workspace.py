@@ -5,6 +5,8 @@ import torch
 
 from . import _binding as fls
 
+_current_raw_stream = torch._C._cuda_getCurrentRawStream
+
 
 def device_of(device) -> torch.device:
     """The CUDA device, made current."""
@@ -24,9 +26,34 @@ def dtype_of(name: str, what: str):
     return (torch.float32, fls.FLS_GRAD_F32) if name == "f32" else (torch.bfloat16, fls.FLS_GRAD_BF16)
 
 
+def matrix(t: torch.Tensor, name: str, rows, cols: int, dtype: torch.dtype):
+    """Checks a 2-D tensor whose rows are contiguous and do not overlap; returns (address, elements between rows, 0 if dense)."""
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 2 or shape[1] != cols or (rows is not None and shape[0] != rows) or not t.is_cuda:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape [{'N' if rows is None else rows}, {cols}] on a CUDA device, "
+                         f"got {t.dtype} {tuple(shape)} on {t.device}")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    row, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous (stride {one})")
+    if row < cols:
+        raise ValueError(f"{name}: rows overlap (stride {row})")
+    return t.data_ptr(), row
+
+
+def vector(t, name: str, n: int, dtype: torch.dtype):
+    """Address of a contiguous tensor of n elements, None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {(n,)} on a CUDA device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
 class Workspace:
-    """`nbytes` of memory that nothing else uses from here on, whichever stream the first call is on; it is not given to
-    anyone else before the work of every call is done."""
+    """`nbytes` of memory that nothing else uses from here on, whichever stream the first call is on, and that is not given to
+    anyone else before the work of every call is done; and the streams and outputs of those calls."""
 
     def __init__(self, nbytes: int, device: torch.device):
         self.device = device
@@ -35,10 +62,15 @@ class Workspace:
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(device).synchronize()
         self._streams = {fls._stream_handle(None)}             # those that torch's allocator knows to use the memory
+        self._like = {t: torch.empty(0, dtype=t, device=device) for t in (torch.float32, torch.bfloat16)}
+
+    def stream(self, stream) -> int:
+        """The call's stream as a handle."""
+        return _current_raw_stream(self.device.index) if stream is None else fls._stream_handle(stream)
 
     def use(self, stream) -> int:
-        """The call's stream as a handle."""
-        handle = fls._stream_handle(stream)
+        """The same, for a call that uses the memory."""
+        handle = self.stream(stream)
         if handle not in self._streams:
             if stream is None:
                 stream = torch.cuda.current_stream(self.device)
@@ -47,3 +79,10 @@ class Workspace:
             self.memory.record_stream(stream)
             self._streams.add(handle)
         return handle
+
+    def new(self, stream, shape, dtype: torch.dtype) -> torch.Tensor:
+        """An output of a call: its memory's reuse is ordered by the stream that writes it, which need not be torch's current one."""
+        if stream is None:
+            return self._like[dtype].new_empty(shape)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
