@@ -616,7 +616,7 @@ typedef struct {
   void* grad_x;                 /* N x d, output; may be grad_total itself (same stride); NULL: not computed    */
   void* grad_weight;            /* d, output; NULL: not computed                                                */
   void* grad_bias;              /* d, output; NULL: not computed                                                */
-  void* workspace;              /* 256-byte aligned; holds nothing between calls                                */
+  void* workspace;              /* 256-byte aligned; its first 256 bytes are zero before the first call, and after every call */
   uint64_t workspace_bytes;
   uint64_t x_stride, grad_y_stride, grad_total_stride, grad_x_stride;
   uint32_t accumulate;          /* 1: grad_weight and grad_bias are added to                                    */

@@ -21,6 +21,7 @@ using namespace fls;
 namespace {
 
 constexpr uint32_t kColTile = 32;          // columns of a CTA of the weight gradients' kernel
+constexpr uint32_t kJoinFloats = 16384;    // of each of the two gradients
 constexpr uint32_t kMaxParts = 296;        // parts of the rows whose sums are joined
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
@@ -37,6 +38,8 @@ struct NormCall {
   uint32_t dim, dp;
   uint32_t rms, weight_f32, grad_f32, accumulate;
   float eps, inv_dim;
+  uint32_t* ticket;                        // 0 between calls: CTAs that have left their sums
+  uint32_t join;                           // the last of them adds the sums up
   float2* coef;                            // [rows]: mean(g) and mean(g xhat)
   float* part;                             // [parts][2][dp]
   uint32_t parts;
@@ -64,6 +67,19 @@ __device__ __forceinline__ float2 block_sum(float2 v, float2* shared) {
     v.y += __shfl_xor_sync(~0u, v.y, o);
   }
   return v;
+}
+
+// The gradient of column `col` of the weight (which = 0) or the bias (1).
+__device__ __forceinline__ void write_gradient(const NormCall& c, uint32_t which, uint32_t col, float sum) {
+  void* out = which ? c.grad_bias : c.grad_weight;
+  if (!out || col >= c.dim) return;
+  if (c.grad_f32) {
+    float* o = static_cast<float*>(out) + col;
+    *o = c.accumulate ? *o + sum : sum;
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(out) + col;
+    Elem<uint16_t>::put(o, c.accumulate ? Elem<uint16_t>::get(o) + sum : sum);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ rows in registers
@@ -471,21 +487,46 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
       }
   }
   __syncthreads();
-  if (group) return;
+  if (group == 0) {
 #pragma unroll 1
-  for (uint32_t o = 0; o + 1 < groups; ++o)
+    for (uint32_t o = 0; o + 1 < groups; ++o)
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+      for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        dw[k][j] = add2(dw[k][j], sh[(o * 8 * K + k * 8 + j) * tpr + t]);
-        db[k][j] = add2(db[k][j], sh[(o * 8 * K + k * 8 + 4 + j) * tpr + t]);
-      }
-  float* part = c.part + uint64_t(2 * blockIdx.x) * c.dp;
+        for (int j = 0; j < 4; ++j) {
+          dw[k][j] = add2(dw[k][j], sh[(o * 8 * K + k * 8 + j) * tpr + t]);
+          db[k][j] = add2(db[k][j], sh[(o * 8 * K + k * 8 + 4 + j) * tpr + t]);
+        }
+    float* part = c.part + uint64_t(2 * blockIdx.x) * c.dp;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    Cell<float, VEC>::store(part, column<VEC>(tpr, t, k, 0), c.dim, dw[k]);
-    Cell<float, VEC>::store(part + c.dp, column<VEC>(tpr, t, k, 0), c.dim, db[k]);
+    for (int k = 0; k < K; ++k) {
+      Cell<float, VEC>::store(part, column<VEC>(tpr, t, k, 0), c.dim, dw[k]);
+      Cell<float, VEC>::store(part + c.dp, column<VEC>(tpr, t, k, 0), c.dim, db[k]);
+    }
+  }
+  if (!c.join) return;
+  // few sums: whoever comes last adds them up, in order of the CTAs
+  __shared__ uint32_t arrived;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) arrived = atomicAdd(c.ticket, 1u);
+  __syncthreads();
+  if (arrived + 1 != gridDim.x) return;
+  __threadfence();
+  if (threadIdx.x == 0) *c.ticket = 0;
+  for (uint32_t q = threadIdx.x; q < c.dp / 2; q += blockDim.x) {       // four columns of the weight's sums, then of the bias's
+    const uint32_t which = q >= c.dp / 4, col = (which ? q - c.dp / 4 : q) * 4;
+    const float4* from = reinterpret_cast<const float4*>(c.part + uint64_t(which) * c.dp + col);
+    float4 sum = __ldcg(from);
+#pragma unroll 8
+    for (uint32_t p = 1; p < gridDim.x; ++p) {
+      const float4 v = __ldcg(from + uint64_t(p) * (c.dp / 2));
+      sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    write_gradient(c, which, col, sum.x);
+    write_gradient(c, which, col + 1, sum.y);
+    write_gradient(c, which, col + 2, sum.z);
+    write_gradient(c, which, col + 3, sum.w);
   }
 }
 
@@ -600,20 +641,13 @@ __global__ void __launch_bounds__(1024) fls_norm_join_kernel(const __grid_consta
 #pragma unroll
   for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
   const uint32_t col = blockIdx.x * kColTile + group;
-  if (lane || col >= c.dim) return;
-  if (c.grad_f32) {
-    float* o = static_cast<float*>(out) + col;
-    *o = c.accumulate ? *o + sum : sum;
-  } else {
-    uint16_t* o = static_cast<uint16_t*>(out) + col;
-    Elem<uint16_t>::put(o, c.accumulate ? Elem<uint16_t>::get(o) + sum : sum);
-  }
+  if (!lane) write_gradient(c, which, col, sum);
 }
 
 struct Regions { uint64_t coef, part, total; };
 Regions regions(const fls_norm_desc& d) {
   Regions r{};
-  uint64_t at = 0;
+  uint64_t at = d.grads ? 256 : 0;         // the ticket
   auto take = [&](uint64_t bytes) { const uint64_t o = at; at += up(bytes, 256); return o; };
   if (d.grads) {
     r.coef = take(std::max<uint64_t>(d.max_rows, 1) * 8);
@@ -678,7 +712,9 @@ int run_forward(fls_norm* h, NormCall& c, cudaStream_t s) {
 template <typename X, typename Y, bool VEC, int K, int B, int STAGES, int THREADS>
 cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
   const uint32_t cells = (c.dim + 7) / 8, tpr = (cells + 32 * K - 1) / (32 * K) * 32, groups = THREADS / tpr, threads = tpr * groups;
-  c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(148, (c.rows + groups - 1) / groups)));
+  c.parts = uint32_t(std::max<uint64_t>(1, std::min<uint64_t>(148, (c.rows + B * groups - 1) / (B * groups))));
+  // Up to 128 KB of sums are added up by one CTA, more of them by a kernel of its own.
+  c.join = c.parts * c.dp <= kJoinFloats;
   const uint32_t row_bytes = K * (Staged<X>::bytes * (c.grad_total ? 2 : 1) + Staged<Y>::bytes);
   const uint32_t smem = std::max(VEC ? STAGES * B * row_bytes * (threads / 32) : 0, (groups - 1) * tpr * 16 * K * 4);
   auto kernel = fls_norm_backward_kernel<X, Y, VEC, K, B, STAGES, THREADS>;
@@ -715,7 +751,7 @@ int run_backward(fls_norm* h, NormCall& c, cudaStream_t s) {
     }
     FLS_LAUNCH(launch(fls_norm_columns_kernel<X, Y>, dim3(tiles, c.parts), 256, 0, dependent, s, c));
   }
-  if (c.grad_weight || c.grad_bias) FLS_LAUNCH(launch(fls_norm_join_kernel, dim3(tiles, 2), 1024, 0, true, s, c));
+  if ((c.grad_weight || c.grad_bias) && !c.join) FLS_LAUNCH(launch(fls_norm_join_kernel, dim3(tiles, 2), 1024, 0, true, s, c));
   return FLS_OK;
 }
 
@@ -850,6 +886,7 @@ int fls_norm_backward(fls_norm* h, const fls_norm_grad_io* io, void* cuda_stream
   c.grad_x = io->grad_x; c.grad_weight = io->grad_weight; c.grad_bias = io->grad_bias;
   c.accumulate = io->accumulate;
   char* w = static_cast<char*>(io->workspace);
+  c.ticket = reinterpret_cast<uint32_t*>(w);
   c.coef = reinterpret_cast<float2*>(w + h->reg.coef);
   c.part = reinterpret_cast<float*>(w + h->reg.part);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

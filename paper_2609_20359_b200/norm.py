@@ -73,7 +73,7 @@ class Norm:
                 raise ValueError("grad_x and grad_total without input_grad")
             io.grad_x, io.grad_x_stride = None, 0
         elif grad_x is None:
-            grad_x = self.workspace.new(stream, (n, dim), xt)
+            grad_x = torch.empty_like(x) if stream is None else self.workspace.new(stream, (n, dim), xt)
             io.grad_x, io.grad_x_stride = grad_x.data_ptr(), 0
         else:
             io.grad_x, io.grad_x_stride = matrix(grad_x, "grad_x", n, dim, xt)
@@ -96,12 +96,12 @@ class Norm:
         else:
             io.residual, io.residual_stride = matrix(residual, "residual", n, dim, xt)
             if total is None:
-                total = new(stream, (n, dim), xt)
+                total = torch.empty_like(x) if stream is None else new(stream, (n, dim), xt)
                 io.total, io.total_stride = total.data_ptr(), 0
             else:
                 io.total, io.total_stride = matrix(total, "total", n, dim, xt)
         if y is None:
-            y = new(stream, (n, dim), yt)
+            y = torch.empty_like(x) if stream is None and xt is yt else new(stream, (n, dim), yt)
             io.y, io.y_stride = y.data_ptr(), 0
         else:
             io.y, io.y_stride = matrix(y, "y", n, dim, yt)

@@ -52,13 +52,14 @@ def vector(t, name: str, n: int, dtype: torch.dtype):
 
 
 class Workspace:
-    """`nbytes` of memory that nothing else uses from here on, whichever stream the first call is on, and that is not given to
+    """`nbytes` of memory, the first 256 of them zero, that nothing else uses from here on, whichever stream the first call is on, and that is not given to
     anyone else before the work of every call is done; and the streams and outputs of those calls."""
 
     def __init__(self, nbytes: int, device: torch.device):
         self.device = device
         self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        # what used this memory before must not come after the first call
+        self.memory[:256].zero_()
+        # the clear, and what used this memory before, must not come after the first call
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream(device).synchronize()
         self._streams = {fls._stream_handle(None)}             # those that torch's allocator knows to use the memory

@@ -84,7 +84,7 @@ def test_backward(kind, x_type, y_type, n, d, pad, shift):
     mean, rstd = (t.float() for t in R.statistics(x.double(), 1e-5, rms))
     mean = None if rms else mean
     op = norm(n, d, kind, 1e-5, x_type, y_type, wt, gt)
-    op.workspace.memory.fill_(255)
+    op.workspace.memory[256:].fill_(255)
     dw, db = (torch.full((d,), float("nan"), dtype=TYPES[gt], device=DEV) for _ in range(2))
     dx, flat = rows(n, d, TYPES[x_type], g, pad, shift)
     got = op.backward(x, w, mean, rstd, dy, dw, db, grad_x=dx)
