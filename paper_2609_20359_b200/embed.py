@@ -5,6 +5,8 @@ tensors it is given.
 """
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import _binding as fls
@@ -35,6 +37,7 @@ class Embedding:
         self.workspace = Workspace(fls.fls_embed_query(self.handle)["workspace_bytes"], self.device)
         mem = self.workspace.memory
         self._args = fls.fls_embed_io(workspace=mem.data_ptr(), workspace_bytes=mem.numel())   # of the call in preparation
+        self._args_ref = ctypes.byref(self._args)
 
     def lookup(self, tokens, weight, out=None, scale: float = 1.0, ignore_token: int = -100, stream=None):
         """scale * weight[tokens], [N, dim]: zeros where a token is ignore_token, NaN where it is outside the table."""
@@ -46,7 +49,7 @@ class Embedding:
         else:
             io.out, io.out_stride = matrix(out, "out", n, self.dim, self.act_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, 0
-        fls.fls_embed_lookup(self.handle, io, self.workspace.stream(stream))
+        fls._check(fls.lib.fls_embed_lookup(self.handle, self._args_ref, self.workspace.stream(stream)))
         return out
 
     def grad(self, tokens, grad_out, grad_weight, scale: float = 1.0, accumulate: bool = False, ignore_token: int = -100,
@@ -56,7 +59,7 @@ class Embedding:
         io.grad_out, io.grad_out_stride = matrix(grad_out, "grad_out", n, self.dim, self.act_torch_dtype)
         io.grad_weight, io.grad_weight_stride = matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, accumulate
-        fls.fls_embed_grad(self.handle, io, self.workspace.use(stream))
+        fls._check(fls.lib.fls_embed_grad(self.handle, self._args_ref, self.workspace.use(stream)))
 
     def _tokens(self, tokens) -> int:
         n = tokens.numel()

@@ -5,6 +5,8 @@ tensors it is given.
 """
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
 from . import _binding as fls
@@ -39,6 +41,7 @@ class Norm:
         mem = self.workspace.memory
         self._io = fls.fls_norm_io()                                                                # of the call in preparation
         self._grad_io = fls.fls_norm_grad_io(workspace=mem.data_ptr(), workspace_bytes=mem.numel())
+        self._io_ref, self._grad_io_ref = ctypes.byref(self._io), ctypes.byref(self._grad_io)
 
     # ------------------------------------------------------------------ calls
     def forward(self, x, weight=None, bias=None, y=None, stats: bool = True, stream=None):
@@ -81,7 +84,7 @@ class Norm:
         io.grad_weight = vector(grad_weight, "grad_weight", dim, gt)
         io.grad_bias = vector(grad_bias, "grad_bias", dim, gt)
         io.accumulate = accumulate
-        fls.fls_norm_backward(self.handle, io, self.workspace.use(stream))
+        fls._check(fls.lib.fls_norm_backward(self.handle, self._grad_io_ref, self.workspace.use(stream)))
         return grad_x
 
     def _forward(self, x, residual, weight, bias, y, total, stats, stream):
@@ -112,7 +115,7 @@ class Norm:
                 io.mean = mean.data_ptr()
             rstd = new(stream, n, torch.float32)
             io.rstd = rstd.data_ptr()
-        fls.fls_norm_forward(self.handle, io, self.workspace.stream(stream))
+        fls._check(fls.lib.fls_norm_forward(self.handle, self._io_ref, self.workspace.stream(stream)))
         return y, total, mean, rstd
 
     def close(self) -> None:

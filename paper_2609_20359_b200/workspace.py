@@ -32,7 +32,7 @@ def matrix(t: torch.Tensor, name: str, rows, cols: int, dtype: torch.dtype):
     if t.dtype is not dtype or len(shape) != 2 or shape[1] != cols or (rows is not None and shape[0] != rows) or not t.is_cuda:
         raise ValueError(f"{name} must be a {dtype} tensor of shape [{'N' if rows is None else rows}, {cols}] on a CUDA device, "
                          f"got {t.dtype} {tuple(shape)} on {t.device}")
-    if t.is_contiguous():
+    if t.is_contiguous():                                  # another device than the current one is the library's to refuse
         return t.data_ptr(), 0
     row, one = t.stride()
     if one != 1 and cols > 1:
@@ -46,7 +46,7 @@ def vector(t, name: str, n: int, dtype: torch.dtype):
     """Address of a contiguous tensor of n elements, None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {(n,)} on a CUDA device, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
