@@ -104,7 +104,8 @@ GRADS = [
     (1000, 400, 264, "ignored", 0, 0), (2048, 97, 300, "few", 4, 4), (4096, 1031, 256, "same", 0, 0), (4097, 1031, 128, "random", 8, 8),
     (5000, 128256, 64, "text", 0, 0), (16384, 511, 64, "few", 0, 0), (16385, 512, 72, "text", 0, 0), (33000, 513, 40, "mixed", 3, 1),
     (70000, 3, 24, "same", 0, 0), (131072, 40000, 8, "text", 0, 0), (131073, 40000, 8, "mixed", 0, 0), (300000, 70001, 9, "text", 0, 0),
-    (300, 300000, 16, "random", 0, 0), (50, 7, 65536, "random", 0, 0), (3000, 1 << 20, 8, "random", 0, 0), (200, 20000, 2048, "text", 0, 0)]
+    (256, 4001, 520, "text", 0, 0), (255, 9, 264, "few", 0, 0), (200, 3, 1000, "same", 0, 0), (257, 4001, 72, "mixed", 8, 8),
+    (512, 1031, 77, "text", 0, 0), (511, 2, 96, "same", 0, 0), (300, 300000, 128, "random", 0, 0), (300, 300000, 16, "random", 0, 0), (50, 7, 65536, "random", 0, 0), (3000, 1 << 20, 8, "random", 0, 0), (200, 20000, 2048, "text", 0, 0)]
 
 
 @pytest.mark.parametrize("act,grad", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
