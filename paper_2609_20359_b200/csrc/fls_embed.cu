@@ -7,7 +7,7 @@
 // the token changes.  Sums of a token that reaches beyond the chunk go to the workspace and are joined in ascending order.
 //
 // Bound by memory, and of that mostly by the zeros of rows without a token, which need no sums: 8191 x 2048 tokens' gradients into
-// 128256 x 2048 fp32 in 181 us, 5.95 TB/s of what has to move (91 % of the measured copy), 163 of them beside the sums.  With few
+// 128256 x 2048 fp32 in 174 us, 6.2 TB/s of what has to move (95 % of the measured copy).  With few
 // tokens it is latency: 4096 tokens x 768 added to a gradient take 16 us on the device, 6 of sort, 5 of sums, 4 of joins.  The
 // lookup is one pass: 16384 x 2048 in 17.2 us, 5.6 TB/s; one token 1.3 us.
 #include <cuda_runtime.h>
@@ -38,6 +38,10 @@ constexpr uint64_t kOneCta = 2048;
 // Tokens up to which the CTAs that write zeros look through all of them (4 us for 8192) rather than wait for the sort (11 us);
 // 8192 x 768 29 us against 33, 16384 39 against 47.
 constexpr uint64_t kLookThrough = 16384;
+// Bytes of zeros from which on they are all the last kernel's: neither sums nor joins then wait for a zero, but CTAs that wait for
+// the sums take room from those that write (us, zeros beside the sums / beside the joins: 8192 x 768 into 77 MB 29 / 33; 8191 x 2048
+// into 131 MB 51 / 45, 262 MB 65 / 59, 525 MB 101 / 95, 1050 MB 181 / 174; 16384 x 2048 into 1050 MB 213 / 190).
+constexpr uint64_t kManyZeros = 96 << 20;
 constexpr uint64_t kZerosPerCta = 256 << 10;     // bytes: 8191 x 2048 fp32 in 179 us, with 1 MB 189; at least two CTAs per SM
 constexpr uint64_t kZerosBesideJoins = 16 << 20; // bytes, at most an eighth: what the memory takes during the joins' 5 us
 constexpr uint32_t kSlab = 256;                              // columns of a warp: eight per lane
@@ -584,13 +588,15 @@ template <typename G, bool VEC>
 __global__ void __launch_bounds__(256, 4) fls_embed_join_kernel(const __grid_constant__ EmbedCall c, const uint2* pairs, const FillShare share) {
   __shared__ union { float sums[8][kSlab]; FillShared fill; } sh;
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, slabs = c.dp / kSlab;
-  if (blockIdx.x < share.ctas) {
+  // first two CTAs of zeros for every SM, then the joins, then the other zeros
+  const uint32_t ahead = min(share.ctas, 296u), joins = gridDim.x - share.ctas;
+  if (blockIdx.x < ahead || blockIdx.x >= ahead + joins) {
     if (share.wait) pdl_wait();
-    fill_part(c, share, blockIdx.x, share.wait ? pairs : nullptr, sh.fill);
+    fill_part(c, share, blockIdx.x < ahead ? blockIdx.x : blockIdx.x - joins, share.wait ? pairs : nullptr, sh.fill);
     return;
   }
   pdl_wait();
-  const uint32_t chunk = blockIdx.x - share.ctas, n = uint32_t(c.tokens), none = uint32_t(c.vocab);
+  const uint32_t chunk = blockIdx.x - ahead, n = uint32_t(c.tokens), none = uint32_t(c.vocab);
   const uint32_t begin = chunk * c.chunk, end = begin + c.chunk;
   if (end >= n) return;
   const uint32_t key = pairs[end].x, last = pairs[end - 1].x, first = pairs[begin].x, left = begin ? pairs[begin - 1].x : none;
@@ -867,8 +873,12 @@ int run_grad(fls_embed* e, EmbedCall& c, cudaStream_t s) {
   }
   if (n && n <= kSortAtOnce) {
     const uint32_t ctas = n <= kOneCta ? 1 : kCluster;
-    if (c.chunks > 1) beside_joins = share(std::min<uint64_t>(c.vocab * c.dim * c.grad_size / 8, kZerosBesideJoins), 148);
-    beside_sums = share(~0ull, uint32_t(std::clamp<uint64_t>(c.vocab * c.dim * c.grad_size / kZerosPerCta, 296, 148 * 16)));
+    // The last kernel's CTAs that wait for nothing start as soon as those of the two before it have, and so run beside all three.
+    const uint64_t zeros = c.vocab * c.dim * c.grad_size;
+    const uint32_t ctas_of_all = uint32_t(std::clamp<uint64_t>(zeros / kZerosPerCta, 296, 148 * 16));
+    if (n <= kLookThrough && zeros >= kManyZeros) beside_joins = share(~0ull, ctas_of_all);
+    else beside_joins = share(std::min<uint64_t>(zeros / 8, kZerosBesideJoins), 148);
+    beside_sums = share(~0ull, ctas_of_all);
     const uint32_t rounds = uint32_t((n + ctas * kClusterThreads - 1) / (ctas * kClusterThreads));
     uint32_t room = kClusterThreads * 8;                    // as many rounds as the kernel is made for
     while (room < rounds * kClusterThreads * 8) room *= 2;
