@@ -513,10 +513,9 @@ __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_cons
   const uint32_t row_bytes = Staged<T>::bytes + (c.accumulate ? Staged<G>::bytes : 0);
   const uint32_t place = uint32_t(__cvta_generic_to_shared(rows)) + threadIdx.x / 32 * (kAhead * row_bytes);
   float sum[8] = {};
-  const uint32_t first = pairs[begin].x, left = begin ? pairs[begin - 1].x : none, right = end < n ? pairs[end].x : none;
-  if (first == none) return;
-  bool from_left = left == first;
-  uint32_t now = first;
+  const uint32_t left = begin ? pairs[begin - 1].x : none, right = end < n ? pairs[end].x : none;
+  bool from_left = false;
+  uint32_t now = none;
   for (uint32_t base = begin; base < end; base += 64) {
     // 64 positions, two per lane, and the key behind each
     const uint32_t here = min(64u, end - base);
@@ -528,6 +527,7 @@ __global__ void __launch_bounds__(256, 3) fls_embed_sum_kernel(const __grid_cons
     if (lane + 1 >= here) lo_next = behind;
     if (lane + 33 >= here) hi_next = behind;
     auto key_at = [&](uint32_t i) { return __shfl_sync(~0u, i < 32 ? lo.x : hi.x, i); };
+    if (base == begin) from_left = left == key_at(0);
     auto row_at = [&](uint32_t i) { return __shfl_sync(~0u, i < 32 ? lo.y : hi.y, i); };
     auto next_at = [&](uint32_t i) { return __shfl_sync(~0u, i < 32 ? lo_next : hi_next, i); };
     auto send = [&](uint32_t i) {
@@ -599,14 +599,17 @@ __global__ void __launch_bounds__(256, 4) fls_embed_join_kernel(const __grid_con
   const uint32_t chunk = blockIdx.x - ahead, n = uint32_t(c.tokens), none = uint32_t(c.vocab);
   const uint32_t begin = chunk * c.chunk, end = begin + c.chunk;
   if (end >= n) return;
+  const uint64_t mine = uint64_t(end) + uint64_t(threadIdx.x) * c.chunk;
+  uint32_t begins = mine < n ? pairs[mine].x : none;               // a token that a chunk after this one begins with
   const uint32_t key = pairs[end].x, last = pairs[end - 1].x, first = pairs[begin].x, left = begin ? pairs[begin - 1].x : none;
   if (key == none || last != key || (first == key && left == key)) return;       // nothing goes on, or began before this chunk
   uint32_t more = 0;                                                             // chunks after this one that begin with the token
   for (;;) {
-    const uint64_t p = uint64_t(end) + uint64_t(more + threadIdx.x) * c.chunk;
-    const int got = __syncthreads_count(p < n && pairs[p].x == key);
+    const int got = __syncthreads_count(begins == key);
     more += got;
     if (got < 256) break;
+    const uint64_t p = mine + uint64_t(more) * c.chunk;
+    begins = p < n ? pairs[p].x : none;
   }
   // the sums are in rows 2 chunk + 1, 2 chunk + 2, 2 chunk + 4, ... 2 (chunk + more)
   const bool few = more < 8;
