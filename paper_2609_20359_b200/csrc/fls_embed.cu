@@ -250,17 +250,31 @@ __device__ __forceinline__ uint32_t first_at_least(const uint2* pairs, uint32_t 
 
 struct FillShared { uint32_t there[kFillRows / 32]; };
 
-// Zeros to the rows v0 .. v1 - 1 whose bit in `there` is not set, a warp each.
+// Zeros to the rows v0 .. v1 - 1 whose bit in `there` is not set, a warp each, or several short rows to a warp.
 __device__ __forceinline__ void fill_rows(const EmbedCall& c, const FillShared& sh, uint64_t v0, uint64_t v1) {
   const uint32_t lane = threadIdx.x % 32, warps = blockDim.x / 32;
-  const uint32_t bytes = c.dim * c.grad_size, whole = c.zero_vec ? bytes / 16 * 16 : 0;
+  const uint32_t bytes = c.dim * c.grad_size;
+  if (c.zero_vec && bytes % 16 == 0 && bytes <= 256) {
+    const uint32_t pieces = bytes / 16, rows = 32 / pieces, own = lane / pieces;
+    char* to = static_cast<char*>(c.grad_weight) + (lane - own * pieces) * 16;
+    if (own < rows)
+#pragma unroll 4
+      for (uint64_t v = v0 + threadIdx.x / 32 * rows + own; v < v1; v += warps * rows) {
+        const uint32_t r = uint32_t(v - v0);
+        if (!(sh.there[r / 32] >> (r % 32) & 1)) __stcs(reinterpret_cast<uint4*>(to + v * c.grad_weight_stride * c.grad_size), make_uint4(0, 0, 0, 0));
+      }
+    return;
+  }
   for (uint64_t v = v0 + threadIdx.x / 32; v < v1; v += warps) {
     const uint32_t r = uint32_t(v - v0);
     if (sh.there[r / 32] >> (r % 32) & 1) continue;
+    // elements up to the first 16-byte boundary, 16 bytes at a time from there, the elements behind the last boundary
     char* row = static_cast<char*>(c.grad_weight) + v * c.grad_weight_stride * c.grad_size;
+    const uint32_t head = min(bytes, uint32_t(-reinterpret_cast<uintptr_t>(row)) % 16), middle = (bytes - head) / 16 * 16, tail = bytes - head - middle;
+    if (lane * 2 < head) *reinterpret_cast<uint16_t*>(row + lane * 2) = 0;
 #pragma unroll 4
-    for (uint32_t j = lane * 16; j < whole; j += 512) __stcs(reinterpret_cast<uint4*>(row + j), make_uint4(0, 0, 0, 0));
-    for (uint32_t j = whole + lane * 2; j < bytes; j += 64) *reinterpret_cast<uint16_t*>(row + j) = 0;
+    for (uint32_t j = lane * 16; j < middle; j += 512) __stcs(reinterpret_cast<uint4*>(row + head + j), make_uint4(0, 0, 0, 0));
+    if (lane * 2 < tail) *reinterpret_cast<uint16_t*>(row + head + middle + lane * 2) = 0;
   }
 }
 
