@@ -630,10 +630,11 @@ int fls_norm_destroy(fls_norm* norm);
 
 /* Enqueued on cuda_stream; nothing is synchronised or allocated.  Without rows the forward pass does nothing and the backward
  * pass writes zeros to grad_weight and grad_bias (or leaves them, with accumulate).  Forward passes may overlap in time;
- * backward passes with one workspace must not.  Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, a backward
- * pass without desc.grads, a stride below d, residual without total or the reverse, grad_total without grad_x, a mean for a
- * root mean square norm), FLS_EPTR (null, host, another device's or overlapping buffers), FLS_EALIGN (buffers off their
- * element size, workspace), FLS_ESIZE (workspace too small), FLS_ECUDA. */
+ * backward passes with one workspace must not (memory that other operators use between them has to be cleared again).
+ * Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, a backward pass without desc.grads, a stride below d,
+ * residual without total or the reverse, grad_total without grad_x, a mean for a root mean square norm), FLS_EPTR (null, host,
+ * another device's or overlapping buffers), FLS_EALIGN (buffers off their element size, workspace), FLS_ESIZE (workspace too
+ * small), FLS_ECUDA. */
 int fls_norm_forward(fls_norm* norm, const fls_norm_io* io, void* cuda_stream);
 int fls_norm_backward(fls_norm* norm, const fls_norm_grad_io* io, void* cuda_stream);
 

@@ -107,3 +107,67 @@ def test_gradient_of_the_chain_against_differences():
             up, dn = (loss(*(t + k * h * step if j == i else t for j, t in enumerate(at))) for k in (1, -1))
             # central differences: h^2 / 6 of a third derivative of order |out|_1; fp32 gradients: 1e-5 of their norm is 100 roundings
             assert abs(float((up - dn) / (2 * h) - (grad.double() * step).sum())) < 1e-5 * float(grad.double().norm()) + h * h * float(out.abs().sum())
+
+
+def test_forward_passes_on_two_streams_at_once():
+    """Lookups and forward passes have no workspace: calls of one object may overlap."""
+    from paper_2609_20359_b200.embed import Embedding
+    from paper_2609_20359_b200.norm import Norm
+    V, d, n = 3000, 1024, 4000
+    g = torch.Generator(device=DEV).manual_seed(3)
+    table = torch.randn(V, d, generator=g, device=DEV).bfloat16()
+    toks = [torch.randint(0, V, (n,), generator=g, device=DEV) for _ in range(2)]
+    emb, norm = Embedding(n, V, d, grads=False), Norm(n, d, "rms", grads=False)
+    want = [norm.add_forward(emb.lookup(t, table), emb.lookup(t.flip(0), table)) for t in toks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(norm.add_forward(emb.lookup(toks[k], table), emb.lookup(toks[k].flip(0), table)))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out in got[k]:
+            assert all(a is b is None or torch.equal(a, b) for a, b in zip(out, want[k]))
+
+
+@pytest.mark.parametrize("n", [100, 700, 6000])
+def test_two_captured_graphs_with_one_workspace(n):
+    """Backward passes of one object captured into two graphs, replayed one after the other in any order."""
+    from paper_2609_20359_b200.embed import Embedding
+    from paper_2609_20359_b200.norm import Norm
+    V, d = 900, 256
+    g = torch.Generator(device=DEV).manual_seed(4)
+    emb, norm = Embedding(n, V, d, grad_dtype="f32"), Norm(n, d, grad_dtype="f32")
+    data, graphs = [], []
+    for _ in range(2):
+        tok = torch.randint(0, 50, (n,), generator=g, device=DEV)
+        x, dy = (torch.randn(n, d, generator=g, device=DEV).bfloat16() for _ in range(2))
+        _, mean, rstd = norm.forward(x)
+        data.append((tok, x, mean, rstd, dy, torch.empty(d, device=DEV), torch.empty(d, device=DEV), torch.empty(V, d, device=DEV),
+                     torch.empty_like(x)))
+
+    def step(tok, x, mean, rstd, dy, dw, db, dt, dx):
+        norm.backward(x, None, mean, rstd, dy, dw, db, grad_x=dx)
+        emb.grad(tok, dx, dt)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for one in data:
+            step(*one)
+    torch.cuda.current_stream().wait_stream(side)
+    for one in data:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(*one)
+        graphs.append(graph)
+    for k in (0, 1, 1, 0, 1):
+        for t in data[k][5:]:
+            t.fill_(float("nan"))
+        graphs[k].replay()
+        tok, x, mean, rstd, dy, dw, db, dt, dx = data[k]
+        R.check_backward(x, None, mean, rstd, dy, None, dx, dw, db)
+        R.check_embed_grad(dt, tok, dx)
+    del graphs, graph
