@@ -6,7 +6,7 @@
 //
 // Bound by memory where rows are fp32 (16384 x 2048 with residual 72 us, 6.5 TB/s, 99 % of the measured copy) or bf16 with a residual
 // (44 us, 6.05 TB/s); bf16 alone by the instructions and sums between a row's load and its store (29 us, 4.6 TB/s).  Backward
-// 32768 x 768 with fp32 rows 47 to 49 us, 6.1 TB/s in the loop and 7 us of start and joins; with bf16 rows 38 us, 3.9 TB/s, bound by
+// 32768 x 768 with fp32 rows 47 to 49 us, 6.1 TB/s in the loop and 7 us of start and joins; with bf16 rows 38 us, 4.0 TB/s, bound by
 // latency and issue.  One row: 2.4 us forward, 5 backward.
 #include <cuda_runtime.h>
 
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(THREADS, ctas_per_sm(VEC, K, sizeof(X), THREAD
 // thread keeps its columns' sums for weight and bias in registers, adds them to the other groups' at the end and leaves the
 // CTA's in the workspace.  VEC: STAGES times B rows are on their way at once, copied asynchronously into shared memory, every
 // warp for itself.
-template <typename X, typename Y, bool VEC, int K, int B, int STAGES, int THREADS>
+template <typename X, typename Y, bool VEC, int K, int B, int STAGES, int THREADS, bool RMS>
 __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __grid_constant__ NormCall c, uint32_t tpr) {
   extern __shared__ __align__(16) float smem[];             // rows on their way, then the groups' sums
   __shared__ __align__(16) float sums[2][THREADS / 32][2 * B];
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
   for (uint32_t i = 0; i < count; i += B) {
     if (i % 32 == 0) {
       const bool there = i + lane < count;
-      means = there && !c.rms ? c.mean_in[begin + i + lane] : 0.f;
+      means = there && !RMS ? c.mean_in[begin + i + lane] : 0.f;
       rstds = there ? c.rstd_in[begin + i + lane] : 0.f;
     }
     if (VEC) {
@@ -425,12 +425,12 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
         dy[k].get(gy[b][k]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (!c.rms) xhat[b][k][j] = add2(xhat[b][k][j], less);
+          if (!RMS) xhat[b][k][j] = add2(xhat[b][k][j], less);
           xhat[b][k][j] = mul2(xhat[b][k][j], scale[b]);
           dw[k][j] = fma2(gy[b][k][j], xhat[b][k][j], dw[k][j]);
           db[k][j] = add2(db[k][j], gy[b][k][j]);
           gy[b][k][j] = mul2(gy[b][k][j], w[k][j]);
-          if (!c.rms) sum_g = add2(sum_g, gy[b][k][j]);
+          if (!RMS) sum_g = add2(sum_g, gy[b][k][j]);
           sum_gx = fma2(gy[b][k][j], xhat[b][k][j], sum_gx);
         }
       }
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, 1) fls_norm_backward_kernel(const __g
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       if (B > 1 && i + b >= count) break;
-      const f2 k1 = make_f2(c.rms ? 0.f : -v[2 * b] * c.inv_dim * rstd[b]), k2 = make_f2(-v[2 * b + 1] * c.inv_dim * rstd[b]);
+      const f2 k1 = make_f2(RMS ? 0.f : -v[2 * b] * c.inv_dim * rstd[b]), k2 = make_f2(-v[2 * b + 1] * c.inv_dim * rstd[b]);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         f2 dx[4];
@@ -722,19 +722,19 @@ cudaError_t backward_rows(NormCall& c, cudaStream_t s) {
   c.join = c.parts * c.dp <= kJoinFloats;
   const uint32_t row_bytes = K * (Staged<X>::bytes * (c.grad_total ? 2 : 1) + Staged<Y>::bytes);
   const uint32_t smem = std::max(VEC ? STAGES * B * row_bytes * (threads / 32) : 0, (groups - 1) * tpr * 16 * K * 4);
-  auto kernel = fls_norm_backward_kernel<X, Y, VEC, K, B, STAGES, THREADS>;
-  static std::atomic<uint64_t> done{0};
-  const cudaError_t e = allow_shared(reinterpret_cast<const void*>(kernel), 226 << 10, done);
+  auto kernel = c.rms ? fls_norm_backward_kernel<X, Y, VEC, K, B, STAGES, THREADS, true> : fls_norm_backward_kernel<X, Y, VEC, K, B, STAGES, THREADS, false>;
+  static std::atomic<uint64_t> done[2];
+  const cudaError_t e = allow_shared(reinterpret_cast<const void*>(kernel), 226 << 10, done[c.rms]);
   if (e != cudaSuccess) return e;
   return launch(kernel, dim3(c.parts), threads, smem, false, s, c, tpr);
 }
 
 template <typename X, typename Y, bool VEC>
 cudaError_t backward_of(NormCall& c, cudaStream_t s) {
-  // One row of two cells per thread, or two rows of one cell: the latter leaves more threads for short rows (us, two cells / two rows:
-  // 32768 x 768 fp32 54.8 / 48.1, 8192 x 4096 bf16 52.9 / 55.3); columns moved one by one want the former (8192 x 1001 33.4 / 39.5).
-  // One row of one cell and 768 threads: 51.7 and 77.7.
-  return VEC && c.dim <= 4096 ? backward_rows<X, Y, VEC, 1, 2, 2, 512>(c, s) : backward_rows<X, Y, VEC, 2, 1, 2, 512>(c, s);
+  // Two rows of one cell per thread, or one row of two cells, which leaves more groups of threads for wide rows (us, two rows / two cells:
+  // 32768 x 768 fp32 48 / 55, 8192 x 2560 bf16 44 / 37, fp32 56 / 60, 8192 x 4096 bf16 56 / 53, fp32 88 / 93); columns moved one by one
+  // want the latter (8192 x 1001 39 / 33).  One row of one cell and 768 threads: 32768 x 768 fp32 52, 8192 x 4096 bf16 78.
+  return VEC && c.dim <= (sizeof(X) == 4 ? 4096 : 2048) ? backward_rows<X, Y, VEC, 1, 2, 2, 512>(c, s) : backward_rows<X, Y, VEC, 2, 1, 2, 512>(c, s);
 }
 
 template <typename X, typename Y>
