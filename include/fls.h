@@ -545,10 +545,11 @@ int fls_embed_query(const fls_embed* embed, fls_embed_layout* out);
 int fls_embed_destroy(fls_embed* embed);
 
 /* Enqueued on cuda_stream; nothing is synchronised or allocated.  A lookup without tokens does nothing; a gradient without
- * tokens writes a zero grad_weight (or leaves it, with accumulate).  Lookups may overlap in time; gradients with one
- * workspace must not.  Errors, before anything is enqueued: FLS_EINVAL (tokens > max_tokens, a gradient without desc.grads, a
- * stride below d, scale not finite in fp32), FLS_EPTR (null, host, another device's or overlapping buffers), FLS_EALIGN
- * (buffers off their element size, workspace), FLS_ESIZE (workspace too small), FLS_ECUDA. */
+ * tokens writes a zero grad_weight (or leaves it, with accumulate).  Lookups may overlap in time, and calls of one handle may
+ * come from several host threads at once; gradients with one workspace must not overlap.  Errors, before anything is enqueued:
+ * FLS_EINVAL (tokens > max_tokens, a gradient without desc.grads, a stride below d, scale not finite in fp32), FLS_EPTR (null,
+ * host, another device's or overlapping buffers), FLS_EALIGN (buffers off their element size, workspace), FLS_ESIZE (workspace
+ * too small), FLS_ECUDA. */
 int fls_embed_lookup(fls_embed* embed, const fls_embed_io* io, void* cuda_stream);
 int fls_embed_grad(fls_embed* embed, const fls_embed_io* io, void* cuda_stream);
 
@@ -631,8 +632,9 @@ int fls_norm_query(const fls_norm* norm, fls_norm_layout* out);
 int fls_norm_destroy(fls_norm* norm);
 
 /* Enqueued on cuda_stream; nothing is synchronised or allocated.  Without rows the forward pass does nothing and the backward
- * pass writes zeros to grad_weight and grad_bias (or leaves them, with accumulate).  Forward passes may overlap in time;
- * backward passes with one workspace must not (memory that other operators use between them has to be cleared again).
+ * pass writes zeros to grad_weight and grad_bias (or leaves them, with accumulate).  Forward passes may overlap in time, and
+ * calls of one handle may come from several host threads at once; backward passes with one workspace must not overlap (memory
+ * that other operators use between them has to be cleared again).
  * Errors, before anything is enqueued: FLS_EINVAL (rows > max_rows, a backward pass without desc.grads, a stride below d,
  * residual without total or the reverse, grad_total without grad_x, a mean for a root mean square norm), FLS_EPTR (null, host,
  * another device's or overlapping buffers), FLS_EALIGN (buffers off their element size, workspace), FLS_ESIZE (workspace too

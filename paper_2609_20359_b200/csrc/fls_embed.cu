@@ -13,6 +13,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -803,7 +804,7 @@ uint64_t span_bytes(uint64_t rows, uint64_t cols, uint64_t stride, uint64_t elem
 struct fls_embed {
   fls_embed_desc desc{};
   Regions reg{};
-  uint64_t launches = 0;
+  std::atomic<uint64_t> launches{0};      // calls that do not share a workspace may come from several host threads
 };
 
 namespace {

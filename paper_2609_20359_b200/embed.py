@@ -5,12 +5,10 @@ tensors it is given.
 """
 from __future__ import annotations
 
-import ctypes
-
 import torch
 
 from . import _binding as fls
-from .workspace import Workspace, device_of, dtype_of, matrix, vector
+from .workspace import Arguments, Workspace, device_of, dtype_of, matrix, vector
 
 
 class Embedding:
@@ -20,10 +18,10 @@ class Embedding:
     their gradients.  grad_dtype: the type of the table's gradient (as `Session`'s gradient buffers, whose units it may be
     written into).  grads=False: lookups only.
 
-    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  Gradients use the
-    workspace, one call at a time: those of one Embedding belong on one stream, or on streams ordered by events.  An Embedding
-    may be dropped while its calls run (a stream given by its handle has to outlive it); a captured graph has to be dropped
-    first.
+    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  Lookups may be made on
+    several streams and from several host threads at once.  Gradients use the workspace, one call at a time: those of one
+    Embedding belong on one stream, or on streams ordered by events.  An Embedding may be dropped while its calls run (a stream
+    given by its handle has to outlive it); a captured graph has to be dropped first.
     """
 
     def __init__(self, max_tokens: int, vocab: int, dim: int, act_dtype: str = "bf16", grad_dtype: str = "bf16", grads: bool = True,
@@ -36,12 +34,13 @@ class Embedding:
         self.handle = fls.fls_embed_create(max_tokens, vocab, dim, grads, act, grad)
         self.workspace = Workspace(fls.fls_embed_query(self.handle)["workspace_bytes"], self.device)
         mem = self.workspace.memory
-        self._args = fls.fls_embed_io(workspace=mem.data_ptr(), workspace_bytes=mem.numel())   # of the call in preparation
-        self._args_ref = ctypes.byref(self._args)
+        self._args = Arguments(io=(fls.fls_embed_io, dict(workspace=mem.data_ptr(), workspace_bytes=mem.numel())))
 
     def lookup(self, tokens, weight, out=None, scale: float = 1.0, ignore_token: int = -100, stream=None):
         """scale * weight[tokens], [N, dim]: zeros where a token is ignore_token, NaN where it is outside the table."""
-        io, n = self._args, self._tokens(tokens)
+        args = self._args
+        io = args.io
+        n = self._tokens(io, tokens)
         io.weight, io.weight_stride = matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16)
         if out is None:
             out = self.workspace.new(stream, (n, self.dim), self.act_torch_dtype)
@@ -49,22 +48,25 @@ class Embedding:
         else:
             io.out, io.out_stride = matrix(out, "out", n, self.dim, self.act_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, 0
-        fls._check(fls.lib.fls_embed_lookup(self.handle, self._args_ref, self.workspace.stream(stream)))
+        fls._check(fls.lib.fls_embed_lookup(self.handle, args.io_ref, self.workspace.stream(stream)))
         return out
 
     def grad(self, tokens, grad_out, grad_weight, scale: float = 1.0, accumulate: bool = False, ignore_token: int = -100,
              stream=None) -> None:
         """grad_weight [vocab, dim] becomes (accumulate: is added) scale times the sums of the rows of grad_out by token."""
-        io, n = self._args, self._tokens(tokens)
+        args = self._args
+        io = args.io
+        n = self._tokens(io, tokens)
         io.grad_out, io.grad_out_stride = matrix(grad_out, "grad_out", n, self.dim, self.act_torch_dtype)
         io.grad_weight, io.grad_weight_stride = matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, accumulate
-        fls._check(fls.lib.fls_embed_grad(self.handle, self._args_ref, self.workspace.use(stream)))
+        fls._check(fls.lib.fls_embed_grad(self.handle, args.io_ref, self.workspace.use(stream)))
 
-    def _tokens(self, tokens) -> int:
+    @staticmethod
+    def _tokens(io, tokens) -> int:
         n = tokens.numel()
-        self._args.token = vector(tokens, "tokens", n, torch.int64)
-        self._args.tokens = n
+        io.token = vector(tokens, "tokens", n, torch.int64)
+        io.tokens = n
         return n
 
     def close(self) -> None:

@@ -5,12 +5,10 @@ tensors it is given.
 """
 from __future__ import annotations
 
-import ctypes
-
 import torch
 
 from . import _binding as fls
-from .workspace import Workspace, device_of, dtype_of, matrix, vector
+from .workspace import Arguments, Workspace, device_of, dtype_of, matrix, vector
 
 
 class Norm:
@@ -20,9 +18,10 @@ class Norm:
     their sum and its gradients; y_dtype of the result and its gradient; weight_dtype of weight and bias; grad_dtype of their
     gradients (as `Session`'s gradient buffers, whose units they may be written into).  grads=False: forward passes only.
 
-    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  Backward passes use the
-    workspace, one call at a time: those of one Norm belong on one stream, or on streams ordered by events.  A Norm may be
-    dropped while its calls run (a stream given by its handle has to outlive it); a captured graph has to be dropped first.
+    Every call is enqueued on `stream` (default: torch's current stream) and returns without waiting.  Forward passes may be made
+    on several streams and from several host threads at once.  Backward passes use the workspace, one call at a time: those of
+    one Norm belong on one stream, or on streams ordered by events.  A Norm may be dropped while its calls run (a stream given
+    by its handle has to outlive it); a captured graph has to be dropped first.
     """
 
     def __init__(self, max_rows: int, dim: int, kind: str = "layer", eps: float = 1e-5, x_dtype: str = "bf16", y_dtype: str = "bf16",
@@ -39,9 +38,8 @@ class Norm:
         self.handle = fls.fls_norm_create(max_rows, dim, fls.FLS_NORM_RMS if kind == "rms" else fls.FLS_NORM_LAYER, eps, x, y, w, g, grads)
         self.workspace = Workspace(fls.fls_norm_query(self.handle)["workspace_bytes"], self.device)
         mem = self.workspace.memory
-        self._io = fls.fls_norm_io()                                                                # of the call in preparation
-        self._grad_io = fls.fls_norm_grad_io(workspace=mem.data_ptr(), workspace_bytes=mem.numel())
-        self._io_ref, self._grad_io_ref = ctypes.byref(self._io), ctypes.byref(self._grad_io)
+        self._args = Arguments(forward=(fls.fls_norm_io, {}),
+                               backward=(fls.fls_norm_grad_io, dict(workspace=mem.data_ptr(), workspace_bytes=mem.numel())))
 
     # ------------------------------------------------------------------ calls
     def forward(self, x, weight=None, bias=None, y=None, stats: bool = True, stream=None):
@@ -60,7 +58,8 @@ class Norm:
         """grad_x, the gradient of what was normalised (`x`: total, after add_forward), plus grad_total if given; the gradients of
         weight and bias go to grad_weight and grad_bias, each optional, accumulate adds to them.  `grad_x` may be grad_total
         itself; input_grad=False leaves it out."""
-        io, dim, xt, gt = self._grad_io, self.dim, self.x_torch_dtype, self.grad_torch_dtype
+        args, dim, xt, gt = self._args, self.dim, self.x_torch_dtype, self.grad_torch_dtype
+        io = args.backward
         io.x, io.x_stride = matrix(x, "x", None, dim, xt)
         n = io.rows = x.shape[0]
         io.weight = vector(weight, "weight", dim, self.weight_torch_dtype)
@@ -84,11 +83,12 @@ class Norm:
         io.grad_weight = vector(grad_weight, "grad_weight", dim, gt)
         io.grad_bias = vector(grad_bias, "grad_bias", dim, gt)
         io.accumulate = accumulate
-        fls._check(fls.lib.fls_norm_backward(self.handle, self._grad_io_ref, self.workspace.use(stream)))
+        fls._check(fls.lib.fls_norm_backward(self.handle, args.backward_ref, self.workspace.use(stream)))
         return grad_x
 
     def _forward(self, x, residual, weight, bias, y, total, stats, stream):
-        io, dim, xt, yt, new = self._io, self.dim, self.x_torch_dtype, self.y_torch_dtype, self.workspace.new
+        args, dim, xt, yt, new = self._args, self.dim, self.x_torch_dtype, self.y_torch_dtype, self.workspace.new
+        io = args.forward
         io.x, io.x_stride = matrix(x, "x", None, dim, xt)
         n = io.rows = x.shape[0]
         io.weight = vector(weight, "weight", dim, self.weight_torch_dtype)
@@ -115,7 +115,7 @@ class Norm:
                 io.mean = mean.data_ptr()
             rstd = new(stream, n, torch.float32)
             io.rstd = rstd.data_ptr()
-        fls._check(fls.lib.fls_norm_forward(self.handle, self._io_ref, self.workspace.stream(stream)))
+        fls._check(fls.lib.fls_norm_forward(self.handle, args.forward_ref, self.workspace.stream(stream)))
         return y, total, mean, rstd
 
     def close(self) -> None:

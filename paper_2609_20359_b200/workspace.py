@@ -1,5 +1,8 @@
-"""Device memory that an operator's calls share, one call at a time."""
+"""What the calls of an operator share: device memory, one call at a time, and argument structures, one set per host thread."""
 from __future__ import annotations
+
+import ctypes
+import threading
 
 import torch
 
@@ -49,6 +52,17 @@ def vector(t, name: str, n: int, dtype: torch.dtype):
     if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {(n,)} on a CUDA device, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+class Arguments(threading.local):
+    """Argument structures of the calls in preparation, as (type, fields that stay) by name; `name`_ref is what the library takes.
+    Each host thread has its own: the interpreter may switch threads between two fields, and does while the library reads them."""
+
+    def __init__(self, **kinds):
+        for name, (kind, fields) in kinds.items():
+            io = kind(**fields)
+            setattr(self, name, io)
+            setattr(self, name + "_ref", ctypes.byref(io))
 
 
 class Workspace:
