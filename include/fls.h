@@ -547,9 +547,9 @@ int fls_embed_destroy(fls_embed* embed);
 /* Enqueued on cuda_stream; nothing is synchronised or allocated.  A lookup without tokens does nothing; a gradient without
  * tokens writes a zero grad_weight (or leaves it, with accumulate).  Lookups may overlap in time, and calls of one handle may
  * come from several host threads at once; gradients with one workspace must not overlap.  Errors, before anything is enqueued:
- * FLS_EINVAL (tokens > max_tokens, a gradient without desc.grads, a stride below d, scale not finite in fp32), FLS_EPTR (null,
- * host, another device's or overlapping buffers), FLS_EALIGN (buffers off their element size, workspace), FLS_ESIZE (workspace
- * too small), FLS_ECUDA. */
+ * FLS_EINVAL (tokens > max_tokens, a gradient without desc.grads, any of the four strides below d or out of range, whichever
+ * the call, scale not finite in fp32), FLS_EPTR (null, host, another device's or overlapping buffers), FLS_EALIGN (buffers off
+ * their element size, workspace), FLS_ESIZE (workspace too small), FLS_ECUDA. */
 int fls_embed_lookup(fls_embed* embed, const fls_embed_io* io, void* cuda_stream);
 int fls_embed_grad(fls_embed* embed, const fls_embed_io* io, void* cuda_stream);
 

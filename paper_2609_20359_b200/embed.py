@@ -34,12 +34,14 @@ class Embedding:
         self.handle = fls.fls_embed_create(max_tokens, vocab, dim, grads, act, grad)
         self.workspace = Workspace(fls.fls_embed_query(self.handle)["workspace_bytes"], self.device)
         mem = self.workspace.memory
-        self._args = Arguments(io=(fls.fls_embed_io, dict(workspace=mem.data_ptr(), workspace_bytes=mem.numel())))
+        # apart, since the library looks at all strides of a structure, and a refused call's must not be in the way of the other's
+        self._args = Arguments(lookup=(fls.fls_embed_io, {}),
+                               grad=(fls.fls_embed_io, dict(workspace=mem.data_ptr(), workspace_bytes=mem.numel())))
 
     def lookup(self, tokens, weight, out=None, scale: float = 1.0, ignore_token: int = -100, stream=None):
         """scale * weight[tokens], [N, dim]: zeros where a token is ignore_token, NaN where it is outside the table."""
         args = self._args
-        io = args.io
+        io = args.lookup
         n = self._tokens(io, tokens)
         io.weight, io.weight_stride = matrix(weight, "weight", self.vocab, self.dim, torch.bfloat16)
         if out is None:
@@ -47,20 +49,20 @@ class Embedding:
             io.out, io.out_stride = out.data_ptr(), 0
         else:
             io.out, io.out_stride = matrix(out, "out", n, self.dim, self.act_torch_dtype)
-        io.scale, io.ignore_token, io.accumulate = scale, ignore_token, 0
-        fls._check(fls.lib.fls_embed_lookup(self.handle, args.io_ref, self.workspace.stream(stream)))
+        io.scale, io.ignore_token = scale, ignore_token
+        fls._check(fls.lib.fls_embed_lookup(self.handle, args.lookup_ref, self.workspace.stream(stream)))
         return out
 
     def grad(self, tokens, grad_out, grad_weight, scale: float = 1.0, accumulate: bool = False, ignore_token: int = -100,
              stream=None) -> None:
         """grad_weight [vocab, dim] becomes (accumulate: is added) scale times the sums of the rows of grad_out by token."""
         args = self._args
-        io = args.io
+        io = args.grad
         n = self._tokens(io, tokens)
         io.grad_out, io.grad_out_stride = matrix(grad_out, "grad_out", n, self.dim, self.act_torch_dtype)
         io.grad_weight, io.grad_weight_stride = matrix(grad_weight, "grad_weight", self.vocab, self.dim, self.grad_torch_dtype)
         io.scale, io.ignore_token, io.accumulate = scale, ignore_token, accumulate
-        fls._check(fls.lib.fls_embed_grad(self.handle, args.io_ref, self.workspace.use(stream)))
+        fls._check(fls.lib.fls_embed_grad(self.handle, args.grad_ref, self.workspace.use(stream)))
 
     @staticmethod
     def _tokens(io, tokens) -> int:
