@@ -74,8 +74,10 @@ class Workspace:
         self.memory = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.memory[:256].zero_()
         # the clear, and what used this memory before, must not come after the first call
-        if not torch.cuda.is_current_stream_capturing():
+        self._clear = not torch.cuda.is_current_stream_capturing()
+        if self._clear:
             torch.cuda.current_stream(device).synchronize()
+        # otherwise only the graph's replays clear it, and a call that is not in that graph may come before the first of them
         self._streams = {fls._stream_handle(None)}             # those that torch's allocator knows to use the memory
         self._like = {t: torch.empty(0, dtype=t, device=device) for t in (torch.float32, torch.bfloat16)}
 
@@ -87,17 +89,22 @@ class Workspace:
         """The same, for a call that uses the memory."""
         handle = self.stream(stream)
         if handle not in self._streams:
-            if stream is None:
-                stream = torch.cuda.current_stream(self.device)
-            elif isinstance(stream, int):
-                stream = torch.cuda.ExternalStream(stream, device=self.device)
-            self.memory.record_stream(stream)
+            self.memory.record_stream(self._torch_stream(stream))
             self._streams.add(handle)
+        if not self._clear:
+            with torch.cuda.stream(self._torch_stream(stream)):
+                self.memory[:256].zero_()
+                self._clear = not torch.cuda.is_current_stream_capturing()
         return handle
 
     def new(self, stream, shape, dtype: torch.dtype) -> torch.Tensor:
         """An output of a call: its memory's reuse is ordered by the stream that writes it, which need not be torch's current one."""
         if stream is None:
             return self._like[dtype].new_empty(shape)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream):
+        with torch.cuda.stream(self._torch_stream(stream)):
             return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _torch_stream(self, stream):
+        if stream is None:
+            return torch.cuda.current_stream(self.device)
+        return torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream
