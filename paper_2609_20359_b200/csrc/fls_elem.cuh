@@ -97,9 +97,6 @@ template <> struct Elem<float> {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) { Elem<T>::unpack(Elem<T>::load_raw(p), x); }
-
 // An asynchronous copy of 16 bytes to shared memory; zeros where `there` is false.
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");

@@ -879,7 +879,7 @@ int fls_norm_backward(fls_norm* h, const fls_norm_grad_io* io, void* cuda_stream
   const bool layer = d.kind == FLS_NORM_LAYER;
   // grad_x may be grad_total itself
   const bool over = io->grad_total && io->grad_total == io->grad_x && c.grad_total_stride == c.grad_x_stride;
-  const Span s[11] = {{io->x, span_bytes(n, d.dim, c.x_stride, xs), xs, false, "x"},
+  const Span s[10] = {{io->x, span_bytes(n, d.dim, c.x_stride, xs), xs, false, "x"},
                       {io->weight, n && io->weight ? d.dim * ws : 0, ws, false, "weight"},
                       {io->mean, layer ? n * 4 : 0, 4, false, "mean"},
                       {io->rstd, n * 4, 4, false, "rstd"},
