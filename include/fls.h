@@ -504,8 +504,10 @@ int fls_top_logits(const void* logits, uint32_t logit_dtype, uint64_t rows, uint
  * Positions with t_n == ignore_token take no part: their row of out is zero, their row of D may hold anything, NaN included.
  * A token outside [0, V) other than ignore_token is not an error the host could see: its row of out is NaN, and it takes no
  * part in the gradient.  Without accumulate every row of G is written, zeros where v is no token; with it only the rows of
- * tokens are touched (tied tables: after fls_head_xent has written the head's gradient; several micro-batches).  The sums
- * are made in an order that depends on the tokens alone, so results do not change from run to run. */
+ * tokens are touched (tied tables: after fls_head_xent has written the head's gradient; several micro-batches), and every call
+ * rounds to G's type once: a bf16 G of two micro-batches carries two roundings.  The order of the sums depends on the tokens,
+ * their number, dim, the table's size in bytes and accumulate alone: the same call gives the same bits every time, a call with
+ * another accumulate may differ in the last ones. */
 typedef struct fls_embed fls_embed; /* opaque, created by fls_embed_create, freed by fls_embed_destroy */
 
 typedef struct {

@@ -8,8 +8,8 @@
 //
 // Bound by memory, and of that mostly by the zeros of rows without a token, which need no sums: 8191 x 2048 tokens' gradients into
 // 128256 x 2048 fp32 in 174 us, 6.2 TB/s of what has to move (95 % of the measured copy).  With few
-// tokens it is latency: 4096 tokens x 768 added to a gradient take 16 us on the device, 6 of sort, 5 of sums, 4 of joins.  The
-// lookup is one pass: 16384 x 2048 in 17.2 us, 5.6 TB/s; one token 1.3 us.
+// tokens it is latency: 4096 tokens x 768 added to a gradient take 16 to 18 us on the device, 6 of sort, 5 of sums, 4 of joins.  The
+// lookup is one pass: 16384 x 2048 in 17.1 us, 5.6 TB/s; one token 1.3 to 1.5 us.
 #include <cuda_runtime.h>
 
 #include <algorithm>
