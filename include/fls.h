@@ -569,10 +569,11 @@ int fls_embed_get_launch_count(const fls_embed* embed, uint64_t* launches);
  *   grad_x = rho (g - mean(g) - xh mean(g xh)) + dt        (root mean square: without mean(g))
  *   grad_weight = sum over rows of dy xh,   grad_bias = sum over rows of dy    (+ what is there, with accumulate)
  * grad_x is the gradient of s: with a residual, of x and of r alike.  Statistics, sums and products are fp32, every output is
- * rounded once; a row whose sum of squares leaves fp32's range (values beyond about 1e19) has no statistics in fp32.  The
- * backward pass takes mean and rstd as fp32, so that (s - mu) carries the rounding of mu, 2^-24 |mu|.  The variance is never below
- * zero; in a row whose values differ by less than fp32's roundings of their mean, s - mu and var are of the size of those
- * roundings (y - b: of the second order in them, times w rho).  Results do not change from run to run.
+ * rounded once; a row whose sum of squares leaves fp32's range (values beyond about 1e19, or with an eps of zero all below about
+ * 1e-19) has no statistics in fp32.  The backward pass takes mean and rstd as fp32, so that (s - mu) carries the rounding of mu,
+ * 2^-24 |mu|.  The variance is never below zero; in a row whose values differ by less than fp32's roundings of their mean, s - mu
+ * and var are of the size of those roundings (y - b: of the second order in them, times w rho).  Results do not change from run
+ * to run.
  * A row without finite statistics gives NaN in itself, and in grad_weight and grad_bias, alone. */
 typedef struct fls_norm fls_norm; /* opaque, created by fls_norm_create, freed by fls_norm_destroy */
 
